@@ -48,6 +48,7 @@
 #ifndef NLB_H
 #define NLB_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -357,6 +358,83 @@ int nlb_rnn_update(nlb_table *h, const int32_t *src, const int32_t *dst, const u
 int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst, const uint32_t *t,
                            uint32_t n, uint64_t first_eid, const nlb_gru_weights *wts, void *status,
                            void *stream);
+
+/* Softmax attention over packed sequences, with a learned bias on the gap
+ * between two positions: the layer that reads retrieved lists (nlb_sample's
+ * answers) or whole histories.  For query row i and key row j of one sequence
+ * and query head h, which reads key/value head h / (heads / kv_heads):
+ *   s_ij = scale q_i . k_j + bias[bucket(pos_i - pos_j)][h]
+ *   o_i  = sum_j softmax_j(s_i) v_j,   lse_i = log sum_j exp(s_ij)
+ * over the keys open to row i.  A row without an open key has o_i = 0 and
+ * lse_i = -infinity.
+ *   Sequences.  Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1
+ * and the key rows k_start[b] .. k_start[b + 1] - 1 (device int32 [batch + 1],
+ * non-decreasing; the host need not know the lengths, which may be zero).
+ * q_start NULL: q_rows / batch rows each; k_start NULL: k_rows / batch keys
+ * each (the division must leave no rest).  Rows before the first and behind
+ * the last sequence are neither read nor written.  Starts outside [0, rows]
+ * are taken as the nearest end, so no call reads or writes outside its rows.
+ * With q_start NULL and q_rows == batch (a retrieved list per query, or one
+ * new token per sequence) the call runs in a form made for single rows.
+ *   Rows.  q, o: [q_rows][heads][dim], k, v: [k_rows][kv_heads][dim], of type
+ * dtype, at any row and head strides (in values, 0 .. 2^31 - 1); a row's dim
+ * values are contiguous, so slices of a joint projection need no copy.
+ * Written rows must not overlap.
+ *   Open keys.  causal = 1: key j is open to row i if j <= i + lk - lq (i, j
+ * counted in the sequence, lq and lk its lengths): the last query row stands
+ * at the last key row.  k_pos (device uint32 [k_rows] or NULL): rows with
+ * k_pos = 0xFFFFFFFF are closed to every query, as nlb_sample's ts marks empty
+ * slots; what their k and v hold is not used.  A key that causal closes to
+ * some rows only must hold finite values, or those rows may become NaN.
+ *   Bias.  buckets = 0: none (bias NULL).  Else bias is a device array
+ * [buckets][heads] of dtype, bounds a device int32 [buckets - 1], increasing,
+ * and bucket(x) the number of bounds <= x.  Positions are q_pos (device uint32
+ * [q_rows]) and k_pos, whose difference is clamped to int32 (as nlb_sample's
+ * tq and ts go in), or without either the places i + lk - lq and j.  A bias at
+ * or below -2^100 closes its bucket.
+ *   Numerics.  Sums, the softmax's maximum and sum, and lse are fp32.  bf16
+ * rows: products of bf16 values are exact in fp32, softmax weights enter the
+ * second product as bf16 (in the single-row form as fp32), o is rounded once.
+ * fp32 rows: fp32 products throughout.  The same call gives the same bits.
+ *   Working memory: nlb_attention_work bytes of device memory (16-byte
+ * aligned, may be NULL if that is 0), used by the call's kernels only; calls
+ * that may overlap in time need one each.  lse (device fp32 [q_rows][heads])
+ * may be NULL where no backward pass follows.  Only enqueues kernels: may be
+ * captured in a HIP graph.  No table is involved; device names the device of
+ * the arrays and the stream (-1: the current one).  Errors: NLB_EINVAL (as
+ * above; more than 2^31 - 1 rows; sizes whose grid passes 2^31 - 1
+ * workgroups), NLB_ESCRATCH (work_bytes too few), NLB_EDEVICE. */
+#define NLB_ATT_MAX_DIM 128
+#define NLB_ATT_MAX_HEADS 256
+#define NLB_ATT_MAX_BUCKETS 64
+
+typedef struct nlb_att_rows {
+    void *data;
+    int64_t row_stride, head_stride;   /* values */
+} nlb_att_rows;
+
+typedef struct nlb_att_call {
+    int32_t device;          /* HIP device ordinal, -1 = current */
+    int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: q, k, v, o, bias and their gradients */
+    int32_t heads, kv_heads; /* heads a multiple of kv_heads, at most NLB_ATT_MAX_HEADS */
+    int32_t dim;             /* 1 .. NLB_ATT_MAX_DIM */
+    int32_t causal;          /* 0 or 1 */
+    int32_t buckets;         /* 0 .. NLB_ATT_MAX_BUCKETS */
+    float scale;
+    uint32_t batch, q_rows, k_rows;
+    const int32_t *q_start, *k_start;
+    const void *bias;
+    const int32_t *bounds;
+    const uint32_t *q_pos, *k_pos;
+    nlb_att_rows q, k, v;    /* not written */
+} nlb_att_call;
+
+/* Device bytes that nlb_attention (backward = 0) or nlb_attention_backward
+ * (1) of this call works in; a host computation.  Errors: NLB_EINVAL. */
+int nlb_attention_work(const nlb_att_call *call, int32_t backward, size_t *bytes);
+
+int nlb_attention(const nlb_att_call *call, const nlb_att_rows *o, float *lse, void *work, size_t work_bytes,
+                  void *stream);
 
 /* Free the table's device memory after synchronising its device.  NULL is a
  * no-op.  Borrowed buffers are not touched. */

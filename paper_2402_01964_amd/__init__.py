@@ -24,12 +24,13 @@ MAX_SLOTS = 1024
 
 # Symbols declared in include/nlb.h.
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
-               "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
+               "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
                "nlb_strerror")
 AGG_HIDDEN = 64
 RNN_MAX_DIM = 1024
 DTYPE_F32, DTYPE_BF16 = 0, 1
 RNN_FORM_NONE, RNN_FORM_TILED, RNN_FORM_WEIGHT_STATIONARY = 0, 1, 2
+ATT_MAX_DIM, ATT_MAX_HEADS, ATT_MAX_BUCKETS = 128, 256, 64
 EID_LAST_BATCH = 2**64 - 1   # first_eid of rnn_update: the links inserted last (device count)
 
 
@@ -64,6 +65,17 @@ class _GruWeights(ctypes.Structure):
     _fields_ = [("status_dim", ctypes.c_int32), ("status_dtype", ctypes.c_int32),
                 ("edge_dtype", ctypes.c_int32)] + \
                [(k, ctypes.c_void_p) for k in ("w_ih", "w_hh", "b_ih", "b_hh")]
+
+
+class _AttRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _AttCall(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "heads", "kv_heads", "dim", "causal", "buckets")] + \
+               [("scale", ctypes.c_float)] + [(k, ctypes.c_uint32) for k in ("batch", "q_rows", "k_rows")] + \
+               [(k, ctypes.c_void_p) for k in ("q_start", "k_start", "bias", "bounds", "q_pos", "k_pos")] + \
+               [(k, _AttRows) for k in ("q", "k", "v")]
 
 
 class _Info(ctypes.Structure):
@@ -111,6 +123,11 @@ def load_library(path: str | None = None):
     lib.nlb_rnn_update.restype = I
     lib.nlb_rnn_update_noalloc.argtypes = [P, P, P, P, U32, U64, ctypes.POINTER(_GruWeights), P, P]
     lib.nlb_rnn_update_noalloc.restype = I
+    S, R = ctypes.c_size_t, ctypes.POINTER(_AttRows)
+    lib.nlb_attention_work.argtypes = [ctypes.POINTER(_AttCall), ctypes.c_int32, ctypes.POINTER(S)]
+    lib.nlb_attention_work.restype = I
+    lib.nlb_attention.argtypes = [ctypes.POINTER(_AttCall), R, P, P, S, P]
+    lib.nlb_attention.restype = I
     lib.nlb_destroy.argtypes = [P]
     lib.nlb_destroy.restype = I
     lib.nlb_get_info.argtypes = [P, ctypes.POINTER(_Info)]
@@ -390,3 +407,148 @@ class Table:
         inf = _Info()
         _check(self._lib.nlb_get_info(self._h, ctypes.byref(inf)), "nlb_get_info")
         return {k: getattr(inf, k) for k, _ in _Info._fields_}
+
+
+# ---------------------------------------------------------------- operators without a table
+def _float_dtype(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+
+
+def _like(t, q, name):
+    if t.dtype != q.dtype or t.device != q.device:
+        raise TypeError(f"{name} must have q's type and device")
+    return t
+
+
+def _att_rows(t, q, shape, name):
+    """[rows, heads, dim] with contiguous values, any row and head strides."""
+    if tuple(_like(t, q, name).shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return _AttRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _int_vector(t, n, q, name):
+    import torch
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.uint32):
+        raise TypeError(f"{name} must be an int32 (or uint32) tensor")
+    if t.device != q.device:
+        raise TypeError(f"{name} must be on q's device")
+    if t.dim() != 1 and name not in ("q_pos", "k_pos"):
+        raise ValueError(f"{name} must be one-dimensional")
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements")
+    return _dev_ptr(t, 4, name)
+
+
+def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos):
+    import torch
+    c = _AttCall()
+    c.dtype = _float_dtype(q, "q")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [rows, heads, dim]")
+    c.device = q.device.index
+    c.q_rows, c.heads, c.dim = q.shape
+    c.k_rows, c.kv_heads = k.shape[0], k.shape[1]
+    if batch is None:
+        starts = q_start if q_start is not None else k_start
+        batch = 1 if starts is None else starts.numel() - 1
+    c.batch = int(batch)
+    c.q_start = _int_vector(q_start, c.batch + 1, q, "q_start")
+    c.k_start = _int_vector(k_start, c.batch + 1, q, "k_start")
+    c.causal = int(bool(causal))
+    c.scale = float(scale) if scale is not None else max(1, c.dim) ** -0.5
+    kv = (c.k_rows, c.kv_heads, c.dim)
+    c.q, c.k, c.v = _att_rows(q, q, q.shape, "q"), _att_rows(k, q, kv, "k"), _att_rows(v, q, kv, "v")
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[1] != c.heads:
+            raise ValueError("bias must be [buckets, heads]")
+        c.buckets = bias.shape[0]
+        c.bias = _dev_ptr(_like(bias, q, "bias"), None, "bias")
+        if bounds is not None or c.buckets != 1:
+            if bounds is None or bounds.dtype != torch.int32:
+                raise TypeError("bounds must be an int32 tensor")
+            c.bounds = _int_vector(bounds, c.buckets - 1, q, "bounds")
+    elif bounds is not None:
+        raise ValueError("bounds without bias")
+    c.q_pos = _int_vector(q_pos, c.q_rows, q, "q_pos")
+    c.k_pos = _int_vector(k_pos, c.k_rows, q, "k_pos")
+    return c
+
+
+class _OnStream:
+    """The stream of a call on tensors of `device` (default: that device's
+    current one), made current so that what the call allocates belongs to it."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.stream = torch.cuda.current_stream(device) if stream is None else stream
+        if self.stream.device != device:
+            raise ValueError("the stream must be on the tensors' device")
+        self._as_current = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self._as_current is not None:
+            self._as_current.__enter__()
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self._as_current is not None:
+            self._as_current.__exit__(*exc)
+
+
+def _work(n, work, like):
+    import torch
+    if work is None:
+        work = torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+    elif not work.is_cuda or work.device != like.device or not work.is_contiguous():
+        raise TypeError("work must be a contiguous tensor on the call's device")
+    return work, None if work is None else work.data_ptr(), 0 if work is None else work.numel() * work.element_size()
+
+
+def attention_work(q, k, v, *, backward=False, batch=None, q_start=None, k_start=None, causal=False, scale=None,
+                   bias=None, bounds=None, q_pos=None, k_pos=None) -> int:
+    """Bytes of working memory that such a call takes (``work=``)."""
+    c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
+    n = ctypes.c_size_t()
+    _check(load_library().nlb_attention_work(ctypes.byref(c), int(bool(backward)), ctypes.byref(n)),
+           "nlb_attention_work")
+    return n.value
+
+
+def attention(q, k, v, *, batch=None, q_start=None, k_start=None, causal=False, scale=None, bias=None, bounds=None,
+              q_pos=None, k_pos=None, out=None, lse=None, work=None, stream=None):
+    """Softmax attention over packed sequences (nlb_attention): ``q``
+    [q_rows, heads, dim] over ``k``, ``v`` [k_rows, kv_heads, dim], float32 or
+    bfloat16, any row and head strides.  ``q_start``, ``k_start``: int32
+    [batch + 1] first rows, or None for rows / batch each.  ``bias``
+    [buckets, heads] with ``bounds`` int32 [buckets - 1] on the gap between
+    ``q_pos`` and ``k_pos`` (a ts answer goes in as k_pos with its tq as
+    q_pos) or, without them, between places.  ``scale`` defaults to
+    dim ** -0.5.  ``work``: working memory of attention_work bytes, allocated
+    if None.  Returns (or fills) out (as q) and lse, fp32 [q_rows, heads]."""
+    import torch
+    lib = load_library()
+    c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
+    with _OnStream(q.device, stream) as s:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        o = _att_rows(out, q, q.shape, "out")
+        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != q.device:
+            raise ValueError("lse must be float32 [q_rows, heads] on q's device")
+        n = ctypes.c_size_t()
+        _check(lib.nlb_attention_work(ctypes.byref(c), 0, ctypes.byref(n)), "nlb_attention")
+        keep, p, size = _work(n.value, work, q)
+        _check(lib.nlb_attention(ctypes.byref(c), ctypes.byref(o), _dev_ptr(lse, 4, "lse"), p, size, s),
+               "nlb_attention")
+    return out, lse

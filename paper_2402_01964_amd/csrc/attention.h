@@ -1,0 +1,512 @@
+// attention.h -- what the attention kernels share: a call's arguments on the
+// device, the packed sequences' tiles, the position bias, tile staging and the
+// matrix products.  Private to libnlb.so.
+//
+// The mathematics, for query row i and key j of one sequence and one head:
+//   t_ij = (scale q_i.k_j + bias[bucket(pos_i - pos_j)]) log2(e)
+//   L_i  = log2 sum_j 2^t_ij over the open keys,  p_ij = 2^(t_ij - L_i)
+//   o_i  = sum_j p_ij v_j
+// Everything after the products of q and k works in powers of two (one
+// hardware exponential); what a caller sees (lse) is natural.
+//
+// Matrix products.  Tiles are 32 x 32 matrix-core blocks.  A block of scores
+// is computed transposed to its use: its columns (one per lane of a half
+// wavefront) are the rows that a wavefront owns, its rows lie in registers,
+// half a wavefront's registers holding rows 8 (r / 4) + 4 (half) + r % 4.
+// Products that contract over those rows take the block as their right
+// operand straight from the registers (any order of the contracted index
+// serves, so the left operand is read in that order), and everything kept per
+// owned row (running maximum, sum, log of the sum) is one value per lane.
+// bf16 inputs run on 32x32x16 products, fp32 inputs on 32x32x2 fp32 products;
+// sums are fp32.  The bf16 kernels round p and ds to bf16 for the products
+// that contract over them (a relative 2^-9 of each term, like the rounding of
+// the result itself); sums and statistics take them unrounded.
+#pragma once
+
+#include "nlb_internal.h"
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef int16_t i16x4 __attribute__((ext_vector_type(4)));
+// 16 and 8 bytes of a row at its element's alignment (global accesses of any
+// alignment are legal on gfx950).
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+constexpr int kThreads = 256;            // four wavefronts, everywhere
+constexpr int kOwned = 128;              // rows that a tiled workgroup owns, 32 per wavefront
+constexpr int kMaxBuckets = NLB_ATT_MAX_BUCKETS;
+static_assert(kMaxBuckets == 64, "bucket_of takes six steps");
+constexpr float kBiasCloses = -0x1p100f; // bias values at or below this close their bucket
+
+struct Strided {
+    const uint8_t *p;
+    int64_t row, head;                   // bytes
+};
+
+// One call on the device.
+struct Attend {
+    Strided q, k, v, o, dout;            // o: written forward, read backward
+    Strided dq, dk, dv;
+    float *lse;                          // [q_rows][heads], natural
+    float *delta;                        // [q_rows][heads]
+    const int32_t *q_start, *k_start;
+    uint32_t batch, q_rows, k_rows, q_len, k_len;   // *_len: rows of every sequence where *_start is null
+    uint32_t heads, kv_heads, group, dim;
+    uint32_t causal, buckets;
+    float scale, scale2;                 // scale2: scale log2(e)
+    const int32_t *bounds;
+    const void *bias;                    // [buckets][heads]
+    const uint32_t *q_pos, *k_pos;
+    float *part;                         // partial results (see the kernels)
+    uint32_t slots, chunk;
+};
+
+struct Seq {
+    uint32_t q0, k0;                     // first rows
+    int32_t lq, lk;
+    uint32_t tile;                       // the workgroup's tile in it
+};
+
+__device__ __forceinline__ uint32_t first_row(const int32_t *start, uint32_t len, uint32_t total, uint32_t b) {
+    if (!start) return b * len;
+    const int32_t s = start[b];
+    return s < 0 ? 0u : min((uint32_t)s, total);
+}
+
+// A sequence's rows, whatever its start values say, lie inside its tensor.
+__device__ __forceinline__ void sequence(const Attend &a, uint32_t b, Seq &s) {
+    s.q0 = first_row(a.q_start, a.q_len, a.q_rows, b);
+    s.lq = max(0, (int32_t)(first_row(a.q_start, a.q_len, a.q_rows, b + 1) - s.q0));
+    s.k0 = first_row(a.k_start, a.k_len, a.k_rows, b);
+    s.lk = max(0, (int32_t)(first_row(a.k_start, a.k_len, a.k_rows, b + 1) - s.k0));
+}
+
+// Packed sequences in tiles of n rows without a list of tiles: sequence b owns
+// the slots from start[b] / n + b on, of which the next sequence's first
+// leaves it at least as many as it has tiles (rounded up), so total / n +
+// batch slots cover any lengths and the host need not know them.  The owner
+// of a slot is found 64 candidates at a time.
+__device__ __forceinline__ uint32_t slot_owner(const int32_t *start, uint32_t len, uint32_t total, uint32_t batch,
+                                               uint32_t n, uint32_t slot, uint32_t &tile) {
+    uint32_t lo = 0, hi = batch;
+    const uint32_t lane = threadIdx.x & 63u;
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo + 63u) / 64u, b = lo + lane * step;
+        const bool below = b < hi && first_row(start, len, total, b) / n + b <= slot;
+        const uint64_t m = __ballot(below);
+        if (!m) break;
+        lo += (63u - (uint32_t)__builtin_clzll(m)) * step;
+        hi = min(hi, lo + step);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    tile = __builtin_amdgcn_readfirstlane(slot - (first_row(start, len, total, lo) / n + lo));
+    return lo;
+}
+
+// ---------------------------------------------------------------- values
+template <typename T> __device__ __forceinline__ float to_float(T x) { return (float)x; }
+
+template <typename T> struct Chunk;      // 16 bytes of a row
+template <> struct Chunk<__bf16> { static constexpr int n = 8; };
+template <> struct Chunk<float> { static constexpr int n = 4; };
+
+// 16 bytes from value c0 of a row of dim values, zeros past its end.
+template <typename T>
+__device__ __forceinline__ u32x4 load_chunk(const uint8_t *row, uint32_t c0, uint32_t dim) {
+    constexpr uint32_t n = Chunk<T>::n;
+    const uint8_t *p = row + c0 * sizeof(T);
+    u32x4 x = {0, 0, 0, 0};
+    if (c0 + n <= dim) {
+        x = *(const u32x4_any *)p;
+    } else if (c0 < dim) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (uint32_t i = 0; i < 3; i++)
+                if (c0 + i < dim) x[i] = ((const uint32_t *)p)[i];
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < 7; i++)
+                if (c0 + i < dim) x[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
+        }
+    }
+    return x;
+}
+
+template <typename T> __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Chunk<T>::n]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) f[i] = __uint_as_float(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            f[2 * i] = __uint_as_float(x[i] << 16);
+            f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        }
+    }
+}
+
+// Values c0 .. c0 + n - 1 of a row of dim values (those past its end are not written).
+template <typename T, int N>
+__device__ __forceinline__ void store_values(uint8_t *row, uint32_t c0, uint32_t dim, const float (&f)[N]) {
+    T v[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = (T)f[i];
+    T *p = (T *)row + c0;
+    if (c0 + N <= dim) {
+        if constexpr (N * sizeof(T) == 16) {
+            u32x4 w;
+            __builtin_memcpy(&w, v, 16);
+            *(u32x4_any *)p = w;
+        } else {
+            static_assert(N * sizeof(T) == 8, "");
+            u32x2 w;
+            __builtin_memcpy(&w, v, 8);
+            *(u32x2_any *)p = w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N - 1; i++)
+            if (c0 + i < dim) p[i] = v[i];
+    }
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+
+// A lane's value with the one of its column in the other half wavefront.
+__device__ __forceinline__ float halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The sum over each group of N neighbouring lanes, in every lane of the group.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
+    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+template <int N> __device__ __forceinline__ float lanes_sum(float x) {
+    if constexpr (N > 1) x = dpp_add<0xB1>(x);     // lane ^ 1
+    if constexpr (N > 2) x = dpp_add<0x4E>(x);     // lane ^ 2
+    if constexpr (N > 4) x = dpp_add<0x141>(x);    // the other half of eight (groups of 4 are equal by now)
+    if constexpr (N > 8) x = dpp_add<0x140>(x);    // the other half of sixteen
+    if constexpr (N > 16) x += __uint_as_float(__builtin_amdgcn_ds_swizzle(__float_as_uint(x), 0x401F));
+    return x;
+}
+
+// ---------------------------------------------------------------- bias
+// The gap between two positions, unsigned 32-bit values, clamped to int32
+// (flipped positions are order-preserving signed ones).
+__device__ __forceinline__ int32_t flip(uint32_t p) { return (int32_t)(p ^ 0x80000000u); }
+__device__ __forceinline__ int32_t gap_of(int32_t qf, int32_t kf) { return __builtin_elementwise_sub_sat(qf, kf); }
+
+// The bounds in LDS, padded to 64 with the largest value.
+__device__ __forceinline__ uint32_t bucket_of(const int32_t *bounds, uint32_t buckets, int32_t gap) {
+    uint32_t n = 0;
+#pragma unroll
+    for (uint32_t step = 32; step; step >>= 1)
+        if (bounds[n + step - 1] <= gap) n += step;
+    return min(n, buckets - 1);
+}
+
+// One head's bias in powers of two.
+template <typename T> __device__ __forceinline__ float bias2_of(const Attend &a, uint32_t b, uint32_t head) {
+    const float x = (float)((const T *)a.bias)[(size_t)b * a.heads + head];
+    return x <= kBiasCloses ? -INFINITY : x * kLog2e;
+}
+
+// ---------------------------------------------------------------- tiles
+// Streamed rows of a tiled kernel, in LDS: `rows` rows of DP values, 16 bytes
+// of padding behind each, so that eight lanes reading 16 bytes of eight
+// consecutive rows use every bank once.
+template <typename T, int DP> struct Tile {
+    static constexpr int rows = sizeof(T) == 2 ? 64 : 32;
+    static constexpr int chunks = DP * sizeof(T) / 16;              // per row
+    static constexpr int stride = DP * sizeof(T) + 16;              // bytes
+    static constexpr int bytes = rows * stride;
+    static constexpr int per_thread = rows * chunks / kThreads;
+    static constexpr int blocks = rows / 32;
+    static_assert(rows * chunks % kThreads == 0, "");
+    typedef u32x4 Regs[per_thread];
+    typedef uint32_t Positions[per_thread];
+};
+
+// This thread's chunks of the tile whose first row is `base`; rows from n on are zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const uint8_t *base, int64_t stride,
+                                          int32_t n, uint32_t dim) {
+    using G = Tile<T, DP>;
+    const uint32_t c = threadIdx.x % G::chunks, r0 = threadIdx.x / G::chunks;
+#pragma unroll
+    for (int i = 0; i < G::per_thread; i++) {
+        const int32_t r = r0 + i * (kThreads / G::chunks);
+        reg[i] = u32x4{0, 0, 0, 0};
+        if (r < n) reg[i] = load_chunk<T>(base + r * stride, c * Chunk<T>::n, dim);
+    }
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void tile_store(uint8_t *lds, const typename Tile<T, DP>::Regs &reg) {
+    using G = Tile<T, DP>;
+    const uint32_t c = threadIdx.x % G::chunks, r0 = threadIdx.x / G::chunks;
+#pragma unroll
+    for (int i = 0; i < G::per_thread; i++)
+        *(u32x4 *)(lds + (r0 + i * (kThreads / G::chunks)) * G::stride + c * 16) = reg[i];
+}
+
+// The positions of the rows of this thread's chunks; from row n on none.
+template <typename T, int DP>
+__device__ __forceinline__ void tile_positions(typename Tile<T, DP>::Positions &pos, const uint32_t *p, int32_t n) {
+    using G = Tile<T, DP>;
+    const uint32_t r0 = threadIdx.x / G::chunks;
+#pragma unroll
+    for (int i = 0; i < G::per_thread; i++) {
+        const int32_t r = r0 + i * (kThreads / G::chunks);
+        pos[i] = r < n ? p[r] : kNoKey;
+    }
+}
+
+// Rows of closed keys may hold anything: they are multiplied as zeros.
+template <typename T, int DP>
+__device__ __forceinline__ void tile_close(typename Tile<T, DP>::Regs &reg,
+                                           const typename Tile<T, DP>::Positions &pos) {
+#pragma unroll
+    for (int i = 0; i < Tile<T, DP>::per_thread; i++)
+        if (pos[i] == kNoKey) reg[i] = u32x4{0, 0, 0, 0};
+}
+
+template <typename T, int DP>
+__device__ __forceinline__ void tile_store_positions(uint32_t *lds, const typename Tile<T, DP>::Positions &pos) {
+    using G = Tile<T, DP>;
+    if (threadIdx.x % G::chunks == 0)
+#pragma unroll
+        for (int i = 0; i < G::per_thread; i++) lds[threadIdx.x / G::chunks + i * (kThreads / G::chunks)] = pos[i];
+}
+
+// Owned rows as the right operand of products that contract over the row's
+// values: lane (column c, half h) holds row c's values 16 s + 8 h + (0..7) of
+// step s (bf16) or 8 s + 4 h + (0..3) (fp32): 16 bytes each.
+template <typename T, int DP> struct Owned {
+    static constexpr int steps = DP * sizeof(T) / 32;
+    u32x4 x[steps];
+};
+
+template <typename T, int DP>
+__device__ __forceinline__ void load_owned(Owned<T, DP> &f, const uint8_t *row, bool there, uint32_t dim) {
+    const uint32_t h = (threadIdx.x >> 5) & 1u;
+#pragma unroll
+    for (int s = 0; s < Owned<T, DP>::steps; s++) {
+        f.x[s] = u32x4{0, 0, 0, 0};
+        if (there) f.x[s] = load_chunk<T>(row, (2 * s + h) * Chunk<T>::n, dim);
+    }
+}
+
+// acc[row][c] += sum over values of tile[32 blk + row] . owned[c]
+template <typename T, int DP>
+__device__ __forceinline__ void product_rows(f32x16 &acc, const uint8_t *tile, int blk, const Owned<T, DP> &own) {
+    using G = Tile<T, DP>;
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint8_t *p = tile + (blk * 32 + (lane & 31u)) * G::stride + (lane >> 5) * 16;
+#pragma unroll
+    for (int s = 0; s < Owned<T, DP>::steps; s++) {
+        const u32x4 x = *(const u32x4 *)(p + s * 32);
+        if constexpr (sizeof(T) == 2) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                          __builtin_bit_cast(bf16x8, own.x[s]), acc, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(own.x[s][e]), acc, 0,
+                                                           0, 0);
+        }
+    }
+}
+
+// A score block as the right operand of a product that contracts over its rows.
+template <typename T> struct Scores;
+template <> struct Scores<__bf16> { bf16x8 x[2]; };
+template <> struct Scores<float> { float x[16]; };
+
+__device__ __forceinline__ void pack(Scores<__bf16> &s, const float (&p)[16]) {
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) s.x[u][e] = (__bf16)p[8 * u + e];
+}
+__device__ __forceinline__ void pack(Scores<float> &s, const float (&p)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; e++) s.x[e] = p[e];
+}
+
+// Four rows of one column of a row-major bf16 tile per lane, by the LDS
+// transposing read: in each group of 16 lanes, lanes 4 r .. 4 r + 3 name the
+// 16 columns of row r, and lane c gets column c of rows 0 .. 3.
+__device__ __forceinline__ i16x4 read_columns(const uint8_t *p) {
+    typedef __attribute__((address_space(3))) i16x4 *lds_ptr;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+}
+
+// acc[d block][value][c] += sum over the block's rows of tile[32 blk + row][value] scores[row][c]
+template <typename T, int DP>
+__device__ __forceinline__ void product_columns(f32x16 (&acc)[DP / 32], const uint8_t *tile, int blk,
+                                                const Scores<T> &s) {
+    using G = Tile<T, DP>;
+    const uint32_t lane = threadIdx.x & 63u, h = lane >> 5;
+    if constexpr (sizeof(T) == 2) {
+        const uint8_t *p = tile + (blk * 32 + 4 * h + ((lane & 15u) >> 2)) * G::stride +
+                           (16 * ((lane >> 4) & 1u) + 4 * (lane & 3u)) * 2;
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+            for (int d = 0; d < DP / 32; d++) {
+                const i16x4 lo = read_columns(p + (16 * u) * G::stride + d * 64);
+                const i16x4 hi = read_columns(p + (16 * u + 8) * G::stride + d * 64);
+                const auto x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), s.x[u], acc[d], 0, 0,
+                                                                 0);
+            }
+    } else {
+        const uint8_t *p = tile + (blk * 32 + 4 * h) * G::stride + (lane & 31u) * 4;
+#pragma unroll
+        for (int r = 0; r < 16; r++)
+#pragma unroll
+            for (int d = 0; d < DP / 32; d++)
+                acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                    *(const float *)(p + (8 * (r / 4) + r % 4) * G::stride + d * 128), s.x[r], acc[d], 0, 0, 0);
+    }
+}
+
+// The transposed result of a wavefront's rows: acc[d][r] is value
+// 32 d + 8 (r / 4) + 4 h + r % 4 of the lane's row.
+template <typename T, int DP>
+__device__ __forceinline__ void store_owned(uint8_t *row, uint32_t dim, const f32x16 (&acc)[DP / 32], float factor) {
+    const uint32_t h = (threadIdx.x >> 5) & 1u;
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const float f[4] = {acc[d][r] * factor, acc[d][r + 1] * factor, acc[d][r + 2] * factor,
+                                acc[d][r + 3] * factor};
+            const uint32_t c = 32 * d + 2 * r + 4 * h;
+            if (c < dim) store_values<T, 4>(row, c, dim, f);
+        }
+}
+
+// Row r of a score block, of the lane's half.
+__device__ __forceinline__ int block_row(int r) {
+    return 8 * (r / 4) + 4 * ((threadIdx.x >> 5) & 1u) + r % 4;
+}
+
+// ---------------------------------------------------------------- host
+// Rows of a call as the kernels take them.
+inline int fill_rows(const nlb_att_call *c, const nlb_att_rows *r, bool needed, Strided &out) {
+    const int64_t e = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
+    if (!r) return NLB_EINVAL;
+    if (needed && !r->data) return NLB_EINVAL;
+    if ((uintptr_t)r->data % e) return NLB_EINVAL;
+    if (r->row_stride < 0 || r->head_stride < 0 || r->row_stride > INT32_MAX || r->head_stride > INT32_MAX)
+        return NLB_EINVAL;
+    out = {(const uint8_t *)r->data, r->row_stride * e, r->head_stride * e};
+    return NLB_OK;
+}
+
+inline int fill_call(const nlb_att_call *c, Attend &a) {
+    a = {};
+    if (!c) return NLB_EINVAL;
+    if (c->dtype != NLB_DTYPE_F32 && c->dtype != NLB_DTYPE_BF16) return NLB_EINVAL;
+    if (c->dim < 1 || c->dim > NLB_ATT_MAX_DIM || c->heads < 1 || c->heads > NLB_ATT_MAX_HEADS) return NLB_EINVAL;
+    if (c->kv_heads < 1 || c->heads % c->kv_heads) return NLB_EINVAL;
+    if (!std::isfinite(c->scale)) return NLB_EINVAL;
+    if (c->causal != 0 && c->causal != 1) return NLB_EINVAL;
+    if (c->batch < 1 || c->batch > INT32_MAX / NLB_ATT_MAX_HEADS || c->q_rows > INT32_MAX || c->k_rows > INT32_MAX)
+        return NLB_EINVAL;
+    if ((!c->q_start && c->q_rows % c->batch) || (!c->k_start && c->k_rows % c->batch)) return NLB_EINVAL;
+    if (c->buckets < 0 || c->buckets > NLB_ATT_MAX_BUCKETS) return NLB_EINVAL;
+    if ((c->buckets > 0) != (c->bias != nullptr) || (c->buckets > 1 && !c->bounds)) return NLB_EINVAL;
+    if (c->q_pos && !c->k_pos && c->k_rows) return NLB_EINVAL;
+    if (c->buckets > 0 && !c->q_pos && c->k_pos && c->q_rows) return NLB_EINVAL;
+    if (((uintptr_t)c->q_start | (uintptr_t)c->k_start | (uintptr_t)c->bounds | (uintptr_t)c->q_pos |
+         (uintptr_t)c->k_pos) % 4)
+        return NLB_EINVAL;
+    if ((uintptr_t)c->bias % (c->dtype == NLB_DTYPE_BF16 ? 2 : 4)) return NLB_EINVAL;
+    if (fill_rows(c, &c->q, c->q_rows > 0, a.q) != NLB_OK || fill_rows(c, &c->k, c->k_rows > 0, a.k) != NLB_OK ||
+        fill_rows(c, &c->v, c->k_rows > 0, a.v) != NLB_OK)
+        return NLB_EINVAL;
+    a.q_start = c->q_start;
+    a.k_start = c->k_start;
+    a.batch = c->batch;
+    a.q_rows = c->q_rows;
+    a.k_rows = c->k_rows;
+    a.q_len = c->q_rows / c->batch;
+    a.k_len = c->k_rows / c->batch;
+    a.heads = c->heads;
+    a.kv_heads = c->kv_heads;
+    a.group = c->heads / c->kv_heads;
+    a.dim = c->dim;
+    a.causal = c->causal;
+    a.buckets = c->buckets;
+    a.scale = c->scale;
+    a.scale2 = c->scale * kLog2e;
+    a.bounds = c->bounds;
+    a.bias = c->bias;
+    a.q_pos = c->q_pos;
+    a.k_pos = c->k_pos;
+    return NLB_OK;
+}
+
+inline int device_of(const nlb_att_call *c, int &dev) {
+    int n = 0;
+    dev = c->device;
+    if (hipGetDeviceCount(&n) != hipSuccess || n < 1) return NLB_EDEVICE;
+    if (dev < 0 && hipGetDevice(&dev) != hipSuccess) return NLB_EDEVICE;
+    return dev < n ? NLB_OK : NLB_EINVAL;
+}
+
+inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Forward {
+    bool one;                            // one query row per sequence
+    uint32_t chunk;                      // keys of a wavefront then
+    uint64_t slots, most;
+    size_t bytes;
+};
+
+// One query row per sequence: a wavefront a list until lists are too few to
+// fill the card (8 wavefronts on each of 1024 SIMDs), then chunks of the keys,
+// of 256 rows at least, so that what a chunk writes stays below a hundredth of
+// what it reads.
+inline Forward plan_forward(const Attend &a) {
+    Forward f = {};
+    f.one = !a.q_start && a.q_len == 1;
+    if (!f.one) {
+        f.slots = (uint64_t)a.q_rows / kOwned + a.batch;
+        f.most = INT32_MAX / a.heads;
+        return f;
+    }
+    const uint64_t even = ((uint64_t)a.k_rows * a.kv_heads + 8191) / 8192;
+    f.chunk = (uint32_t)(((even < 256 ? 256 : even) + 63) / 64 * 64);
+    const bool split = a.k_start ? a.k_rows > f.chunk : a.k_len > f.chunk;
+    f.slots = split ? (uint64_t)a.k_rows / f.chunk + a.batch : a.batch;
+    f.most = INT32_MAX;
+    f.bytes = split ? align256(f.slots * a.heads * (a.dim + 2) * 4) : 0;
+    return f;
+}
+
+struct Backward {
+    size_t bytes;
+};
+
+inline Backward plan_backward(const Attend &a) {
+    Backward p = {};
+    p.bytes = align256((size_t)a.q_rows * a.heads * 4);
+    return p;
+}
+
+}  // namespace

@@ -1,0 +1,439 @@
+// attention.hip -- softmax attention over packed sequences, forward: tiles of
+// query rows (attend_tiles), and one query row per sequence (attend_one,
+// attend_join).
+#include "attention.h"
+
+#include <algorithm>
+
+namespace {
+
+// ---------------------------------------------------------------- tiles
+// A workgroup owns 128 query rows of one head and streams the keys and values
+// in tiles of 64 (fp32: 32) rows through two LDS buffers: the next tile's
+// global loads are in flight in registers while this one is multiplied, one
+// barrier a tile.  A wavefront owns 32 rows; its scores are columns (see
+// attention.h), so its softmax statistics are one value per lane and the
+// probabilities go to the second product from the registers they are in.
+// The running maximum follows a row's scores only when they pass it by more
+// than 2^8: until then the sums carry factors of at most 2^8 and the
+// accumulated values need no scaling.
+//
+// POS: 0 no bias and no closed keys; 1 bias by places: of a tile's gaps there
+// are 32 + 128 - 1 at most, so their bias values are looked up once per tile;
+// 2 positions given (bias by their gaps, closed keys).
+constexpr int kGaps = 192;
+
+template <typename T, int DP> constexpr uint32_t tiles_lds() {
+    return 4 * Tile<T, DP>::bytes + 2 * kGaps * 4 + kMaxBuckets * 8;
+}
+
+template <typename T, int DP, int POS>
+__global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
+    using G = Tile<T, DP>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float *extra = (float *)(lds + 4 * G::bytes);             // [2][kGaps]: bias by gap, or positions
+    int32_t *bounds = (int32_t *)(extra + 2 * kGaps);
+    float *bias = (float *)(bounds + kMaxBuckets);
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
+
+    // heads of one key/value head follow each other at a distance of kv_heads:
+    // workgroups that are dispatched to one XCD share keys and values
+    const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
+    const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
+    Seq sq;
+    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, kOwned, slot, sq.tile);
+    sequence(a, b, sq);
+    if (sq.tile >= ((uint32_t)sq.lq + kOwned - 1) / kOwned) return;
+    const int32_t row0 = sq.tile * kOwned, row = row0 + wave * 32 + col, off = sq.lk - sq.lq;
+    const bool there = row < sq.lq;
+
+    if constexpr (POS != 0) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads) {
+            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+            bias[i] = i < a.buckets ? bias2_of<T>(a, i, head) : 0.0f;
+        }
+        __syncthreads();
+    }
+
+    Owned<T, DP> q;
+    load_owned(q, a.q.p + (int64_t)(sq.q0 + row) * a.q.row + head * a.q.head, there, a.dim);
+    int32_t qpos = 0;
+    if constexpr (POS == 2)
+        if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
+
+    // keys [0, kend) are open to some row of the workgroup, [0, wend) of the wavefront
+    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wlast = min(row0 + (int32_t)wave * 32 + 32, sq.lq) - 1;
+    const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
+    const int32_t wend = a.causal ? min(sq.lk, wlast + off + 1) : sq.lk;
+    const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;   // keys open to this lane's row
+    const uint8_t *kbase = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
+    const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
+
+    u32x4 kreg[G::per_thread], vreg[G::per_thread];
+    uint32_t preg[POS == 2 ? G::per_thread : 1];
+    const auto fetch = [&](int32_t k0) {
+        tile_load<T, DP>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
+    };
+    // writes the fetched tile and what the bias needs of it
+    const auto stage = [&](int32_t k0, int buf) {
+        uint8_t *kt = lds + buf * 2 * G::bytes;
+        if constexpr (POS == 2) {
+            tile_close<T, DP>(kreg, preg);
+            tile_close<T, DP>(vreg, preg);
+            tile_store_positions<T, DP>((uint32_t *)extra + buf * kGaps, preg);
+        }
+        tile_store<T, DP>(kt, kreg);
+        tile_store<T, DP>(kt + G::bytes, vreg);
+        if constexpr (POS == 1) {
+            const int32_t x = (int32_t)threadIdx.x;   // gap of x: row0 + off - k0 + x - (rows - 1)
+            if (x < kOwned + G::rows - 1)
+                extra[buf * kGaps + x] = bias[bucket_of(bounds, a.buckets, row0 + off - k0 + x - (G::rows - 1))];
+        }
+    };
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++) acc[d] = f32x16{};
+    float m = -INFINITY, sum = 0.0f;
+
+    if (kend > 0) {
+        fetch(0);
+        stage(0, 0);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= 1) {
+        const bool more = k0 + G::rows < kend;
+        if (more) fetch(k0 + G::rows);
+        if (k0 < wend) {
+            const uint8_t *kt = lds + buf * 2 * G::bytes, *vt = kt + G::bytes;
+            float t[G::blocks][16];
+            const bool ragged = k0 + G::rows > (a.causal ? min(sq.lk, row0 + (int32_t)wave * 32 + off + 1) : sq.lk);
+            float top = -INFINITY;
+#pragma unroll
+            for (int blk = 0; blk < G::blocks; blk++) {
+                f32x16 s = {};
+                product_rows<T, DP>(s, kt, blk, q);
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const int kr = blk * 32 + block_row(r);
+                    float x = s[r] * a.scale2;
+                    if constexpr (POS == 1) x += extra[buf * kGaps + wave * 32 + col + (G::rows - 1) - kr];
+                    if constexpr (POS == 2) {
+                        const uint32_t kp = ((const uint32_t *)extra)[buf * kGaps + kr];
+                        if (a.buckets) x += bias[bucket_of(bounds, a.buckets, gap_of(qpos, flip(kp)))];
+                        if (kp == kNoKey) x = -INFINITY;
+                    }
+                    if (ragged && k0 + kr >= limit) x = -INFINITY;
+                    t[blk][r] = x;
+                    top = fmaxf(top, x);
+                }
+            }
+            top = halves_max(top);
+            if (__any(top > m + 8.0f)) {
+                const float up = fmaxf(m, top);
+                const float f = up == -INFINITY ? 1.0f : exp2_fast(m - up);
+                m = up;
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+                    for (int r = 0; r < 16; r++) acc[d][r] *= f;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+            for (int blk = 0; blk < G::blocks; blk++) {
+                Scores<T> p;
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    t[blk][r] = exp2_fast(t[blk][r] - base);
+                    sum += t[blk][r];
+                }
+                pack(p, t[blk]);
+                product_columns<T, DP>(acc, vt, blk, p);
+            }
+        }
+        if (more) stage(k0 + G::rows, buf ^ 1);
+        __syncthreads();
+    }
+    sum = halves_sum(sum);
+    if (!there) return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    store_owned<T, DP>((uint8_t *)a.o.p + (int64_t)(sq.q0 + row) * a.o.row + head * a.o.head, a.dim, acc, inv);
+    if (a.lse && lane < 32)
+        a.lse[(size_t)(sq.q0 + row) * a.heads + head] = sum == 0.0f ? -INFINITY : (m + log2_fast(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------- one query row
+// A sequence's single query row (a retrieved list, or a new token over a long
+// history) is bound by reading its keys and values once.  A wavefront takes up
+// to GB query heads of one key/value head over at most `chunk` keys; a row's
+// values lie across DP / (values in 16 bytes) neighbouring lanes, so one load
+// takes a row from each of 64 / that many keys, and U such loads of keys and
+// of values are in flight.  Each group of lanes keeps its own running maximum,
+// sum and weighted values; the groups join once at the end.  Longer sequences
+// have several chunks, whose results (maximum, sum, values in fp32) go to
+// `part` and are joined by attend_join.  Wavefronts take chunk after chunk, so
+// the bias table is staged once.
+template <typename T, int DP> struct Lanes {
+    static constexpr int per_row = DP / Chunk<T>::n;
+    static constexpr int rows = 64 / per_row;
+};
+
+template <typename T, int DP, int GB>
+__global__ __launch_bounds__(kThreads) void attend_one(Attend a) {
+    using L = Lanes<T, DP>;
+    constexpr int N = Chunk<T>::n, U = 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    int32_t *bounds = (int32_t *)lds;
+    float *bias = (float *)(bounds + kMaxBuckets);            // [buckets][heads]
+    if (a.buckets) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads)
+            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+        for (uint32_t i = threadIdx.x; i < a.buckets * a.heads; i += kThreads)
+            bias[i] = bias2_of<T>(a, i / a.heads, i % a.heads);
+        __syncthreads();
+    }
+    const uint32_t lane = threadIdx.x & 63u, c0 = (lane % L::per_row) * N, kr = lane / L::per_row;
+    const uint32_t parts = (a.group + GB - 1) / GB, per_slot = a.kv_heads * parts;
+    const uint64_t units = (uint64_t)a.slots * per_slot;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (uint64_t unit = blockIdx.x * 4ull + wave; unit < units; unit += gridDim.x * 4ull) {
+        const uint32_t slot = unit / per_slot, kvh = unit % a.kv_heads, g0 = (unit % per_slot) / a.kv_heads * GB;
+        const uint32_t head0 = kvh * a.group + g0, ng = min((uint32_t)GB, a.group - g0);
+        Seq sq;
+        uint32_t b = slot;
+        sq.tile = 0;
+        if (a.slots != a.batch) b = slot_owner(a.k_start, a.k_len, a.k_rows, a.batch, a.chunk, slot, sq.tile);
+        sequence(a, b, sq);
+        const uint32_t chunks = max(1u, ((uint32_t)sq.lk + a.chunk - 1) / a.chunk);
+        if (sq.tile >= chunks) continue;
+        const int32_t first = sq.tile * a.chunk, n = min((int32_t)a.chunk, sq.lk - first);
+
+        float q[GB][N], acc[GB][N], m[GB], sum[GB];
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            u32x4 x = {0, 0, 0, 0};
+            if ((uint32_t)g < ng)
+                x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
+            unpack<T>(x, q[g]);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                q[g][i] *= a.scale2;
+                acc[g][i] = 0.0f;
+            }
+            m[g] = -INFINITY;
+            sum[g] = 0.0f;
+        }
+        const int32_t qpos = a.buckets ? (a.q_pos ? flip(a.q_pos[b]) : flip((uint32_t)sq.lk - 1)) : 0;
+        const uint8_t *kp = a.k.p + (int64_t)(sq.k0 + first) * a.k.row + kvh * a.k.head;
+        const uint8_t *vp = a.v.p + (int64_t)(sq.k0 + first) * a.v.row + kvh * a.v.head;
+        for (int32_t j0 = 0; j0 < n; j0 += L::rows * U) {
+            u32x4 k[U], v[U];
+            uint32_t pos[U];
+            bool open[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const int32_t j = j0 + u * L::rows + kr;
+                open[u] = j < n;
+                pos[u] = first + j;
+                if (a.k_pos && open[u]) {
+                    pos[u] = a.k_pos[sq.k0 + first + j];
+                    open[u] = pos[u] != kNoKey;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const int32_t j = j0 + u * L::rows + kr;
+                k[u] = v[u] = u32x4{0, 0, 0, 0};
+                if (open[u]) {
+                    k[u] = load_chunk<T>(kp + j * a.k.row, c0, a.dim);
+                    v[u] = load_chunk<T>(vp + j * a.v.row, c0, a.dim);
+                }
+            }
+            float t[U][GB];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                float x[N];
+                unpack<T>(k[u], x);
+#pragma unroll
+                for (int g = 0; g < GB; g++) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < N; i++) s = fmaf(q[g][i], x[i], s);
+                    t[u][g] = lanes_sum<L::per_row>(s);
+                }
+                const uint32_t at =
+                    a.buckets ? bucket_of(bounds, a.buckets, gap_of(qpos, flip(pos[u]))) * a.heads + head0 : 0;
+#pragma unroll
+                for (int g = 0; g < GB; g++) {
+                    if (a.buckets && (uint32_t)g < ng) t[u][g] += bias[at + g];
+                    if (!open[u]) t[u][g] = -INFINITY;
+                }
+            }
+            float p[U][GB];
+#pragma unroll
+            for (int g = 0; g < GB; g++) {
+                float up = m[g];
+#pragma unroll
+                for (int u = 0; u < U; u++) up = fmaxf(up, t[u][g]);
+                const float base = up == -INFINITY ? 0.0f : up, f = exp2_fast(m[g] - base);
+                m[g] = up;
+                sum[g] *= f;
+#pragma unroll
+                for (int i = 0; i < N; i++) acc[g][i] *= f;
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    p[u][g] = exp2_fast(t[u][g] - base);
+                    sum[g] += p[u][g];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                float x[N];
+                unpack<T>(v[u], x);
+#pragma unroll
+                for (int g = 0; g < GB; g++)
+#pragma unroll
+                    for (int i = 0; i < N; i++) acc[g][i] = fmaf(p[u][g], x[i], acc[g][i]);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            if ((uint32_t)g >= ng) break;
+            float up = m[g];
+#pragma unroll
+            for (int w = L::per_row; w < 64; w *= 2) up = fmaxf(up, __shfl_xor(up, w));
+            const float base = up == -INFINITY ? 0.0f : up, f = exp2_fast(m[g] - base);
+            sum[g] *= f;
+#pragma unroll
+            for (int i = 0; i < N; i++) acc[g][i] *= f;
+#pragma unroll
+            for (int w = L::per_row; w < 64; w *= 2) {
+                sum[g] += __shfl_xor(sum[g], w);
+#pragma unroll
+                for (int i = 0; i < N; i++) acc[g][i] += __shfl_xor(acc[g][i], w);
+            }
+            const uint32_t head = head0 + g;
+            if (chunks == 1) {
+                const float inv = sum[g] == 0.0f ? 0.0f : 1.0f / sum[g];
+#pragma unroll
+                for (int i = 0; i < N; i++) acc[g][i] *= inv;
+                if (kr == 0 && c0 < a.dim)
+                    store_values<T, N>((uint8_t *)a.o.p + (int64_t)b * a.o.row + head * a.o.head, c0, a.dim, acc[g]);
+                if (lane == 0 && a.lse)
+                    a.lse[(size_t)b * a.heads + head] =
+                        sum[g] == 0.0f ? -INFINITY : (up + log2_fast(sum[g])) * kLn2;
+            } else {
+                float *part = a.part + ((size_t)slot * a.heads + head) * (a.dim + 2);
+                if (lane == 0) {
+                    part[0] = up;
+                    part[1] = sum[g];
+                }
+                if (kr == 0)
+#pragma unroll
+                    for (int i = 0; i < N; i++)
+                        if (c0 + i < a.dim) part[2 + c0 + i] = acc[g][i];
+            }
+        }
+    }
+}
+
+// Joins the chunks of the sequences that have more than one: a wavefront per
+// sequence and head, values across its lanes.
+template <typename T>
+__global__ __launch_bounds__(64) void attend_join(Attend a) {
+    const uint32_t b = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = threadIdx.x;
+    Seq sq;
+    sequence(a, b, sq);
+    const uint32_t chunks = ((uint32_t)sq.lk + a.chunk - 1) / a.chunk;
+    if (chunks < 2) return;
+    const size_t step = (size_t)a.heads * (a.dim + 2);
+    const float *part = a.part + (size_t)(sq.k0 / a.chunk + b) * step + head * (a.dim + 2);
+    float m = -INFINITY;
+    for (uint32_t i = lane; i < chunks; i += 64) m = fmaxf(m, part[i * step]);
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) m = fmaxf(m, __shfl_xor(m, w));
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
+    for (uint32_t i = 0; i < chunks; i++) {
+        const float *p = part + i * step;
+        const float f = exp2_fast(p[0] - base);
+        sum = fmaf(f, p[1], sum);
+        if (lane < a.dim) x0 = fmaf(f, p[2 + lane], x0);
+        if (lane + 64 < a.dim) x1 = fmaf(f, p[2 + lane + 64], x1);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    T *o = (T *)(a.o.p + (int64_t)b * a.o.row + head * a.o.head);
+    if (lane < a.dim) o[lane] = (T)(x0 * inv);
+    if (lane + 64 < a.dim) o[lane + 64] = (T)(x1 * inv);
+    if (lane == 0 && a.lse) a.lse[(size_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (m + log2_fast(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------- launches
+template <typename T, int DP>
+int launch_tiles(const Attend &a, hipStream_t stream) {
+    const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
+    const auto kernel = pos == 2 ? attend_tiles<T, DP, 2> : pos == 1 ? attend_tiles<T, DP, 1> : attend_tiles<T, DP, 0>;
+    constexpr uint32_t bytes = tiles_lds<T, DP>();
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
+        return NLB_EDEVICE;
+    hipLaunchKernelGGL(kernel, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
+    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+}
+
+template <typename T, int DP>
+int launch_one(const Attend &a, hipStream_t stream) {
+    const int gb = a.group >= 4 ? 4 : a.group >= 2 ? 2 : 1;
+    const auto kernel = gb == 4 ? attend_one<T, DP, 4> : gb == 2 ? attend_one<T, DP, 2> : attend_one<T, DP, 1>;
+    const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4;
+    const uint64_t units = (uint64_t)a.slots * a.kv_heads * ((a.group + gb - 1) / gb);
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
+        return NLB_EDEVICE;
+    const uint32_t blocks = (uint32_t)std::min<uint64_t>((units + 3) / 4, 256 * 8);
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, stream, a);
+    if (a.slots != a.batch)
+        hipLaunchKernelGGL((attend_join<T>), dim3(a.batch * a.heads), dim3(64), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+}
+
+template <typename T> int launch(const Attend &a, bool one, hipStream_t s) {
+    if (a.dim <= 32) return one ? launch_one<T, 32>(a, s) : launch_tiles<T, 32>(a, s);
+    if (a.dim <= 64) return one ? launch_one<T, 64>(a, s) : launch_tiles<T, 64>(a, s);
+    return one ? launch_one<T, 128>(a, s) : launch_tiles<T, 128>(a, s);
+}
+
+}  // namespace
+
+extern "C" int nlb_attention_work(const nlb_att_call *c, int32_t backward, size_t *bytes) {
+    Attend a;
+    if (!bytes) return NLB_EINVAL;
+    const int rc = fill_call(c, a);
+    if (rc != NLB_OK) return rc;
+    *bytes = backward ? plan_backward(a).bytes : plan_forward(a).bytes;
+    return NLB_OK;
+}
+
+extern "C" int nlb_attention(const nlb_att_call *c, const nlb_att_rows *o, float *lse, void *work, size_t work_bytes,
+                             void *stream) {
+    Attend a;
+    int rc = fill_call(c, a);
+    if (rc != NLB_OK) return rc;
+    if ((rc = fill_rows(c, o, true, a.o)) != NLB_OK || (uintptr_t)lse % 4 || (uintptr_t)work % 16) return NLB_EINVAL;
+    const Forward f = plan_forward(a);
+    if (f.slots > f.most) return NLB_EINVAL;
+    if (work_bytes < f.bytes || (f.bytes && !work)) return NLB_ESCRATCH;
+    int dev;
+    if ((rc = device_of(c, dev)) != NLB_OK) return rc;
+    if (a.q_rows == 0) return NLB_OK;
+    DeviceGuard guard(dev);
+    if (!guard.ok()) return NLB_EDEVICE;
+    a.lse = lse;
+    a.part = (float *)work;
+    a.slots = (uint32_t)f.slots;
+    a.chunk = f.chunk;
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, f.one, (hipStream_t)stream)
+                                      : launch<float>(a, f.one, (hipStream_t)stream);
+}

@@ -1,0 +1,278 @@
+"""Attention over packed sequences on the GPU (nlb_attention and its backward
+pass) against 64 bits, within the bounds that attention_ref derives."""
+import numpy as np
+import pytest
+
+from tests import attention_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+BOUNDS = [-5, 0, 1, 2, 4, 9, 30, 100]
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+def _dtype(name):
+    import torch
+    return {"bf16": torch.bfloat16, "f32": torch.float32}[name]
+
+
+def make(dtype, lq, lk, heads, kv_heads, dim, *, bias=False, times=False, closed=0.2, train=False, seed=0, gap=0,
+         sharp=2.0):
+    """Inputs on the CPU; gap: values between a row's end and the next row's
+    head, so that nothing is contiguous or aligned."""
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    dt = _dtype(dtype)
+
+    def rows(n, h, scale=1.0):
+        return (scale * torch.randn(n, h, dim + gap, generator=gen)).to(dt)[:, :, gap // 2:gap // 2 + dim]
+    c = {"q": rows(sum(lq), heads, sharp), "k": rows(sum(lk), kv_heads), "v": rows(sum(lk), kv_heads), "bias": None,
+         "bounds": None, "q_pos": None, "k_pos": None, "do": rows(sum(lq), heads) if train else None}
+    if bias:
+        c["bias"] = torch.randn(len(BOUNDS) + 1, heads, generator=gen).to(dt)
+        c["bounds"] = torch.tensor(BOUNDS, dtype=torch.int32)
+    if times:
+        c["q_pos"] = torch.randint(0, 300, (sum(lq),), generator=gen, dtype=torch.int32)
+        c["k_pos"] = torch.randint(0, 300, (sum(lk),), generator=gen, dtype=torch.int32)
+        c["k_pos"][torch.rand(sum(lk), generator=gen) < closed] = -1
+    return c
+
+
+def _f64(t):
+    return None if t is None else t.double().numpy()
+
+
+def _u32(t):
+    return None if t is None else t.numpy().view(np.uint32)
+
+
+def _cuda(t):
+    """On the GPU with the strides it has."""
+    import torch
+    if t is None or t.is_contiguous():
+        return None if t is None else t.cuda()
+    full = torch.empty(t.untyped_storage().nbytes() // t.element_size(), dtype=t.dtype, device="cuda")
+    full = full.as_strided(t.size(), t.stride(), t.storage_offset())
+    full.copy_(t)
+    return full
+
+
+def run(c, lq, lk, *, causal, one=False, scale=None, **more):
+    """The library's outputs; one: single query rows without q_start."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    how = dict(batch=len(lq), causal=causal, scale=scale, **more)
+    if not one:
+        how["q_start"] = torch.from_numpy(ref.starts(lq)).cuda()
+    if len(set(lk)) > 1:
+        how["k_start"] = torch.from_numpy(ref.starts(lk)).cuda()
+    for n in ("bias", "bounds", "q_pos", "k_pos"):
+        how[n] = _cuda(c[n])
+    q, k, v, do = (_cuda(c[n]) for n in ("q", "k", "v", "do"))
+    o, lse = nlb.attention(q, k, v, **how)
+    got = {"o": o, "lse": lse}
+    if do is not None:
+        got["dq"], got["dk"], got["dv"], dbias = nlb.attention_backward(do, q, k, v, o, lse, **how)
+        if dbias is not None:
+            got["dbias"] = dbias
+    torch.cuda.synchronize()
+    return got
+
+
+def check(c, lq, lk, got, *, causal, dtype, scale=None, what=""):
+    dim = c["q"].shape[2]
+    want, far = ref.attention(_f64(c["q"]), _f64(c["k"]), _f64(c["v"]), lq, lk, u=HALF_STEP[dtype], causal=causal,
+                              scale=dim ** -0.5 if scale is None else scale, bias=_f64(c["bias"]),
+                              bounds=None if c["bounds"] is None else c["bounds"].numpy(), q_pos=_u32(c["q_pos"]),
+                              k_pos=_u32(c["k_pos"]), do=_f64(c["do"]))
+    for n, x in want.items():
+        g = got[n].double().cpu().numpy()
+        assert g.shape == x.shape, (what, n)
+        fine = np.isfinite(x)
+        assert np.array_equal(g[~fine], x[~fine]), (what, n, "infinities")
+        off = np.abs(g[fine] - x[fine]) - far[n][fine]
+        assert np.isfinite(g[fine]).all() and (off <= 0).all(), (
+            what, n, f"{(off > 0).sum()} of {off.size} values too far, worst by {np.nanmax(off):.3g}")
+
+
+LENGTHS = {
+    "one": ([1], [1]),
+    "odd": ([33, 1, 200, 0, 64], [40, 7, 200, 3, 20]),
+    "no keys": ([5, 70, 3], [0, 70, 0]),
+    "edges": ([127, 128, 129, 63, 64, 65], [127, 128, 129, 31, 300, 65]),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("mode", ["plain", "places", "times"])
+@pytest.mark.parametrize("dim", [1, 8, 25, 32, 50, 64, 100, 128])
+def test_packed_sequences(dtype, causal, mode, dim):
+    for name, (lq, lk) in LENGTHS.items():
+        heads, kv_heads = (4, 2) if dim != 25 else (3, 3)
+        c = make(dtype, lq, lk, heads, kv_heads, dim, bias=mode != "plain", times=mode == "times", seed=dim)
+        check(c, lq, lk, run(c, lq, lk, causal=causal), causal=causal, dtype=dtype, what=name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["plain", "places", "times"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 1), (4, 1, 25), (6, 2, 50), (7, 1, 64), (8, 8, 128), (2, 2, 33)])
+def test_single_rows(dtype, mode, heads, kv_heads, dim):
+    """Lists of one length (1, 10, 64, 700 slots) and of many, empty ones too."""
+    for lk in ([1] * 3, [10] * 50, [64] * 5, [700] * 2, [2000, 0, 3, 255, 256, 257, 513], [0, 0]):
+        lq = [1] * len(lk)
+        c = make(dtype, lq, lk, heads, kv_heads, dim, bias=mode != "plain", times=mode == "times", seed=dim)
+        for causal in (False, True):
+            check(c, lq, lk, run(c, lq, lk, causal=causal, one=True), causal=causal, dtype=dtype, what=str(lk))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_fixed_lengths_without_starts(dtype):
+    """q_start and k_start left out: every sequence has rows / batch rows."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    lq, lk = [50] * 6, [70] * 6
+    c = make(dtype, lq, lk, 4, 4, 40, bias=True)
+    o, lse = nlb.attention(c["q"].cuda(), c["k"].cuda(), c["v"].cuda(), batch=6, causal=True, bias=c["bias"].cuda(),
+                           bounds=c["bounds"].cuda())
+    torch.cuda.synchronize()
+    check(c, lq, lk, {"o": o, "lse": lse}, causal=True, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gap", [3, 8])
+def test_strided_rows(dtype, gap):
+    for one, lq, lk in ((False, [40, 90], [50, 90]), (True, [1] * 9, [30] * 9)):
+        c = make(dtype, lq, lk, 4, 2, 50, bias=True, times=True, gap=gap)
+        assert not c["q"].is_contiguous()
+        check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype=dtype)
+
+
+def test_long_and_wide_groups():
+    """Thousands of keys (many chunks, many tiles), sixteen heads on one."""
+    for one, lq, lk in ((True, [1, 1], [9000, 40]), (False, [300], [5000])):
+        c = make("bf16", lq, lk, 16, 1, 64, bias=True)
+        check(c, lq, lk, run(c, lq, lk, causal=True, one=one), causal=True, dtype="bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("one", [False, True])
+def test_closed_keys_may_hold_anything(dtype, one):
+    """NaN and infinities in rows that no query may see leave no trace."""
+    lq, lk = ([1] * 4, [100] * 4) if one else ([60, 5, 9], [60, 70, 80])
+    c = make(dtype, lq, lk, 2, 2, 64, bias=True, times=True, closed=0.5)
+    c["k_pos"][:lk[0]] = -1                                   # nothing open at all in the first
+    shut = c["k_pos"] == -1
+    clean = run(c, lq, lk, causal=False, one=one)
+    for n, x in (("k", float("nan")), ("v", float("inf"))):
+        c[n][shut] = x
+    got = run(c, lq, lk, causal=False, one=one)
+    for n in clean:
+        assert (got[n] == clean[n]).all(), n
+    assert (got["o"][:lq[0]] == 0).all() and (got["lse"][:lq[0]] == -float("inf")).all()
+    check(c, lq, lk, got, causal=False, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("one", [False, True])
+@pytest.mark.parametrize("low", ["inf", "lowest"])
+def test_bias_that_closes_a_bucket(dtype, one, low):
+    """Minus infinity or the type's lowest value close a bucket, all of a
+    row's keys too."""
+    import torch
+    lq, lk = ([1] * 3, [50, 9, 200]) if one else ([50, 9, 150], [50, 9, 200])
+    for shut in ([0, 1], [5, 6, 7, 8], list(range(9))):
+        c = make(dtype, lq, lk, 2, 1, 32, bias=True)
+        c["bias"][shut] = -float("inf") if low == "inf" else torch.finfo(_dtype(dtype)).min
+        check(c, lq, lk, run(c, lq, lk, causal=True, one=one), causal=True, dtype=dtype, what=str(shut))
+
+
+def test_gaps_of_unsigned_positions_are_clamped():
+    """Positions over the whole unsigned range; gaps beyond int32."""
+    import torch
+    for one, lq, lk in ((True, [1] * 6, [6] * 6), (False, [6], [6])):
+        c = make("f32", lq, lk, 2, 2, 16, bias=True, times=True, closed=0)
+        at = torch.tensor([0, 1, 2**31 - 1, 2**31, 2**32 - 2, 2**32 - 3], dtype=torch.int64)
+        c["q_pos"] = at.to(torch.uint32).view(torch.int32)
+        c["k_pos"] = at.repeat(len(lk)).to(torch.uint32).view(torch.int32)
+        c["bounds"] = torch.tensor([-2**31 + 1, -2**31 + 2, -3, 0, 1, 2, 2**31 - 2, 2**31 - 1], dtype=torch.int32)
+        check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype="f32")
+
+
+def test_rows_outside_the_sequences_stay():
+    """Rows before the first and behind the last sequence are not written, and
+    start values outside the rows are taken as the nearest end."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    c = make("bf16", [100], [100], 2, 2, 32)
+    q, k, v = (c[n].cuda() for n in "qkv")
+    o, lse = torch.full_like(q, 7.0), torch.full((100, 2), 7.0, device="cuda")
+    st = torch.tensor([10, 40, 40, 90], dtype=torch.int32, device="cuda")
+    nlb.attention(q, k, v, q_start=st, k_start=st, causal=True, out=o, lse=lse)
+    torch.cuda.synchronize()
+    for t in (o, lse):
+        assert (t[:10] == 7).all() and (t[90:] == 7).all() and (t[10:90] != 7).any(-1).all()
+    check({n: None if x is None else x[10:90] if n in "qkv" else x for n, x in c.items()}, [30, 0, 50], [30, 0, 50],
+          {"o": o[10:90], "lse": lse[10:90]}, causal=True, dtype="bf16")
+    wild = torch.tensor([-5, 40, 2**31 - 1, 50], dtype=torch.int32, device="cuda")
+    o.fill_(7.0)
+    nlb.attention(q, k, v, q_start=wild, k_start=wild, causal=True, out=o, lse=lse)
+    torch.cuda.synchronize()
+    check({n: None if x is None else x[:40] if n in "qkv" else x for n, x in c.items()}, [40], [40],
+          {"o": o[:40], "lse": lse[:40]}, causal=True, dtype="bf16")
+
+
+def test_graph_and_streams():
+    """A captured call replayed with new inputs, on a stream of its own; two
+    calls in flight on two streams, each with its working memory."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    lq, lk = [1, 1], [3000, 100]
+    cs = [make("bf16", lq, lk, 4, 2, 64, bias=True, seed=s) for s in range(2)]
+    st = torch.from_numpy(ref.starts(lk)).cuda()
+    how = dict(batch=2, k_start=st, bounds=cs[0]["bounds"].cuda())
+    ins = [[c[n].cuda() for n in ("q", "k", "v", "bias")] for c in cs]
+    want = [nlb.attention(q, k, v, bias=b, **how)[0].clone() for q, k, v, b in ins]
+    q, k, v, b = [x.clone() for x in ins[0]]
+    work = torch.empty(nlb.attention_work(q, k, v, bias=b, **how), dtype=torch.uint8, device="cuda")
+    assert work.numel() > 0
+    o, lse = torch.empty_like(q), torch.empty((2, 4), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        nlb.attention(q, k, v, bias=b, out=o, lse=lse, work=work, **how)
+    for turn in range(4):
+        for x, y in zip((q, k, v, b), ins[turn % 2]):
+            x.copy_(y)
+        o.fill_(0)
+        graph.replay()
+        other = nlb.attention(*ins[1][:3], bias=ins[1][3], stream=side, **how)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[turn % 2]) and torch.equal(other, want[1])
+
+
+def test_same_bits_each_time():
+    import torch
+    c = make("bf16", [300, 5], [400, 5], 4, 2, 64, bias=True, times=True, train=False)
+    a = run(c, [300, 5], [400, 5], causal=True)
+    b = run(c, [300, 5], [400, 5], causal=True)
+    for n in a:
+        assert torch.equal(a[n], b[n])
+
+
+def test_offsets_beyond_32_bits():
+    """Rows so far apart that their byte offsets pass 2^32."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    n, far = 70, 50_000_000                                   # 70 rows x 100 MB
+    c = make("bf16", [1, n - 1], [1, n - 1], 1, 1, 32)
+    big = torch.empty(n * far + 64, dtype=torch.bfloat16, device="cuda")
+    st = torch.tensor([0, 1, n], dtype=torch.int32, device="cuda")
+    k = big.as_strided((n, 1, 32), (far, 32, 1), 0)
+    k.copy_(c["k"])
+    for q, starts in ((c["q"].cuda(), dict(q_start=st, k_start=st)), (c["q"][:1].cuda(), dict(batch=1))):
+        o, lse = nlb.attention(q, k, k, **starts)
+        torch.cuda.synchronize()
+        lens = ([1, n - 1], [1, n - 1]) if len(q) > 1 else ([1], [n])
+        check({**c, "q": q.cpu(), "v": c["k"]}, *lens, {"o": o, "lse": lse}, causal=False, dtype="bf16")

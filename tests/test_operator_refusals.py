@@ -1,0 +1,79 @@
+"""What the operators without a table refuse, on the host, before any device
+work: no GPU is needed, and nothing here would launch a kernel."""
+import ctypes
+
+import pytest
+
+import paper_2402_01964_amd as nlb
+
+P = 4096                                                      # a stand-in pointer, never followed
+
+
+def _call(**kw):
+    c = nlb._AttCall()
+    c.device, c.dtype, c.heads, c.kv_heads, c.dim, c.scale = -1, nlb.DTYPE_BF16, 4, 2, 64, 0.125
+    c.batch, c.q_rows, c.k_rows = 2, 10, 10
+    for k in ("q", "k", "v"):
+        setattr(c, k, nlb._AttRows(P, 256, 64))
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+ROWS = nlb._AttRows(P, 256, 64)
+BAD_CALLS = [
+    dict(dtype=2), dict(heads=0), dict(heads=257, kv_heads=257), dict(kv_heads=0), dict(kv_heads=3), dict(dim=0),
+    dict(dim=129), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2), dict(batch=0), dict(batch=2**31),
+    dict(q_rows=2**31), dict(k_rows=2**31), dict(q_rows=11), dict(k_rows=11), dict(buckets=-1), dict(buckets=65, bias=P,
+                                                                                                     bounds=P),
+    dict(buckets=4), dict(bias=P), dict(buckets=4, bias=P), dict(buckets=4, bias=P, bounds=P + 2),
+    dict(buckets=4, bias=P + 1, bounds=P), dict(q_pos=P), dict(q_start=P + 1), dict(k_start=P + 2), dict(k_pos=P + 1),
+    dict(buckets=4, bias=P, bounds=P, k_pos=P), dict(q=nlb._AttRows(None, 256, 64)), dict(k=nlb._AttRows(None, 256, 64)),
+    dict(v=nlb._AttRows(P + 1, 256, 64)), dict(q=nlb._AttRows(P, -1, 64)), dict(k=nlb._AttRows(P, 2**31, 64)),
+    dict(v=nlb._AttRows(P, 256, -64)),
+]
+
+
+@pytest.mark.parametrize("bad", BAD_CALLS, ids=lambda b: ",".join(b))
+def test_attention_refuses(bad):
+    lib, n = nlb.load_library(), ctypes.c_size_t(7)
+    c = _call(**bad)
+    assert lib.nlb_attention_work(ctypes.byref(c), 0, ctypes.byref(n)) == nlb.NLB_EINVAL
+    assert n.value == 7
+    assert lib.nlb_attention(ctypes.byref(c), ctypes.byref(ROWS), None, None, 0, None) == nlb.NLB_EINVAL
+
+
+def test_attention_refuses_null_and_misaligned():
+    lib, n = nlb.load_library(), ctypes.c_size_t()
+    c = _call()
+    assert lib.nlb_attention_work(None, 0, ctypes.byref(n)) == nlb.NLB_EINVAL
+    assert lib.nlb_attention_work(ctypes.byref(c), 0, None) == nlb.NLB_EINVAL
+    for o, lse, work in ((None, None, None), (nlb._AttRows(None, 256, 64), None, None),
+                         (nlb._AttRows(P, 2**31, 64), None, None), (ROWS, P + 2, None), (ROWS, None, P + 8)):
+        assert lib.nlb_attention(ctypes.byref(c), o, lse, work, 0, None) == nlb.NLB_EINVAL
+
+
+def test_attention_work_is_checked():
+    """Single rows over long sequences work in chunks; too little memory for
+    them is refused."""
+    lib, n = nlb.load_library(), ctypes.c_size_t()
+    for c, some in ((_call(), False), (_call(q_rows=2, k_rows=2000), True), (_call(q_rows=2, k_rows=20), False),
+                    (_call(q_rows=2, k_rows=2001, k_start=P), True), (_call(q_rows=20, k_rows=2000), False)):
+        assert lib.nlb_attention_work(ctypes.byref(c), 0, ctypes.byref(n)) == nlb.NLB_OK
+        assert (n.value > 0) == some
+        if some:
+            for work, size in ((P, n.value - 1), (None, n.value), (None, 0)):
+                assert lib.nlb_attention(ctypes.byref(c), ROWS, None, work, size, None) == nlb.NLB_ESCRATCH
+
+
+def test_attention_grid_limit():
+    lib = nlb.load_library()
+    c = _call(heads=256, kv_heads=256, q_rows=2**31 - 1, q_start=P)
+    assert lib.nlb_attention(ctypes.byref(c), ROWS, None, None, 0, None) == nlb.NLB_EINVAL
+
+
+def test_binding_checks_its_tensors():
+    import torch
+    x = torch.zeros(4, 2, 8)
+    with pytest.raises(TypeError):
+        nlb.attention(x, x, x)
