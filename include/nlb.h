@@ -436,6 +436,25 @@ int nlb_attention_work(const nlb_att_call *call, int32_t backward, size_t *bytes
 int nlb_attention(const nlb_att_call *call, const nlb_att_rows *o, float *lse, void *work, size_t work_bytes,
                   void *stream);
 
+/* Gradients of nlb_attention: from the same call (its sequences, positions and
+ * bias unchanged), its outputs o and lse, and the gradient dout of o (rows as
+ * o), with p_ij = exp(s_ij - lse_i):
+ *   ds_ij = p_ij (dout_i . v_j - D_i),   D_i = sum_j p_ij dout_i . v_j
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
+ *   dbias[b][h] = the sum of ds_ij over the pairs of bucket b
+ * dk and dv sum over the query heads of a key/value head.  All rows of the
+ * sequences are written (zeros for closed keys and for rows without open
+ * keys), rows outside them are not.  dbias: device [buckets][heads] of dtype,
+ * or NULL where it is not wanted (with it, D_i comes from a pass over the keys
+ * of its own, else from o).  Numerics: as nlb_attention; ds enters the
+ * products as bf16 for bf16 rows (not in the single-row form), dbias sums it
+ * in fp32 and fp64, rounded once.  No atomics on results: the same call gives
+ * the same bits.  Work, capture and errors: as nlb_attention (NLB_EINVAL also
+ * for dbias without buckets). */
+int nlb_attention_backward(const nlb_att_call *call, const nlb_att_rows *o, const float *lse,
+                           const nlb_att_rows *dout, const nlb_att_rows *dq, const nlb_att_rows *dk,
+                           const nlb_att_rows *dv, void *dbias, void *work, size_t work_bytes, void *stream);
+
 /* Free the table's device memory after synchronising its device.  NULL is a
  * no-op.  Borrowed buffers are not touched. */
 int nlb_destroy(nlb_table *h);

@@ -24,7 +24,8 @@ MAX_SLOTS = 1024
 
 # Symbols declared in include/nlb.h.
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
-               "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
+               "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
+               "nlb_attention_backward", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
                "nlb_strerror")
 AGG_HIDDEN = 64
 RNN_MAX_DIM = 1024
@@ -128,6 +129,8 @@ def load_library(path: str | None = None):
     lib.nlb_attention_work.restype = I
     lib.nlb_attention.argtypes = [ctypes.POINTER(_AttCall), R, P, P, S, P]
     lib.nlb_attention.restype = I
+    lib.nlb_attention_backward.argtypes = [ctypes.POINTER(_AttCall), R, P, R, R, R, R, P, P, S, P]
+    lib.nlb_attention_backward.restype = I
     lib.nlb_destroy.argtypes = [P]
     lib.nlb_destroy.restype = I
     lib.nlb_get_info.argtypes = [P, ctypes.POINTER(_Info)]
@@ -552,3 +555,39 @@ def attention(q, k, v, *, batch=None, q_start=None, k_start=None, causal=False, 
         _check(lib.nlb_attention(ctypes.byref(c), ctypes.byref(o), _dev_ptr(lse, 4, "lse"), p, size, s),
                "nlb_attention")
     return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, *, batch=None, q_start=None, k_start=None, causal=False, scale=None,
+                       bias=None, bounds=None, q_pos=None, k_pos=None, dq=None, dk=None, dv=None, dbias=None,
+                       need_dbias=True, work=None, stream=None):
+    """Gradients of ``attention`` (nlb_attention_backward) from the same
+    arguments, its results ``out`` and ``lse`` and the gradient ``dout`` of
+    out.  Returns (or fills) dq, dk, dv and dbias (None without a bias, or
+    with need_dbias=False).  ``work``: attention_work(..., backward=True)
+    bytes, allocated if None."""
+    import torch
+    lib = load_library()
+    c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != q.device:
+        raise ValueError("lse must be float32 [q_rows, heads] on q's device")
+    if dbias is not None and bias is None:
+        raise ValueError("dbias without bias")
+    with _OnStream(q.device, stream) as s:
+        dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) if d is None else d
+                      for d, t in ((dq, q), (dk, k), (dv, v)))
+        if bias is None or not need_dbias:
+            dbias = None
+        elif dbias is None:
+            dbias = torch.empty_like(bias)
+        elif dbias.shape != bias.shape:
+            raise ValueError("dbias must have bias's shape")
+        rows = [_att_rows(t, q, like.shape, name) for t, like, name in
+                ((out, q, "out"), (dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"))]
+        n = ctypes.c_size_t()
+        _check(lib.nlb_attention_work(ctypes.byref(c), 1, ctypes.byref(n)), "nlb_attention_backward")
+        keep, p, size = _work(n.value, work, q)
+        r = [ctypes.byref(x) for x in rows]
+        _check(lib.nlb_attention_backward(ctypes.byref(c), r[0], _dev_ptr(lse, 4, "lse"), r[1], r[2], r[3], r[4],
+                                          None if dbias is None else _dev_ptr(_like(dbias, q, "dbias"), None, "dbias"),
+                                          p, size, s), "nlb_attention_backward")
+    return dq, dk, dv, dbias

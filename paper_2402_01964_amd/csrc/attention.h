@@ -500,12 +500,35 @@ inline Forward plan_forward(const Attend &a) {
 }
 
 struct Backward {
-    size_t bytes;
+    bool one;
+    uint32_t blocks, shares;             // workgroups of the single-row form; shares of the first sum of bias gradients
+    uint64_t q_slots, q_most, k_slots, k_most;
+    uint64_t parts;                      // partial bias gradients
+    size_t delta_bytes, bytes;
 };
 
+// The single-row form takes a list per wavefront, so lists have to be short:
+// 256 keys on average at most.  A group's heads are in registers there, four
+// at most.  Everything else, single rows over long histories among it, goes
+// through tiles, whose second kernel spreads over the keys.
 inline Backward plan_backward(const Attend &a) {
     Backward p = {};
-    p.bytes = align256((size_t)a.q_rows * a.heads * 4);
+    p.one = !a.q_start && a.q_len == 1 && a.group <= 4 && a.k_rows / 256 <= a.batch;
+    if (p.one) {
+        const uint64_t waves = (uint64_t)a.batch * a.kv_heads;
+        const uint64_t most = 256 * 8 / a.kv_heads, need = (waves + 4 * a.kv_heads - 1) / (4 * a.kv_heads);
+        p.blocks = (uint32_t)((need < most ? need : most) * a.kv_heads);
+        p.parts = p.blocks * 4 / a.kv_heads;
+    } else {
+        p.q_slots = (uint64_t)a.q_rows / kOwned + a.batch;
+        p.k_slots = (uint64_t)a.k_rows / kOwned + a.batch;
+        p.q_most = INT32_MAX / a.heads;
+        p.k_most = INT32_MAX / a.kv_heads;
+        p.parts = a.q_rows ? p.q_slots : 0;
+        p.delta_bytes = align256((size_t)a.q_rows * a.heads * 4);
+    }
+    p.shares = p.parts > 64 ? 64 : 0;
+    p.bytes = p.delta_bytes + align256((p.parts + p.shares) * a.heads * a.buckets * 4);
     return p;
 }
 

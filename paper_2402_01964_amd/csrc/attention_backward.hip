@@ -1,0 +1,604 @@
+// attention_backward.hip -- gradients of softmax attention over packed
+// sequences.  With p_ij as in the forward pass and D_i = sum_j p_ij dp_ij:
+//   dp_ij = do_i . v_j,   ds_ij = p_ij (dp_ij - D_i)
+//   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i
+//   dv_j = sum_i p_ij do_i,   dbias[b][h] = sum of ds_ij over the pairs of bucket b
+// The probabilities are computed again from the scores and lse.  Sums over
+// rows and sums over keys are taken by different kernels (backward_rows,
+// backward_keys), each of which owns what it sums: no atomics on results, the
+// same bits each time, at the price of computing the scores and dp twice.
+#include "attention.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int kGaps = 192;               // gaps of a tile of owned rows and streamed rows
+
+// 2^(t - L) is zero for a row without open keys.
+__device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// ---------------------------------------------------------------- rows
+// A workgroup owns 128 query rows of one head and streams keys and values as
+// the forward pass does.  D is do . o without a bias gradient.  With one, D is
+// summed from the probabilities in a pass of its own over the keys: a bucket's
+// gradient is a difference of large sums (all ds of a row add up to zero),
+// which the rounding of o would drown.
+//
+// The bias gradient: each thread adds its ds to its own column of an LDS table
+// [buckets][threads] (by LDS adds in program order: no two threads share a
+// word), tiles whose gaps all lie beyond the last or before the first bound
+// to a register.  The columns are summed at the end in a fixed order into
+// part[slot][head][bucket].
+template <typename T, int DP> constexpr uint32_t rows_lds(uint32_t buckets) {
+    return 4 * Tile<T, DP>::bytes + 2 * kGaps * 4 + kMaxBuckets * 8 + buckets * kThreads * 4;
+}
+
+template <typename T, int DP, int POS>
+__global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
+    using G = Tile<T, DP>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float *extra = (float *)(lds + 4 * G::bytes);
+    int32_t *bounds = (int32_t *)(extra + 2 * kGaps);
+    float *bias = (float *)(bounds + kMaxBuckets);
+    float *hist = bias + kMaxBuckets;                         // [buckets][threads]
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
+    const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
+    const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
+    const bool want = POS != 0 && a.part;                     // the bias gradient
+    Seq sq;
+    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, kOwned, slot, sq.tile);
+    sequence(a, b, sq);
+    if (sq.tile >= ((uint32_t)sq.lq + kOwned - 1) / kOwned) {
+        if (want && threadIdx.x < a.buckets) a.part[((size_t)slot * a.heads + head) * a.buckets + threadIdx.x] = 0.0f;
+        return;
+    }
+    const int32_t row0 = sq.tile * kOwned, row = row0 + wave * 32 + col, off = sq.lk - sq.lq;
+    const bool there = row < sq.lq;
+    const size_t stat = (size_t)(sq.q0 + row) * a.heads + head;
+
+    if constexpr (POS != 0) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads) {
+            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+            bias[i] = i < a.buckets ? bias2_of<T>(a, i, head) : 0.0f;
+        }
+        if (want)
+            for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
+        __syncthreads();
+    }
+    Owned<T, DP> q, dout;
+    load_owned(q, a.q.p + (int64_t)(sq.q0 + row) * a.q.row + head * a.q.head, there, a.dim);
+    load_owned(dout, a.dout.p + (int64_t)(sq.q0 + row) * a.dout.row + head * a.dout.head, there, a.dim);
+    int32_t qpos = 0;
+    if constexpr (POS == 2)
+        if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
+    const float L = there ? row_log2(a.lse[stat]) : INFINITY;
+    float D = 0.0f;
+    if (!want) {
+        Owned<T, DP> o;
+        load_owned(o, a.o.p + (int64_t)(sq.q0 + row) * a.o.row + head * a.o.head, there, a.dim);
+#pragma unroll
+        for (int s = 0; s < Owned<T, DP>::steps; s++) {
+            float x[Chunk<T>::n], y[Chunk<T>::n];
+            unpack<T>(o.x[s], x);
+            unpack<T>(dout.x[s], y);
+#pragma unroll
+            for (int i = 0; i < Chunk<T>::n; i++) D = fmaf(x[i], y[i], D);
+        }
+        D = halves_sum(D);
+    }
+
+    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wlast = min(row0 + (int32_t)wave * 32 + 32, sq.lq) - 1;
+    const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
+    const int32_t wend = a.causal ? min(sq.lk, wlast + off + 1) : sq.lk;
+    const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;
+    const uint8_t *kbase = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
+    const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
+
+    typename G::Regs kreg, vreg;
+    uint32_t preg[POS == 2 ? G::per_thread : 1];
+    const auto fetch = [&](int32_t k0) {
+        tile_load<T, DP>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
+    };
+    const auto stage = [&](int32_t k0, int buf) {
+        uint8_t *kt = lds + buf * 2 * G::bytes;
+        if constexpr (POS == 2) {
+            tile_close<T, DP>(kreg, preg);
+            tile_close<T, DP>(vreg, preg);
+            tile_store_positions<T, DP>((uint32_t *)extra + buf * kGaps, preg);
+        }
+        tile_store<T, DP>(kt, kreg);
+        tile_store<T, DP>(kt + G::bytes, vreg);
+        if constexpr (POS == 1) {
+            const int32_t x = (int32_t)threadIdx.x;
+            if (x < kOwned + G::rows - 1)
+                extra[buf * kGaps + x] =
+                    __uint_as_float(bucket_of(bounds, a.buckets, row0 + off - k0 + x - (G::rows - 1)));
+        }
+    };
+
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++) acc[d] = f32x16{};
+    // one pass over the keys: FIRST sums D, the other dq (and the bias gradient)
+    const auto pass = [&](auto first_pass) {
+        constexpr bool FIRST = decltype(first_pass)::value;
+        if (kend > 0) {
+            fetch(0);
+            stage(0, 0);
+        }
+        __syncthreads();
+        int buf = 0;
+        for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= 1) {
+            const bool more = k0 + G::rows < kend;
+            if (more) fetch(k0 + G::rows);
+            if (k0 < wend) {
+                const uint8_t *kt = lds + buf * 2 * G::bytes, *vt = kt + G::bytes;
+#pragma unroll
+                for (int blk = 0; blk < G::blocks; blk++) {
+                    f32x16 s = {}, dp = {};
+                    product_rows<T, DP>(s, kt, blk, q);
+                    product_rows<T, DP>(dp, vt, blk, dout);
+                    float ds[16];
+#pragma unroll
+                    for (int r = 0; r < 16; r++) {
+                        const int kr = blk * 32 + block_row(r);
+                        float x = s[r] * a.scale2;
+                        uint32_t bk = 0;
+                        if constexpr (POS == 1) {
+                            bk = __float_as_uint(extra[buf * kGaps + wave * 32 + col + (G::rows - 1) - kr]);
+                            x += bias[bk];
+                        }
+                        if constexpr (POS == 2) {
+                            const uint32_t kp = ((const uint32_t *)extra)[buf * kGaps + kr];
+                            if (a.buckets) {
+                                bk = bucket_of(bounds, a.buckets, gap_of(qpos, flip(kp)));
+                                x += bias[bk];
+                            }
+                            if (kp == kNoKey) x = -INFINITY;
+                        }
+                        if (k0 + kr >= limit) x = -INFINITY;
+                        const float p = exp2_fast(x - L);
+                        if constexpr (FIRST) {
+                            D = fmaf(p, dp[r], D);
+                        } else {
+                            ds[r] = p * (dp[r] - D);
+                            if (want) __hip_atomic_fetch_add(hist + bk * kThreads + threadIdx.x, ds[r],
+                                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                        }
+                    }
+                    if constexpr (!FIRST) {
+                        Scores<T> p;
+                        pack(p, ds);
+                        product_columns<T, DP>(acc, kt, blk, p);
+                    }
+                }
+            }
+            if (more) stage(k0 + G::rows, buf ^ 1);
+            __syncthreads();
+        }
+    };
+    if (want) {
+        pass(std::true_type{});
+        D = halves_sum(D);
+    }
+    if (there && lane < 32) a.delta[stat] = D;
+    pass(std::false_type{});
+    if (there)
+        store_owned<T, DP>((uint8_t *)a.dq.p + (int64_t)(sq.q0 + row) * a.dq.row + head * a.dq.head, a.dim, acc,
+                           a.scale);
+    if (want)                                                 // (the pass ended with a barrier)
+        for (uint32_t i = wave; i < a.buckets; i += 4) {
+            float x = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; w++) x += hist[i * kThreads + w * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < 64; w *= 2) x += __shfl_xor(x, w);
+            if (lane == 0) a.part[((size_t)slot * a.heads + head) * a.buckets + i] = x;
+        }
+}
+
+// ---------------------------------------------------------------- keys
+// A workgroup owns 128 keys of one key/value head and streams the query rows
+// that see them, head by head of its group: q and do in tiles through two LDS
+// buffers, lse and D beside them.  Blocks of scores have the owned keys as
+// columns here, so p and ds go to the products that sum over rows from the
+// registers they are in.
+template <typename T, int DP> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
+    return 4 * Tile<T, DP>::bytes + 2 * (kGaps + 2 * Tile<T, DP>::rows) * 4 +
+           (bias ? kMaxBuckets * 4 * (1 + group) : 0);
+}
+
+template <typename T, int DP, int POS>
+__global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
+    using G = Tile<T, DP>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    constexpr int kExtra = kGaps + 2 * G::rows;
+    float *extra = (float *)(lds + 4 * G::bytes);             // [2]: L, D of the tile's rows; bias by gap, or positions
+    int32_t *bounds = (int32_t *)(extra + 2 * kExtra);
+    float *bias = (float *)(bounds + kMaxBuckets);            // [group][buckets]
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
+    const uint32_t kvh = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
+    Seq sq;
+    const uint32_t b = slot_owner(a.k_start, a.k_len, a.k_rows, a.batch, kOwned, slot, sq.tile);
+    sequence(a, b, sq);
+    if (sq.tile >= ((uint32_t)sq.lk + kOwned - 1) / kOwned) return;
+    const int32_t key0 = sq.tile * kOwned, key = key0 + wave * 32 + col, off = sq.lk - sq.lq;
+    const bool there = key < sq.lk;
+    if (POS != 0 && a.buckets) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets * a.group; i += kThreads) {
+            const uint32_t n = i % kMaxBuckets;
+            if (i < kMaxBuckets) bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+            bias[i] = n < a.buckets ? bias2_of<T>(a, n, kvh * a.group + i / kMaxBuckets) : 0.0f;
+        }
+        __syncthreads();
+    }
+    uint32_t kpos = 0;
+    if constexpr (POS == 2) kpos = there ? a.k_pos[sq.k0 + key] : kNoKey;
+    const bool open = there && (POS != 2 || kpos != kNoKey);
+    Owned<T, DP> k, v;
+    load_owned(k, a.k.p + (int64_t)(sq.k0 + key) * a.k.row + kvh * a.k.head, open, a.dim);
+    load_owned(v, a.v.p + (int64_t)(sq.k0 + key) * a.v.row + kvh * a.v.head, open, a.dim);
+
+    // rows from `first` on see a key of the workgroup
+    const int32_t first = a.causal ? max(0, key0 - off) / G::rows * G::rows : 0;
+    const int32_t tiles = sq.lq > first ? (sq.lq - first + G::rows - 1) / G::rows : 0;
+    const int32_t least = a.causal ? key - off : 0;           // the first row that sees this lane's key
+    const int32_t wleast = a.causal ? key0 + (int32_t)wave * 32 - off : 0;
+
+    typename G::Regs qreg, oreg;
+    float Lreg = 0.0f, Dreg = 0.0f;
+    uint32_t preg = 0;
+    const auto fetch = [&](int32_t g, int32_t i0) {
+        const uint32_t head = kvh * a.group + g;
+        const int64_t r = sq.q0 + i0;
+        tile_load<T, DP>(qreg, a.q.p + r * a.q.row + head * a.q.head, a.q.row, sq.lq - i0, a.dim);
+        tile_load<T, DP>(oreg, a.dout.p + r * a.dout.row + head * a.dout.head, a.dout.row, sq.lq - i0, a.dim);
+        if (threadIdx.x < G::rows) {
+            const bool in = i0 + (int32_t)threadIdx.x < sq.lq;
+            const size_t stat = (size_t)(r + threadIdx.x) * a.heads + head;
+            Lreg = in ? row_log2(a.lse[stat]) : INFINITY;
+            Dreg = in ? a.delta[stat] : 0.0f;
+            if (POS == 2 && a.q_pos) preg = in ? a.q_pos[r + threadIdx.x] : 0;
+        }
+    };
+    const auto stage = [&](int32_t g, int32_t i0, int buf) {
+        uint8_t *qt = lds + buf * 2 * G::bytes;
+        float *e = extra + buf * kExtra;
+        tile_store<T, DP>(qt, qreg);
+        tile_store<T, DP>(qt + G::bytes, oreg);
+        if (threadIdx.x < G::rows) {
+            e[threadIdx.x] = Lreg;
+            e[G::rows + threadIdx.x] = Dreg;
+            if (POS == 2) ((uint32_t *)e)[2 * G::rows + threadIdx.x] = preg;
+        }
+        if constexpr (POS == 1) {
+            const int32_t x = (int32_t)threadIdx.x;           // gap of x: i0 + off - key0 + x - (owned - 1)
+            if (x < kOwned + G::rows - 1)
+                e[2 * G::rows + x] =
+                    bias[g * kMaxBuckets + bucket_of(bounds, a.buckets, i0 + off - key0 + x - (kOwned - 1))];
+        }
+    };
+
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; d++) dk[d] = dv[d] = f32x16{};
+    const int32_t total = tiles * (int32_t)a.group;
+    if (total > 0) {
+        fetch(0, first);
+        stage(0, first, 0);
+    }
+    __syncthreads();
+    int buf = 0;
+    int32_t g = 0, i0 = first;
+    for (int32_t it = 0; it < total; it++, buf ^= 1) {
+        int32_t gn = g, in = i0 + G::rows;
+        if (in >= sq.lq) {
+            in = first;
+            gn++;
+        }
+        const bool more = it + 1 < total;
+        if (more) fetch(gn, in);
+        if (i0 + G::rows > wleast) {
+            const uint8_t *qt = lds + buf * 2 * G::bytes, *ot = qt + G::bytes;
+            const float *e = extra + buf * kExtra;
+#pragma unroll
+            for (int blk = 0; blk < G::blocks; blk++) {
+                f32x16 s = {}, dp = {};
+                product_rows<T, DP>(s, qt, blk, k);
+                product_rows<T, DP>(dp, ot, blk, v);
+                float p[16], ds[16];
+#pragma unroll
+                for (int r = 0; r < 16; r++) {
+                    const int ir = blk * 32 + block_row(r);
+                    float x = s[r] * a.scale2;
+                    if constexpr (POS == 1) x += e[2 * G::rows + ir + (kOwned - 1) - wave * 32 - col];
+                    if constexpr (POS == 2)
+                        if (a.buckets)
+                            x += bias[g * kMaxBuckets +
+                                      bucket_of(bounds, a.buckets,
+                                                gap_of(flip(((const uint32_t *)e)[2 * G::rows + ir]), flip(kpos)))];
+                    if (!open || i0 + ir < least) x = -INFINITY;
+                    p[r] = exp2_fast(x - e[ir]);
+                    ds[r] = p[r] * (dp[r] - e[G::rows + ir]);
+                }
+                Scores<T> w;
+                pack(w, p);
+                product_columns<T, DP>(dv, ot, blk, w);
+                pack(w, ds);
+                product_columns<T, DP>(dk, qt, blk, w);
+            }
+        }
+        if (more) stage(gn, in, buf ^ 1);
+        __syncthreads();
+        g = gn;
+        i0 = in;
+    }
+    if (!there) return;
+    store_owned<T, DP>((uint8_t *)a.dk.p + (int64_t)(sq.k0 + key) * a.dk.row + kvh * a.dk.head, a.dim, dk, a.scale);
+    store_owned<T, DP>((uint8_t *)a.dv.p + (int64_t)(sq.k0 + key) * a.dv.row + kvh * a.dv.head, a.dim, dv, 1.0f);
+}
+
+// ---------------------------------------------------------------- one query row
+// The gradients of lists with one query row each, of up to GB query heads on a
+// key/value head: a wavefront a list and key/value head, rows across lanes as
+// in the forward pass.  Bound by reading keys and values and writing their
+// gradients once; a bias gradient makes two passes over a list, the second
+// from the caches (for D, as in backward_rows).
+template <typename T, int DP, int GB>
+__global__ __launch_bounds__(kThreads) void backward_one(Attend a) {
+    constexpr int N = Chunk<T>::n, U = 2, per_row = DP / N, rows = 64 / per_row;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    int32_t *bounds = (int32_t *)lds;
+    float *bias = (float *)(bounds + kMaxBuckets);            // [buckets][heads]
+    const uint32_t lane = threadIdx.x & 63u, c = lane % per_row, c0 = c * N, kr = lane / per_row;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t w = blockIdx.x * 4 + wave, waves = gridDim.x * 4;
+    // this wavefront's columns of the bias gradient: [buckets][GB][rows]
+    float *hist = bias + a.buckets * a.heads + wave * a.buckets * GB * rows;
+    const bool want = a.part;
+    if (a.buckets) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads)
+            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+        for (uint32_t i = threadIdx.x; i < a.buckets * a.heads; i += kThreads)
+            bias[i] = bias2_of<T>(a, i / a.heads, i % a.heads);
+        if (want)
+            for (uint32_t i = lane; i < a.buckets * GB * rows; i += 64) hist[i] = 0.0f;
+        __syncthreads();
+    }
+    // (the number of wavefronts is a multiple of kv_heads: each keeps its heads)
+    const uint32_t kvh = w % a.kv_heads, head0 = kvh * a.group;
+    for (uint32_t b = w / a.kv_heads; b < a.batch; b += waves / a.kv_heads) {
+        Seq sq;
+        sequence(a, b, sq);
+        float q[GB][N], dout[GB][N], dq[GB][N], L[GB], D[GB];
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            u32x4 x = {0, 0, 0, 0}, y = x, z = x;
+            L[g] = INFINITY;
+            D[g] = 0.0f;
+            if ((uint32_t)g < a.group) {
+                x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
+                y = load_chunk<T>(a.dout.p + (int64_t)b * a.dout.row + (head0 + g) * a.dout.head, c0, a.dim);
+                if (!want) z = load_chunk<T>(a.o.p + (int64_t)b * a.o.row + (head0 + g) * a.o.head, c0, a.dim);
+                L[g] = row_log2(a.lse[(size_t)b * a.heads + head0 + g]);
+            }
+            unpack<T>(x, q[g]);
+            unpack<T>(y, dout[g]);
+            float o[N];
+            unpack<T>(z, o);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                dq[g][i] = 0.0f;
+                D[g] = fmaf(o[i], dout[g][i], D[g]);
+            }
+            if (!want) D[g] = lanes_sum<per_row>(D[g]);
+        }
+        const int32_t qpos = a.buckets ? (a.q_pos ? flip(a.q_pos[b]) : flip((uint32_t)sq.lk - 1)) : 0;
+        const auto pass = [&](auto first_pass) {
+            constexpr bool FIRST = decltype(first_pass)::value;
+            for (int32_t j0 = 0; j0 < sq.lk; j0 += rows * U) {
+                u32x4 k[U], v[U];
+                uint32_t pos[U];
+                bool open[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int32_t j = j0 + u * rows + kr;
+                    open[u] = j < sq.lk;
+                    pos[u] = j;
+                    if (a.k_pos && open[u]) {
+                        pos[u] = a.k_pos[sq.k0 + j];
+                        open[u] = pos[u] != kNoKey;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int64_t j = (int64_t)sq.k0 + j0 + u * rows + kr;
+                    k[u] = v[u] = u32x4{0, 0, 0, 0};
+                    if (open[u]) {
+                        k[u] = load_chunk<T>(a.k.p + j * a.k.row + kvh * a.k.head, c0, a.dim);
+                        v[u] = load_chunk<T>(a.v.p + j * a.v.row + kvh * a.v.head, c0, a.dim);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int32_t j = j0 + u * rows + kr;
+                    float x[N], y[N], dk[N] = {}, dv[N] = {};
+                    unpack<T>(k[u], x);
+                    unpack<T>(v[u], y);
+                    const uint32_t bk = a.buckets ? bucket_of(bounds, a.buckets, gap_of(qpos, flip(pos[u]))) : 0;
+                    float mine = 0.0f;
+#pragma unroll
+                    for (int g = 0; g < GB; g++) {
+                        float s = 0.0f, dp = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < N; i++) {
+                            s = fmaf(q[g][i], x[i], s);
+                            dp = fmaf(dout[g][i], y[i], dp);
+                        }
+                        s = lanes_sum<per_row>(s) * a.scale2;
+                        dp = lanes_sum<per_row>(dp);
+                        if (a.buckets && (uint32_t)g < a.group) s += bias[bk * a.heads + head0 + g];
+                        const float p = open[u] ? exp2_fast(s - L[g]) : 0.0f;
+                        if constexpr (FIRST) {
+                            D[g] = fmaf(p, dp, D[g]);
+                        } else {
+                            const float ds = p * (dp - D[g]), dss = ds * a.scale;
+                            if (c == (uint32_t)g) mine = ds;
+#pragma unroll
+                            for (int i = 0; i < N; i++) {
+                                dk[i] = fmaf(dss, q[g][i], dk[i]);
+                                dv[i] = fmaf(p, dout[g][i], dv[i]);
+                                dq[g][i] = fmaf(dss, x[i], dq[g][i]);
+                            }
+                        }
+                    }
+                    if constexpr (!FIRST) {
+                        if (want && c < GB && open[u])
+                            __hip_atomic_fetch_add(hist + (bk * GB + c) * rows + kr, mine, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_WORKGROUP);
+                        if (j < sq.lk && c0 < a.dim) {
+                            const int64_t r = (int64_t)sq.k0 + j;
+                            store_values<T, N>((uint8_t *)a.dk.p + r * a.dk.row + kvh * a.dk.head, c0, a.dim, dk);
+                            store_values<T, N>((uint8_t *)a.dv.p + r * a.dv.row + kvh * a.dv.head, c0, a.dim, dv);
+                        }
+                    }
+                }
+            }
+        };
+        if (want) {
+            pass(std::true_type{});
+#pragma unroll
+            for (int g = 0; g < GB; g++)
+#pragma unroll
+                for (int x = per_row; x < 64; x *= 2) D[g] += __shfl_xor(D[g], x);
+        }
+        pass(std::false_type{});
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            if ((uint32_t)g >= a.group) break;
+#pragma unroll
+            for (int x = per_row; x < 64; x *= 2)
+#pragma unroll
+                for (int i = 0; i < N; i++) dq[g][i] += __shfl_xor(dq[g][i], x);
+            if (kr == 0 && c0 < a.dim)
+                store_values<T, N>((uint8_t *)a.dq.p + (int64_t)b * a.dq.row + (head0 + g) * a.dq.head, c0, a.dim,
+                                   dq[g]);
+        }
+    }
+    if (want)
+        for (uint32_t i = lane; i < a.buckets * a.group; i += 64) {
+            const uint32_t bk = i % a.buckets, g = i / a.buckets;
+            float x = 0.0f;
+            for (int r = 0; r < rows; r++) x += hist[(bk * GB + g) * rows + r];
+            a.part[((size_t)(w / a.kv_heads) * a.heads + head0 + g) * a.buckets + bk] = x;
+        }
+}
+
+// ---------------------------------------------------------------- bias gradient
+// Sums n partial tables [heads][buckets] in a fixed order: block (head, p) the
+// p-th of `outs` even shares into out[p]; the last call writes the gradient.
+// 64-bit sums: the terms cancel.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sum_bias(const float *part, uint32_t n, uint32_t heads, uint32_t buckets,
+                                                     uint32_t outs, float *out, T *dbias) {
+    __shared__ double sums[4][64];
+    const uint32_t head = blockIdx.x % heads, p = blockIdx.x / heads, lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
+    const uint32_t each = (n + outs - 1) / outs, lo = p * each, hi = min(n, lo + each);
+    double x = 0.0;
+    if (lane < buckets)
+        for (uint32_t i = lo + w; i < hi; i += 4) x += (double)part[((size_t)i * heads + head) * buckets + lane];
+    sums[w][lane] = x;
+    __syncthreads();
+    if (w == 0 && lane < buckets) {
+        x = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+        if (out) out[((size_t)p * heads + head) * buckets + lane] = (float)x;
+        else dbias[(size_t)lane * heads + head] = (T)(float)x;
+    }
+}
+
+// ---------------------------------------------------------------- launches
+template <typename K> bool allow_lds(K kernel, uint32_t bytes) {
+    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+
+template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
+    const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
+    const auto rows = pos == 2   ? backward_rows<T, DP, 2>
+                      : pos == 1 ? backward_rows<T, DP, 1>
+                                 : backward_rows<T, DP, 0>;
+    const auto keys = pos == 2   ? backward_keys<T, DP, 2>
+                      : pos == 1 ? backward_keys<T, DP, 1>
+                                 : backward_keys<T, DP, 0>;
+    const uint32_t rb = rows_lds<T, DP>(a.part ? a.buckets : 0), kb = keys_lds<T, DP>(a.group, a.buckets > 0);
+    if (!allow_lds(rows, rb) || !allow_lds(keys, kb)) return NLB_EDEVICE;
+    a.slots = (uint32_t)p.q_slots;
+    if (a.q_rows) hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), rb, stream, a);
+    a.slots = (uint32_t)p.k_slots;
+    if (a.k_rows) hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
+    return NLB_OK;
+}
+
+template <typename T, int DP> int launch_one(const Attend &a, const Backward &p, hipStream_t stream) {
+    const int gb = a.group > 2 ? 4 : (int)a.group;
+    const auto kernel = gb == 4 ? backward_one<T, DP, 4> : gb == 2 ? backward_one<T, DP, 2> : backward_one<T, DP, 1>;
+    const uint32_t rows = 64 / (DP / Chunk<T>::n);
+    const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4 + (a.part ? 4 * a.buckets * gb * rows * 4 : 0);
+    if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
+    hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(kThreads), bytes, stream, a);
+    return NLB_OK;
+}
+
+template <typename T> int launch(const Attend &a, const Backward &p, void *dbias, hipStream_t s) {
+    int rc;
+    if (a.dim <= 32) rc = p.one ? launch_one<T, 32>(a, p, s) : launch_tiles<T, 32>(a, p, s);
+    else if (a.dim <= 64) rc = p.one ? launch_one<T, 64>(a, p, s) : launch_tiles<T, 64>(a, p, s);
+    else rc = p.one ? launch_one<T, 128>(a, p, s) : launch_tiles<T, 128>(a, p, s);
+    if (rc != NLB_OK) return rc;
+    if (dbias) {
+        const float *from = a.part;
+        uint32_t n = (uint32_t)p.parts;
+        if (p.shares) {
+            float *mid = a.part + (size_t)n * a.heads * a.buckets;
+            hipLaunchKernelGGL((sum_bias<T>), dim3(p.shares * a.heads), dim3(kThreads), 0, s, from, n, a.heads,
+                               a.buckets, p.shares, mid, (T *)nullptr);
+            from = mid;
+            n = p.shares;
+        }
+        hipLaunchKernelGGL((sum_bias<T>), dim3(a.heads), dim3(kThreads), 0, s, from, n, a.heads, a.buckets, 1u,
+                           (float *)nullptr, (T *)dbias);
+    }
+    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+}
+
+}  // namespace
+
+extern "C" int nlb_attention_backward(const nlb_att_call *c, const nlb_att_rows *o, const float *lse,
+                                      const nlb_att_rows *dout, const nlb_att_rows *dq, const nlb_att_rows *dk,
+                                      const nlb_att_rows *dv, void *dbias, void *work, size_t work_bytes,
+                                      void *stream) {
+    Attend a;
+    int rc = fill_call(c, a);
+    if (rc != NLB_OK) return rc;
+    const bool q = c->q_rows > 0, k = c->k_rows > 0;
+    if (fill_rows(c, o, q, a.o) != NLB_OK || fill_rows(c, dout, q, a.dout) != NLB_OK ||
+        fill_rows(c, dq, q, a.dq) != NLB_OK || fill_rows(c, dk, k, a.dk) != NLB_OK ||
+        fill_rows(c, dv, k, a.dv) != NLB_OK)
+        return NLB_EINVAL;
+    if ((q && !lse) || (uintptr_t)lse % 4 || (uintptr_t)work % 16) return NLB_EINVAL;
+    if ((uintptr_t)dbias % (c->dtype == NLB_DTYPE_BF16 ? 2 : 4) || (dbias && !a.buckets)) return NLB_EINVAL;
+    const Backward p = plan_backward(a);
+    if (p.q_slots > p.q_most || p.k_slots > p.k_most) return NLB_EINVAL;
+    if (work_bytes < p.bytes || (p.bytes && !work)) return NLB_ESCRATCH;
+    int dev;
+    if ((rc = device_of(c, dev)) != NLB_OK) return rc;
+    DeviceGuard guard(dev);
+    if (!guard.ok()) return NLB_EDEVICE;
+    a.lse = const_cast<float *>(lse);
+    a.delta = (float *)work;
+    a.part = dbias ? (float *)((uint8_t *)work + p.delta_bytes) : nullptr;
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, p, dbias, (hipStream_t)stream)
+                                      : launch<float>(a, p, dbias, (hipStream_t)stream);
+}

@@ -143,7 +143,7 @@ def test_fixed_lengths_without_starts(dtype):
 @pytest.mark.parametrize("gap", [3, 8])
 def test_strided_rows(dtype, gap):
     for one, lq, lk in ((False, [40, 90], [50, 90]), (True, [1] * 9, [30] * 9)):
-        c = make(dtype, lq, lk, 4, 2, 50, bias=True, times=True, gap=gap)
+        c = make(dtype, lq, lk, 4, 2, 50, bias=True, times=True, gap=gap, train=True)
         assert not c["q"].is_contiguous()
         check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype=dtype)
 
@@ -151,7 +151,7 @@ def test_strided_rows(dtype, gap):
 def test_long_and_wide_groups():
     """Thousands of keys (many chunks, many tiles), sixteen heads on one."""
     for one, lq, lk in ((True, [1, 1], [9000, 40]), (False, [300], [5000])):
-        c = make("bf16", lq, lk, 16, 1, 64, bias=True)
+        c = make("bf16", lq, lk, 16, 1, 64, bias=True, train=True)
         check(c, lq, lk, run(c, lq, lk, causal=True, one=one), causal=True, dtype="bf16")
 
 
@@ -160,7 +160,7 @@ def test_long_and_wide_groups():
 def test_closed_keys_may_hold_anything(dtype, one):
     """NaN and infinities in rows that no query may see leave no trace."""
     lq, lk = ([1] * 4, [100] * 4) if one else ([60, 5, 9], [60, 70, 80])
-    c = make(dtype, lq, lk, 2, 2, 64, bias=True, times=True, closed=0.5)
+    c = make(dtype, lq, lk, 2, 2, 64, bias=True, times=True, closed=0.5, train=True)
     c["k_pos"][:lk[0]] = -1                                   # nothing open at all in the first
     shut = c["k_pos"] == -1
     clean = run(c, lq, lk, causal=False, one=one)
@@ -182,7 +182,7 @@ def test_bias_that_closes_a_bucket(dtype, one, low):
     import torch
     lq, lk = ([1] * 3, [50, 9, 200]) if one else ([50, 9, 150], [50, 9, 200])
     for shut in ([0, 1], [5, 6, 7, 8], list(range(9))):
-        c = make(dtype, lq, lk, 2, 1, 32, bias=True)
+        c = make(dtype, lq, lk, 2, 1, 32, bias=True, train=True)
         c["bias"][shut] = -float("inf") if low == "inf" else torch.finfo(_dtype(dtype)).min
         check(c, lq, lk, run(c, lq, lk, causal=True, one=one), causal=True, dtype=dtype, what=str(shut))
 
@@ -191,7 +191,7 @@ def test_gaps_of_unsigned_positions_are_clamped():
     """Positions over the whole unsigned range; gaps beyond int32."""
     import torch
     for one, lq, lk in ((True, [1] * 6, [6] * 6), (False, [6], [6])):
-        c = make("f32", lq, lk, 2, 2, 16, bias=True, times=True, closed=0)
+        c = make("f32", lq, lk, 2, 2, 16, bias=True, times=True, closed=0, train=True)
         at = torch.tensor([0, 1, 2**31 - 1, 2**31, 2**32 - 2, 2**32 - 3], dtype=torch.int64)
         c["q_pos"] = at.to(torch.uint32).view(torch.int32)
         c["k_pos"] = at.repeat(len(lk)).to(torch.uint32).view(torch.int32)
@@ -254,11 +254,137 @@ def test_graph_and_streams():
 
 def test_same_bits_each_time():
     import torch
-    c = make("bf16", [300, 5], [400, 5], 4, 2, 64, bias=True, times=True, train=False)
-    a = run(c, [300, 5], [400, 5], causal=True)
-    b = run(c, [300, 5], [400, 5], causal=True)
-    for n in a:
-        assert torch.equal(a[n], b[n])
+    for one, lq, lk in ((False, [300, 5], [400, 5]), (True, [1] * 300, [60] * 300)):
+        c = make("bf16", lq, lk, 4, 2, 64, bias=True, times=True, train=True)
+        a, b = (run(c, lq, lk, causal=True, one=one) for _ in range(2))
+        for n in a:
+            assert torch.equal(a[n], b[n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("mode", ["plain", "places", "times"])
+@pytest.mark.parametrize("dim", [1, 8, 25, 32, 50, 64, 100, 128])
+def test_gradients_of_packed_sequences(dtype, causal, mode, dim):
+    for name, (lq, lk) in LENGTHS.items():
+        heads, kv_heads = (4, 2) if dim != 25 else (3, 3)
+        c = make(dtype, lq, lk, heads, kv_heads, dim, bias=mode != "plain", times=mode == "times", seed=dim,
+                 train=True)
+        check(c, lq, lk, run(c, lq, lk, causal=causal), causal=causal, dtype=dtype, what=name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["plain", "places", "times"])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 1), (4, 1, 25), (6, 2, 50), (7, 1, 64), (8, 8, 128), (2, 2, 33)])
+def test_gradients_of_single_rows(dtype, mode, heads, kv_heads, dim):
+    """Lists that the single-row form takes, and lists too long for it."""
+    for lk in ([1] * 3, [10] * 50, [64] * 5, [700] * 2, [600, 0, 3, 255, 256, 257, 1, 1, 1], [0, 0]):
+        lq = [1] * len(lk)
+        c = make(dtype, lq, lk, heads, kv_heads, dim, bias=mode != "plain", times=mode == "times", seed=dim,
+                 train=True)
+        check(c, lq, lk, run(c, lq, lk, causal=True, one=True), causal=True, dtype=dtype, what=str(lk))
+
+
+def test_many_lists_keep_their_heads():
+    """More lists than wavefronts in flight, an odd number of key/value heads."""
+    for kv_heads, n in ((3, 5000), (5, 3000)):
+        c = make("f32", [1] * n, [7] * n, kv_heads, kv_heads, 16, bias=True, times=True, train=True)
+        check(c, [1] * n, [7] * n, run(c, [1] * n, [7] * n, causal=False, one=True), causal=False, dtype="f32")
+
+
+def test_gradients_against_differences():
+    """dq, dk, dv and dbias against differences of the forward pass itself."""
+    import torch
+    lq, lk = [5, 9], [8, 9]
+    c = make("f32", lq, lk, 2, 1, 16, bias=True, train=True, sharp=1.0)
+    got = run(c, lq, lk, causal=True)
+    gen = torch.Generator().manual_seed(5)
+    for n, grad in (("q", "dq"), ("k", "dk"), ("v", "dv"), ("bias", "dbias")):
+        step = torch.randn(c[n].shape, generator=gen)
+        vals, h = [], 2.0 ** -7
+        for sign in (1.0, -1.0):
+            d = dict(c, do=None)
+            d[n] = c[n] + sign * h * step
+            vals.append((run(d, lq, lk, causal=True)["o"].cpu().double() * c["do"].double()).sum())
+        slope = float(vals[0] - vals[1]) / (2 * h)
+        want = float((got[grad].cpu().double() * step.double()).sum())
+        # the forward pass is off by about 2^-24 of each of 448 terms of size 1 or so, over 2 h: 2^-24 448 64 = 2e-3;
+        # the difference's own third-order term is h^2 times a third derivative of some tens: 6e-5 x 100
+        assert abs(slope - want) <= 8e-3 + 1e-2 * abs(want) ** 0.5, (n, slope, want)
+
+
+def test_gradients_into_a_joint_projection():
+    """q, k, v as slices of one tensor, their gradients into slices of another."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    c = make("bf16", [70, 60], [70, 60], 4, 2, 64, bias=True, train=True)
+    qkv = torch.cat([c["q"], c["k"], c["v"]], 1).cuda()
+    grad = torch.full_like(qkv, 7.0)
+    part = lambda t: (t[:, :4], t[:, 4:6], t[:, 6:])  # noqa: E731
+    st = torch.from_numpy(ref.starts([70, 60])).cuda()
+    how = dict(q_start=st, k_start=st, causal=True, bias=c["bias"].cuda(), bounds=c["bounds"].cuda())
+    o, lse = nlb.attention(*part(qkv), **how)
+    dq, dk, dv = part(grad)
+    dbias = nlb.attention_backward(c["do"].cuda(), *part(qkv), o, lse, dq=dq, dk=dk, dv=dv, **how)[3]
+    torch.cuda.synchronize()
+    got = {"o": o, "lse": lse, "dq": grad[:, :4], "dk": grad[:, 4:6], "dv": grad[:, 6:], "dbias": dbias}
+    check(c, [70, 60], [70, 60], got, causal=True, dtype="bf16")
+    more = nlb.attention_backward(c["do"].cuda(), *part(qkv), o, lse, need_dbias=False, **how)
+    torch.cuda.synchronize()
+    assert more[3] is None
+    check({**c}, [70, 60], [70, 60], {**got, "dq": more[0], "dk": more[1], "dv": more[2]}, causal=True, dtype="bf16")
+
+
+def test_gradient_rows_outside_the_sequences_stay():
+    import torch
+    import paper_2402_01964_amd as nlb
+    c = make("bf16", [100], [100], 2, 2, 32, train=True)
+    q, k, v, do = (c[n].cuda() for n in ("q", "k", "v", "do"))
+    st = torch.tensor([10, 40, 40, 90], dtype=torch.int32, device="cuda")
+    kw = dict(q_start=st, k_start=st, causal=True)
+    o, lse = nlb.attention(q, k, v, **kw)
+    d = [torch.full_like(q, 7.0) for _ in range(3)]
+    nlb.attention_backward(do, q, k, v, o, lse, dq=d[0], dk=d[1], dv=d[2], **kw)
+    torch.cuda.synchronize()
+    for t in d:
+        assert (t[:10] == 7).all() and (t[90:] == 7).all() and (t[10:90] != 7).flatten(1).any(-1).all()
+
+
+@pytest.mark.parametrize("one", [False, True])
+def test_captured_training_step(one):
+    """Forward and backward captured with their working memory, replayed with
+    new inputs, eager calls between."""
+    import torch
+    import paper_2402_01964_amd as nlb
+    lq, lk = ([1] * 40, [20] * 40) if one else ([100, 33], [100, 70])
+    cs = [make("bf16", lq, lk, 4, 2, 64, bias=True, times=True, train=True, seed=s) for s in range(2)]
+    how = dict(batch=len(lq), bounds=cs[0]["bounds"].cuda())
+    if not one:
+        how.update(q_start=torch.from_numpy(ref.starts(lq)).cuda(), k_start=torch.from_numpy(ref.starts(lk)).cuda())
+    names = ("q", "k", "v", "do", "bias", "q_pos", "k_pos")
+
+    def step(t):
+        kw = dict(how, **{n: t[n] for n in names[4:]})
+        o, lse = nlb.attention(t["q"], t["k"], t["v"], **kw)
+        return (o, lse) + nlb.attention_backward(t["do"], t["q"], t["k"], t["v"], o, lse, **kw)
+    ins = [{n: c[n].cuda() for n in names} for c in cs]
+    want = [[x.clone() for x in step(t)] for t in ins]
+    t = {n: x.clone() for n, x in ins[0].items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = step(t)
+    for turn in range(4):
+        for n in names:
+            t[n].copy_(ins[turn % 2][n])
+        for x in got:
+            x.fill_(0)
+        graph.replay()
+        other = step(ins[1])
+        torch.cuda.synchronize()
+        for a, b, x, y in zip(got, want[turn % 2], other, want[1]):
+            assert torch.equal(a, b) and torch.equal(x, y)
 
 
 def test_offsets_beyond_32_bits():

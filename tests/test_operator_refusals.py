@@ -72,6 +72,42 @@ def test_attention_grid_limit():
     assert lib.nlb_attention(ctypes.byref(c), ROWS, None, None, 0, None) == nlb.NLB_EINVAL
 
 
+def _backward(lib, c, o=ROWS, lse=P, dout=ROWS, dq=ROWS, dk=ROWS, dv=ROWS, dbias=None, work=None, size=0):
+    return lib.nlb_attention_backward(ctypes.byref(c), o, lse, dout, dq, dk, dv, dbias, work, size, None)
+
+
+@pytest.mark.parametrize("bad", BAD_CALLS, ids=lambda b: ",".join(b))
+def test_attention_backward_refuses(bad):
+    lib, n = nlb.load_library(), ctypes.c_size_t(7)
+    c = _call(**bad)
+    assert lib.nlb_attention_work(ctypes.byref(c), 1, ctypes.byref(n)) == nlb.NLB_EINVAL
+    assert n.value == 7
+    assert _backward(lib, c, work=P, size=1 << 40) == nlb.NLB_EINVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(o=None), dict(dout=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(lse=None), dict(lse=P + 2),
+    dict(o=nlb._AttRows(None, 256, 64)), dict(dout=nlb._AttRows(P + 1, 256, 64)), dict(dq=nlb._AttRows(P, -1, 0)),
+    dict(dk=nlb._AttRows(None, 0, 0)), dict(dv=nlb._AttRows(P, 0, 2**31)), dict(dbias=P), dict(work=P + 4)],
+    ids=lambda b: ",".join(b))
+def test_attention_backward_refuses_its_own_arguments(bad):
+    lib = nlb.load_library()
+    assert _backward(lib, _call(), **{"work": P, "size": 1 << 40, **bad}) == nlb.NLB_EINVAL
+    c = _call(buckets=4, bias=P, bounds=P)
+    assert _backward(lib, c, dbias=P + 1, work=P, size=1 << 40) == nlb.NLB_EINVAL
+
+
+def test_attention_backward_work_is_checked():
+    lib, n = nlb.load_library(), ctypes.c_size_t()
+    for c in (_call(), _call(buckets=4, bias=P, bounds=P), _call(q_rows=2, buckets=4, bias=P, bounds=P)):
+        assert lib.nlb_attention_work(ctypes.byref(c), 1, ctypes.byref(n)) == nlb.NLB_OK
+        assert n.value > 0
+        for work, size in ((P, n.value - 1), (None, n.value), (None, 0)):
+            assert _backward(lib, c, work=work, size=size) == nlb.NLB_ESCRATCH
+    c = _call(heads=256, kv_heads=256, k_rows=2**31 - 1, k_start=P)
+    assert _backward(lib, c, work=P, size=1 << 50) == nlb.NLB_EINVAL      # more workgroups than a grid has
+
+
 def test_binding_checks_its_tensors():
     import torch
     x = torch.zeros(4, 2, 8)
