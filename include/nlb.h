@@ -455,6 +455,46 @@ int nlb_attention_backward(const nlb_att_call *call, const nlb_att_rows *o, cons
                            const nlb_att_rows *dout, const nlb_att_rows *dq, const nlb_att_rows *dk,
                            const nlb_att_rows *dv, void *dbias, void *work, size_t work_bytes, void *stream);
 
+/* Layer norm of rows, before and after such a layer:
+ *   mean = sum x / width,  rstd = (sum (x - mean)^2 / width + eps)^-1/2
+ *   y = (x - mean) rstd w + b
+ * x, y: device rows of `width` contiguous values of dtype, x_stride and
+ * y_stride values apart (0 .. 2^31 - 1; y may be x).  w, b: device fp32
+ * [width], NULL for ones and zeros.  mean, rstd: device fp32 [rows], written
+ * (NULL where no backward pass follows).  All sums are fp32, each row's values
+ * are read once; y is rounded once.  rows = 0 is a no-op.
+ *   nlb_layer_norm_backward, from the same call with mean and rstd as written,
+ * and the gradient dy of y:
+ *   g = dy w,  xh = (x - mean) rstd
+ *   dx = rstd (g - sum g / width - xh sum (g xh) / width)
+ *   dw = sum over rows of dy xh,  db = sum over rows of dy
+ * dx may be dy.  dw, db: device fp32 [width], written (not added to), either
+ * may be NULL; with both NULL no work is needed, else nlb_layer_norm_work
+ * bytes of device memory (16-byte aligned) that the call's kernels use.  Sums
+ * over rows are fp32 within a workgroup, then fp64, in a fixed order.
+ *   Only enqueues kernels: may be captured in a HIP graph.  Errors: NLB_EINVAL
+ * (NULL rows, mean or rstd, a bad size, type, stride, alignment or eps),
+ * NLB_ESCRATCH, NLB_EDEVICE. */
+#define NLB_NORM_MAX_WIDTH 8192
+
+typedef struct nlb_norm_call {
+    int32_t device;          /* HIP device ordinal, -1 = current */
+    int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: x, y, dy, dx */
+    uint32_t rows;
+    int32_t width;           /* 1 .. NLB_NORM_MAX_WIDTH */
+    const void *x;
+    int64_t x_stride;        /* values */
+    const float *w;
+    float *mean, *rstd;
+} nlb_norm_call;
+
+int nlb_layer_norm(const nlb_norm_call *call, const float *b, float eps, void *y, int64_t y_stride, void *stream);
+
+int nlb_layer_norm_work(const nlb_norm_call *call, size_t *bytes);
+
+int nlb_layer_norm_backward(const nlb_norm_call *call, const void *dy, int64_t dy_stride, void *dx,
+                            int64_t dx_stride, float *dw, float *db, void *work, size_t work_bytes, void *stream);
+
 /* Free the table's device memory after synchronising its device.  NULL is a
  * no-op.  Borrowed buffers are not touched. */
 int nlb_destroy(nlb_table *h);

@@ -25,13 +25,14 @@ MAX_SLOTS = 1024
 # Symbols declared in include/nlb.h.
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
                "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
-               "nlb_attention_backward", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
+               "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
                "nlb_strerror")
 AGG_HIDDEN = 64
 RNN_MAX_DIM = 1024
 DTYPE_F32, DTYPE_BF16 = 0, 1
 RNN_FORM_NONE, RNN_FORM_TILED, RNN_FORM_WEIGHT_STATIONARY = 0, 1, 2
 ATT_MAX_DIM, ATT_MAX_HEADS, ATT_MAX_BUCKETS = 128, 256, 64
+NORM_MAX_WIDTH = 8192
 EID_LAST_BATCH = 2**64 - 1   # first_eid of rnn_update: the links inserted last (device count)
 
 
@@ -77,6 +78,12 @@ class _AttCall(ctypes.Structure):
                [("scale", ctypes.c_float)] + [(k, ctypes.c_uint32) for k in ("batch", "q_rows", "k_rows")] + \
                [(k, ctypes.c_void_p) for k in ("q_start", "k_start", "bias", "bounds", "q_pos", "k_pos")] + \
                [(k, _AttRows) for k in ("q", "k", "v")]
+
+
+class _NormCall(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_uint32),
+                ("width", ctypes.c_int32), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64)] + \
+               [(k, ctypes.c_void_p) for k in ("w", "mean", "rstd")]
 
 
 class _Info(ctypes.Structure):
@@ -131,6 +138,13 @@ def load_library(path: str | None = None):
     lib.nlb_attention.restype = I
     lib.nlb_attention_backward.argtypes = [ctypes.POINTER(_AttCall), R, P, R, R, R, R, P, P, S, P]
     lib.nlb_attention_backward.restype = I
+    N, I64 = ctypes.POINTER(_NormCall), ctypes.c_int64
+    lib.nlb_layer_norm.argtypes = [N, P, ctypes.c_float, P, I64, P]
+    lib.nlb_layer_norm.restype = I
+    lib.nlb_layer_norm_work.argtypes = [N, ctypes.POINTER(S)]
+    lib.nlb_layer_norm_work.restype = I
+    lib.nlb_layer_norm_backward.argtypes = [N, P, I64, P, I64, P, P, P, S, P]
+    lib.nlb_layer_norm_backward.restype = I
     lib.nlb_destroy.argtypes = [P]
     lib.nlb_destroy.restype = I
     lib.nlb_get_info.argtypes = [P, ctypes.POINTER(_Info)]
@@ -591,3 +605,78 @@ def attention_backward(dout, q, k, v, out, lse, *, batch=None, q_start=None, k_s
                                           None if dbias is None else _dev_ptr(_like(dbias, q, "dbias"), None, "dbias"),
                                           p, size, s), "nlb_attention_backward")
     return dq, dk, dv, dbias
+
+
+def _norm_rows(t, x, name):
+    """[..., width] as rows: their stride in values."""
+    if t.shape != x.shape:
+        raise ValueError(f"{name} must have x's shape")
+    _like(t, x, name)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    if t.dim() > 2 and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, or of two dimensions")
+    return t.stride(0) if t.dim() == 2 else t.shape[-1]
+
+
+def _fp32_vector(t, n, x, name):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or t.device != x.device:
+        raise ValueError(f"{name} must be float32 with {n} elements, on x's device")
+    return _dev_ptr(t, 4, name)
+
+
+def _norm_call(x, w, mean, rstd):
+    c = _NormCall()
+    c.dtype = _float_dtype(x, "x")
+    if x.dim() < 1:
+        raise ValueError("x must have a last dimension")
+    c.device, c.width = x.device.index, x.shape[-1]
+    c.rows = x.numel() // max(1, c.width)
+    c.x, c.x_stride = x.data_ptr(), _norm_rows(x, x, "x")
+    c.w = _fp32_vector(w, c.width, x, "w")
+    c.mean, c.rstd = _fp32_vector(mean, c.rows, x, "mean"), _fp32_vector(rstd, c.rows, x, "rstd")
+    return c
+
+
+def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rstd=None, stream=None):
+    """Layer norm over the last dimension (nlb_layer_norm): ``x`` float32 or
+    bfloat16, two-dimensional with any row stride or contiguous; ``w``, ``b``
+    float32 or None.  Returns (or fills) out (as x), mean and rstd (float32,
+    one per row)."""
+    import torch
+    lib = load_library()
+    _float_dtype(x, "x")
+    with _OnStream(x.device, stream) as s:
+        rows = x.shape[:-1]
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) if t is None else t for t in (mean, rstd))
+        c = _norm_call(x, w, mean, rstd)
+        _check(lib.nlb_layer_norm(ctypes.byref(c), _fp32_vector(b, c.width, x, "b"), float(eps), out.data_ptr(),
+                                  _norm_rows(out, x, "out"), s), "nlb_layer_norm")
+    return out, mean, rstd
+
+
+def layer_norm_backward(dy, x, w, mean, rstd, *, dx=None, dw=None, db=None, work=None, stream=None):
+    """Gradients of ``layer_norm`` (nlb_layer_norm_backward) from its x, w,
+    mean and rstd and the gradient ``dy`` of its result.  Returns (or fills)
+    dx (as x), dw and db (float32)."""
+    import torch
+    lib = load_library()
+    _float_dtype(x, "x")
+    with _OnStream(x.device, stream) as s:
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        c = _norm_call(x, w, mean, rstd)
+        dw, db = (torch.empty(c.width, dtype=torch.float32, device=x.device) if t is None else t for t in (dw, db))
+        n = ctypes.c_size_t()
+        _check(lib.nlb_layer_norm_work(ctypes.byref(c), ctypes.byref(n)), "nlb_layer_norm_backward")
+        keep, p, size = _work(n.value, work, x)
+        _check(lib.nlb_layer_norm_backward(ctypes.byref(c), dy.data_ptr(), _norm_rows(dy, x, "dy"), dx.data_ptr(),
+                                           _norm_rows(dx, x, "dx"), _fp32_vector(dw, c.width, x, "dw"),
+                                           _fp32_vector(db, c.width, x, "db"), p, size, s),
+               "nlb_layer_norm_backward")
+    return dx, dw, db

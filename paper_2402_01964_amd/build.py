@@ -4,7 +4,8 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", f) for f in ("nlb.hip", "aggregate.hip", "rnn.hip", "attention.hip", "attention_backward.hip")]
+SRCS = [os.path.join(HERE, "csrc", f) for f in (
+    "nlb.hip", "aggregate.hip", "rnn.hip", "attention.hip", "attention_backward.hip", "layer_norm.hip")]
 LIB = os.path.join(HERE, "libnlb.so")
 
 HIPCC_FLAGS = [

@@ -108,8 +108,53 @@ def test_attention_backward_work_is_checked():
     assert _backward(lib, c, work=P, size=1 << 50) == nlb.NLB_EINVAL      # more workgroups than a grid has
 
 
+def _norm(**kw):
+    c = nlb._NormCall()
+    c.device, c.dtype, c.rows, c.width, c.x, c.x_stride, c.mean, c.rstd = -1, nlb.DTYPE_BF16, 10, 100, P, 100, P, P
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+BAD_NORMS = [dict(dtype=2), dict(rows=2**31), dict(width=0), dict(width=8193), dict(x=None), dict(x=P + 1), dict(w=P + 2),
+             dict(mean=P + 2), dict(rstd=P + 1), dict(x_stride=-1), dict(x_stride=2**31)]
+
+
+@pytest.mark.parametrize("bad", BAD_NORMS, ids=lambda b: ",".join(b))
+def test_layer_norm_refuses(bad):
+    lib, n = nlb.load_library(), ctypes.c_size_t(7)
+    c = _norm(**bad)
+    assert lib.nlb_layer_norm(ctypes.byref(c), None, 1e-5, P, 100, None) == nlb.NLB_EINVAL
+    assert lib.nlb_layer_norm_work(ctypes.byref(c), ctypes.byref(n)) == nlb.NLB_EINVAL and n.value == 7
+    assert lib.nlb_layer_norm_backward(ctypes.byref(c), P, 100, P, 100, P, P, P, 1 << 40, None) == nlb.NLB_EINVAL
+
+
+def test_layer_norm_refuses_its_own_arguments():
+    lib, n = nlb.load_library(), ctypes.c_size_t()
+    c = _norm()
+    for b, eps, y, stride in ((P + 2, 1e-5, P, 100), (None, -1.0, P, 100), (None, float("nan"), P, 100),
+                              (None, float("inf"), P, 100), (None, 1e-5, None, 100), (None, 1e-5, P + 1, 100),
+                              (None, 1e-5, P, -1), (None, 1e-5, P, 2**31)):
+        assert lib.nlb_layer_norm(ctypes.byref(c), b, eps, y, stride, None) == nlb.NLB_EINVAL
+    assert lib.nlb_layer_norm(None, None, 1e-5, P, 100, None) == nlb.NLB_EINVAL
+    assert lib.nlb_layer_norm_work(ctypes.byref(c), None) == nlb.NLB_EINVAL
+    assert lib.nlb_layer_norm_work(ctypes.byref(c), ctypes.byref(n)) == nlb.NLB_OK and n.value > 0
+    back = lib.nlb_layer_norm_backward
+    for dy, dys, dx, dxs, dw, db, work in ((None, 100, P, 100, P, P, P), (P, -1, P, 100, P, P, P),
+                                           (P, 100, None, 100, P, P, P), (P, 100, P, 2**31, P, P, P),
+                                           (P, 100, P, 100, P + 2, P, P), (P, 100, P, 100, P, P + 1, P),
+                                           (P, 100, P, 100, P, P, P + 8)):
+        assert back(ctypes.byref(c), dy, dys, dx, dxs, dw, db, work, 1 << 40, None) == nlb.NLB_EINVAL
+    for bad in (dict(mean=None), dict(rstd=None)):
+        assert back(ctypes.byref(_norm(**bad)), P, 100, P, 100, P, P, P, 1 << 40, None) == nlb.NLB_EINVAL
+    for work, size in ((None, 1 << 40), (P, n.value - 1)):
+        assert back(ctypes.byref(c), P, 100, P, 100, P, None, work, size, None) == nlb.NLB_ESCRATCH
+
+
 def test_binding_checks_its_tensors():
     import torch
     x = torch.zeros(4, 2, 8)
     with pytest.raises(TypeError):
         nlb.attention(x, x, x)
+    with pytest.raises(TypeError):
+        nlb.layer_norm(x)
