@@ -23,27 +23,42 @@ struct Norm {
 
 template <typename T> struct Chunk { static constexpr int n = 16 / sizeof(T); };
 
-// 16 bytes of values from c0 on of a row of `width`, zeros past its end
+// 16 bytes of values from c0 on of a row of `width`, zeros past its end.
 template <typename T>
-__device__ __forceinline__ void load_values(const uint8_t *row, uint32_t c0, uint32_t width,
-                                            float (&f)[Chunk<T>::n]) {
-    constexpr int n = Chunk<T>::n;
-    const T *p = (const T *)row + c0;
+__device__ __forceinline__ u32x4 load_chunk(const uint8_t *row, uint32_t c0, uint32_t width) {
+    constexpr uint32_t n = Chunk<T>::n;
+    const uint8_t *p = row + c0 * sizeof(T);
+    u32x4 x = {0, 0, 0, 0};
     if (c0 + n <= width) {
-        const u32x4 v = *(const u32x4_any *)p;
+        x = *(const u32x4_any *)p;
+    } else if (c0 < width) {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if constexpr (sizeof(T) == 4) {
-                f[i] = __uint_as_float(v[i]);
-            } else {
-                f[2 * i] = __uint_as_float(v[i] << 16);
-                f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
+        for (uint32_t i = 0; i < n - 1; i++)
+            if (c0 + i < width) {
+                if constexpr (sizeof(T) == 4) x[i] = ((const uint32_t *)p)[i];
+                else x[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
             }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < n; i++) f[i] = c0 + i < width ? (float)p[i] : 0.0f;
     }
+    return x;
+}
+
+template <typename T> __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Chunk<T>::n]) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (sizeof(T) == 4) {
+            f[i] = __uint_as_float(x[i]);
+        } else {
+            f[2 * i] = __uint_as_float(x[i] << 16);
+            f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        }
+    }
+}
+
+// Values c0 .. c0 + n - 1 of a vector of `width`, `other` without one or past its end.
+template <int n>
+__device__ __forceinline__ void load_weights(const float *p, uint32_t c0, uint32_t width, float other, float (&f)[n]) {
+#pragma unroll
+    for (int i = 0; i < n; i++) f[i] = p && c0 + i < width ? p[c0 + i] : other;
 }
 
 template <typename T, int n>
@@ -67,68 +82,86 @@ __device__ __forceinline__ void store_row(uint8_t *row, uint32_t c0, uint32_t wi
 }
 
 // The sum of x over the N threads that share a row (a power of two, up to the
-// 256 of the workgroup), in each of them.
+// 256 of the workgroup), in each of them: within a wavefront by lane
+// permutations of the vector units, over wavefronts through LDS.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
+    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
 template <int N> __device__ __forceinline__ float row_sum(float x, float (&lds)[4]) {
-#pragma unroll
-    for (int w = 1; w < (N < 64 ? N : 64); w *= 2) x += __shfl_xor(x, w);
+    x = dpp_add<0xB1>(x);
+    x = dpp_add<0x4E>(x);
+    if constexpr (N > 4) x = dpp_add<0x141>(x);
+    if constexpr (N > 8) x = dpp_add<0x140>(x);
+    if constexpr (N > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (N > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     if constexpr (N > 64) {
         __syncthreads();
         if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
         __syncthreads();
-        const uint32_t w0 = threadIdx.x / N * (N / 64);
-        x = lds[w0];
+        x = lds[0];
 #pragma unroll
-        for (int i = 1; i < N / 64; i++) x += lds[w0 + i];
+        for (int i = 1; i < N / 64; i++) x += lds[i];
     }
     return x;
 }
 
 // A row is held in registers by N threads, C chunks of 16 bytes each (chunk
-// i of a thread: values (i N + thread) n on).
+// i of a thread: values (i N + thread) n on), the next row's loads in flight
+// while this one is summed; weights stay in registers over the rows of a
+// workgroup.
 template <typename T, int N, int C>
 __global__ __launch_bounds__(256) void norm_rows(Norm a) {
     constexpr int n = Chunk<T>::n, per = 256 / N;
     __shared__ float lds[4];
-    const uint32_t t = threadIdx.x % N;
+    const uint32_t t = threadIdx.x % N, step = gridDim.x * per;
     const float inv = 1.0f / a.width;
-    for (uint32_t r0 = blockIdx.x * per; r0 < a.rows; r0 += gridDim.x * per) {
-        const uint32_t r = r0 + threadIdx.x / N;
-        const bool there = r < a.rows;
+    float w[C][n], b[C][n];
+#pragma unroll
+    for (int i = 0; i < C; i++) {
+        load_weights<n>(a.w, (i * N + t) * n, a.width, 1.0f, w[i]);
+        load_weights<n>(a.b, (i * N + t) * n, a.width, 0.0f, b[i]);
+    }
+    u32x4 raw[C];
+    const auto fetch = [&](uint32_t r) {
+#pragma unroll
+        for (int i = 0; i < C; i++)
+            raw[i] = load_chunk<T>(a.x + (int64_t)r * a.x_row, (i * N + t) * n, r < a.rows ? a.width : 0);
+    };
+    uint32_t r = blockIdx.x * per + threadIdx.x / N;
+    fetch(r);
+    // (as many turns for every thread of the workgroup: the first row decides)
+    for (uint32_t r0 = blockIdx.x * per; r0 < a.rows; r0 += step, r += step) {
         float x[C][n], sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < C; i++) {
-            load_values<T>(a.x + (int64_t)r * a.x_row, (i * N + t) * n, there ? a.width : 0, x[i]);
+            unpack<T>(raw[i], x[i]);
 #pragma unroll
             for (int e = 0; e < n; e++) sum += x[i][e];
         }
+        if (r0 + step < a.rows) fetch(r + step);
         const float mean = row_sum<N>(sum, lds) * inv;
         float sq = 0.0f;
 #pragma unroll
         for (int i = 0; i < C; i++)
 #pragma unroll
             for (int e = 0; e < n; e++) {
-                x[i][e] -= mean;
-                if ((i * N + t) * n + e < a.width) sq = fmaf(x[i][e], x[i][e], sq);
+                x[i][e] = (i * N + t) * n + e < a.width ? x[i][e] - mean : 0.0f;
+                sq = fmaf(x[i][e], x[i][e], sq);
             }
         const float rstd = 1.0f / sqrtf(row_sum<N>(sq, lds) * inv + a.eps);
-        if (!there) continue;
+        if (r >= a.rows) continue;
 #pragma unroll
         for (int i = 0; i < C; i++) {
             const uint32_t c = (i * N + t) * n;
             if (c >= a.width) break;
-            float w[n], b[n];
 #pragma unroll
-            for (int e = 0; e < n; e += 4) {
-                float v[4];
-                load_values<float>((const uint8_t *)a.w, c + e, a.w ? a.width : 0, v);
-#pragma unroll
-                for (int f = 0; f < 4; f++) w[e + f] = a.w ? v[f] : 1.0f;
-                load_values<float>((const uint8_t *)a.b, c + e, a.b ? a.width : 0, v);
-#pragma unroll
-                for (int f = 0; f < 4; f++) b[e + f] = v[f];
-            }
-#pragma unroll
-            for (int e = 0; e < n; e++) x[i][e] = fmaf(x[i][e] * rstd, w[e], b[e]);
+            for (int e = 0; e < n; e++) x[i][e] = fmaf(x[i][e] * rstd, w[i][e], b[i][e]);
             store_row<T, n>(a.out + (int64_t)r * a.out_row, c, a.width, x[i]);
         }
         if (t == 0) {
@@ -139,53 +172,61 @@ __global__ __launch_bounds__(256) void norm_rows(Norm a) {
 }
 
 // As norm_rows; a thread keeps its values' sums of dy xh and dy over the rows
-// of its workgroup and leaves them in part[workgroup].
+// of its workgroup, which leaves them in part[workgroup].
 template <typename T, int N, int C>
 __global__ __launch_bounds__(256) void norm_rows_backward(Norm a) {
     constexpr int n = Chunk<T>::n, per = 256 / N;
     __shared__ float lds[4];
-    const uint32_t t = threadIdx.x % N;
+    const uint32_t t = threadIdx.x % N, step = gridDim.x * per;
     const float inv = 1.0f / a.width;
     float w[C][n], dw[C][n], db[C][n];
 #pragma unroll
-    for (int i = 0; i < C; i++)
+    for (int i = 0; i < C; i++) {
+        load_weights<n>(a.w, (i * N + t) * n, a.width, 1.0f, w[i]);
 #pragma unroll
-        for (int e = 0; e < n; e++) {
-            const uint32_t c = (i * N + t) * n + e;
-            w[i][e] = c < a.width ? (a.w ? a.w[c] : 1.0f) : 0.0f;
-            dw[i][e] = db[i][e] = 0.0f;
-        }
-    for (uint32_t r0 = blockIdx.x * per; r0 < a.rows; r0 += gridDim.x * per) {
-        const uint32_t r = r0 + threadIdx.x / N;
-        const bool there = r < a.rows;
-        float xh[C][n], g[C][n], s1 = 0.0f, s2 = 0.0f;
-        const float mean = there ? a.mean[r] : 0.0f, rstd = there ? a.rstd[r] : 0.0f;
+        for (int e = 0; e < n; e++) dw[i][e] = db[i][e] = 0.0f;
+    }
+    u32x4 rawx[C], rawg[C];
+    float mean = 0.0f, rstd = 0.0f;
+    const auto fetch = [&](uint32_t r) {
+        const uint32_t width = r < a.rows ? a.width : 0;
 #pragma unroll
         for (int i = 0; i < C; i++) {
-            const uint32_t c = (i * N + t) * n;
-            load_values<T>(a.x + (int64_t)r * a.x_row, c, there ? a.width : 0, xh[i]);
-            load_values<T>(a.dy + (int64_t)r * a.dy_row, c, there ? a.width : 0, g[i]);
+            rawx[i] = load_chunk<T>(a.x + (int64_t)r * a.x_row, (i * N + t) * n, width);
+            rawg[i] = load_chunk<T>(a.dy + (int64_t)r * a.dy_row, (i * N + t) * n, width);
         }
+        mean = width ? a.mean[r] : 0.0f;
+        rstd = width ? a.rstd[r] : 0.0f;
+    };
+    uint32_t r = blockIdx.x * per + threadIdx.x / N;
+    fetch(r);
+    for (uint32_t r0 = blockIdx.x * per; r0 < a.rows; r0 += step, r += step) {
+        float xh[C][n], g[C][n], s1 = 0.0f, s2 = 0.0f;
+        const float sd = rstd;
 #pragma unroll
-        for (int i = 0; i < C; i++)
+        for (int i = 0; i < C; i++) {
+            unpack<T>(rawx[i], xh[i]);
+            unpack<T>(rawg[i], g[i]);
 #pragma unroll
             for (int e = 0; e < n; e++) {
-                xh[i][e] = (i * N + t) * n + e < a.width ? (xh[i][e] - mean) * rstd : 0.0f;
+                xh[i][e] = (i * N + t) * n + e < a.width ? (xh[i][e] - mean) * sd : 0.0f;
                 dw[i][e] = fmaf(g[i][e], xh[i][e], dw[i][e]);
                 db[i][e] += g[i][e];
                 g[i][e] *= w[i][e];
                 s1 += g[i][e];
                 s2 = fmaf(g[i][e], xh[i][e], s2);
             }
+        }
+        if (r0 + step < a.rows) fetch(r + step);
         s1 = row_sum<N>(s1, lds) * inv;
         s2 = row_sum<N>(s2, lds) * inv;
-        if (!there) continue;
+        if (r >= a.rows) continue;
 #pragma unroll
         for (int i = 0; i < C; i++) {
             const uint32_t c = (i * N + t) * n;
             if (c >= a.width) break;
 #pragma unroll
-            for (int e = 0; e < n; e++) g[i][e] = rstd * (g[i][e] - s1 - xh[i][e] * s2);
+            for (int e = 0; e < n; e++) g[i][e] = sd * (g[i][e] - s1 - xh[i][e] * s2);
             store_row<T, n>(a.out + (int64_t)r * a.out_row, c, a.width, g[i]);
         }
     }
@@ -219,23 +260,34 @@ __global__ __launch_bounds__(256) void norm_rows_backward(Norm a) {
     }
 }
 
-// dw and db from the workgroups' shares: 64 columns a workgroup, its four
-// wavefronts a quarter of the shares each, in 64 bits and a fixed order.
-__global__ __launch_bounds__(256) void sum_shares(const float *part, uint32_t shares, uint32_t width, float *dw,
-                                                  float *db) {
-    __shared__ double sums[4][64];
+// dw and db from the workgroups' shares: 64 columns a workgroup, every 16th
+// share a wavefront, in 64 bits and a fixed order.
+__global__ __launch_bounds__(1024) void sum_shares(const float *part, uint32_t shares, uint32_t width, float *dw,
+                                                   float *db) {
+    __shared__ double sums[16][64];
     const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
     double x = 0.0;
-    if (c < 2 * width)
-        for (uint32_t i = wave; i < shares; i += 4) x += (double)part[(size_t)i * 2 * width + c];
+    if (c < 2 * width) {
+        const size_t step = 2 * (size_t)width;
+        uint32_t i = wave;
+        for (; i + 112 < shares; i += 128) {                  // eight loads in flight
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) v[u] = part[(i + 16 * u) * step + c];
+#pragma unroll
+            for (int u = 0; u < 8; u++) x += (double)v[u];
+        }
+        for (; i < shares; i += 16) x += (double)part[i * step + c];
+    }
     sums[wave][lane] = x;
     __syncthreads();
     if (wave || c >= 2 * width) return;
-    const float s = (float)(sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]);
+#pragma unroll
+    for (int i = 1; i < 16; i++) x += sums[i][lane];
     if (c < width) {
-        if (dw) dw[c] = s;
+        if (dw) dw[c] = (float)x;
     } else if (db) {
-        db[c - width] = s;
+        db[c - width] = (float)x;
     }
 }
 
@@ -309,7 +361,7 @@ template <typename T> int launch(const Norm &a, hipStream_t s) {
     return with_shape<T>(a.width, [&](auto n, auto c) {
         constexpr int N = decltype(n)::value, C = decltype(c)::value;
         const uint32_t per = 256 / N, blocks = (a.rows + per - 1) / per;
-        hipLaunchKernelGGL((norm_rows<T, N, C>), dim3(blocks < 8192 ? blocks : 8192), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((norm_rows<T, N, C>), dim3(blocks < 2048 ? blocks : 2048), dim3(256), 0, s, a);
         return NLB_OK;
     });
 }
@@ -320,7 +372,7 @@ template <typename T> int launch_backward(const Norm &a, float *dw, float *db, h
         const uint32_t blocks = backward_blocks(a.rows, 256 / N);
         hipLaunchKernelGGL((norm_rows_backward<T, N, C>), dim3(blocks), dim3(256), 0, s, a);
         if (a.part)
-            hipLaunchKernelGGL(sum_shares, dim3((2 * a.width + 63) / 64), dim3(256), 0, s, a.part, blocks, a.width, dw,
+            hipLaunchKernelGGL(sum_shares, dim3((2 * a.width + 63) / 64), dim3(1024), 0, s, a.part, blocks, a.width, dw,
                                db);
         return NLB_OK;
     });
