@@ -23,6 +23,8 @@
 // the result itself); sums and statistics take them unrounded.
 #pragma once
 
+#include <algorithm>
+
 #include "nlb_internal.h"
 
 namespace {
@@ -57,7 +59,7 @@ struct Attend {
     const int32_t *q_start, *k_start;
     uint32_t batch, q_rows, k_rows, q_len, k_len;   // *_len: rows of every sequence where *_start is null
     uint32_t heads, kv_heads, group, dim;
-    uint32_t causal, buckets;
+    uint32_t causal, buckets, dtype_bytes;
     float scale, scale2;                 // scale2: scale log2(e)
     const int32_t *bounds;
     const void *bias;                    // [buckets][heads]
@@ -404,6 +406,46 @@ __device__ __forceinline__ int block_row(int r) {
     return 8 * (r / 4) + 4 * ((threadIdx.x >> 5) & 1u) + r % 4;
 }
 
+// ---------------------------------------------------------------- lists
+// How a row's values lie across lanes where rows are read one by one.
+template <typename T, int DP> struct Lanes {
+    static constexpr int per_row = DP / Chunk<T>::n;
+    static constexpr int rows = 64 / per_row;
+};
+constexpr int kListKeys = 64;            // keys of a list whose open ones are looked up at once
+
+// The open keys among j0 .. j0 + 63 of each lane group's list, as a bit mask
+// in each of its lanes, and their buckets in codes[group][64].  A lane looks
+// up every per_row-th key, so each bucket is searched once.
+template <int PER>
+__device__ __forceinline__ uint64_t open_keys(const Attend &a, const int32_t *bounds, uint8_t *codes, uint32_t k0,
+                                              int32_t lk, int32_t j0, int32_t qpos) {
+    const uint32_t lane = threadIdx.x & 63u, c = lane % PER, base = lane - c;
+    uint64_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < kListKeys / PER; i++) {
+        if (!__any(j0 + i * PER < lk)) break;
+        const int32_t j = j0 + i * PER + c;
+        uint32_t pos = j;
+        bool open = j < lk;
+        if (a.k_pos && open) {
+            pos = a.k_pos[k0 + j];
+            open = pos != kNoKey;
+        }
+        const uint64_t m = __ballot(open);
+        mine |= ((m >> base) & ((1ull << PER) - 1)) << (i * PER);
+        if (a.buckets) codes[base / PER * kListKeys + i * PER + c] = bucket_of(bounds, a.buckets, gap_of(qpos, flip(pos)));
+    }
+    return mine;
+}
+
+// The LDS writes of the wavefront's lanes before its reads after.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // ---------------------------------------------------------------- host
 // Rows of a call as the kernels take them.
 inline int fill_rows(const nlb_att_call *c, const nlb_att_rows *r, bool needed, Strided &out) {
@@ -452,6 +494,7 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
     a.dim = c->dim;
     a.causal = c->causal;
     a.buckets = c->buckets;
+    a.dtype_bytes = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
     a.scale = c->scale;
     a.scale2 = c->scale * kLog2e;
     a.bounds = c->bounds;
@@ -469,56 +512,84 @@ inline int device_of(const nlb_att_call *c, int &dev) {
     return dev < n ? NLB_OK : NLB_EINVAL;
 }
 
+// Kernels that take more LDS than 64 KiB need to be allowed it.
+template <typename K> bool allow_lds(K kernel, uint32_t bytes) {
+    if (bytes <= 65536) return true;
+    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Which kernels a call runs.
+enum Form { kTiles, kOne, kLists };
+
 struct Forward {
-    bool one;                            // one query row per sequence
-    uint32_t chunk;                      // keys of a wavefront then
+    Form form;
+    uint32_t chunk;                      // kOne: keys of a wavefront
     uint64_t slots, most;
     size_t bytes;
 };
 
-// One query row per sequence: a wavefront a list until lists are too few to
-// fill the card (8 wavefronts on each of 1024 SIMDs), then chunks of the keys,
-// of 256 rows at least, so that what a chunk writes stays below a hundredth of
-// what it reads.
+// One query row per sequence.  Short lists, many of them, take a group of
+// lanes each (kLists).  Else a wavefront takes a list (kOne), or where lists
+// are too few to fill the card (8 wavefronts on each of 1024 SIMDs) a chunk of
+// its keys, of 256 rows at least, so that what a chunk writes stays below a
+// hundredth of what it reads.
+inline bool short_lists(const Attend &a) { return a.k_rows / kListKeys <= a.batch; }
+
 inline Forward plan_forward(const Attend &a) {
     Forward f = {};
-    f.one = !a.q_start && a.q_len == 1;
-    if (!f.one) {
+    if (a.q_start || a.q_len != 1) {
         f.slots = (uint64_t)a.q_rows / kOwned + a.batch;
         f.most = INT32_MAX / a.heads;
         return f;
     }
+    f.most = INT32_MAX;
+    f.slots = a.batch;
+    f.form = kLists;
+    if (short_lists(a)) return f;
+    f.form = kOne;
     const uint64_t even = ((uint64_t)a.k_rows * a.kv_heads + 8191) / 8192;
     f.chunk = (uint32_t)(((even < 256 ? 256 : even) + 63) / 64 * 64);
     const bool split = a.k_start ? a.k_rows > f.chunk : a.k_len > f.chunk;
-    f.slots = split ? (uint64_t)a.k_rows / f.chunk + a.batch : a.batch;
-    f.most = INT32_MAX;
+    if (split) f.slots += (uint64_t)a.k_rows / f.chunk;
     f.bytes = split ? align256(f.slots * a.heads * (a.dim + 2) * 4) : 0;
     return f;
 }
 
 struct Backward {
-    bool one;
-    uint32_t blocks, shares;             // workgroups of the single-row form; shares of the first sum of bias gradients
+    bool lists;
+    uint32_t blocks, keep;               // kLists: workgroups; keys whose probabilities stay in LDS
+    uint32_t shares;                     // shares of the first sum of bias gradients
     uint64_t q_slots, q_most, k_slots, k_most;
     uint64_t parts;                      // partial bias gradients
     size_t delta_bytes, bytes;
 };
 
-// The single-row form takes a list per wavefront, so lists have to be short:
-// 256 keys on average at most.  A group's heads are in registers there, four
-// at most.  Everything else, single rows over long histories among it, goes
-// through tiles, whose second kernel spreads over the keys.
+// Short lists with one query row take a group of lanes each; a group's heads
+// are in registers there, four at most.  Everything else, single rows over
+// long histories among it, goes through tiles, whose second kernel spreads
+// over the keys.
 inline Backward plan_backward(const Attend &a) {
     Backward p = {};
-    p.one = !a.q_start && a.q_len == 1 && a.group <= 4 && a.k_rows / 256 <= a.batch;
-    if (p.one) {
-        const uint64_t waves = (uint64_t)a.batch * a.kv_heads;
-        const uint64_t most = 256 * 8 / a.kv_heads, need = (waves + 4 * a.kv_heads - 1) / (4 * a.kv_heads);
-        p.blocks = (uint32_t)((need < most ? need : most) * a.kv_heads);
-        p.parts = p.blocks * 4 / a.kv_heads;
+    p.lists = !a.q_start && a.q_len == 1 && a.group <= 4 && short_lists(a);
+    if (p.lists) {
+        const uint32_t n = a.dtype_bytes == 2 ? 8 : 4, dp = a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128;
+        const uint32_t rows = 64 / (dp / n), gb = a.group > 2 ? 4 : a.group;
+        // every lane group keeps its key/value head: a whole number of heads in a turn of all groups
+        uint32_t x = a.kv_heads, y = 4 * rows;
+        while (y) {
+            const uint32_t z = x % y;
+            x = y;
+            y = z;
+        }
+        const uint32_t unit = a.kv_heads / x, cap = (a.heads * a.buckets > 1024 ? 512 : 2048) / unit * unit;
+        const uint64_t need = ((uint64_t)a.batch * a.kv_heads + 4 * rows - 1) / (4 * rows);
+        p.blocks = (uint32_t)std::min<uint64_t>(cap, (need + unit - 1) / unit * unit);
+        // (beside the other tables of a workgroup, which take 132 KiB at most)
+        const uint32_t rest = kMaxBuckets * 4 + 8 + a.buckets * (a.heads + gb * 4 * rows) * 4 + 4 * rows * kListKeys;
+        p.keep = std::min<uint32_t>(kListKeys, std::min(65536u, 155648u - rest) / (4 * rows * gb * 8));
+        p.parts = p.blocks;
     } else {
         p.q_slots = (uint64_t)a.q_rows / kOwned + a.batch;
         p.k_slots = (uint64_t)a.k_rows / kOwned + a.batch;

@@ -3,8 +3,6 @@
 // attend_join).
 #include "attention.h"
 
-#include <algorithm>
-
 namespace {
 
 // ---------------------------------------------------------------- tiles
@@ -177,11 +175,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
 // have several chunks, whose results (maximum, sum, values in fp32) go to
 // `part` and are joined by attend_join.  Wavefronts take chunk after chunk, so
 // the bias table is staged once.
-template <typename T, int DP> struct Lanes {
-    static constexpr int per_row = DP / Chunk<T>::n;
-    static constexpr int rows = 64 / per_row;
-};
-
 template <typename T, int DP, int GB>
 __global__ __launch_bounds__(kThreads) void attend_one(Attend a) {
     using L = Lanes<T, DP>;
@@ -341,11 +334,14 @@ __global__ __launch_bounds__(kThreads) void attend_one(Attend a) {
     }
 }
 
-// Joins the chunks of the sequences that have more than one: a wavefront per
-// sequence and head, values across its lanes.
+// Joins the chunks of the sequences that have more than one: a workgroup per
+// sequence and head, values across the lanes, every fourth run of 64 chunks a
+// wavefront.
 template <typename T>
-__global__ __launch_bounds__(64) void attend_join(Attend a) {
-    const uint32_t b = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = threadIdx.x;
+__global__ __launch_bounds__(kThreads) void attend_join(Attend a) {
+    __shared__ float tops[4], sums[4], values[4][128];
+    const uint32_t b = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     Seq sq;
     sequence(a, b, sq);
     const uint32_t chunks = ((uint32_t)sq.lk + a.chunk - 1) / a.chunk;
@@ -353,23 +349,178 @@ __global__ __launch_bounds__(64) void attend_join(Attend a) {
     const size_t step = (size_t)a.heads * (a.dim + 2);
     const float *part = a.part + (size_t)(sq.k0 / a.chunk + b) * step + head * (a.dim + 2);
     float m = -INFINITY;
-    for (uint32_t i = lane; i < chunks; i += 64) m = fmaxf(m, part[i * step]);
+    for (uint32_t i = threadIdx.x; i < chunks; i += kThreads) m = fmaxf(m, part[i * step]);
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) m = fmaxf(m, __shfl_xor(m, w));
+    if (lane == 0) tops[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const float base = m == -INFINITY ? 0.0f : m;
+    const uint32_t c0 = min(lane, a.dim - 1), c1 = min(lane + 64, a.dim - 1);
     float sum = 0.0f, x0 = 0.0f, x1 = 0.0f;
-    for (uint32_t i = 0; i < chunks; i++) {
-        const float *p = part + i * step;
-        const float f = exp2_fast(p[0] - base);
-        sum = fmaf(f, p[1], sum);
-        if (lane < a.dim) x0 = fmaf(f, p[2 + lane], x0);
-        if (lane + 64 < a.dim) x1 = fmaf(f, p[2 + lane + 64], x1);
+    for (uint32_t i0 = wave * 64; i0 < chunks; i0 += kThreads) {
+        const uint32_t n = min(64u, chunks - i0);
+        const float f = lane < n ? exp2_fast(part[(i0 + lane) * step] - base) : 0.0f;
+        if (lane < n) sum = fmaf(f, part[(i0 + lane) * step + 1], sum);
+        for (uint32_t u0 = 0; u0 < n; u0 += 8) {              // sixteen loads in flight
+            float v0[8], v1[8];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; u++) {
+                const float *p = part + (i0 + min(u0 + u, n - 1)) * step + 2;
+                v0[u] = p[c0];
+                v1[u] = p[c1];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 8; u++) {
+                const float g = u0 + u < n ? __shfl(f, u0 + u) : 0.0f;
+                x0 = fmaf(g, v0[u], x0);
+                x1 = fmaf(g, v1[u], x1);
+            }
+        }
     }
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
+    values[wave][lane] = x0;
+    values[wave][lane + 64] = x1;
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = sums[0] + sums[1] + sums[2] + sums[3];
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    T *o = (T *)(a.o.p + (int64_t)b * a.o.row + head * a.o.head);
-    if (lane < a.dim) o[lane] = (T)(x0 * inv);
-    if (lane + 64 < a.dim) o[lane + 64] = (T)(x1 * inv);
-    if (lane == 0 && a.lse) a.lse[(size_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (m + log2_fast(sum)) * kLn2;
+    const uint32_t t = threadIdx.x;
+    if (t < a.dim)
+        ((T *)(a.o.p + (int64_t)b * a.o.row + head * a.o.head))[t] =
+            (T)((values[0][t] + values[1][t] + values[2][t] + values[3][t]) * inv);
+    if (t == 0 && a.lse) a.lse[(size_t)b * a.heads + head] = sum == 0.0f ? -INFINITY : (m + log2_fast(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------- short lists
+// Many short lists with a query row each: a group of lanes that spans one row
+// takes a whole list (and up to GB query heads of one key/value head), so a
+// wavefront works on 4 to 16 lists and nothing is joined across lanes but a
+// score's own sum.  A list's open keys are found 64 at a time; closed ones are
+// neither read nor multiplied.
+template <typename T, int DP, int GB>
+__global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
+    using L = Lanes<T, DP>;
+    constexpr int N = Chunk<T>::n, U = 4;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    int32_t *bounds = (int32_t *)lds;
+    float *bias = (float *)(bounds + kMaxBuckets);            // [buckets][heads]
+    uint8_t *codes = (uint8_t *)(bias + a.buckets * a.heads) + (threadIdx.x >> 6) * L::rows * kListKeys;
+    if (a.buckets) {
+        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads)
+            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+        for (uint32_t i = threadIdx.x; i < a.buckets * a.heads; i += kThreads)
+            bias[i] = bias2_of<T>(a, i / a.heads, i % a.heads);
+        __syncthreads();
+    }
+    const uint32_t lane = threadIdx.x & 63u, c0 = (lane % L::per_row) * N, kr = lane / L::per_row;
+    const uint32_t parts = (a.group + GB - 1) / GB, per_list = a.kv_heads * parts;
+    const uint64_t units = (uint64_t)a.batch * per_list, turn = (uint64_t)gridDim.x * 4 * L::rows;
+    for (uint64_t unit0 = (blockIdx.x * 4ull + (threadIdx.x >> 6)) * L::rows; unit0 < units; unit0 += turn) {
+        const bool there = unit0 + kr < units;
+        const uint64_t unit = there ? unit0 + kr : 0;
+        const uint32_t b = unit / per_list, in = unit % per_list;
+        const uint32_t kvh = in % a.kv_heads, g0 = in / a.kv_heads * GB;
+        const uint32_t head0 = kvh * a.group + g0, ng = min((uint32_t)GB, a.group - g0);
+        Seq sq;
+        sequence(a, b, sq);
+        if (!there) sq.lk = 0;
+        float q[GB][N], acc[GB][N], m[GB], sum[GB];
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            u32x4 x = {0, 0, 0, 0};
+            if ((uint32_t)g < ng)
+                x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
+            unpack<T>(x, q[g]);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                q[g][i] *= a.scale2;
+                acc[g][i] = 0.0f;
+            }
+            m[g] = -INFINITY;
+            sum[g] = 0.0f;
+        }
+        const int32_t qpos = a.buckets ? (a.q_pos ? flip(a.q_pos[b]) : flip((uint32_t)sq.lk - 1)) : 0;
+        const uint8_t *kp = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
+        const uint8_t *vp = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
+        for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
+            wave_lds_fence();
+            uint64_t mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+            wave_lds_fence();
+            while (__any(mine != 0)) {
+                u32x4 k[U], v[U];
+                bool open[U];
+                uint32_t at[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    open[u] = mine != 0;
+                    at[u] = open[u] ? __builtin_ctzll(mine) : 0;
+                    mine &= mine - 1;
+                    k[u] = v[u] = u32x4{0, 0, 0, 0};
+                    if (open[u]) {
+                        k[u] = load_chunk<T>(kp + (int64_t)(j0 + at[u]) * a.k.row, c0, a.dim);
+                        v[u] = load_chunk<T>(vp + (int64_t)(j0 + at[u]) * a.v.row, c0, a.dim);
+                    }
+                }
+                float t[U][GB];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    float x[N];
+                    unpack<T>(k[u], x);
+                    const uint32_t bk = a.buckets ? codes[kr * kListKeys + at[u]] * a.heads + head0 : 0;
+#pragma unroll
+                    for (int g = 0; g < GB; g++) {
+                        float s = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < N; i++) s = fmaf(q[g][i], x[i], s);
+                        t[u][g] = lanes_sum<L::per_row>(s);
+                        if (a.buckets && (uint32_t)g < ng) t[u][g] += bias[bk + g];
+                        if (!open[u]) t[u][g] = -INFINITY;
+                    }
+                }
+                float p[U][GB];
+#pragma unroll
+                for (int g = 0; g < GB; g++) {
+                    float up = m[g];
+#pragma unroll
+                    for (int u = 0; u < U; u++) up = fmaxf(up, t[u][g]);
+                    const float base = up == -INFINITY ? 0.0f : up, f = exp2_fast(m[g] - base);
+                    m[g] = up;
+                    sum[g] *= f;
+#pragma unroll
+                    for (int i = 0; i < N; i++) acc[g][i] *= f;
+#pragma unroll
+                    for (int u = 0; u < U; u++) {
+                        p[u][g] = exp2_fast(t[u][g] - base);
+                        sum[g] += p[u][g];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    float x[N];
+                    unpack<T>(v[u], x);
+#pragma unroll
+                    for (int g = 0; g < GB; g++)
+#pragma unroll
+                        for (int i = 0; i < N; i++) acc[g][i] = fmaf(p[u][g], x[i], acc[g][i]);
+                }
+            }
+        }
+        if (!there) continue;
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            if ((uint32_t)g >= ng) break;
+            const uint32_t head = head0 + g;
+            const float inv = sum[g] == 0.0f ? 0.0f : 1.0f / sum[g];
+#pragma unroll
+            for (int i = 0; i < N; i++) acc[g][i] *= inv;
+            if (c0 < a.dim)
+                store_values<T, N>((uint8_t *)a.o.p + (int64_t)b * a.o.row + head * a.o.head, c0, a.dim, acc[g]);
+            if (c0 == 0 && a.lse)
+                a.lse[(size_t)b * a.heads + head] = sum[g] == 0.0f ? -INFINITY : (m[g] + log2_fast(sum[g])) * kLn2;
+        }
+    }
 }
 
 // ---------------------------------------------------------------- launches
@@ -378,31 +529,38 @@ int launch_tiles(const Attend &a, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
     const auto kernel = pos == 2 ? attend_tiles<T, DP, 2> : pos == 1 ? attend_tiles<T, DP, 1> : attend_tiles<T, DP, 0>;
     constexpr uint32_t bytes = tiles_lds<T, DP>();
-    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
-        return NLB_EDEVICE;
+    if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
     hipLaunchKernelGGL(kernel, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
 template <typename T, int DP>
-int launch_one(const Attend &a, hipStream_t stream) {
+int launch_single(const Attend &a, Form form, hipStream_t stream) {
     const int gb = a.group >= 4 ? 4 : a.group >= 2 ? 2 : 1;
-    const auto kernel = gb == 4 ? attend_one<T, DP, 4> : gb == 2 ? attend_one<T, DP, 2> : attend_one<T, DP, 1>;
-    const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4;
-    const uint64_t units = (uint64_t)a.slots * a.kv_heads * ((a.group + gb - 1) / gb);
-    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess)
-        return NLB_EDEVICE;
-    const uint32_t blocks = (uint32_t)std::min<uint64_t>((units + 3) / 4, 256 * 8);
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), bytes, stream, a);
-    if (a.slots != a.batch)
-        hipLaunchKernelGGL((attend_join<T>), dim3(a.batch * a.heads), dim3(64), 0, stream, a);
+    const uint64_t parts = (a.group + gb - 1) / gb;
+    uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4;
+    if (form == kLists) {
+        constexpr uint32_t rows = 4 * Lanes<T, DP>::rows;
+        const auto kernel = gb == 4 ? attend_lists<T, DP, 4> : gb == 2 ? attend_lists<T, DP, 2> : attend_lists<T, DP, 1>;
+        bytes += rows * kListKeys;
+        if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
+        const uint64_t need = ((uint64_t)a.batch * a.kv_heads * parts + rows - 1) / rows;
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(need, 256 * 8)), dim3(kThreads), bytes, stream, a);
+    } else {
+        const auto kernel = gb == 4 ? attend_one<T, DP, 4> : gb == 2 ? attend_one<T, DP, 2> : attend_one<T, DP, 1>;
+        if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
+        const uint64_t need = ((uint64_t)a.slots * a.kv_heads * parts + 3) / 4;
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(need, 256 * 8)), dim3(kThreads), bytes, stream, a);
+        if (a.slots != a.batch)
+            hipLaunchKernelGGL((attend_join<T>), dim3(a.batch * a.heads), dim3(kThreads), 0, stream, a);
+    }
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
-template <typename T> int launch(const Attend &a, bool one, hipStream_t s) {
-    if (a.dim <= 32) return one ? launch_one<T, 32>(a, s) : launch_tiles<T, 32>(a, s);
-    if (a.dim <= 64) return one ? launch_one<T, 64>(a, s) : launch_tiles<T, 64>(a, s);
-    return one ? launch_one<T, 128>(a, s) : launch_tiles<T, 128>(a, s);
+template <typename T> int launch(const Attend &a, Form form, hipStream_t s) {
+    if (a.dim <= 32) return form == kTiles ? launch_tiles<T, 32>(a, s) : launch_single<T, 32>(a, form, s);
+    if (a.dim <= 64) return form == kTiles ? launch_tiles<T, 64>(a, s) : launch_single<T, 64>(a, form, s);
+    return form == kTiles ? launch_tiles<T, 128>(a, s) : launch_single<T, 128>(a, form, s);
 }
 
 }  // namespace
@@ -434,6 +592,6 @@ extern "C" int nlb_attention(const nlb_att_call *c, const nlb_att_rows *o, float
     a.part = (float *)work;
     a.slots = (uint32_t)f.slots;
     a.chunk = f.chunk;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, f.one, (hipStream_t)stream)
-                                      : launch<float>(a, f.one, (hipStream_t)stream);
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, f.form, (hipStream_t)stream)
+                                      : launch<float>(a, f.form, (hipStream_t)stream);
 }

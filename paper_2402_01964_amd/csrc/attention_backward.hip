@@ -9,8 +9,6 @@
 // same bits each time, at the price of computing the scores and dp twice.
 #include "attention.h"
 
-#include <algorithm>
-
 namespace {
 
 constexpr int kGaps = 192;               // gaps of a tile of owned rows and streamed rows
@@ -341,160 +339,232 @@ __global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
     store_owned<T, DP>((uint8_t *)a.dv.p + (int64_t)(sq.k0 + key) * a.dv.row + kvh * a.dv.head, a.dim, dv, 1.0f);
 }
 
-// ---------------------------------------------------------------- one query row
-// The gradients of lists with one query row each, of up to GB query heads on a
-// key/value head: a wavefront a list and key/value head, rows across lanes as
-// in the forward pass.  Bound by reading keys and values and writing their
-// gradients once; a bias gradient makes two passes over a list, the second
-// from the caches (for D, as in backward_rows).
+// ---------------------------------------------------------------- short lists
+// The gradients of many short lists with a query row each, of up to GB query
+// heads on a key/value head: a group of lanes takes a list, as in attend_lists.
+// One pass over a list's keys and values gives, with d_j = dp_j - dp of the
+// first open key,
+//   D' = sum p_j d_j,  A = sum p_j d_j k_j,  B = sum p_j k_j,  dq = scale (A - D' B)
+// and ds_j = p_j (d_j - D'), so dk_j = scale ds_j q and dv_j = p_j do need
+// neither k nor v again: p_j and d_j of the list's first `keep` keys wait in
+// LDS, a longer list is read again for the others.  Bound by reading k and v
+// and writing dk and dv once.
+struct PD {
+    float p, d;
+};
+
 template <typename T, int DP, int GB>
-__global__ __launch_bounds__(kThreads) void backward_one(Attend a) {
-    constexpr int N = Chunk<T>::n, U = 2, per_row = DP / N, rows = 64 / per_row;
+__global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t keep) {
+    using L = Lanes<T, DP>;
+    constexpr int N = Chunk<T>::n, U = 2;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63u, c = lane % L::per_row, c0 = c * N, kr = lane / L::per_row;
+    const uint32_t wave = threadIdx.x >> 6, group = wave * L::rows + kr;   // lane group of the workgroup
     int32_t *bounds = (int32_t *)lds;
     float *bias = (float *)(bounds + kMaxBuckets);            // [buckets][heads]
-    const uint32_t lane = threadIdx.x & 63u, c = lane % per_row, c0 = c * N, kr = lane / per_row;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t w = blockIdx.x * 4 + wave, waves = gridDim.x * 4;
-    // this wavefront's columns of the bias gradient: [buckets][GB][rows]
-    float *hist = bias + a.buckets * a.heads + wave * a.buckets * GB * rows;
+    PD *kept = (PD *)(((uintptr_t)(bias + a.buckets * a.heads) + 7) & ~(uintptr_t)7);   // [groups][keep][GB]
+    float *hist = (float *)(kept + 4 * L::rows * keep * GB);  // the bias gradient: [buckets][GB][groups]
     const bool want = a.part;
+    uint8_t *codes = (uint8_t *)(hist + (want ? a.buckets * GB * 4 * L::rows : 0)) + wave * L::rows * kListKeys;
+    kept += group * keep * GB;
     if (a.buckets) {
         for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads)
             bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
         for (uint32_t i = threadIdx.x; i < a.buckets * a.heads; i += kThreads)
             bias[i] = bias2_of<T>(a, i / a.heads, i % a.heads);
         if (want)
-            for (uint32_t i = lane; i < a.buckets * GB * rows; i += 64) hist[i] = 0.0f;
+            for (uint32_t i = threadIdx.x; i < a.buckets * GB * 4 * L::rows; i += kThreads) hist[i] = 0.0f;
         __syncthreads();
     }
-    // (the number of wavefronts is a multiple of kv_heads: each keeps its heads)
-    const uint32_t kvh = w % a.kv_heads, head0 = kvh * a.group;
-    for (uint32_t b = w / a.kv_heads; b < a.batch; b += waves / a.kv_heads) {
+    // (all groups' turn is a multiple of kv_heads: each group keeps its heads)
+    const uint64_t units = (uint64_t)a.batch * a.kv_heads, turn = (uint64_t)gridDim.x * 4 * L::rows;
+    for (uint64_t unit0 = (blockIdx.x * 4ull + wave) * L::rows; unit0 < units; unit0 += turn) {
+        const bool there = unit0 + kr < units;
+        const uint64_t unit = there ? unit0 + kr : 0;
+        const uint32_t b = unit / a.kv_heads, kvh = unit % a.kv_heads, head0 = kvh * a.group;
         Seq sq;
         sequence(a, b, sq);
-        float q[GB][N], dout[GB][N], dq[GB][N], L[GB], D[GB];
+        if (!there) sq.lk = 0;
+        float q[GB][N], dout[GB][N], A[GB][N], B[GB][N], lse[GB], first[GB], D[GB];
 #pragma unroll
         for (int g = 0; g < GB; g++) {
-            u32x4 x = {0, 0, 0, 0}, y = x, z = x;
-            L[g] = INFINITY;
-            D[g] = 0.0f;
+            u32x4 x = {0, 0, 0, 0}, y = x;
+            lse[g] = INFINITY;
+            first[g] = D[g] = 0.0f;
             if ((uint32_t)g < a.group) {
                 x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
                 y = load_chunk<T>(a.dout.p + (int64_t)b * a.dout.row + (head0 + g) * a.dout.head, c0, a.dim);
-                if (!want) z = load_chunk<T>(a.o.p + (int64_t)b * a.o.row + (head0 + g) * a.o.head, c0, a.dim);
-                L[g] = row_log2(a.lse[(size_t)b * a.heads + head0 + g]);
+                lse[g] = row_log2(a.lse[(size_t)b * a.heads + head0 + g]);
             }
             unpack<T>(x, q[g]);
             unpack<T>(y, dout[g]);
-            float o[N];
-            unpack<T>(z, o);
 #pragma unroll
-            for (int i = 0; i < N; i++) {
-                dq[g][i] = 0.0f;
-                D[g] = fmaf(o[i], dout[g][i], D[g]);
-            }
-            if (!want) D[g] = lanes_sum<per_row>(D[g]);
+            for (int i = 0; i < N; i++) A[g][i] = B[g][i] = 0.0f;
         }
         const int32_t qpos = a.buckets ? (a.q_pos ? flip(a.q_pos[b]) : flip((uint32_t)sq.lk - 1)) : 0;
-        const auto pass = [&](auto first_pass) {
-            constexpr bool FIRST = decltype(first_pass)::value;
-            for (int32_t j0 = 0; j0 < sq.lk; j0 += rows * U) {
-                u32x4 k[U], v[U];
-                uint32_t pos[U];
-                bool open[U];
+        const uint8_t *kp = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
+        const uint8_t *vp = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
+        uint8_t *dkp = (uint8_t *)a.dk.p + (int64_t)sq.k0 * a.dk.row + kvh * a.dk.head;
+        uint8_t *dvp = (uint8_t *)a.dv.p + (int64_t)sq.k0 * a.dv.row + kvh * a.dv.head;
+        bool began = false;
+
+        // p and d of U open keys (0 where there is none)
+        const auto weigh = [&](int32_t j0, uint64_t &mine, uint32_t (&at)[U], bool (&open)[U], float (&p)[U][GB],
+                               float (&d)[U][GB], auto summing) {
+            u32x4 k[U], v[U];
 #pragma unroll
-                for (int u = 0; u < U; u++) {
-                    const int32_t j = j0 + u * rows + kr;
-                    open[u] = j < sq.lk;
-                    pos[u] = j;
-                    if (a.k_pos && open[u]) {
-                        pos[u] = a.k_pos[sq.k0 + j];
-                        open[u] = pos[u] != kNoKey;
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; u++) {
-                    const int64_t j = (int64_t)sq.k0 + j0 + u * rows + kr;
-                    k[u] = v[u] = u32x4{0, 0, 0, 0};
-                    if (open[u]) {
-                        k[u] = load_chunk<T>(a.k.p + j * a.k.row + kvh * a.k.head, c0, a.dim);
-                        v[u] = load_chunk<T>(a.v.p + j * a.v.row + kvh * a.v.head, c0, a.dim);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; u++) {
-                    const int32_t j = j0 + u * rows + kr;
-                    float x[N], y[N], dk[N] = {}, dv[N] = {};
-                    unpack<T>(k[u], x);
-                    unpack<T>(v[u], y);
-                    const uint32_t bk = a.buckets ? bucket_of(bounds, a.buckets, gap_of(qpos, flip(pos[u]))) : 0;
-                    float mine = 0.0f;
-#pragma unroll
-                    for (int g = 0; g < GB; g++) {
-                        float s = 0.0f, dp = 0.0f;
-#pragma unroll
-                        for (int i = 0; i < N; i++) {
-                            s = fmaf(q[g][i], x[i], s);
-                            dp = fmaf(dout[g][i], y[i], dp);
-                        }
-                        s = lanes_sum<per_row>(s) * a.scale2;
-                        dp = lanes_sum<per_row>(dp);
-                        if (a.buckets && (uint32_t)g < a.group) s += bias[bk * a.heads + head0 + g];
-                        const float p = open[u] ? exp2_fast(s - L[g]) : 0.0f;
-                        if constexpr (FIRST) {
-                            D[g] = fmaf(p, dp, D[g]);
-                        } else {
-                            const float ds = p * (dp - D[g]), dss = ds * a.scale;
-                            if (c == (uint32_t)g) mine = ds;
-#pragma unroll
-                            for (int i = 0; i < N; i++) {
-                                dk[i] = fmaf(dss, q[g][i], dk[i]);
-                                dv[i] = fmaf(p, dout[g][i], dv[i]);
-                                dq[g][i] = fmaf(dss, x[i], dq[g][i]);
-                            }
-                        }
-                    }
-                    if constexpr (!FIRST) {
-                        if (want && c < GB && open[u])
-                            __hip_atomic_fetch_add(hist + (bk * GB + c) * rows + kr, mine, __ATOMIC_RELAXED,
-                                                   __HIP_MEMORY_SCOPE_WORKGROUP);
-                        if (j < sq.lk && c0 < a.dim) {
-                            const int64_t r = (int64_t)sq.k0 + j;
-                            store_values<T, N>((uint8_t *)a.dk.p + r * a.dk.row + kvh * a.dk.head, c0, a.dim, dk);
-                            store_values<T, N>((uint8_t *)a.dv.p + r * a.dv.row + kvh * a.dv.head, c0, a.dim, dv);
-                        }
-                    }
+            for (int u = 0; u < U; u++) {
+                open[u] = mine != 0;
+                at[u] = open[u] ? __builtin_ctzll(mine) : 0;
+                mine &= mine - 1;
+                k[u] = v[u] = u32x4{0, 0, 0, 0};
+                if (open[u]) {
+                    k[u] = load_chunk<T>(kp + (int64_t)(j0 + at[u]) * a.k.row, c0, a.dim);
+                    v[u] = load_chunk<T>(vp + (int64_t)(j0 + at[u]) * a.v.row, c0, a.dim);
                 }
             }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                float x[N], y[N];
+                unpack<T>(k[u], x);
+                unpack<T>(v[u], y);
+                const uint32_t bk = a.buckets ? codes[kr * kListKeys + at[u]] * a.heads + head0 : 0;
+#pragma unroll
+                for (int g = 0; g < GB; g++) {
+                    float s = 0.0f, dp = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < N; i++) {
+                        s = fmaf(q[g][i], x[i], s);
+                        dp = fmaf(dout[g][i], y[i], dp);
+                    }
+                    s = lanes_sum<L::per_row>(s) * a.scale2;
+                    dp = lanes_sum<L::per_row>(dp);
+                    if (a.buckets && (uint32_t)g < a.group) s += bias[bk + g];
+                    p[u][g] = open[u] ? exp2_fast(s - lse[g]) : 0.0f;
+                    if (!began && open[u]) first[g] = dp;
+                    d[u][g] = open[u] ? dp - first[g] : 0.0f;
+                    if constexpr (decltype(summing)::value) {
+                        const float pd = p[u][g] * d[u][g];
+                        D[g] += pd;
+#pragma unroll
+                        for (int i = 0; i < N; i++) {
+                            A[g][i] = fmaf(pd, x[i], A[g][i]);
+                            B[g][i] = fmaf(p[u][g], x[i], B[g][i]);
+                        }
+                    }
+                }
+                began |= open[u];
+            }
         };
-        if (want) {
-            pass(std::true_type{});
+        // dk, dv (and the bias gradient) of key j0 + at
+        const auto give = [&](int32_t j0, uint32_t at, bool open, const float (&p)[GB], const float (&d)[GB]) {
+            float dk[N] = {}, dv[N] = {}, mine = 0.0f;
 #pragma unroll
-            for (int g = 0; g < GB; g++)
+            for (int g = 0; g < GB; g++) {
+                const float ds = p[g] * (d[g] - D[g]), dss = ds * a.scale;
+                if (c == (uint32_t)g) mine = ds;
 #pragma unroll
-                for (int x = per_row; x < 64; x *= 2) D[g] += __shfl_xor(D[g], x);
+                for (int i = 0; i < N; i++) {
+                    dk[i] = fmaf(dss, q[g][i], dk[i]);
+                    dv[i] = fmaf(p[g], dout[g][i], dv[i]);
+                }
+            }
+            if (!open) return;
+            if (want && c < GB)
+                __hip_atomic_fetch_add(hist + (codes[kr * kListKeys + at] * GB + c) * 4 * L::rows + group, mine,
+                                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            if (c0 < a.dim) {
+                store_values<T, N>(dkp + (int64_t)(j0 + at) * a.dk.row, c0, a.dim, dk);
+                store_values<T, N>(dvp + (int64_t)(j0 + at) * a.dv.row, c0, a.dim, dv);
+            }
+        };
+
+        uint64_t opened = 0;                                  // of the list's first 64 keys
+        for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
+            wave_lds_fence();
+            uint64_t mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+            wave_lds_fence();
+            if (j0 == 0) opened = mine;
+            while (__any(mine != 0)) {
+                uint32_t at[U];
+                bool open[U];
+                float p[U][GB], d[U][GB];
+                weigh(j0, mine, at, open, p, d, std::true_type{});
+#pragma unroll
+                for (int u = 0; u < U; u++)
+                    if (c < GB && open[u] && j0 == 0 && at[u] < keep) {
+                        float x = p[u][0], y = d[u][0];
+#pragma unroll
+                        for (int g = 1; g < GB; g++)
+                            if (c == (uint32_t)g) {
+                                x = p[u][g];
+                                y = d[u][g];
+                            }
+                        kept[at[u] * GB + c] = PD{x, y};
+                    }
+            }
         }
-        pass(std::false_type{});
+        wave_lds_fence();
+        for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
+            uint64_t mine = opened;
+            if (__any(sq.lk > kListKeys)) {                   // (else the codes are still there)
+                wave_lds_fence();
+                mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+                wave_lds_fence();
+            }
+            // rows of closed keys
+            for (int32_t j = j0; __any(j < min(sq.lk, j0 + kListKeys)); j++)
+                if (j < sq.lk && !((mine >> (j - j0)) & 1) && c0 < a.dim) {
+                    const float zero[N] = {};
+                    store_values<T, N>(dkp + (int64_t)j * a.dk.row, c0, a.dim, zero);
+                    store_values<T, N>(dvp + (int64_t)j * a.dv.row, c0, a.dim, zero);
+                }
+            uint64_t waits = j0 == 0 ? mine & (keep < 64 ? (1ull << keep) - 1 : ~0ull) : 0;
+            mine &= ~waits;
+            while (__any(waits != 0)) {
+                const bool open = waits != 0;
+                const uint32_t at = open ? __builtin_ctzll(waits) : 0;
+                waits &= waits - 1;
+                float p[GB], d[GB];
+#pragma unroll
+                for (int g = 0; g < GB; g++) {
+                    const PD x = kept[at * GB + g];
+                    p[g] = open ? x.p : 0.0f;
+                    d[g] = open ? x.d : 0.0f;
+                }
+                give(j0, at, open, p, d);
+            }
+            while (__any(mine != 0)) {
+                uint32_t at[U];
+                bool open[U];
+                float p[U][GB], d[U][GB];
+                weigh(j0, mine, at, open, p, d, std::false_type{});
+#pragma unroll
+                for (int u = 0; u < U; u++) give(j0, at[u], open[u], p[u], d[u]);
+            }
+        }
+        if (!there) continue;
 #pragma unroll
         for (int g = 0; g < GB; g++) {
             if ((uint32_t)g >= a.group) break;
+            float dq[N];
 #pragma unroll
-            for (int x = per_row; x < 64; x *= 2)
-#pragma unroll
-                for (int i = 0; i < N; i++) dq[g][i] += __shfl_xor(dq[g][i], x);
-            if (kr == 0 && c0 < a.dim)
-                store_values<T, N>((uint8_t *)a.dq.p + (int64_t)b * a.dq.row + (head0 + g) * a.dq.head, c0, a.dim,
-                                   dq[g]);
+            for (int i = 0; i < N; i++) dq[i] = a.scale * (A[g][i] - D[g] * B[g][i]);
+            if (c0 < a.dim)
+                store_values<T, N>((uint8_t *)a.dq.p + (int64_t)b * a.dq.row + (head0 + g) * a.dq.head, c0, a.dim, dq);
         }
     }
-    if (want)
-        for (uint32_t i = lane; i < a.buckets * a.group; i += 64) {
-            const uint32_t bk = i % a.buckets, g = i / a.buckets;
-            float x = 0.0f;
-            for (int r = 0; r < rows; r++) x += hist[(bk * GB + g) * rows + r];
-            a.part[((size_t)(w / a.kv_heads) * a.heads + head0 + g) * a.buckets + bk] = x;
-        }
+    if (!want) return;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < a.heads * a.buckets; i += kThreads) {
+        const uint32_t bk = i % a.buckets, head = i / a.buckets, kvh = head / a.group, g = head % a.group;
+        // the lane groups of this workgroup that work on the head
+        float x = 0.0f;
+        const uint32_t first = (blockIdx.x * 4ull * L::rows) % a.kv_heads;
+        for (uint32_t r = (kvh + a.kv_heads - first) % a.kv_heads; r < 4 * L::rows; r += a.kv_heads)
+            x += hist[(bk * GB + g) * 4 * L::rows + r];
+        a.part[((size_t)blockIdx.x * a.heads + head) * a.buckets + bk] = x;
+    }
 }
 
 // ---------------------------------------------------------------- bias gradient
@@ -520,10 +590,6 @@ __global__ __launch_bounds__(kThreads) void sum_bias(const float *part, uint32_t
 }
 
 // ---------------------------------------------------------------- launches
-template <typename K> bool allow_lds(K kernel, uint32_t bytes) {
-    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
-}
-
 template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
     const auto rows = pos == 2   ? backward_rows<T, DP, 2>
@@ -541,21 +607,23 @@ template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipS
     return NLB_OK;
 }
 
-template <typename T, int DP> int launch_one(const Attend &a, const Backward &p, hipStream_t stream) {
+template <typename T, int DP> int launch_lists(const Attend &a, const Backward &p, hipStream_t stream) {
     const int gb = a.group > 2 ? 4 : (int)a.group;
-    const auto kernel = gb == 4 ? backward_one<T, DP, 4> : gb == 2 ? backward_one<T, DP, 2> : backward_one<T, DP, 1>;
-    const uint32_t rows = 64 / (DP / Chunk<T>::n);
-    const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4 + (a.part ? 4 * a.buckets * gb * rows * 4 : 0);
+    const auto kernel =
+        gb == 4 ? backward_lists<T, DP, 4> : gb == 2 ? backward_lists<T, DP, 2> : backward_lists<T, DP, 1>;
+    const uint32_t groups = 4 * Lanes<T, DP>::rows;
+    const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4 + 8 + groups * p.keep * gb * 8 +
+                           (a.part ? a.buckets * gb * groups * 4 : 0) + groups * kListKeys;
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
-    hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(kThreads), bytes, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(kThreads), bytes, stream, a, p.keep);
     return NLB_OK;
 }
 
 template <typename T> int launch(const Attend &a, const Backward &p, void *dbias, hipStream_t s) {
     int rc;
-    if (a.dim <= 32) rc = p.one ? launch_one<T, 32>(a, p, s) : launch_tiles<T, 32>(a, p, s);
-    else if (a.dim <= 64) rc = p.one ? launch_one<T, 64>(a, p, s) : launch_tiles<T, 64>(a, p, s);
-    else rc = p.one ? launch_one<T, 128>(a, p, s) : launch_tiles<T, 128>(a, p, s);
+    if (a.dim <= 32) rc = p.lists ? launch_lists<T, 32>(a, p, s) : launch_tiles<T, 32>(a, p, s);
+    else if (a.dim <= 64) rc = p.lists ? launch_lists<T, 64>(a, p, s) : launch_tiles<T, 64>(a, p, s);
+    else rc = p.lists ? launch_lists<T, 128>(a, p, s) : launch_tiles<T, 128>(a, p, s);
     if (rc != NLB_OK) return rc;
     if (dbias) {
         const float *from = a.part;
