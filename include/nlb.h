@@ -386,6 +386,7 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  * k_pos = 0xFFFFFFFF are closed to every query, as nlb_sample's ts marks empty
  * slots; what their k and v hold is not used.  A key that causal closes to
  * some rows only must hold finite values, or those rows may become NaN.
+ *   scale: 0, or of a magnitude from 2^-20 to 2^20.
  *   Bias.  buckets = 0: none (bias NULL).  Else bias is a device array
  * [buckets][heads] of dtype, bounds a device int32 [buckets - 1], increasing,
  * and bucket(x) the number of bounds <= x.  Positions are q_pos (device uint32

@@ -39,6 +39,7 @@ typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+constexpr int32_t kNoKeyFlipped = INT32_MAX;
 constexpr int kThreads = 256;            // four wavefronts, everywhere
 constexpr int kOwned = 128;              // rows that a tiled workgroup owns, 32 per wavefront
 constexpr int kMaxBuckets = NLB_ATT_MAX_BUCKETS;
@@ -60,7 +61,7 @@ struct Attend {
     uint32_t batch, q_rows, k_rows, q_len, k_len;   // *_len: rows of every sequence where *_start is null
     uint32_t heads, kv_heads, group, dim;
     uint32_t causal, buckets, dtype_bytes;
-    float scale, scale2;                 // scale2: scale log2(e)
+    float scale, scale2, signed2;        // scale2: |scale| log2(e), 1 where scale is 0; signed2: scale log2(e)
     const int32_t *bounds;
     const void *bias;                    // [buckets][heads]
     const uint32_t *q_pos, *k_pos;
@@ -224,14 +225,75 @@ template <typename T> __device__ __forceinline__ float bias2_of(const Attend &a,
     return x <= kBiasCloses ? -INFINITY : x * kLog2e;
 }
 
+// The bounds of a workgroup's buckets and one head's bias as tiled kernels add
+// it, to scores in steps of 1 / scale2.
+template <typename T>
+__device__ __forceinline__ void stage_bias(const Attend &a, uint32_t head, int32_t *bounds, float *bias) {
+    for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads) {
+        if (bounds) bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
+        bias[i] = i < a.buckets ? bias2_of<T>(a, i, head) / a.scale2 : 0.0f;
+    }
+}
+
+// Whether all gaps from lo to hi lie in the first or in the last bucket, and
+// which it is.
+__device__ __forceinline__ bool one_bucket(const int32_t *bounds, uint32_t buckets, int32_t lo, int32_t hi,
+                                           uint32_t &bucket) {
+    const bool last = buckets == 1 || lo >= bounds[buckets - 2], first = buckets > 1 && hi < bounds[0];
+    bucket = last ? buckets - 1 : 0;
+    return __builtin_amdgcn_readfirstlane(last || first);
+}
+
+// Buckets of many gaps.  The gaps are cut into cells, four to a power of two
+// on either side of zero (by a gap's sign, exponent and two bits of its
+// mantissa); a table in LDS has each cell's first bucket, and a gap takes as
+// many further comparisons as the fullest cell has bounds (`more`; one or two
+// for bounds in steps of one, then in equal ratios).  Against a search of six
+// dependent LDS reads, two or three.
+constexpr int kCells = 256;
+__device__ __forceinline__ int32_t cell_of(int32_t gap) {
+    // |gap| in fp32 rounds monotonically; 1 is cell 1, 2^31 cell 125
+    const int32_t bits = (int32_t)(__float_as_uint(fabsf((float)gap)) >> 21) - 507;
+    const int32_t n = max(bits, 0);
+    return gap < 0 ? 128 - n : 128 + n;
+}
+struct Buckets {
+    int32_t *bounds;                     // [64]
+    uint8_t *cells;                      // [kCells]
+    uint32_t last, more;                 // the last bucket; comparisons after a cell's first
+};
+__device__ __forceinline__ void fill_cells(Buckets &t, const Attend &a, uint32_t *most) {
+    // most: one LDS word, zeroed by the caller; bounds are there
+    for (int32_t c = threadIdx.x; c < kCells; c += kThreads) {
+        uint32_t n = 0, in = 0;
+        for (uint32_t i = 0; i + 1 < a.buckets; i++) {
+            const int32_t x = cell_of(t.bounds[i]);
+            n += x < c;
+            in += x == c;
+        }
+        t.cells[c] = (uint8_t)n;
+        if (in) atomicMax(most, in);
+    }
+}
+__device__ __forceinline__ uint32_t bucket_in(const Buckets &t, int32_t gap) {
+    uint32_t n = t.cells[cell_of(gap)];
+    for (uint32_t i = 0; i < t.more; i++) n += n < t.last && t.bounds[n] <= gap ? 1u : 0u;
+    return n;
+}
+
 // ---------------------------------------------------------------- tiles
-// Streamed rows of a tiled kernel, in LDS: `rows` rows of DP values, 16 bytes
-// of padding behind each, so that eight lanes reading 16 bytes of eight
-// consecutive rows use every bank once.
-template <typename T, int DP> struct Tile {
+// Streamed rows of a tiled kernel, in LDS.  What pads a row depends on how the
+// tile is read, 256 bytes a cycle: by rows (16 lanes read 16 bytes of 16
+// rows: rows 16 bytes apart modulo 256 use every bank once), by columns (bf16:
+// 32 lanes read 64 bytes of each of 4 rows; fp32: 128 bytes of rows 4 apart),
+// or both ways, each at half speed.
+enum Use { kByRows, kByColumns, kBothWays };
+
+template <typename T, int DP, Use USE = kByRows> struct Tile {
     static constexpr int rows = sizeof(T) == 2 ? 64 : 32;
     static constexpr int chunks = DP * sizeof(T) / 16;              // per row
-    static constexpr int stride = DP * sizeof(T) + 16;              // bytes
+    static constexpr int pad = USE == kByRows ? 16 : USE == kBothWays || sizeof(T) == 4 ? 32 : DP == 32 ? 0 : 64;
+    static constexpr int stride = DP * sizeof(T) + pad;             // bytes
     static constexpr int bytes = rows * stride;
     static constexpr int per_thread = rows * chunks / kThreads;
     static constexpr int blocks = rows / 32;
@@ -254,9 +316,9 @@ __device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const
     }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, Use USE>
 __device__ __forceinline__ void tile_store(uint8_t *lds, const typename Tile<T, DP>::Regs &reg) {
-    using G = Tile<T, DP>;
+    using G = Tile<T, DP, USE>;
     const uint32_t c = threadIdx.x % G::chunks, r0 = threadIdx.x / G::chunks;
 #pragma unroll
     for (int i = 0; i < G::per_thread; i++)
@@ -285,11 +347,12 @@ __device__ __forceinline__ void tile_close(typename Tile<T, DP>::Regs &reg,
 }
 
 template <typename T, int DP>
-__device__ __forceinline__ void tile_store_positions(uint32_t *lds, const typename Tile<T, DP>::Positions &pos) {
+__device__ __forceinline__ void tile_store_positions(int32_t *lds, const typename Tile<T, DP>::Positions &pos) {
     using G = Tile<T, DP>;
     if (threadIdx.x % G::chunks == 0)
 #pragma unroll
-        for (int i = 0; i < G::per_thread; i++) lds[threadIdx.x / G::chunks + i * (kThreads / G::chunks)] = pos[i];
+        for (int i = 0; i < G::per_thread; i++)
+            lds[threadIdx.x / G::chunks + i * (kThreads / G::chunks)] = flip(pos[i]);
 }
 
 // Owned rows as the right operand of products that contract over the row's
@@ -299,6 +362,16 @@ template <typename T, int DP> struct Owned {
     static constexpr int steps = DP * sizeof(T) / 32;
     u32x4 x[steps];
 };
+
+// A score in steps of 1 / scale2: q (or k) takes the sign of scale, and zero.
+template <typename T, int DP> __device__ __forceinline__ void sign_owned(Owned<T, DP> &f, float scale) {
+    const uint32_t sign = scale < 0.0f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
+    const uint32_t keep = scale == 0.0f ? 0u : 0xFFFFFFFFu;
+#pragma unroll
+    for (int s = 0; s < Owned<T, DP>::steps; s++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) f.x[s][i] = (f.x[s][i] ^ sign) & keep;
+}
 
 template <typename T, int DP>
 __device__ __forceinline__ void load_owned(Owned<T, DP> &f, const uint8_t *row, bool there, uint32_t dim) {
@@ -311,9 +384,9 @@ __device__ __forceinline__ void load_owned(Owned<T, DP> &f, const uint8_t *row, 
 }
 
 // acc[row][c] += sum over values of tile[32 blk + row] . owned[c]
-template <typename T, int DP>
+template <typename T, int DP, Use USE>
 __device__ __forceinline__ void product_rows(f32x16 &acc, const uint8_t *tile, int blk, const Owned<T, DP> &own) {
-    using G = Tile<T, DP>;
+    using G = Tile<T, DP, USE>;
     const uint32_t lane = threadIdx.x & 63u;
     const uint8_t *p = tile + (blk * 32 + (lane & 31u)) * G::stride + (lane >> 5) * 16;
 #pragma unroll
@@ -356,10 +429,10 @@ __device__ __forceinline__ i16x4 read_columns(const uint8_t *p) {
 }
 
 // acc[d block][value][c] += sum over the block's rows of tile[32 blk + row][value] scores[row][c]
-template <typename T, int DP>
+template <typename T, int DP, Use USE>
 __device__ __forceinline__ void product_columns(f32x16 (&acc)[DP / 32], const uint8_t *tile, int blk,
                                                 const Scores<T> &s) {
-    using G = Tile<T, DP>;
+    using G = Tile<T, DP, USE>;
     const uint32_t lane = threadIdx.x & 63u, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
         const uint8_t *p = tile + (blk * 32 + 4 * h + ((lane & 15u) >> 2)) * G::stride +
@@ -465,7 +538,8 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
     if (c->dtype != NLB_DTYPE_F32 && c->dtype != NLB_DTYPE_BF16) return NLB_EINVAL;
     if (c->dim < 1 || c->dim > NLB_ATT_MAX_DIM || c->heads < 1 || c->heads > NLB_ATT_MAX_HEADS) return NLB_EINVAL;
     if (c->kv_heads < 1 || c->heads % c->kv_heads) return NLB_EINVAL;
-    if (!std::isfinite(c->scale)) return NLB_EINVAL;
+    const float size = std::fabs(c->scale);
+    if (!(size == 0.0f || (size >= 0x1p-20f && size <= 0x1p20f))) return NLB_EINVAL;
     if (c->causal != 0 && c->causal != 1) return NLB_EINVAL;
     if (c->batch < 1 || c->batch > INT32_MAX / NLB_ATT_MAX_HEADS || c->q_rows > INT32_MAX || c->k_rows > INT32_MAX)
         return NLB_EINVAL;
@@ -496,7 +570,8 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
     a.buckets = c->buckets;
     a.dtype_bytes = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
     a.scale = c->scale;
-    a.scale2 = c->scale * kLog2e;
+    a.signed2 = c->scale * kLog2e;
+    a.scale2 = c->scale == 0.0f ? 1.0f : std::fabs(c->scale) * kLog2e;
     a.bounds = c->bounds;
     a.bias = c->bias;
     a.q_pos = c->q_pos;

@@ -19,19 +19,30 @@ namespace {
 // POS: 0 no bias and no closed keys; 1 bias by places: of a tile's gaps there
 // are 32 + 128 - 1 at most, so their bias values are looked up once per tile;
 // 2 positions given (bias by their gaps, closed keys).
+//
+// What the vector units do for a score bounds the kernel beside the matrix
+// products (16 products of 32 cycles a block of 32 x 32 for 128 values, 16
+// exponentials of 16 cycles and four other operations a lane's score), so
+// scores stay in steps of 1 / scale2 and meet scale and maximum in the one
+// fused operation before the exponential; masks run only in tiles that need
+// them, and tiles whose gaps are all in one bucket add their bias to the
+// maximum's term.
 constexpr int kGaps = 192;
 
 template <typename T, int DP> constexpr uint32_t tiles_lds() {
-    return 4 * Tile<T, DP>::bytes + 2 * kGaps * 4 + kMaxBuckets * 8;
+    return 2 * (Tile<T, DP, kByRows>::bytes + Tile<T, DP, kByColumns>::bytes) + 2 * kGaps * 4 + kMaxBuckets * 8 +
+           kCells + 16;
 }
 
 template <typename T, int DP, int POS>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     using G = Tile<T, DP>;
+    using KT = Tile<T, DP, kByRows>;
+    using VT = Tile<T, DP, kByColumns>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    float *extra = (float *)(lds + 4 * G::bytes);             // [2][kGaps]: bias by gap, or positions
-    int32_t *bounds = (int32_t *)(extra + 2 * kGaps);
-    float *bias = (float *)(bounds + kMaxBuckets);
+    float *extra = (float *)(lds + 2 * (KT::bytes + VT::bytes));   // [2][kGaps]: bias by gap, or positions
+    float *bias = extra + 2 * kGaps;
+    Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
 
     // heads of one key/value head follow each other at a distance of kv_heads:
@@ -45,56 +56,66 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     const int32_t row0 = sq.tile * kOwned, row = row0 + wave * 32 + col, off = sq.lk - sq.lq;
     const bool there = row < sq.lq;
 
-    if constexpr (POS != 0) {
-        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads) {
-            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
-            bias[i] = i < a.buckets ? bias2_of<T>(a, i, head) : 0.0f;
-        }
-        __syncthreads();
-    }
-
     Owned<T, DP> q;
     load_owned(q, a.q.p + (int64_t)(sq.q0 + row) * a.q.row + head * a.q.head, there, a.dim);
+    sign_owned(q, a.scale);
     int32_t qpos = 0;
     if constexpr (POS == 2)
         if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
+    if (POS != 0 && a.buckets) {
+        stage_bias<T>(a, head, buckets.bounds, bias);
+        uint32_t *most = (uint32_t *)(buckets.cells + kCells);
+        if (threadIdx.x == 0) *most = 0;
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, a, most);
+            __syncthreads();
+            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+        }
+    }
 
     // keys [0, kend) are open to some row of the workgroup, [0, wend) of the wavefront
-    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wlast = min(row0 + (int32_t)wave * 32 + 32, sq.lq) - 1;
+    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wrow0 = row0 + (int32_t)wave * 32;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
-    const int32_t wend = a.causal ? min(sq.lk, wlast + off + 1) : sq.lk;
+    const int32_t wend = a.causal ? min(sq.lk, min(wrow0 + 32, sq.lq) + off) : sq.lk;
     const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;   // keys open to this lane's row
+    const int32_t whole = a.causal ? min(sq.lk, wrow0 + off + 1) : sq.lk; // and to all of the wavefront's
     const uint8_t *kbase = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
     const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
 
-    u32x4 kreg[G::per_thread], vreg[G::per_thread];
+    typename G::Regs kreg, vreg;
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
         tile_load<T, DP>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
         tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
         if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
+    // the gaps of the tile at k0: from least to least + owned + rows - 2
+    const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
     // writes the fetched tile and what the bias needs of it
     const auto stage = [&](int32_t k0, int buf) {
-        uint8_t *kt = lds + buf * 2 * G::bytes;
+        uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
         if constexpr (POS == 2) {
             tile_close<T, DP>(kreg, preg);
             tile_close<T, DP>(vreg, preg);
-            tile_store_positions<T, DP>((uint32_t *)extra + buf * kGaps, preg);
+            tile_store_positions<T, DP>((int32_t *)extra + buf * kGaps, preg);
         }
-        tile_store<T, DP>(kt, kreg);
-        tile_store<T, DP>(kt + G::bytes, vreg);
+        tile_store<T, DP, kByRows>(kt, kreg);
+        tile_store<T, DP, kByColumns>(kt + KT::bytes, vreg);
         if constexpr (POS == 1) {
-            const int32_t x = (int32_t)threadIdx.x;   // gap of x: row0 + off - k0 + x - (rows - 1)
-            if (x < kOwned + G::rows - 1)
-                extra[buf * kGaps + x] = bias[bucket_of(bounds, a.buckets, row0 + off - k0 + x - (G::rows - 1))];
+            const int32_t x = (int32_t)threadIdx.x, lo = least(k0);
+            uint32_t one;
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) && x < kOwned + G::rows - 1)
+                extra[buf * kGaps + x] = bias[bucket_of(buckets.bounds, a.buckets, lo + x)];
         }
     };
 
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) acc[d] = f32x16{};
+    // m: the maximum in the scores' steps; up to 2^8 behind it
     float m = -INFINITY, sum = 0.0f;
+    const float behind = 8.0f / a.scale2;
 
     if (kend > 0) {
         fetch(0);
@@ -106,33 +127,51 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
         const bool more = k0 + G::rows < kend;
         if (more) fetch(k0 + G::rows);
         if (k0 < wend) {
-            const uint8_t *kt = lds + buf * 2 * G::bytes, *vt = kt + G::bytes;
-            float t[G::blocks][16];
-            const bool ragged = k0 + G::rows > (a.causal ? min(sq.lk, row0 + (int32_t)wave * 32 + off + 1) : sq.lk);
+            const uint8_t *kt = lds + buf * (KT::bytes + VT::bytes), *vt = kt + KT::bytes;
+            const float *ex = extra + buf * kGaps;
+            const bool ragged = k0 + G::rows > whole;
+            float shift = 0.0f;                                // the bias where the tile has one bucket
+            bool far = true, shut = false;
+            if constexpr (POS == 1) {
+                uint32_t one;
+                far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + kOwned + G::rows - 2, one);
+                if (far) shift = bias[one];
+            }
+            if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[lane % G::rows] == kNoKeyFlipped);
+            f32x16 s[G::blocks];
             float top = -INFINITY;
 #pragma unroll
             for (int blk = 0; blk < G::blocks; blk++) {
-                f32x16 s = {};
-                product_rows<T, DP>(s, kt, blk, q);
+                s[blk] = f32x16{};
+                product_rows<T, DP, kByRows>(s[blk], kt, blk, q);
+                if (POS == 1 && !far) {
+                    const float *e = ex + wave * 32 + col + (G::rows - 1) - blk * 32;
 #pragma unroll
-                for (int r = 0; r < 16; r++) {
-                    const int kr = blk * 32 + block_row(r);
-                    float x = s[r] * a.scale2;
-                    if constexpr (POS == 1) x += extra[buf * kGaps + wave * 32 + col + (G::rows - 1) - kr];
-                    if constexpr (POS == 2) {
-                        const uint32_t kp = ((const uint32_t *)extra)[buf * kGaps + kr];
-                        if (a.buckets) x += bias[bucket_of(bounds, a.buckets, gap_of(qpos, flip(kp)))];
-                        if (kp == kNoKey) x = -INFINITY;
-                    }
-                    if (ragged && k0 + kr >= limit) x = -INFINITY;
-                    t[blk][r] = x;
-                    top = fmaxf(top, x);
+                    for (int r = 0; r < 16; r++) s[blk][r] += e[-block_row(r)];
                 }
+                if (POS == 2 && a.buckets) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        s[blk][r] += bias[bucket_in(
+                            buckets, gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]))];
+                }
+                if (POS == 2 && shut) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        if (((const int32_t *)ex)[blk * 32 + block_row(r)] == kNoKeyFlipped) s[blk][r] = -INFINITY;
+                }
+                if (ragged) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        if (k0 + blk * 32 + block_row(r) >= limit) s[blk][r] = -INFINITY;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; r++) top = fmaxf(top, s[blk][r]);
             }
-            top = halves_max(top);
-            if (__any(top > m + 8.0f)) {
+            top = halves_max(top) + shift;
+            if (__any(top > m + behind)) {
                 const float up = fmaxf(m, top);
-                const float f = up == -INFINITY ? 1.0f : exp2_fast(m - up);
+                const float f = up == -INFINITY ? 1.0f : exp2_fast((m - up) * a.scale2);
                 m = up;
                 sum *= f;
 #pragma unroll
@@ -140,17 +179,18 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
 #pragma unroll
                     for (int r = 0; r < 16; r++) acc[d][r] *= f;
             }
-            const float base = m == -INFINITY ? 0.0f : m;
+            const float base = fmaf(shift, a.scale2, m == -INFINITY ? 0.0f : -m * a.scale2);
 #pragma unroll
             for (int blk = 0; blk < G::blocks; blk++) {
-                Scores<T> p;
+                float t[16];
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
-                    t[blk][r] = exp2_fast(t[blk][r] - base);
-                    sum += t[blk][r];
+                    t[r] = exp2_fast(fmaf(s[blk][r], a.scale2, base));
+                    sum += t[r];
                 }
-                pack(p, t[blk]);
-                product_columns<T, DP>(acc, vt, blk, p);
+                Scores<T> p;
+                pack(p, t);
+                product_columns<T, DP, kByColumns>(acc, vt, blk, p);
             }
         }
         if (more) stage(k0 + G::rows, buf ^ 1);
@@ -161,7 +201,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     store_owned<T, DP>((uint8_t *)a.o.p + (int64_t)(sq.q0 + row) * a.o.row + head * a.o.head, a.dim, acc, inv);
     if (a.lse && lane < 32)
-        a.lse[(size_t)(sq.q0 + row) * a.heads + head] = sum == 0.0f ? -INFINITY : (m + log2_fast(sum)) * kLn2;
+        a.lse[(size_t)(sq.q0 + row) * a.heads + head] =
+            sum == 0.0f ? -INFINITY : (m * a.scale2 + log2_fast(sum)) * kLn2;
 }
 
 // ---------------------------------------------------------------- one query row
@@ -214,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void attend_one(Attend a) {
             unpack<T>(x, q[g]);
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                q[g][i] *= a.scale2;
+                q[g][i] *= a.signed2;
                 acc[g][i] = 0.0f;
             }
             m[g] = -INFINITY;
@@ -435,7 +476,7 @@ __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
             unpack<T>(x, q[g]);
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                q[g][i] *= a.scale2;
+                q[g][i] *= a.signed2;
                 acc[g][i] = 0.0f;
             }
             m[g] = -INFINITY;

@@ -24,22 +24,46 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 // which the rounding of o would drown.
 //
 // The bias gradient: each thread adds its ds to its own column of an LDS table
-// [buckets][threads] (by LDS adds in program order: no two threads share a
-// word), tiles whose gaps all lie beyond the last or before the first bound
-// to a register.  The columns are summed at the end in a fixed order into
-// part[slot][head][bucket].
+// [buckets][threads], four at a time: reads, sums over equal buckets among the
+// four, writes in order (LDS float atomics, about three cycles a lane, made
+// the pass four times as long).  Tiles whose gaps all lie in the first or the
+// last bucket add to a register.  The columns are summed at the end in a fixed
+// order into part[slot][head][bucket].
 template <typename T, int DP> constexpr uint32_t rows_lds(uint32_t buckets) {
-    return 4 * Tile<T, DP>::bytes + 2 * kGaps * 4 + kMaxBuckets * 8 + buckets * kThreads * 4;
+    return 2 * (Tile<T, DP, kBothWays>::bytes + Tile<T, DP, kByRows>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
+           kCells + 16 + buckets * kThreads * 4;
 }
 
+__device__ __forceinline__ void add_four(float *column, const uint32_t (&b)[4], const float (&x)[4]) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = column[b[i] * kThreads];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        v[i] += x[i];
+#pragma unroll
+        for (int j = 0; j < i; j++)
+            if (b[j] == b[i]) v[i] += x[j];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++) column[b[i] * kThreads] = v[i];
+}
+
+// (rows of 512 bytes leave registers for one wavefront on a SIMD, rows of 256
+// with the bias table LDS for one workgroup on a CU)
 template <typename T, int DP, int POS>
-__global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
+__global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 2) void backward_rows(Attend a) {
     using G = Tile<T, DP>;
+    using KT = Tile<T, DP, kBothWays>;
+    using VT = Tile<T, DP, kByRows>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    float *extra = (float *)(lds + 4 * G::bytes);
-    int32_t *bounds = (int32_t *)(extra + 2 * kGaps);
-    float *bias = (float *)(bounds + kMaxBuckets);
-    float *hist = bias + kMaxBuckets;                         // [buckets][threads]
+    // [2][kGaps] bias by gap, or positions; [2][kGaps] buckets by gap
+    float *extra = (float *)(lds + 2 * (KT::bytes + VT::bytes));
+    uint32_t *code = (uint32_t *)(extra + 2 * kGaps);
+    float *bias = (float *)(code + 2 * kGaps);
+    Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
+    uint32_t *most = (uint32_t *)(buckets.cells + kCells);
+    float *hist = (float *)(most + 4);                        // [buckets][threads]
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
     const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
@@ -55,18 +79,10 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
     const bool there = row < sq.lq;
     const size_t stat = (size_t)(sq.q0 + row) * a.heads + head;
 
-    if constexpr (POS != 0) {
-        for (uint32_t i = threadIdx.x; i < kMaxBuckets; i += kThreads) {
-            bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
-            bias[i] = i < a.buckets ? bias2_of<T>(a, i, head) : 0.0f;
-        }
-        if (want)
-            for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
-        __syncthreads();
-    }
     Owned<T, DP> q, dout;
     load_owned(q, a.q.p + (int64_t)(sq.q0 + row) * a.q.row + head * a.q.head, there, a.dim);
     load_owned(dout, a.dout.p + (int64_t)(sq.q0 + row) * a.dout.row + head * a.dout.head, there, a.dim);
+    sign_owned(q, a.scale);
     int32_t qpos = 0;
     if constexpr (POS == 2)
         if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
@@ -85,11 +101,24 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
         }
         D = halves_sum(D);
     }
+    if (POS != 0 && a.buckets) {
+        stage_bias<T>(a, head, buckets.bounds, bias);
+        if (threadIdx.x == 0) *most = 0;
+        if (want)
+            for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, a, most);
+            __syncthreads();
+            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+        }
+    }
 
-    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wlast = min(row0 + (int32_t)wave * 32 + 32, sq.lq) - 1;
+    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wrow0 = row0 + (int32_t)wave * 32;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
-    const int32_t wend = a.causal ? min(sq.lk, wlast + off + 1) : sq.lk;
+    const int32_t wend = a.causal ? min(sq.lk, min(wrow0 + 32, sq.lq) + off) : sq.lk;
     const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;
+    const int32_t whole = a.causal ? min(sq.lk, wrow0 + off + 1) : sq.lk;
     const uint8_t *kbase = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
     const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
 
@@ -100,26 +129,32 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
         tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
         if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
+    const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
     const auto stage = [&](int32_t k0, int buf) {
-        uint8_t *kt = lds + buf * 2 * G::bytes;
+        uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
         if constexpr (POS == 2) {
             tile_close<T, DP>(kreg, preg);
             tile_close<T, DP>(vreg, preg);
-            tile_store_positions<T, DP>((uint32_t *)extra + buf * kGaps, preg);
+            tile_store_positions<T, DP>((int32_t *)extra + buf * kGaps, preg);
         }
-        tile_store<T, DP>(kt, kreg);
-        tile_store<T, DP>(kt + G::bytes, vreg);
+        tile_store<T, DP, kBothWays>(kt, kreg);
+        tile_store<T, DP, kByRows>(kt + KT::bytes, vreg);
         if constexpr (POS == 1) {
-            const int32_t x = (int32_t)threadIdx.x;
-            if (x < kOwned + G::rows - 1)
-                extra[buf * kGaps + x] =
-                    __uint_as_float(bucket_of(bounds, a.buckets, row0 + off - k0 + x - (G::rows - 1)));
+            const int32_t x = (int32_t)threadIdx.x, lo = least(k0);
+            uint32_t one;
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) &&
+                x < kOwned + G::rows - 1) {
+                const uint32_t n = bucket_of(buckets.bounds, a.buckets, lo + x);
+                code[buf * kGaps + x] = n;
+                extra[buf * kGaps + x] = bias[n];
+            }
         }
     };
 
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) acc[d] = f32x16{};
+    float ends[2] = {0.0f, 0.0f};                             // ds of the first and the last bucket
     // one pass over the keys: FIRST sums D, the other dq (and the bias gradient)
     const auto pass = [&](auto first_pass) {
         constexpr bool FIRST = decltype(first_pass)::value;
@@ -133,44 +168,77 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
             const bool more = k0 + G::rows < kend;
             if (more) fetch(k0 + G::rows);
             if (k0 < wend) {
-                const uint8_t *kt = lds + buf * 2 * G::bytes, *vt = kt + G::bytes;
+                const uint8_t *kt = lds + buf * (KT::bytes + VT::bytes), *vt = kt + KT::bytes;
+                const float *ex = extra + buf * kGaps;
+                const bool ragged = k0 + G::rows > whole;
+                bool far = true, shut = false;
+                uint32_t one = 0;
+                float base = -L;
+                if constexpr (POS == 1) {
+                    far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + kOwned + G::rows - 2, one);
+                    if (far) base = fmaf(bias[one], a.scale2, base);
+                }
+                if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[lane % G::rows] == kNoKeyFlipped);
 #pragma unroll
                 for (int blk = 0; blk < G::blocks; blk++) {
                     f32x16 s = {}, dp = {};
-                    product_rows<T, DP>(s, kt, blk, q);
-                    product_rows<T, DP>(dp, vt, blk, dout);
+                    product_rows<T, DP, kBothWays>(s, kt, blk, q);
+                    product_rows<T, DP, kByRows>(dp, vt, blk, dout);
+                    uint32_t bk[POS == 0 ? 1 : 16];
+                    if (POS == 1 && !far) {
+                        const uint32_t at = wave * 32 + col + (G::rows - 1) - blk * 32;
+#pragma unroll
+                        for (int r = 0; r < 16; r++) {
+                            s[r] += ex[at - block_row(r)];
+                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = code[buf * kGaps + at - block_row(r)];
+                        }
+                    }
+                    if (POS == 2 && a.buckets) {
+#pragma unroll
+                        for (int r = 0; r < 16; r++) {
+                            const uint32_t n = bucket_in(
+                                buckets, gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]));
+                            s[r] += bias[n];
+                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = n;
+                        }
+                    }
+                    if (POS == 2 && shut) {
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            if (((const int32_t *)ex)[blk * 32 + block_row(r)] == kNoKeyFlipped) s[r] = -INFINITY;
+                    }
+                    if (ragged) {
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            if (k0 + blk * 32 + block_row(r) >= limit) s[r] = -INFINITY;
+                    }
                     float ds[16];
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
-                        const int kr = blk * 32 + block_row(r);
-                        float x = s[r] * a.scale2;
-                        uint32_t bk = 0;
-                        if constexpr (POS == 1) {
-                            bk = __float_as_uint(extra[buf * kGaps + wave * 32 + col + (G::rows - 1) - kr]);
-                            x += bias[bk];
-                        }
-                        if constexpr (POS == 2) {
-                            const uint32_t kp = ((const uint32_t *)extra)[buf * kGaps + kr];
-                            if (a.buckets) {
-                                bk = bucket_of(bounds, a.buckets, gap_of(qpos, flip(kp)));
-                                x += bias[bk];
-                            }
-                            if (kp == kNoKey) x = -INFINITY;
-                        }
-                        if (k0 + kr >= limit) x = -INFINITY;
-                        const float p = exp2_fast(x - L);
-                        if constexpr (FIRST) {
-                            D = fmaf(p, dp[r], D);
-                        } else {
-                            ds[r] = p * (dp[r] - D);
-                            if (want) __hip_atomic_fetch_add(hist + bk * kThreads + threadIdx.x, ds[r],
-                                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                        }
+                        const float p = exp2_fast(fmaf(s[r], a.scale2, base));
+                        if constexpr (FIRST) D = fmaf(p, dp[r], D);
+                        else ds[r] = p * (dp[r] - D);
                     }
                     if constexpr (!FIRST) {
+                        if (want && POS == 1 && far) {
+                            float x = 0.0f;
+#pragma unroll
+                            for (int r = 0; r < 16; r++) x += ds[r];
+                            ends[0] += one == 0 ? x : 0.0f;
+                            ends[1] += one == 0 ? 0.0f : x;
+                        } else if (want) {
+#pragma unroll
+                            for (int r = 0; r < 16; r += 4) {
+                                const uint32_t n[4] = {bk[r % (POS == 0 ? 1 : 16)], bk[(r + 1) % (POS == 0 ? 1 : 16)],
+                                                       bk[(r + 2) % (POS == 0 ? 1 : 16)],
+                                                       bk[(r + 3) % (POS == 0 ? 1 : 16)]};
+                                const float x[4] = {ds[r], ds[r + 1], ds[r + 2], ds[r + 3]};
+                                add_four(hist + threadIdx.x, n, x);
+                            }
+                        }
                         Scores<T> p;
                         pack(p, ds);
-                        product_columns<T, DP>(acc, kt, blk, p);
+                        product_columns<T, DP, kBothWays>(acc, kt, blk, p);
                     }
                 }
             }
@@ -187,7 +255,12 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
     if (there)
         store_owned<T, DP>((uint8_t *)a.dq.p + (int64_t)(sq.q0 + row) * a.dq.row + head * a.dq.head, a.dim, acc,
                            a.scale);
-    if (want)                                                 // (the pass ended with a barrier)
+    if (want) {
+        if (POS == 1) {
+            hist[threadIdx.x] += ends[0];
+            hist[(a.buckets - 1) * kThreads + threadIdx.x] += ends[1];
+            __syncthreads();
+        }
         for (uint32_t i = wave; i < a.buckets; i += 4) {
             float x = 0.0f;
 #pragma unroll
@@ -196,6 +269,7 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
             for (int w = 1; w < 64; w *= 2) x += __shfl_xor(x, w);
             if (lane == 0) a.part[((size_t)slot * a.heads + head) * a.buckets + i] = x;
         }
+    }
 }
 
 // ---------------------------------------------------------------- keys
@@ -204,19 +278,27 @@ __global__ __launch_bounds__(kThreads, 1) void backward_rows(Attend a) {
 // buffers, lse and D beside them.  Blocks of scores have the owned keys as
 // columns here, so p and ds go to the products that sum over rows from the
 // registers they are in.
+//
+// WHAT: 1 dv, 2 dk, 3 both.  Both at once keep k, v, dk and dv of a
+// wavefront's keys in registers: rows of 256 bytes and more take two launches
+// instead, which compute the scores twice and run two wavefronts on a SIMD
+// where the one would run one (rows of 128 bf16 values, 8095 rows in two
+// sequences, 16 heads in 4 groups: 1030 us in one launch).
 template <typename T, int DP> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
-    return 4 * Tile<T, DP>::bytes + 2 * (kGaps + 2 * Tile<T, DP>::rows) * 4 +
-           (bias ? kMaxBuckets * 4 * (1 + group) : 0);
+    return 4 * Tile<T, DP, kBothWays>::bytes + 2 * (kGaps + 2 * Tile<T, DP>::rows) * 4 +
+           (bias ? kMaxBuckets * 4 * (1 + group) + kCells + 16 : 0);
 }
 
-template <typename T, int DP, int POS>
-__global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
-    using G = Tile<T, DP>;
+template <typename T, int DP, int POS, int WHAT>
+__global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backward_keys(Attend a) {
+    using G = Tile<T, DP, kBothWays>;
+    constexpr bool DK = WHAT & 2, DV = WHAT & 1;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int kExtra = kGaps + 2 * G::rows;
     float *extra = (float *)(lds + 4 * G::bytes);             // [2]: L, D of the tile's rows; bias by gap, or positions
-    int32_t *bounds = (int32_t *)(extra + 2 * kExtra);
-    float *bias = (float *)(bounds + kMaxBuckets);            // [group][buckets]
+    float *bias = extra + 2 * kExtra;                         // [group][buckets]
+    Buckets buckets = {(int32_t *)(bias + kMaxBuckets * a.group), (uint8_t *)(bias + kMaxBuckets * (1 + a.group)),
+                       a.buckets - 1, 0};
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
     const uint32_t kvh = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
     Seq sq;
@@ -225,26 +307,33 @@ __global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
     if (sq.tile >= ((uint32_t)sq.lk + kOwned - 1) / kOwned) return;
     const int32_t key0 = sq.tile * kOwned, key = key0 + wave * 32 + col, off = sq.lk - sq.lq;
     const bool there = key < sq.lk;
-    if (POS != 0 && a.buckets) {
-        for (uint32_t i = threadIdx.x; i < kMaxBuckets * a.group; i += kThreads) {
-            const uint32_t n = i % kMaxBuckets;
-            if (i < kMaxBuckets) bounds[i] = i + 1 < a.buckets ? a.bounds[i] : INT32_MAX;
-            bias[i] = n < a.buckets ? bias2_of<T>(a, n, kvh * a.group + i / kMaxBuckets) : 0.0f;
-        }
-        __syncthreads();
-    }
-    uint32_t kpos = 0;
-    if constexpr (POS == 2) kpos = there ? a.k_pos[sq.k0 + key] : kNoKey;
-    const bool open = there && (POS != 2 || kpos != kNoKey);
+    int32_t kpos = 0;
+    if constexpr (POS == 2) kpos = there ? flip(a.k_pos[sq.k0 + key]) : kNoKeyFlipped;
+    const bool open = there && (POS != 2 || kpos != kNoKeyFlipped);
     Owned<T, DP> k, v;
     load_owned(k, a.k.p + (int64_t)(sq.k0 + key) * a.k.row + kvh * a.k.head, open, a.dim);
-    load_owned(v, a.v.p + (int64_t)(sq.k0 + key) * a.v.row + kvh * a.v.head, open, a.dim);
+    if constexpr (DK) load_owned(v, a.v.p + (int64_t)(sq.k0 + key) * a.v.row + kvh * a.v.head, open, a.dim);
+    sign_owned(k, a.scale);
+    if (POS != 0 && a.buckets) {
+        for (uint32_t g = 0; g < a.group; g++)
+            stage_bias<T>(a, kvh * a.group + g, g ? nullptr : buckets.bounds, bias + g * kMaxBuckets);
+        uint32_t *most = (uint32_t *)(buckets.cells + kCells);
+        if (threadIdx.x == 0) *most = 0;
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, a, most);
+            __syncthreads();
+            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+        }
+    }
 
-    // rows from `first` on see a key of the workgroup
+    // rows from `first` on see a key of the workgroup, from `whole` on all of the wavefront's
     const int32_t first = a.causal ? max(0, key0 - off) / G::rows * G::rows : 0;
     const int32_t tiles = sq.lq > first ? (sq.lq - first + G::rows - 1) / G::rows : 0;
-    const int32_t least = a.causal ? key - off : 0;           // the first row that sees this lane's key
-    const int32_t wleast = a.causal ? key0 + (int32_t)wave * 32 - off : 0;
+    const int32_t seen = a.causal ? key - off : 0;            // the first row that sees this lane's key
+    const int32_t wseen = a.causal ? key0 + (int32_t)wave * 32 - off : 0;
+    const int32_t whole = a.causal ? wseen + 31 : 0;
+    const bool shut = __any(!open);
 
     typename G::Regs qreg, oreg;
     float Lreg = 0.0f, Dreg = 0.0f;
@@ -258,31 +347,36 @@ __global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
             const bool in = i0 + (int32_t)threadIdx.x < sq.lq;
             const size_t stat = (size_t)(r + threadIdx.x) * a.heads + head;
             Lreg = in ? row_log2(a.lse[stat]) : INFINITY;
-            Dreg = in ? a.delta[stat] : 0.0f;
+            if (DK) Dreg = in ? a.delta[stat] : 0.0f;
             if (POS == 2 && a.q_pos) preg = in ? a.q_pos[r + threadIdx.x] : 0;
         }
     };
+    const auto least = [&](int32_t i0) { return i0 + off - key0 - (kOwned - 1); };
     const auto stage = [&](int32_t g, int32_t i0, int buf) {
         uint8_t *qt = lds + buf * 2 * G::bytes;
         float *e = extra + buf * kExtra;
-        tile_store<T, DP>(qt, qreg);
-        tile_store<T, DP>(qt + G::bytes, oreg);
+        tile_store<T, DP, kBothWays>(qt, qreg);
+        tile_store<T, DP, kBothWays>(qt + G::bytes, oreg);
         if (threadIdx.x < G::rows) {
-            e[threadIdx.x] = Lreg;
-            e[G::rows + threadIdx.x] = Dreg;
-            if (POS == 2) ((uint32_t *)e)[2 * G::rows + threadIdx.x] = preg;
+            e[threadIdx.x] = -Lreg;
+            if (DK) e[G::rows + threadIdx.x] = Dreg;
+            if (POS == 2) ((int32_t *)e)[2 * G::rows + threadIdx.x] = flip(preg);
         }
         if constexpr (POS == 1) {
-            const int32_t x = (int32_t)threadIdx.x;           // gap of x: i0 + off - key0 + x - (owned - 1)
-            if (x < kOwned + G::rows - 1)
-                e[2 * G::rows + x] =
-                    bias[g * kMaxBuckets + bucket_of(bounds, a.buckets, i0 + off - key0 + x - (kOwned - 1))];
+            const int32_t x = (int32_t)threadIdx.x, lo = least(i0);
+            uint32_t one;
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) &&
+                x < kOwned + G::rows - 1)
+                e[2 * G::rows + x] = bias[g * kMaxBuckets + bucket_of(buckets.bounds, a.buckets, lo + x)];
         }
     };
 
-    f32x16 dk[DP / 32], dv[DP / 32];
+    f32x16 dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
-    for (int d = 0; d < DP / 32; d++) dk[d] = dv[d] = f32x16{};
+    for (int d = 0; d < DP / 32; d++) {
+        if constexpr (DK) dk[d] = f32x16{};
+        if constexpr (DV) dv[d] = f32x16{};
+    }
     const int32_t total = tiles * (int32_t)a.group;
     if (total > 0) {
         fetch(0, first);
@@ -299,34 +393,64 @@ __global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
         }
         const bool more = it + 1 < total;
         if (more) fetch(gn, in);
-        if (i0 + G::rows > wleast) {
+        if (i0 + G::rows > wseen) {
             const uint8_t *qt = lds + buf * 2 * G::bytes, *ot = qt + G::bytes;
             const float *e = extra + buf * kExtra;
+            const bool ragged = i0 < whole;
+            bool far = true;
+            float shift = 0.0f;
+            if constexpr (POS == 1) {
+                uint32_t one;
+                far = one_bucket(buckets.bounds, a.buckets, least(i0), least(i0) + kOwned + G::rows - 2, one);
+                if (far) shift = bias[g * kMaxBuckets + one];
+            }
 #pragma unroll
             for (int blk = 0; blk < G::blocks; blk++) {
                 f32x16 s = {}, dp = {};
-                product_rows<T, DP>(s, qt, blk, k);
-                product_rows<T, DP>(dp, ot, blk, v);
+                product_rows<T, DP, kBothWays>(s, qt, blk, k);
+                if constexpr (DK) product_rows<T, DP, kBothWays>(dp, ot, blk, v);
+                if (POS == 1) {
+                    if (far) {
+#pragma unroll
+                        for (int r = 0; r < 16; r++) s[r] += shift;
+                    } else {
+                        const float *x = e + 2 * G::rows + blk * 32 + (kOwned - 1) - wave * 32 - col;
+#pragma unroll
+                        for (int r = 0; r < 16; r++) s[r] += x[block_row(r)];
+                    }
+                }
+                if (POS == 2 && a.buckets) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        s[r] += bias[g * kMaxBuckets +
+                                     bucket_in(buckets, gap_of(((const int32_t *)e)[2 * G::rows + blk * 32 +
+                                                                                   block_row(r)], kpos))];
+                }
+                if (ragged) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++)
+                        if (i0 + blk * 32 + block_row(r) < seen) s[r] = -INFINITY;
+                }
+                if (shut) {
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[r] = open ? s[r] : -INFINITY;
+                }
                 float p[16], ds[16];
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
                     const int ir = blk * 32 + block_row(r);
-                    float x = s[r] * a.scale2;
-                    if constexpr (POS == 1) x += e[2 * G::rows + ir + (kOwned - 1) - wave * 32 - col];
-                    if constexpr (POS == 2)
-                        if (a.buckets)
-                            x += bias[g * kMaxBuckets +
-                                      bucket_of(bounds, a.buckets,
-                                                gap_of(flip(((const uint32_t *)e)[2 * G::rows + ir]), flip(kpos)))];
-                    if (!open || i0 + ir < least) x = -INFINITY;
-                    p[r] = exp2_fast(x - e[ir]);
-                    ds[r] = p[r] * (dp[r] - e[G::rows + ir]);
+                    p[r] = exp2_fast(fmaf(s[r], a.scale2, e[ir]));
+                    if constexpr (DK) ds[r] = p[r] * (dp[r] - e[G::rows + ir]);
                 }
                 Scores<T> w;
-                pack(w, p);
-                product_columns<T, DP>(dv, ot, blk, w);
-                pack(w, ds);
-                product_columns<T, DP>(dk, qt, blk, w);
+                if constexpr (DV) {
+                    pack(w, p);
+                    product_columns<T, DP, kBothWays>(dv, ot, blk, w);
+                }
+                if constexpr (DK) {
+                    pack(w, ds);
+                    product_columns<T, DP, kBothWays>(dk, qt, blk, w);
+                }
             }
         }
         if (more) stage(gn, in, buf ^ 1);
@@ -335,8 +459,10 @@ __global__ __launch_bounds__(kThreads, 1) void backward_keys(Attend a) {
         i0 = in;
     }
     if (!there) return;
-    store_owned<T, DP>((uint8_t *)a.dk.p + (int64_t)(sq.k0 + key) * a.dk.row + kvh * a.dk.head, a.dim, dk, a.scale);
-    store_owned<T, DP>((uint8_t *)a.dv.p + (int64_t)(sq.k0 + key) * a.dv.row + kvh * a.dv.head, a.dim, dv, 1.0f);
+    const int64_t at = sq.k0 + key;
+    if constexpr (DK)
+        store_owned<T, DP>((uint8_t *)a.dk.p + at * a.dk.row + kvh * a.dk.head, a.dim, dk, a.scale);
+    if constexpr (DV) store_owned<T, DP>((uint8_t *)a.dv.p + at * a.dv.row + kvh * a.dv.head, a.dim, dv, 1.0f);
 }
 
 // ---------------------------------------------------------------- short lists
@@ -437,7 +563,7 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
                         s = fmaf(q[g][i], x[i], s);
                         dp = fmaf(dout[g][i], y[i], dp);
                     }
-                    s = lanes_sum<L::per_row>(s) * a.scale2;
+                    s = lanes_sum<L::per_row>(s) * a.signed2;
                     dp = lanes_sum<L::per_row>(dp);
                     if (a.buckets && (uint32_t)g < a.group) s += bias[bk + g];
                     p[u][g] = open[u] ? exp2_fast(s - lse[g]) : 0.0f;
@@ -595,15 +721,23 @@ template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipS
     const auto rows = pos == 2   ? backward_rows<T, DP, 2>
                       : pos == 1 ? backward_rows<T, DP, 1>
                                  : backward_rows<T, DP, 0>;
-    const auto keys = pos == 2   ? backward_keys<T, DP, 2>
-                      : pos == 1 ? backward_keys<T, DP, 1>
-                                 : backward_keys<T, DP, 0>;
+    constexpr bool twice = DP * sizeof(T) >= 256;
+    constexpr int A = twice ? 1 : 3, B = twice ? 2 : 3;
+    const auto keys = pos == 2   ? backward_keys<T, DP, 2, A>
+                      : pos == 1 ? backward_keys<T, DP, 1, A>
+                                 : backward_keys<T, DP, 0, A>;
+    const auto more = pos == 2   ? backward_keys<T, DP, 2, B>
+                      : pos == 1 ? backward_keys<T, DP, 1, B>
+                                 : backward_keys<T, DP, 0, B>;
     const uint32_t rb = rows_lds<T, DP>(a.part ? a.buckets : 0), kb = keys_lds<T, DP>(a.group, a.buckets > 0);
-    if (!allow_lds(rows, rb) || !allow_lds(keys, kb)) return NLB_EDEVICE;
+    if (!allow_lds(rows, rb) || !allow_lds(keys, kb) || !allow_lds(more, kb)) return NLB_EDEVICE;
     a.slots = (uint32_t)p.q_slots;
     if (a.q_rows) hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), rb, stream, a);
     a.slots = (uint32_t)p.k_slots;
-    if (a.k_rows) hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
+    if (a.k_rows) {
+        hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
+        if (twice) hipLaunchKernelGGL(more, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
+    }
     return NLB_OK;
 }
 

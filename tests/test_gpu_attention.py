@@ -140,6 +140,31 @@ def test_fixed_lengths_without_starts(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.7, 2.0 ** -20])
+def test_scales(dtype, scale):
+    """Zero, negative and other scales, with and without a bias."""
+    for one, lq, lk in ((False, [40, 90], [50, 90]), (True, [1] * 9, [30] * 9), (True, [1], [700])):
+        for mode in (False, True):
+            c = make(dtype, lq, lk, 4, 2, 32, bias=mode, train=True, sharp=0.5)
+            check(c, lq, lk, run(c, lq, lk, causal=True, one=one, scale=scale), causal=True, dtype=dtype, scale=scale)
+
+
+def test_many_buckets():
+    """64 buckets, so close that many share a cell of the search, and few."""
+    import torch
+    for bounds in (range(-20, 43), range(1000, 1063), [3 * i * i for i in range(63)], [0], []):
+        for times in (False, True):
+            for one, lq, lk in ((False, [150], [220]), (True, [1] * 4, [60] * 4)):
+                c = make("f32", lq, lk, 2, 1, 16, bias=True, times=times, train=True)
+                c["bounds"] = torch.tensor(list(bounds), dtype=torch.int32)
+                c["bias"] = torch.randn(len(c["bounds"]) + 1, 2, generator=torch.Generator().manual_seed(1))
+                if times:
+                    c["k_pos"] = torch.where(c["k_pos"] >= 0, c["k_pos"] * 8, c["k_pos"])
+                    c["q_pos"] = c["q_pos"] * 9
+                check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype="f32", what=str(bounds))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("gap", [3, 8])
 def test_strided_rows(dtype, gap):
     for one, lq, lk in ((False, [40, 90], [50, 90]), (True, [1] * 9, [30] * 9)):

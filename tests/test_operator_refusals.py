@@ -23,7 +23,7 @@ def _call(**kw):
 ROWS = nlb._AttRows(P, 256, 64)
 BAD_CALLS = [
     dict(dtype=2), dict(heads=0), dict(heads=257, kv_heads=257), dict(kv_heads=0), dict(kv_heads=3), dict(dim=0),
-    dict(dim=129), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2), dict(batch=0), dict(batch=2**31),
+    dict(dim=129), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2.0**21), dict(scale=2.0**-21), dict(causal=2), dict(batch=0), dict(batch=2**31),
     dict(q_rows=2**31), dict(k_rows=2**31), dict(q_rows=11), dict(k_rows=11), dict(buckets=-1), dict(buckets=65, bias=P,
                                                                                                      bounds=P),
     dict(buckets=4), dict(bias=P), dict(buckets=4, bias=P), dict(buckets=4, bias=P, bounds=P + 2),
