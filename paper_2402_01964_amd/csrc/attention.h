@@ -66,7 +66,8 @@ struct Attend {
     const void *bias;                    // [buckets][heads]
     const uint32_t *q_pos, *k_pos;
     float *part;                         // partial results (see the kernels)
-    uint32_t slots, chunk;
+    float *kpart;                        // [2][split][k_rows][kv_heads][dim rounded up to 4]: shares of dk, dv
+    uint32_t slots, chunk, split;
 };
 
 struct Seq {
@@ -637,8 +638,9 @@ struct Backward {
     uint32_t blocks, keep;               // kLists: workgroups; keys whose probabilities stay in LDS
     uint32_t shares;                     // shares of the first sum of bias gradients
     uint64_t q_slots, q_most, k_slots, k_most;
+    uint32_t split;                      // workgroups that share a group's query heads
     uint64_t parts;                      // partial bias gradients
-    size_t delta_bytes, bytes;
+    size_t delta_bytes, part_bytes, bytes;
 };
 
 // Short lists with one query row take a group of lanes each; a group's heads
@@ -672,9 +674,17 @@ inline Backward plan_backward(const Attend &a) {
         p.k_most = INT32_MAX / a.kv_heads;
         p.parts = a.q_rows ? p.q_slots : 0;
         p.delta_bytes = align256((size_t)a.q_rows * a.heads * 4);
+        // Two workgroups of backward_keys run on a CU.  Where key tiles are too
+        // few for two turns of them (which causal sequences of one length need
+        // to even out), a group's heads are spread over workgroups, whose
+        // shares of dk and dv are summed afterwards.
+        const uint64_t tiles = ((uint64_t)a.k_rows / kOwned + 1) * a.kv_heads;
+        p.split = (uint32_t)std::min<uint64_t>(a.group, (1024 + tiles - 1) / tiles);
     }
     p.shares = p.parts > 64 ? 64 : 0;
-    p.bytes = p.delta_bytes + align256((p.parts + p.shares) * a.heads * a.buckets * 4);
+    p.part_bytes = align256((p.parts + p.shares) * a.heads * a.buckets * 4);
+    p.bytes = p.delta_bytes + p.part_bytes;
+    if (p.split > 1) p.bytes += 2 * p.split * (size_t)a.k_rows * a.kv_heads * ((a.dim + 3) / 4) * 16;
     return p;
 }
 

@@ -8,6 +8,9 @@
 // backward_keys), each of which owns what it sums: no atomics on results, the
 // same bits each time, at the price of computing the scores and dp twice.
 #include "attention.h"
+#ifndef TWICE
+#define TWICE 256
+#endif
 
 namespace {
 
@@ -300,7 +303,10 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets * a.group), (uint8_t *)(bias + kMaxBuckets * (1 + a.group)),
                        a.buckets - 1, 0};
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
-    const uint32_t kvh = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
+    const uint32_t kvh = blockIdx.x % a.kv_heads, share = blockIdx.x / a.kv_heads % a.split;
+    const uint32_t slot = blockIdx.x / (a.kv_heads * a.split);
+    // query heads of the group: this workgroup's share
+    const int32_t g0 = a.group * share / a.split, g1 = a.group * (share + 1) / a.split;
     Seq sq;
     const uint32_t b = slot_owner(a.k_start, a.k_len, a.k_rows, a.batch, kOwned, slot, sq.tile);
     sequence(a, b, sq);
@@ -377,14 +383,14 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         if constexpr (DK) dk[d] = f32x16{};
         if constexpr (DV) dv[d] = f32x16{};
     }
-    const int32_t total = tiles * (int32_t)a.group;
+    const int32_t total = tiles * (g1 - g0);
     if (total > 0) {
-        fetch(0, first);
-        stage(0, first, 0);
+        fetch(g0, first);
+        stage(g0, first, 0);
     }
     __syncthreads();
     int buf = 0;
-    int32_t g = 0, i0 = first;
+    int32_t g = g0, i0 = first;
     for (int32_t it = 0; it < total; it++, buf ^= 1) {
         int32_t gn = g, in = i0 + G::rows;
         if (in >= sq.lq) {
@@ -460,9 +466,35 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     }
     if (!there) return;
     const int64_t at = sq.k0 + key;
+    if (a.split > 1) {
+        const size_t width = (a.dim + 3) / 4 * 4, all = (size_t)a.k_rows * a.kv_heads * width;
+        float *p = a.kpart + share * all + (at * a.kv_heads + kvh) * width;
+        if constexpr (DK) store_owned<float, DP>((uint8_t *)p, a.dim, dk, a.scale);
+        if constexpr (DV) store_owned<float, DP>((uint8_t *)(p + a.split * all), a.dim, dv, 1.0f);
+        return;
+    }
     if constexpr (DK)
         store_owned<T, DP>((uint8_t *)a.dk.p + at * a.dk.row + kvh * a.dk.head, a.dim, dk, a.scale);
     if constexpr (DV) store_owned<T, DP>((uint8_t *)a.dv.p + at * a.dv.row + kvh * a.dv.head, a.dim, dv, 1.0f);
+}
+
+// The sum of the shares of dk (blockIdx.y 0) and dv: a thread four values.
+template <typename T> __global__ __launch_bounds__(kThreads) void sum_heads(Attend a) {
+    const uint32_t chunks = (a.dim + 3) / 4;
+    const uint32_t lo = first_row(a.k_start, a.k_len, a.k_rows, 0);
+    const uint32_t hi = first_row(a.k_start, a.k_len, a.k_rows, a.batch);
+    const size_t all = (size_t)a.k_rows * a.kv_heads * chunks;
+    const f32x4 *part = (const f32x4 *)a.kpart + blockIdx.y * a.split * all;
+    const Strided &out = blockIdx.y ? a.dv : a.dk;
+    for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < all; i += (size_t)gridDim.x * kThreads) {
+        const size_t row = i / chunks / a.kv_heads;
+        if (row < lo || row >= hi) continue;
+        f32x4 x = part[i];
+        for (uint32_t s = 1; s < a.split; s++) x += part[s * all + i];
+        const float f[4] = {x[0], x[1], x[2], x[3]};
+        store_values<T, 4>((uint8_t *)out.p + row * out.row + i / chunks % a.kv_heads * out.head, i % chunks * 4,
+                           a.dim, f);
+    }
 }
 
 // ---------------------------------------------------------------- short lists
@@ -721,7 +753,7 @@ template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipS
     const auto rows = pos == 2   ? backward_rows<T, DP, 2>
                       : pos == 1 ? backward_rows<T, DP, 1>
                                  : backward_rows<T, DP, 0>;
-    constexpr bool twice = DP * sizeof(T) >= 256;
+    constexpr bool twice = DP * sizeof(T) >= TWICE;
     constexpr int A = twice ? 1 : 3, B = twice ? 2 : 3;
     const auto keys = pos == 2   ? backward_keys<T, DP, 2, A>
                       : pos == 1 ? backward_keys<T, DP, 1, A>
@@ -735,8 +767,10 @@ template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipS
     if (a.q_rows) hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), rb, stream, a);
     a.slots = (uint32_t)p.k_slots;
     if (a.k_rows) {
-        hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
-        if (twice) hipLaunchKernelGGL(more, dim3(a.slots * a.kv_heads), dim3(kThreads), kb, stream, a);
+        const dim3 grid(a.slots * a.kv_heads * a.split);
+        hipLaunchKernelGGL(keys, grid, dim3(kThreads), kb, stream, a);
+        if (twice) hipLaunchKernelGGL(more, grid, dim3(kThreads), kb, stream, a);
+        if (a.split > 1) hipLaunchKernelGGL((sum_heads<T>), dim3(1024, 2), dim3(kThreads), 0, stream, a);
     }
     return NLB_OK;
 }
@@ -800,6 +834,8 @@ extern "C" int nlb_attention_backward(const nlb_att_call *c, const nlb_att_rows 
     if (!guard.ok()) return NLB_EDEVICE;
     a.lse = const_cast<float *>(lse);
     a.delta = (float *)work;
+    a.split = p.split;
+    a.kpart = (float *)((uint8_t *)work + p.delta_bytes + p.part_bytes);
     a.part = dbias ? (float *)((uint8_t *)work + p.delta_bytes) : nullptr;
     return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, p, dbias, (hipStream_t)stream)
                                       : launch<float>(a, p, dbias, (hipStream_t)stream);
