@@ -303,17 +303,35 @@ template <typename T, int DP, Use USE = kByRows> struct Tile {
     typedef uint32_t Positions[per_thread];
 };
 
-// This thread's chunks of the tile whose first row is `base`; rows from n on are zeros.
-template <typename T, int DP>
+// This thread's chunks of the tile whose first row is `base`, which has n > 0
+// rows.  EXACT: a row is a whole number of chunks and a tile's rows lie within
+// 2^31 bytes; rows from n on repeat the last one (their scores are masked, or
+// their probabilities zero), so that the loads of a tile are nothing but loads
+// (with a test for each chunk, vector operations for them took as long as the
+// exponentials).  Else rows from n on are zeros.
+template <typename T, int DP, bool EXACT>
 __device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const uint8_t *base, int64_t stride,
                                           int32_t n, uint32_t dim) {
     using G = Tile<T, DP>;
-    const uint32_t c = threadIdx.x % G::chunks, r0 = threadIdx.x / G::chunks;
+    const uint32_t c0 = threadIdx.x % G::chunks * Chunk<T>::n, r0 = threadIdx.x / G::chunks;
+    if constexpr (EXACT) {
+        if (c0 < dim) {
 #pragma unroll
-    for (int i = 0; i < G::per_thread; i++) {
-        const int32_t r = r0 + i * (kThreads / G::chunks);
-        reg[i] = u32x4{0, 0, 0, 0};
-        if (r < n) reg[i] = load_chunk<T>(base + r * stride, c * Chunk<T>::n, dim);
+            for (int i = 0; i < G::per_thread; i++) {
+                const uint32_t r = min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1);
+                reg[i] = *(const u32x4_any *)(base + (r * (uint32_t)stride + c0 * (uint32_t)sizeof(T)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < G::per_thread; i++) {
+            const int32_t r = r0 + i * (kThreads / G::chunks);
+            reg[i] = u32x4{0, 0, 0, 0};
+            if (r < n) reg[i] = load_chunk<T>(base + r * stride, c0, dim);
+        }
     }
 }
 
@@ -578,6 +596,11 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
     a.q_pos = c->q_pos;
     a.k_pos = c->k_pos;
     return NLB_OK;
+}
+
+// Whether rows take the short form of tile_load.
+inline bool exact_rows(const Attend &a, const Strided &r) {
+    return a.dim * a.dtype_bytes % 16 == 0 && r.row <= 1 << 25;
 }
 
 inline int device_of(const nlb_att_call *c, int &dev) {

@@ -34,7 +34,7 @@ template <typename T, int DP> constexpr uint32_t tiles_lds() {
            kCells + 16;
 }
 
-template <typename T, int DP, int POS>
+template <typename T, int DP, int POS, bool EXACT>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     using G = Tile<T, DP>;
     using KT = Tile<T, DP, kByRows>;
@@ -86,8 +86,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     typename G::Regs kreg, vreg;
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
-        tile_load<T, DP>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
-        tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        tile_load<T, DP, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<T, DP, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
         if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
     // the gaps of the tile at k0: from least to least + owned + rows - 2
@@ -565,10 +565,12 @@ __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
 }
 
 // ---------------------------------------------------------------- launches
-template <typename T, int DP>
+template <typename T, int DP, bool EXACT>
 int launch_tiles(const Attend &a, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
-    const auto kernel = pos == 2 ? attend_tiles<T, DP, 2> : pos == 1 ? attend_tiles<T, DP, 1> : attend_tiles<T, DP, 0>;
+    const auto kernel = pos == 2   ? attend_tiles<T, DP, 2, EXACT>
+                        : pos == 1 ? attend_tiles<T, DP, 1, EXACT>
+                                   : attend_tiles<T, DP, 0, EXACT>;
     constexpr uint32_t bytes = tiles_lds<T, DP>();
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
     hipLaunchKernelGGL(kernel, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
@@ -598,10 +600,15 @@ int launch_single(const Attend &a, Form form, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
+template <typename T, int DP> int launch_form(const Attend &a, Form form, hipStream_t s) {
+    if (form != kTiles) return launch_single<T, DP>(a, form, s);
+    return exact_rows(a, a.k) && exact_rows(a, a.v) ? launch_tiles<T, DP, true>(a, s) : launch_tiles<T, DP, false>(a, s);
+}
+
 template <typename T> int launch(const Attend &a, Form form, hipStream_t s) {
-    if (a.dim <= 32) return form == kTiles ? launch_tiles<T, 32>(a, s) : launch_single<T, 32>(a, form, s);
-    if (a.dim <= 64) return form == kTiles ? launch_tiles<T, 64>(a, s) : launch_single<T, 64>(a, form, s);
-    return form == kTiles ? launch_tiles<T, 128>(a, s) : launch_single<T, 128>(a, form, s);
+    return a.dim <= 32   ? launch_form<T, 32>(a, form, s)
+           : a.dim <= 64 ? launch_form<T, 64>(a, form, s)
+                         : launch_form<T, 128>(a, form, s);
 }
 
 }  // namespace

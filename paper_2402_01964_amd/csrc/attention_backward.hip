@@ -8,9 +8,6 @@
 // backward_keys), each of which owns what it sums: no atomics on results, the
 // same bits each time, at the price of computing the scores and dp twice.
 #include "attention.h"
-#ifndef TWICE
-#define TWICE 256
-#endif
 
 namespace {
 
@@ -54,7 +51,7 @@ __device__ __forceinline__ void add_four(float *column, const uint32_t (&b)[4], 
 
 // (rows of 512 bytes leave registers for one wavefront on a SIMD, rows of 256
 // with the bias table LDS for one workgroup on a CU)
-template <typename T, int DP, int POS>
+template <typename T, int DP, int POS, bool EXACT>
 __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 2) void backward_rows(Attend a) {
     using G = Tile<T, DP>;
     using KT = Tile<T, DP, kBothWays>;
@@ -128,8 +125,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     typename G::Regs kreg, vreg;
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
-        tile_load<T, DP>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
-        tile_load<T, DP>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        tile_load<T, DP, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<T, DP, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
         if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
     const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
@@ -292,7 +289,7 @@ template <typename T, int DP> constexpr uint32_t keys_lds(uint32_t group, bool b
            (bias ? kMaxBuckets * 4 * (1 + group) + kCells + 16 : 0);
 }
 
-template <typename T, int DP, int POS, int WHAT>
+template <typename T, int DP, int POS, int WHAT, bool EXACT>
 __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backward_keys(Attend a) {
     using G = Tile<T, DP, kBothWays>;
     constexpr bool DK = WHAT & 2, DV = WHAT & 1;
@@ -347,8 +344,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     const auto fetch = [&](int32_t g, int32_t i0) {
         const uint32_t head = kvh * a.group + g;
         const int64_t r = sq.q0 + i0;
-        tile_load<T, DP>(qreg, a.q.p + r * a.q.row + head * a.q.head, a.q.row, sq.lq - i0, a.dim);
-        tile_load<T, DP>(oreg, a.dout.p + r * a.dout.row + head * a.dout.head, a.dout.row, sq.lq - i0, a.dim);
+        tile_load<T, DP, EXACT>(qreg, a.q.p + r * a.q.row + head * a.q.head, a.q.row, sq.lq - i0, a.dim);
+        tile_load<T, DP, EXACT>(oreg, a.dout.p + r * a.dout.row + head * a.dout.head, a.dout.row, sq.lq - i0, a.dim);
         if (threadIdx.x < G::rows) {
             const bool in = i0 + (int32_t)threadIdx.x < sq.lq;
             const size_t stat = (size_t)(r + threadIdx.x) * a.heads + head;
@@ -748,19 +745,19 @@ __global__ __launch_bounds__(kThreads) void sum_bias(const float *part, uint32_t
 }
 
 // ---------------------------------------------------------------- launches
-template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
+template <typename T, int DP, bool EXACT> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
-    const auto rows = pos == 2   ? backward_rows<T, DP, 2>
-                      : pos == 1 ? backward_rows<T, DP, 1>
-                                 : backward_rows<T, DP, 0>;
-    constexpr bool twice = DP * sizeof(T) >= TWICE;
+    const auto rows = pos == 2   ? backward_rows<T, DP, 2, EXACT>
+                      : pos == 1 ? backward_rows<T, DP, 1, EXACT>
+                                 : backward_rows<T, DP, 0, EXACT>;
+    constexpr bool twice = DP * sizeof(T) >= 256;
     constexpr int A = twice ? 1 : 3, B = twice ? 2 : 3;
-    const auto keys = pos == 2   ? backward_keys<T, DP, 2, A>
-                      : pos == 1 ? backward_keys<T, DP, 1, A>
-                                 : backward_keys<T, DP, 0, A>;
-    const auto more = pos == 2   ? backward_keys<T, DP, 2, B>
-                      : pos == 1 ? backward_keys<T, DP, 1, B>
-                                 : backward_keys<T, DP, 0, B>;
+    const auto keys = pos == 2   ? backward_keys<T, DP, 2, A, EXACT>
+                      : pos == 1 ? backward_keys<T, DP, 1, A, EXACT>
+                                 : backward_keys<T, DP, 0, A, EXACT>;
+    const auto more = pos == 2   ? backward_keys<T, DP, 2, B, EXACT>
+                      : pos == 1 ? backward_keys<T, DP, 1, B, EXACT>
+                                 : backward_keys<T, DP, 0, B, EXACT>;
     const uint32_t rb = rows_lds<T, DP>(a.part ? a.buckets : 0), kb = keys_lds<T, DP>(a.group, a.buckets > 0);
     if (!allow_lds(rows, rb) || !allow_lds(keys, kb) || !allow_lds(more, kb)) return NLB_EDEVICE;
     a.slots = (uint32_t)p.q_slots;
@@ -787,11 +784,17 @@ template <typename T, int DP> int launch_lists(const Attend &a, const Backward &
     return NLB_OK;
 }
 
+template <typename T, int DP> int launch_form(const Attend &a, const Backward &p, hipStream_t s) {
+    if (p.lists) return launch_lists<T, DP>(a, p, s);
+    return exact_rows(a, a.q) && exact_rows(a, a.k) && exact_rows(a, a.v) && exact_rows(a, a.dout)
+               ? launch_tiles<T, DP, true>(a, p, s)
+               : launch_tiles<T, DP, false>(a, p, s);
+}
+
 template <typename T> int launch(const Attend &a, const Backward &p, void *dbias, hipStream_t s) {
-    int rc;
-    if (a.dim <= 32) rc = p.lists ? launch_lists<T, 32>(a, p, s) : launch_tiles<T, 32>(a, p, s);
-    else if (a.dim <= 64) rc = p.lists ? launch_lists<T, 64>(a, p, s) : launch_tiles<T, 64>(a, p, s);
-    else rc = p.lists ? launch_lists<T, 128>(a, p, s) : launch_tiles<T, 128>(a, p, s);
+    const int rc = a.dim <= 32   ? launch_form<T, 32>(a, p, s)
+                   : a.dim <= 64 ? launch_form<T, 64>(a, p, s)
+                                 : launch_form<T, 128>(a, p, s);
     if (rc != NLB_OK) return rc;
     if (dbias) {
         const float *from = a.part;
