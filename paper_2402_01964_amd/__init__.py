@@ -73,11 +73,12 @@ class _AttRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
-class _AttCall(ctypes.Structure):
+class _AttCall(ctypes.Structure):                             # (q, k, v: nlb_att_rows each)
     _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "heads", "kv_heads", "dim", "causal", "buckets")] + \
                [("scale", ctypes.c_float)] + [(k, ctypes.c_uint32) for k in ("batch", "q_rows", "k_rows")] + \
                [(k, ctypes.c_void_p) for k in ("q_start", "k_start", "bias", "bounds", "q_pos", "k_pos")] + \
-               [(k, _AttRows) for k in ("q", "k", "v")]
+               [(t + f, c) for t in ("q", "k", "v")
+                for f, c in (("", ctypes.c_void_p), ("_row", ctypes.c_int64), ("_head", ctypes.c_int64))]
 
 
 class _NormCall(ctypes.Structure):
@@ -427,108 +428,106 @@ class Table:
 
 
 # ---------------------------------------------------------------- operators without a table
+# (A small call's time is the host's: tensors are looked at once, structures
+# filled in one go, and nothing is allocated that the caller brings.)
 def _float_dtype(t, name):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"{name} must be float32 or bfloat16")
-    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    raise TypeError(f"{name} must be float32 or bfloat16")
 
 
-def _like(t, q, name):
-    if t.dtype != q.dtype or t.device != q.device:
-        raise TypeError(f"{name} must have q's type and device")
-    return t
+def _on(stream, device):
+    """`stream` as the current one, so that what a call allocates belongs to it."""
+    import torch
+    if stream.device != device:
+        raise ValueError("the stream must be on the tensors' device")
+    return torch.cuda.stream(stream)
+
+
+def _current_stream(device):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _att_rows(t, q, shape, name):
-    """[rows, heads, dim] with contiguous values, any row and head strides."""
-    if tuple(_like(t, q, name).shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    """A tensor [rows, heads, dim] with contiguous values, any row and head
+    strides, as (pointer, row stride, head stride)."""
+    if t.dtype != q.dtype or t.device != q.device:
+        raise TypeError(f"{name} must have q's type and device")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    s = t.stride()
+    if s[2] != 1 and shape[2] > 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return _AttRows(t.data_ptr(), t.stride(0), t.stride(1))
+    return t.data_ptr(), s[0], s[1]
 
 
-def _int_vector(t, n, q, name):
-    import torch
+def _vector(t, n, like, dtypes, name):
+    """A contiguous vector's pointer (None for None)."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.uint32):
-        raise TypeError(f"{name} must be an int32 (or uint32) tensor")
-    if t.device != q.device:
-        raise TypeError(f"{name} must be on q's device")
-    if t.dim() != 1 and name not in ("q_pos", "k_pos"):
-        raise ValueError(f"{name} must be one-dimensional")
-    if t.numel() != n:
-        raise ValueError(f"{name} must have {n} elements")
-    return _dev_ptr(t, 4, name)
+    if t.dtype not in dtypes or t.device != like.device:
+        raise TypeError(f"{name} must be {' or '.join(str(d)[6:] for d in dtypes)}, on the other tensors' device")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, with {n} elements")
+    return t.data_ptr()
 
 
 def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos):
     import torch
-    c = _AttCall()
-    c.dtype = _float_dtype(q, "q")
+    dtype = _float_dtype(q, "q")
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k and v must be [rows, heads, dim]")
-    c.device = q.device.index
-    c.q_rows, c.heads, c.dim = q.shape
-    c.k_rows, c.kv_heads = k.shape[0], k.shape[1]
+    q_rows, heads, dim = shape = q.shape
+    k_rows, kv_heads, _ = k.shape
     if batch is None:
         starts = q_start if q_start is not None else k_start
         batch = 1 if starts is None else starts.numel() - 1
-    c.batch = int(batch)
-    c.q_start = _int_vector(q_start, c.batch + 1, q, "q_start")
-    c.k_start = _int_vector(k_start, c.batch + 1, q, "k_start")
-    c.causal = int(bool(causal))
-    c.scale = float(scale) if scale is not None else max(1, c.dim) ** -0.5
-    kv = (c.k_rows, c.kv_heads, c.dim)
-    c.q, c.k, c.v = _att_rows(q, q, q.shape, "q"), _att_rows(k, q, kv, "k"), _att_rows(v, q, kv, "v")
+    ints = (torch.int32,)
+    buckets, bias_ptr, bounds_ptr = 0, None, None
     if bias is not None:
-        if bias.dim() != 2 or bias.shape[1] != c.heads:
+        if bias.dim() != 2 or bias.shape[1] != heads:
             raise ValueError("bias must be [buckets, heads]")
-        c.buckets = bias.shape[0]
-        c.bias = _dev_ptr(_like(bias, q, "bias"), None, "bias")
-        if bounds is not None or c.buckets != 1:
-            if bounds is None or bounds.dtype != torch.int32:
-                raise TypeError("bounds must be an int32 tensor")
-            c.bounds = _int_vector(bounds, c.buckets - 1, q, "bounds")
+        buckets = bias.shape[0]
+        bias_ptr = _vector(bias, buckets * heads, q, (q.dtype,), "bias")
+        if bounds is None and buckets != 1:
+            raise ValueError("bias needs its bounds")
+        bounds_ptr = _vector(bounds, buckets - 1, q, ints, "bounds")
     elif bounds is not None:
         raise ValueError("bounds without bias")
-    c.q_pos = _int_vector(q_pos, c.q_rows, q, "q_pos")
-    c.k_pos = _int_vector(k_pos, c.k_rows, q, "k_pos")
-    return c
+    words = (torch.int32, torch.uint32)
+    return _AttCall(q.device.index, dtype, heads, kv_heads, dim, 1 if causal else 0, buckets,
+                    dim ** -0.5 if scale is None and dim else scale or 0.0, batch, q_rows, k_rows,
+                    _vector(q_start, batch + 1, q, ints, "q_start"), _vector(k_start, batch + 1, q, ints, "k_start"),
+                    bias_ptr, bounds_ptr, _vector(q_pos, q_rows, q, words, "q_pos"),
+                    _vector(k_pos, k_rows, q, words, "k_pos"), *_att_rows(q, q, shape, "q"),
+                    *_att_rows(k, q, (k_rows, kv_heads, dim), "k"), *_att_rows(v, q, k.shape, "v"))
 
 
-class _OnStream:
-    """The stream of a call on tensors of `device` (default: that device's
-    current one), made current so that what the call allocates belongs to it."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.stream = torch.cuda.current_stream(device) if stream is None else stream
-        if self.stream.device != device:
-            raise ValueError("the stream must be on the tensors' device")
-        self._as_current = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self._as_current is not None:
-            self._as_current.__enter__()
-        return ctypes.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *exc):
-        if self._as_current is not None:
-            self._as_current.__exit__(*exc)
-
-
-def _work(n, work, like):
+def _lse(lse, q):
     import torch
+    if lse.shape != q.shape[:2]:
+        raise ValueError("lse must be [q_rows, heads]")
+    return _vector(lse, lse.numel(), q, (torch.float32,), "lse")
+
+
+def _work(lib_work, call, args, work, like, what):
+    """Working memory (allocated if None): the tensor, its pointer and size."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib_work(call, *args, n), what)
     if work is None:
-        work = torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
-    elif not work.is_cuda or work.device != like.device or not work.is_contiguous():
+        if not n.value:
+            return None, None, 0
+        work = like.new_empty(n.value, dtype=torch.uint8)
+    elif work.device != like.device or not work.is_contiguous():
         raise TypeError("work must be a contiguous tensor on the call's device")
-    return work, None if work is None else work.data_ptr(), 0 if work is None else work.numel() * work.element_size()
+    return work, work.data_ptr(), work.numel() * work.element_size()
 
 
 def attention_work(q, k, v, *, backward=False, batch=None, q_start=None, k_start=None, causal=False, scale=None,
@@ -536,8 +535,7 @@ def attention_work(q, k, v, *, backward=False, batch=None, q_start=None, k_start
     """Bytes of working memory that such a call takes (``work=``)."""
     c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
     n = ctypes.c_size_t()
-    _check(load_library().nlb_attention_work(ctypes.byref(c), int(bool(backward)), ctypes.byref(n)),
-           "nlb_attention_work")
+    _check(load_library().nlb_attention_work(c, int(bool(backward)), n), "nlb_attention_work")
     return n.value
 
 
@@ -555,19 +553,17 @@ def attention(q, k, v, *, batch=None, q_start=None, k_start=None, causal=False, 
     import torch
     lib = load_library()
     c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
-    with _OnStream(q.device, stream) as s:
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        o = _att_rows(out, q, q.shape, "out")
-        if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != q.device:
-            raise ValueError("lse must be float32 [q_rows, heads] on q's device")
-        n = ctypes.c_size_t()
-        _check(lib.nlb_attention_work(ctypes.byref(c), 0, ctypes.byref(n)), "nlb_attention")
-        keep, p, size = _work(n.value, work, q)
-        _check(lib.nlb_attention(ctypes.byref(c), ctypes.byref(o), _dev_ptr(lse, 4, "lse"), p, size, s),
-               "nlb_attention")
+    if stream is not None:
+        with _on(stream, q.device):
+            return attention(q, k, v, batch=batch, q_start=q_start, k_start=k_start, causal=causal, scale=scale,
+                             bias=bias, bounds=bounds, q_pos=q_pos, k_pos=k_pos, out=out, lse=lse, work=work)
+    if out is None:
+        out = q.new_empty(q.shape)
+    if lse is None:
+        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+    o = _AttRows(*_att_rows(out, q, q.shape, "out"))
+    keep, p, size = _work(lib.nlb_attention_work, c, (0,), work, q, "nlb_attention")
+    _check(lib.nlb_attention(c, o, _lse(lse, q), p, size, _current_stream(q.device)), "nlb_attention")
     return out, lse
 
 
@@ -579,66 +575,59 @@ def attention_backward(dout, q, k, v, out, lse, *, batch=None, q_start=None, k_s
     out.  Returns (or fills) dq, dk, dv and dbias (None without a bias, or
     with need_dbias=False).  ``work``: attention_work(..., backward=True)
     bytes, allocated if None."""
-    import torch
     lib = load_library()
     c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
-    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or lse.device != q.device:
-        raise ValueError("lse must be float32 [q_rows, heads] on q's device")
-    if dbias is not None and bias is None:
+    if stream is not None:
+        with _on(stream, q.device):
+            return attention_backward(dout, q, k, v, out, lse, batch=batch, q_start=q_start, k_start=k_start,
+                                      causal=causal, scale=scale, bias=bias, bounds=bounds, q_pos=q_pos, k_pos=k_pos,
+                                      dq=dq, dk=dk, dv=dv, dbias=dbias, need_dbias=need_dbias, work=work)
+    if bias is None and dbias is not None:
         raise ValueError("dbias without bias")
-    with _OnStream(q.device, stream) as s:
-        dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) if d is None else d
-                      for d, t in ((dq, q), (dk, k), (dv, v)))
-        if bias is None or not need_dbias:
-            dbias = None
-        elif dbias is None:
-            dbias = torch.empty_like(bias)
+    dq, dk, dv = (q.new_empty(t.shape) if d is None else d for d, t in ((dq, q), (dk, k), (dv, v)))
+    grad = None
+    if bias is None or not need_dbias:
+        dbias = None
+    else:
+        if dbias is None:
+            dbias = q.new_empty(bias.shape)
         elif dbias.shape != bias.shape:
             raise ValueError("dbias must have bias's shape")
-        rows = [_att_rows(t, q, like.shape, name) for t, like, name in
-                ((out, q, "out"), (dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"))]
-        n = ctypes.c_size_t()
-        _check(lib.nlb_attention_work(ctypes.byref(c), 1, ctypes.byref(n)), "nlb_attention_backward")
-        keep, p, size = _work(n.value, work, q)
-        r = [ctypes.byref(x) for x in rows]
-        _check(lib.nlb_attention_backward(ctypes.byref(c), r[0], _dev_ptr(lse, 4, "lse"), r[1], r[2], r[3], r[4],
-                                          None if dbias is None else _dev_ptr(_like(dbias, q, "dbias"), None, "dbias"),
-                                          p, size, s), "nlb_attention_backward")
+        grad = _vector(dbias, dbias.numel(), q, (q.dtype,), "dbias")
+    rows = [_AttRows(*_att_rows(t, q, like.shape, name)) for t, like, name in
+            ((out, q, "out"), (dout, q, "dout"), (dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"))]
+    keep, p, size = _work(lib.nlb_attention_work, c, (1,), work, q, "nlb_attention_backward")
+    _check(lib.nlb_attention_backward(c, rows[0], _lse(lse, q), *rows[1:], grad, p, size, _current_stream(q.device)),
+           "nlb_attention_backward")
     return dq, dk, dv, dbias
 
 
 def _norm_rows(t, x, name):
-    """[..., width] as rows: their stride in values."""
+    """A tensor [..., width] as rows: (pointer, row stride)."""
     if t.shape != x.shape:
         raise ValueError(f"{name} must have x's shape")
-    _like(t, x, name)
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.dtype != x.dtype or t.device != x.device:
+        raise TypeError(f"{name} must have x's type and device")
+    s = t.stride()
+    if s[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    if t.dim() > 2 and not t.is_contiguous():
+    if len(s) == 2:
+        return t.data_ptr(), s[0]
+    if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous, or of two dimensions")
-    return t.stride(0) if t.dim() == 2 else t.shape[-1]
-
-
-def _fp32_vector(t, n, x, name):
-    import torch
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.numel() != n or t.device != x.device:
-        raise ValueError(f"{name} must be float32 with {n} elements, on x's device")
-    return _dev_ptr(t, 4, name)
+    return t.data_ptr(), t.shape[-1]
 
 
 def _norm_call(x, w, mean, rstd):
-    c = _NormCall()
-    c.dtype = _float_dtype(x, "x")
+    import torch
+    dtype = _float_dtype(x, "x")
     if x.dim() < 1:
         raise ValueError("x must have a last dimension")
-    c.device, c.width = x.device.index, x.shape[-1]
-    c.rows = x.numel() // max(1, c.width)
-    c.x, c.x_stride = x.data_ptr(), _norm_rows(x, x, "x")
-    c.w = _fp32_vector(w, c.width, x, "w")
-    c.mean, c.rstd = _fp32_vector(mean, c.rows, x, "mean"), _fp32_vector(rstd, c.rows, x, "rstd")
-    return c
+    width = x.shape[-1]
+    rows = x.numel() // max(1, width)
+    fp32 = (torch.float32,)
+    return _NormCall(x.device.index, dtype, rows, width, *_norm_rows(x, x, "x"), _vector(w, width, x, fp32, "w"),
+                     _vector(mean, rows, x, fp32, "mean"), _vector(rstd, rows, x, fp32, "rstd"))
 
 
 def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rstd=None, stream=None):
@@ -649,14 +638,18 @@ def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rst
     import torch
     lib = load_library()
     _float_dtype(x, "x")
-    with _OnStream(x.device, stream) as s:
-        rows = x.shape[:-1]
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) if t is None else t for t in (mean, rstd))
-        c = _norm_call(x, w, mean, rstd)
-        _check(lib.nlb_layer_norm(ctypes.byref(c), _fp32_vector(b, c.width, x, "b"), float(eps), out.data_ptr(),
-                                  _norm_rows(out, x, "out"), s), "nlb_layer_norm")
+    if stream is not None:
+        with _on(stream, x.device):
+            return layer_norm(x, w, b, eps, out=out, mean=mean, rstd=rstd)
+    if out is None:
+        out = x.new_empty(x.shape)
+    if mean is None:
+        mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    if rstd is None:
+        rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    c = _norm_call(x, w, mean, rstd)
+    _check(lib.nlb_layer_norm(c, _vector(b, c.width, x, (torch.float32,), "b"), eps, *_norm_rows(out, x, "out"),
+                              _current_stream(x.device)), "nlb_layer_norm")
     return out, mean, rstd
 
 
@@ -667,16 +660,15 @@ def layer_norm_backward(dy, x, w, mean, rstd, *, dx=None, dw=None, db=None, work
     import torch
     lib = load_library()
     _float_dtype(x, "x")
-    with _OnStream(x.device, stream) as s:
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        c = _norm_call(x, w, mean, rstd)
-        dw, db = (torch.empty(c.width, dtype=torch.float32, device=x.device) if t is None else t for t in (dw, db))
-        n = ctypes.c_size_t()
-        _check(lib.nlb_layer_norm_work(ctypes.byref(c), ctypes.byref(n)), "nlb_layer_norm_backward")
-        keep, p, size = _work(n.value, work, x)
-        _check(lib.nlb_layer_norm_backward(ctypes.byref(c), dy.data_ptr(), _norm_rows(dy, x, "dy"), dx.data_ptr(),
-                                           _norm_rows(dx, x, "dx"), _fp32_vector(dw, c.width, x, "dw"),
-                                           _fp32_vector(db, c.width, x, "db"), p, size, s),
-               "nlb_layer_norm_backward")
+    if stream is not None:
+        with _on(stream, x.device):
+            return layer_norm_backward(dy, x, w, mean, rstd, dx=dx, dw=dw, db=db, work=work)
+    fp32 = (torch.float32,)
+    c = _norm_call(x, w, mean, rstd)
+    dx = x.new_empty(x.shape) if dx is None else dx
+    dw, db = (x.new_empty(c.width, dtype=torch.float32) if t is None else t for t in (dw, db))
+    keep, p, size = _work(lib.nlb_layer_norm_work, c, (), work, x, "nlb_layer_norm_backward")
+    _check(lib.nlb_layer_norm_backward(c, *_norm_rows(dy, x, "dy"), *_norm_rows(dx, x, "dx"),
+                                       _vector(dw, c.width, x, fp32, "dw"), _vector(db, c.width, x, fp32, "db"), p,
+                                       size, _current_stream(x.device)), "nlb_layer_norm_backward")
     return dx, dw, db

@@ -25,6 +25,7 @@
 
 #include <algorithm>
 
+#include "call_device.h"
 #include "nlb_internal.h"
 
 namespace {
@@ -601,14 +602,6 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
 // Whether rows take the short form of tile_load.
 inline bool exact_rows(const Attend &a, const Strided &r) {
     return a.dim * a.dtype_bytes % 16 == 0 && r.row <= 1 << 25;
-}
-
-inline int device_of(const nlb_att_call *c, int &dev) {
-    int n = 0;
-    dev = c->device;
-    if (hipGetDeviceCount(&n) != hipSuccess || n < 1) return NLB_EDEVICE;
-    if (dev < 0 && hipGetDevice(&dev) != hipSuccess) return NLB_EDEVICE;
-    return dev < n ? NLB_OK : NLB_EINVAL;
 }
 
 // Kernels that take more LDS than 64 KiB need to be allowed it.

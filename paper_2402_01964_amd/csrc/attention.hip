@@ -631,11 +631,9 @@ extern "C" int nlb_attention(const nlb_att_call *c, const nlb_att_rows *o, float
     const Forward f = plan_forward(a);
     if (f.slots > f.most) return NLB_EINVAL;
     if (work_bytes < f.bytes || (f.bytes && !work)) return NLB_ESCRATCH;
-    int dev;
-    if ((rc = device_of(c, dev)) != NLB_OK) return rc;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
     if (a.q_rows == 0) return NLB_OK;
-    DeviceGuard guard(dev);
-    if (!guard.ok()) return NLB_EDEVICE;
     a.lse = lse;
     a.part = (float *)work;
     a.slots = (uint32_t)f.slots;

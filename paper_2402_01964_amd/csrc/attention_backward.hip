@@ -831,10 +831,8 @@ extern "C" int nlb_attention_backward(const nlb_att_call *c, const nlb_att_rows 
     const Backward p = plan_backward(a);
     if (p.q_slots > p.q_most || p.k_slots > p.k_most) return NLB_EINVAL;
     if (work_bytes < p.bytes || (p.bytes && !work)) return NLB_ESCRATCH;
-    int dev;
-    if ((rc = device_of(c, dev)) != NLB_OK) return rc;
-    DeviceGuard guard(dev);
-    if (!guard.ok()) return NLB_EDEVICE;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
     a.lse = const_cast<float *>(lse);
     a.delta = (float *)work;
     a.split = p.split;

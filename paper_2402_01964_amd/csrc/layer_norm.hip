@@ -4,6 +4,7 @@
 //   g = dy w,  dx = rstd (g - mean(g) - xh mean(g xh))
 //   dw = sum over rows of dy xh,  db = sum over rows of dy
 // Both passes are bound by reading their rows and writing one of the same size.
+#include "call_device.h"
 #include "nlb_internal.h"
 
 namespace {
@@ -340,14 +341,6 @@ int fill(const nlb_norm_call *c, Norm &a) {
     return NLB_OK;
 }
 
-int device_of(int32_t device, int &dev) {
-    int n = 0;
-    dev = device;
-    if (hipGetDeviceCount(&n) != hipSuccess || n < 1) return NLB_EDEVICE;
-    if (dev < 0 && hipGetDevice(&dev) != hipSuccess) return NLB_EDEVICE;
-    return dev < n ? NLB_OK : NLB_EINVAL;
-}
-
 bool bad_rows(const void *p, int64_t stride, uint32_t rows, int32_t dtype) {
     return (rows && !p) || (uintptr_t)p % (dtype == NLB_DTYPE_BF16 ? 2 : 4) || stride < 0 || stride > INT32_MAX;
 }
@@ -383,14 +376,13 @@ template <typename T> int launch_backward(const Norm &a, float *dw, float *db, h
 extern "C" int nlb_layer_norm(const nlb_norm_call *c, const float *b, float eps, void *y, int64_t y_stride,
                               void *stream) {
     Norm a;
-    int rc = fill(c, a), dev;
+    int rc = fill(c, a);
     if (rc != NLB_OK) return rc;
     if (bad_rows(y, y_stride, c->rows, c->dtype) || (uintptr_t)b % 4 || !(eps >= 0.0f) || std::isinf(eps))
         return NLB_EINVAL;
-    if ((rc = device_of(c->device, dev)) != NLB_OK) return rc;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
     if (c->rows == 0) return NLB_OK;
-    DeviceGuard guard(dev);
-    if (!guard.ok()) return NLB_EDEVICE;
     a.b = b;
     a.eps = eps;
     a.out = (uint8_t *)y;
@@ -413,15 +405,14 @@ extern "C" int nlb_layer_norm_backward(const nlb_norm_call *c, const void *dy, i
                                        int64_t dx_stride, float *dw, float *db, void *work, size_t work_bytes,
                                        void *stream) {
     Norm a;
-    int rc = fill(c, a), dev;
+    int rc = fill(c, a);
     if (rc != NLB_OK) return rc;
     if (bad_rows(dy, dy_stride, c->rows, c->dtype) || bad_rows(dx, dx_stride, c->rows, c->dtype)) return NLB_EINVAL;
     if (c->rows && (!c->mean || !c->rstd)) return NLB_EINVAL;
     if (((uintptr_t)dw | (uintptr_t)db) % 4 || (uintptr_t)work % 16) return NLB_EINVAL;
     if ((dw || db) && (!work || work_bytes < work_of(c))) return NLB_ESCRATCH;
-    if ((rc = device_of(c->device, dev)) != NLB_OK) return rc;
-    DeviceGuard guard(dev);
-    if (!guard.ok()) return NLB_EDEVICE;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
     const int64_t e = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
     a.dy = (const uint8_t *)dy;
     a.dy_row = dy_stride * e;

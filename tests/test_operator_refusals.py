@@ -14,7 +14,9 @@ def _call(**kw):
     c.device, c.dtype, c.heads, c.kv_heads, c.dim, c.scale = -1, nlb.DTYPE_BF16, 4, 2, 64, 0.125
     c.batch, c.q_rows, c.k_rows = 2, 10, 10
     for k in ("q", "k", "v"):
-        setattr(c, k, nlb._AttRows(P, 256, 64))
+        setattr(c, k, P)
+        setattr(c, k + "_row", 256)
+        setattr(c, k + "_head", 64)
     for k, v in kw.items():
         setattr(c, k, v)
     return c
@@ -28,9 +30,8 @@ BAD_CALLS = [
                                                                                                      bounds=P),
     dict(buckets=4), dict(bias=P), dict(buckets=4, bias=P), dict(buckets=4, bias=P, bounds=P + 2),
     dict(buckets=4, bias=P + 1, bounds=P), dict(q_pos=P), dict(q_start=P + 1), dict(k_start=P + 2), dict(k_pos=P + 1),
-    dict(buckets=4, bias=P, bounds=P, k_pos=P), dict(q=nlb._AttRows(None, 256, 64)), dict(k=nlb._AttRows(None, 256, 64)),
-    dict(v=nlb._AttRows(P + 1, 256, 64)), dict(q=nlb._AttRows(P, -1, 64)), dict(k=nlb._AttRows(P, 2**31, 64)),
-    dict(v=nlb._AttRows(P, 256, -64)),
+    dict(buckets=4, bias=P, bounds=P, k_pos=P), dict(q=None), dict(k=None),
+    dict(v=P + 1), dict(q_row=-1), dict(k_row=2**31), dict(v_head=-64),
 ]
 
 
