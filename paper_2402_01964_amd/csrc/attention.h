@@ -264,23 +264,41 @@ struct Buckets {
     uint8_t *cells;                      // [kCells]
     uint32_t last, more;                 // the last bucket; comparisons after a cell's first
 };
-__device__ __forceinline__ void fill_cells(Buckets &t, const Attend &a, uint32_t *most) {
-    // most: one LDS word, zeroed by the caller; bounds are there
-    for (int32_t c = threadIdx.x; c < kCells; c += kThreads) {
-        uint32_t n = 0, in = 0;
-        for (uint32_t i = 0; i + 1 < a.buckets; i++) {
-            const int32_t x = cell_of(t.bounds[i]);
-            n += x < c;
-            in += x == c;
-        }
-        t.cells[c] = (uint8_t)n;
-        if (in) atomicMax(most, in);
+// Fills the table; bounds are there, and `ends` has room for 64 words.  Ends
+// with a barrier.
+__device__ __forceinline__ void fill_cells(Buckets &t, int32_t *ends) {
+    if (threadIdx.x < kMaxBuckets)
+        ends[threadIdx.x] = threadIdx.x < t.last ? cell_of(t.bounds[threadIdx.x]) : INT32_MAX;
+    __syncthreads();
+    // bounds below cell c, and in it
+    static_assert(kCells == kThreads, "a thread a cell");
+    const int32_t c = threadIdx.x;
+    uint32_t below = 0, upto = 0;
+#pragma unroll
+    for (uint32_t step = 32; step; step >>= 1) {
+        if (ends[below + step - 1] < c) below += step;
+        if (ends[upto + step - 1] <= c) upto += step;
     }
+    t.cells[c] = (uint8_t)below;
+    uint32_t in = upto - below;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) in = max(in, (uint32_t)__shfl_xor((int)in, w));
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) ends[threadIdx.x / 64] = in;
+    __syncthreads();
+    t.more = __builtin_amdgcn_readfirstlane(max(max(ends[0], ends[1]), max(ends[2], ends[3])));
 }
-__device__ __forceinline__ uint32_t bucket_in(const Buckets &t, int32_t gap) {
-    uint32_t n = t.cells[cell_of(gap)];
-    for (uint32_t i = 0; i < t.more; i++) n += n < t.last && t.bounds[n] <= gap ? 1u : 0u;
-    return n;
+// The buckets of 16 gaps at once, so that each step's LDS reads overlap.
+__device__ __forceinline__ void buckets_in(const Buckets &t, const int32_t (&gap)[16], uint32_t (&n)[16]) {
+#pragma unroll
+    for (int r = 0; r < 16; r++) n[r] = t.cells[cell_of(gap[r])];
+    for (uint32_t i = 0; i < t.more; i++) {
+        int32_t next[16];
+#pragma unroll
+        for (int r = 0; r < 16; r++) next[r] = t.bounds[min(n[r], (uint32_t)kMaxBuckets - 1)];
+#pragma unroll
+        for (int r = 0; r < 16; r++) n[r] += n[r] < t.last && next[r] <= gap[r] ? 1u : 0u;
+    }
 }
 
 // ---------------------------------------------------------------- tiles
@@ -305,34 +323,53 @@ template <typename T, int DP, Use USE = kByRows> struct Tile {
 };
 
 // This thread's chunks of the tile whose first row is `base`, which has n > 0
-// rows.  EXACT: a row is a whole number of chunks and a tile's rows lie within
-// 2^31 bytes; rows from n on repeat the last one (their scores are masked, or
-// their probabilities zero), so that the loads of a tile are nothing but loads
-// (with a test for each chunk, vector operations for them took as long as the
-// exponentials).  Else rows from n on are zeros.
+// rows; rows from n on repeat the last one (their scores are masked, or their
+// probabilities zero), so that the loads of a tile are nothing but loads (with
+// a test for each chunk, vector operations for them took as long as the
+// exponentials).  EXACT: a row is a whole number of chunks and a tile's rows
+// lie within 2^31 bytes.  Else a row's last chunk is loaded where the row
+// ends, and moved into place by tile_settle when it is staged.
 template <typename T, int DP, bool EXACT>
 __device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const uint8_t *base, int64_t stride,
                                           int32_t n, uint32_t dim) {
     using G = Tile<T, DP>;
-    const uint32_t c0 = threadIdx.x % G::chunks * Chunk<T>::n, r0 = threadIdx.x / G::chunks;
-    if constexpr (EXACT) {
-        if (c0 < dim) {
+    constexpr uint32_t N = Chunk<T>::n;
+    const uint32_t c0 = threadIdx.x % G::chunks * N, r0 = threadIdx.x / G::chunks;
+    if (c0 >= dim) {
 #pragma unroll
-            for (int i = 0; i < G::per_thread; i++) {
-                const uint32_t r = min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1);
-                reg[i] = *(const u32x4_any *)(base + (r * (uint32_t)stride + c0 * (uint32_t)sizeof(T)));
-            }
-        } else {
+        for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
+    } else if (EXACT || dim >= N) {
+        const uint32_t at = (EXACT ? c0 : min(c0, dim - N)) * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < G::per_thread; i++) {
+            const uint32_t r = min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1);
+            if constexpr (EXACT) reg[i] = *(const u32x4_any *)(base + (r * (uint32_t)stride + at));
+            else reg[i] = *(const u32x4_any *)(base + (r * stride + at));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < G::per_thread; i++) {
-            const int32_t r = r0 + i * (kThreads / G::chunks);
-            reg[i] = u32x4{0, 0, 0, 0};
-            if (r < n) reg[i] = load_chunk<T>(base + r * stride, c0, dim);
-        }
+        for (int i = 0; i < G::per_thread; i++)
+            reg[i] = load_chunk<T>(base + min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1) * stride, 0, dim);
+    }
+}
+
+// A row's last chunk, whose `dim % N` values were loaded as the last of N.
+template <typename T, int DP>
+__device__ __forceinline__ void tile_settle(typename Tile<T, DP>::Regs &reg, uint32_t dim) {
+    using G = Tile<T, DP>;
+    constexpr uint32_t N = Chunk<T>::n;
+    const uint32_t c0 = threadIdx.x % G::chunks * N, gone = (N - dim % N) % N * sizeof(T);   // bytes to drop
+    if (dim < N || gone == 0) return;
+    const bool last = c0 < dim && c0 + N > dim;
+#pragma unroll
+    for (int i = 0; i < G::per_thread; i++) {
+        u32x4 x = reg[i];
+        if (gone & 8) x = u32x4{x[2], x[3], 0, 0};
+        if (gone & 4) x = u32x4{x[1], x[2], x[3], 0};
+        if (gone & 2)
+            x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16),
+                      __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+        if (last) reg[i] = x;
     }
 }
 

@@ -31,7 +31,7 @@ constexpr int kGaps = 192;
 
 template <typename T, int DP> constexpr uint32_t tiles_lds() {
     return 2 * (Tile<T, DP, kByRows>::bytes + Tile<T, DP, kByColumns>::bytes) + 2 * kGaps * 4 + kMaxBuckets * 8 +
-           kCells + 16;
+           kCells + kMaxBuckets * 4;
 }
 
 template <typename T, int DP, int POS, bool EXACT>
@@ -64,13 +64,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
         if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
     if (POS != 0 && a.buckets) {
         stage_bias<T>(a, head, buckets.bounds, bias);
-        uint32_t *most = (uint32_t *)(buckets.cells + kCells);
-        if (threadIdx.x == 0) *most = 0;
+        int32_t *ends = (int32_t *)(buckets.cells + kCells);
         __syncthreads();
         if constexpr (POS == 2) {
-            fill_cells(buckets, a, most);
-            __syncthreads();
-            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+            fill_cells(buckets, ends);
         }
     }
 
@@ -95,6 +92,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     // writes the fetched tile and what the bias needs of it
     const auto stage = [&](int32_t k0, int buf) {
         uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
+        if constexpr (!EXACT) {
+            tile_settle<T, DP>(kreg, a.dim);
+            tile_settle<T, DP>(vreg, a.dim);
+        }
         if constexpr (POS == 2) {
             tile_close<T, DP>(kreg, preg);
             tile_close<T, DP>(vreg, preg);
@@ -150,10 +151,13 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
                     for (int r = 0; r < 16; r++) s[blk][r] += e[-block_row(r)];
                 }
                 if (POS == 2 && a.buckets) {
+                    int32_t gap[16];
+                    uint32_t bk[16];
 #pragma unroll
-                    for (int r = 0; r < 16; r++)
-                        s[blk][r] += bias[bucket_in(
-                            buckets, gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]))];
+                    for (int r = 0; r < 16; r++) gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]);
+                    buckets_in(buckets, gap, bk);
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[blk][r] += bias[bk[r]];
                 }
                 if (POS == 2 && shut) {
 #pragma unroll

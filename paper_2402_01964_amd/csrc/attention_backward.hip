@@ -31,7 +31,7 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 // order into part[slot][head][bucket].
 template <typename T, int DP> constexpr uint32_t rows_lds(uint32_t buckets) {
     return 2 * (Tile<T, DP, kBothWays>::bytes + Tile<T, DP, kByRows>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
-           kCells + 16 + buckets * kThreads * 4;
+           kCells + kMaxBuckets * 4 + buckets * kThreads * 4;
 }
 
 __device__ __forceinline__ void add_four(float *column, const uint32_t (&b)[4], const float (&x)[4]) {
@@ -62,8 +62,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     uint32_t *code = (uint32_t *)(extra + 2 * kGaps);
     float *bias = (float *)(code + 2 * kGaps);
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
-    uint32_t *most = (uint32_t *)(buckets.cells + kCells);
-    float *hist = (float *)(most + 4);                        // [buckets][threads]
+    int32_t *cell_ends = (int32_t *)(buckets.cells + kCells);
+    float *hist = (float *)(cell_ends + kMaxBuckets);         // [buckets][threads]
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
     const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
@@ -103,14 +103,11 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     }
     if (POS != 0 && a.buckets) {
         stage_bias<T>(a, head, buckets.bounds, bias);
-        if (threadIdx.x == 0) *most = 0;
         if (want)
             for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
         __syncthreads();
         if constexpr (POS == 2) {
-            fill_cells(buckets, a, most);
-            __syncthreads();
-            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+            fill_cells(buckets, cell_ends);
         }
     }
 
@@ -132,6 +129,10 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
     const auto stage = [&](int32_t k0, int buf) {
         uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
+        if constexpr (!EXACT) {
+            tile_settle<T, DP>(kreg, a.dim);
+            tile_settle<T, DP>(vreg, a.dim);
+        }
         if constexpr (POS == 2) {
             tile_close<T, DP>(kreg, preg);
             tile_close<T, DP>(vreg, preg);
@@ -194,12 +195,16 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
                         }
                     }
                     if (POS == 2 && a.buckets) {
+                        int32_t gap[16];
+                        uint32_t n[16];
+#pragma unroll
+                        for (int r = 0; r < 16; r++)
+                            gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]);
+                        buckets_in(buckets, gap, n);
 #pragma unroll
                         for (int r = 0; r < 16; r++) {
-                            const uint32_t n = bucket_in(
-                                buckets, gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]));
-                            s[r] += bias[n];
-                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = n;
+                            s[r] += bias[n[r]];
+                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = n[r];
                         }
                     }
                     if (POS == 2 && shut) {
@@ -286,7 +291,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 // sequences, 16 heads in 4 groups: 1030 us in one launch).
 template <typename T, int DP> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
     return 4 * Tile<T, DP, kBothWays>::bytes + 2 * (kGaps + 2 * Tile<T, DP>::rows) * 4 +
-           (bias ? kMaxBuckets * 4 * (1 + group) + kCells + 16 : 0);
+           (bias ? kMaxBuckets * 4 * (1 + group) + kCells + kMaxBuckets * 4 : 0);
 }
 
 template <typename T, int DP, int POS, int WHAT, bool EXACT>
@@ -320,13 +325,10 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     if (POS != 0 && a.buckets) {
         for (uint32_t g = 0; g < a.group; g++)
             stage_bias<T>(a, kvh * a.group + g, g ? nullptr : buckets.bounds, bias + g * kMaxBuckets);
-        uint32_t *most = (uint32_t *)(buckets.cells + kCells);
-        if (threadIdx.x == 0) *most = 0;
+        int32_t *cell_ends = (int32_t *)(buckets.cells + kCells);
         __syncthreads();
         if constexpr (POS == 2) {
-            fill_cells(buckets, a, most);
-            __syncthreads();
-            buckets.more = __builtin_amdgcn_readfirstlane(*most);
+            fill_cells(buckets, cell_ends);
         }
     }
 
@@ -358,6 +360,10 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     const auto stage = [&](int32_t g, int32_t i0, int buf) {
         uint8_t *qt = lds + buf * 2 * G::bytes;
         float *e = extra + buf * kExtra;
+        if constexpr (!EXACT) {
+            tile_settle<T, DP>(qreg, a.dim);
+            tile_settle<T, DP>(oreg, a.dim);
+        }
         tile_store<T, DP, kBothWays>(qt, qreg);
         tile_store<T, DP, kBothWays>(qt + G::bytes, oreg);
         if (threadIdx.x < G::rows) {
@@ -423,11 +429,14 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
                     }
                 }
                 if (POS == 2 && a.buckets) {
+                    int32_t gap[16];
+                    uint32_t n[16];
 #pragma unroll
                     for (int r = 0; r < 16; r++)
-                        s[r] += bias[g * kMaxBuckets +
-                                     bucket_in(buckets, gap_of(((const int32_t *)e)[2 * G::rows + blk * 32 +
-                                                                                   block_row(r)], kpos))];
+                        gap[r] = gap_of(((const int32_t *)e)[2 * G::rows + blk * 32 + block_row(r)], kpos);
+                    buckets_in(buckets, gap, n);
+#pragma unroll
+                    for (int r = 0; r < 16; r++) s[r] += bias[g * kMaxBuckets + n[r]];
                 }
                 if (ragged) {
 #pragma unroll
