@@ -120,25 +120,37 @@ template <typename T> struct Chunk;      // 16 bytes of a row
 template <> struct Chunk<__bf16> { static constexpr int n = 8; };
 template <> struct Chunk<float> { static constexpr int n = 4; };
 
-// 16 bytes from value c0 of a row of dim values, zeros past its end.
+// Drops the first `gone` bytes (the same for all lanes) of a chunk.
+template <typename T> __device__ __forceinline__ u32x4 drop_bytes(u32x4 x, uint32_t gone) {
+    if (gone & 8) x = u32x4{x[2], x[3], 0, 0};
+    if (gone & 4) x = u32x4{x[1], x[2], x[3], 0};
+    if (sizeof(T) == 2 && (gone & 2))
+        x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16),
+                  __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+    return x;
+}
+
+// 16 bytes from value c0 of a row of dim values, zeros past its end: a row's
+// last chunk is loaded where the row ends, and moved.
 template <typename T>
 __device__ __forceinline__ u32x4 load_chunk(const uint8_t *row, uint32_t c0, uint32_t dim) {
     constexpr uint32_t n = Chunk<T>::n;
-    const uint8_t *p = row + c0 * sizeof(T);
     u32x4 x = {0, 0, 0, 0};
-    if (c0 + n <= dim) {
-        x = *(const u32x4_any *)p;
-    } else if (c0 < dim) {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (uint32_t i = 0; i < 3; i++)
-                if (c0 + i < dim) x[i] = ((const uint32_t *)p)[i];
-        } else {
-#pragma unroll
-            for (uint32_t i = 0; i < 7; i++)
-                if (c0 + i < dim) x[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
+    if (c0 >= dim) return x;
+    if (dim >= n) {
+        x = *(const u32x4_any *)(row + min(c0, dim - n) * sizeof(T));
+        if (dim % n) {
+            const u32x4 y = drop_bytes<T>(x, (n - dim % n) * sizeof(T));
+            if (c0 + n > dim) x = y;
         }
+        return x;
     }
+#pragma unroll
+    for (uint32_t i = 0; i < n - 1; i++)
+        if (i < dim) {
+            if constexpr (sizeof(T) == 4) x[i] = ((const uint32_t *)row)[i];
+            else x[i / 2] |= (uint32_t)((const uint16_t *)row)[i] << (16 * (i % 2));
+        }
     return x;
 }
 
@@ -309,18 +321,55 @@ __device__ __forceinline__ void buckets_in(const Buckets &t, const int32_t (&gap
 // or both ways, each at half speed.
 enum Use { kByRows, kByColumns, kBothWays };
 
-template <typename T, int DP, Use USE = kByRows> struct Tile {
-    static constexpr int rows = sizeof(T) == 2 ? 64 : 32;
+// NARROW: see Span.
+template <typename T, int DP, Use USE, bool NARROW> struct Tile {
+    typedef T Value;
+    static constexpr bool narrow = NARROW;
+    static constexpr int rows = NARROW ? 128 : sizeof(T) == 2 ? 64 : 32;
     static constexpr int chunks = DP * sizeof(T) / 16;              // per row
     static constexpr int pad = USE == kByRows ? 16 : USE == kBothWays || sizeof(T) == 4 ? 32 : DP == 32 ? 0 : 64;
     static constexpr int stride = DP * sizeof(T) + pad;             // bytes
     static constexpr int bytes = rows * stride;
-    static constexpr int per_thread = rows * chunks / kThreads;
-    static constexpr int blocks = rows / 32;
+    static constexpr int step = kThreads / chunks;                  // rows of one load of the workgroup
+    static constexpr int per_thread = rows / step;
     static_assert(rows * chunks % kThreads == 0, "");
     typedef u32x4 Regs[per_thread];
     typedef uint32_t Positions[per_thread];
 };
+
+// What a workgroup owns and what its wavefronts take of a tile.  Usually it
+// owns 128 rows, 32 a wavefront, every wavefront takes the whole tile, and the
+// next tile is staged in a second buffer.  A NARROW workgroup owns 32 rows;
+// tiles have 128 rows, a wavefront takes every fourth 32 of them, and their
+// results are joined at the end: for sequences of few rows, and for calls of
+// few workgroups, whose time is that of one workgroup's way along its tiles.
+template <bool NARROW, int ROWS> struct Span {
+    static constexpr int owned = NARROW ? 32 : kOwned;
+    static constexpr int buffers = NARROW ? 1 : 2;
+    static constexpr int rows = NARROW ? 32 : ROWS;                 // of a tile, a wavefront's
+    static constexpr int blocks = rows / 32;
+    uint32_t own, take;                  // a wavefront's first owned row, and first row of a tile
+    __device__ __forceinline__ Span() {
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        own = NARROW ? 0 : wave * 32;
+        take = NARROW ? wave * 32 : 0;
+    }
+};
+
+// The sum of the wavefronts' results, in the first one; lds: 3 DP 128 bytes
+// that no wavefront reads any more.
+template <int DP> __device__ __forceinline__ void join_waves(f32x16 (&acc)[DP / 32], float *lds) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    if (wave)
+#pragma unroll
+        for (int i = 0; i < DP / 2; i++) lds[((wave - 1) * (DP / 2) + i) * 64 + lane] = acc[i / 16][i % 16];
+    __syncthreads();
+    if (wave == 0)
+#pragma unroll
+        for (int w = 0; w < 3; w++)
+#pragma unroll
+            for (int i = 0; i < DP / 2; i++) acc[i / 16][i % 16] += lds[(w * (DP / 2) + i) * 64 + lane];
+}
 
 // This thread's chunks of the tile whose first row is `base`, which has n > 0
 // rows; rows from n on repeat the last one (their scores are masked, or their
@@ -329,10 +378,10 @@ template <typename T, int DP, Use USE = kByRows> struct Tile {
 // exponentials).  EXACT: a row is a whole number of chunks and a tile's rows
 // lie within 2^31 bytes.  Else a row's last chunk is loaded where the row
 // ends, and moved into place by tile_settle when it is staged.
-template <typename T, int DP, bool EXACT>
-__device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const uint8_t *base, int64_t stride,
-                                          int32_t n, uint32_t dim) {
-    using G = Tile<T, DP>;
+template <typename G, bool EXACT>
+__device__ __forceinline__ void tile_load(typename G::Regs &reg, const uint8_t *base, int64_t stride, int32_t n,
+                                          uint32_t dim) {
+    using T = typename G::Value;
     constexpr uint32_t N = Chunk<T>::n;
     const uint32_t c0 = threadIdx.x % G::chunks * N, r0 = threadIdx.x / G::chunks;
     if (c0 >= dim) {
@@ -340,76 +389,75 @@ __device__ __forceinline__ void tile_load(typename Tile<T, DP>::Regs &reg, const
         for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
     } else if (EXACT || dim >= N) {
         const uint32_t at = (EXACT ? c0 : min(c0, dim - N)) * (uint32_t)sizeof(T);
-#pragma unroll
-        for (int i = 0; i < G::per_thread; i++) {
-            const uint32_t r = min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1);
+        const auto load = [&](int i) {
+            const uint32_t r = min(r0 + i * G::step, (uint32_t)n - 1);
             if constexpr (EXACT) reg[i] = *(const u32x4_any *)(base + (r * (uint32_t)stride + at));
             else reg[i] = *(const u32x4_any *)(base + (r * stride + at));
+        };
+        if (!G::narrow || n >= G::rows) {
+#pragma unroll
+            for (int i = 0; i < G::per_thread; i++) load(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < G::per_thread; i++)
+                if (i * G::step < n) load(i);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < G::per_thread; i++)
-            reg[i] = load_chunk<T>(base + min(r0 + i * (kThreads / G::chunks), (uint32_t)n - 1) * stride, 0, dim);
+            reg[i] = load_chunk<T>(base + min(r0 + i * G::step, (uint32_t)n - 1) * stride, 0, dim);
     }
 }
 
 // A row's last chunk, whose `dim % N` values were loaded as the last of N.
-template <typename T, int DP>
-__device__ __forceinline__ void tile_settle(typename Tile<T, DP>::Regs &reg, uint32_t dim) {
-    using G = Tile<T, DP>;
+template <typename G> __device__ __forceinline__ void tile_settle(typename G::Regs &reg, uint32_t dim) {
+    using T = typename G::Value;
     constexpr uint32_t N = Chunk<T>::n;
     const uint32_t c0 = threadIdx.x % G::chunks * N, gone = (N - dim % N) % N * sizeof(T);   // bytes to drop
     if (dim < N || gone == 0) return;
     const bool last = c0 < dim && c0 + N > dim;
 #pragma unroll
     for (int i = 0; i < G::per_thread; i++) {
-        u32x4 x = reg[i];
-        if (gone & 8) x = u32x4{x[2], x[3], 0, 0};
-        if (gone & 4) x = u32x4{x[1], x[2], x[3], 0};
-        if (gone & 2)
-            x = u32x4{__builtin_amdgcn_alignbit(x[1], x[0], 16), __builtin_amdgcn_alignbit(x[2], x[1], 16),
-                      __builtin_amdgcn_alignbit(x[3], x[2], 16), x[3] >> 16};
+        const u32x4 x = drop_bytes<T>(reg[i], gone);
         if (last) reg[i] = x;
     }
 }
 
-template <typename T, int DP, Use USE>
-__device__ __forceinline__ void tile_store(uint8_t *lds, const typename Tile<T, DP>::Regs &reg) {
-    using G = Tile<T, DP, USE>;
+// A narrow tile of n rows is written as far as wavefronts read it.
+template <typename G> __device__ __forceinline__ void tile_store(uint8_t *lds, const typename G::Regs &reg, int32_t n) {
     const uint32_t c = threadIdx.x % G::chunks, r0 = threadIdx.x / G::chunks;
 #pragma unroll
-    for (int i = 0; i < G::per_thread; i++)
-        *(u32x4 *)(lds + (r0 + i * (kThreads / G::chunks)) * G::stride + c * 16) = reg[i];
+    for (int i = 0; i < G::per_thread; i++) {
+        if (G::narrow && i * G::step >= (n + 31) / 32 * 32) break;
+        *(u32x4 *)(lds + (r0 + i * G::step) * G::stride + c * 16) = reg[i];
+    }
 }
 
 // The positions of the rows of this thread's chunks; from row n on none.
-template <typename T, int DP>
-__device__ __forceinline__ void tile_positions(typename Tile<T, DP>::Positions &pos, const uint32_t *p, int32_t n) {
-    using G = Tile<T, DP>;
+template <typename G>
+__device__ __forceinline__ void tile_positions(typename G::Positions &pos, const uint32_t *p, int32_t n) {
     const uint32_t r0 = threadIdx.x / G::chunks;
 #pragma unroll
     for (int i = 0; i < G::per_thread; i++) {
-        const int32_t r = r0 + i * (kThreads / G::chunks);
+        const int32_t r = r0 + i * G::step;
         pos[i] = r < n ? p[r] : kNoKey;
     }
 }
 
 // Rows of closed keys may hold anything: they are multiplied as zeros.
-template <typename T, int DP>
-__device__ __forceinline__ void tile_close(typename Tile<T, DP>::Regs &reg,
-                                           const typename Tile<T, DP>::Positions &pos) {
+template <typename G>
+__device__ __forceinline__ void tile_close(typename G::Regs &reg, const typename G::Positions &pos) {
 #pragma unroll
-    for (int i = 0; i < Tile<T, DP>::per_thread; i++)
+    for (int i = 0; i < G::per_thread; i++)
         if (pos[i] == kNoKey) reg[i] = u32x4{0, 0, 0, 0};
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ void tile_store_positions(int32_t *lds, const typename Tile<T, DP>::Positions &pos) {
-    using G = Tile<T, DP>;
+template <typename G>
+__device__ __forceinline__ void tile_store_positions(int32_t *lds, const typename G::Positions &pos) {
     if (threadIdx.x % G::chunks == 0)
 #pragma unroll
         for (int i = 0; i < G::per_thread; i++)
-            lds[threadIdx.x / G::chunks + i * (kThreads / G::chunks)] = flip(pos[i]);
+            lds[threadIdx.x / G::chunks + i * G::step] = flip(pos[i]);
 }
 
 // Owned rows as the right operand of products that contract over the row's
@@ -440,12 +488,11 @@ __device__ __forceinline__ void load_owned(Owned<T, DP> &f, const uint8_t *row, 
     }
 }
 
-// acc[row][c] += sum over values of tile[32 blk + row] . owned[c]
-template <typename T, int DP, Use USE>
+// acc[row][c] += sum over values of tile[blk + row] . owned[c]
+template <typename G, typename T, int DP>
 __device__ __forceinline__ void product_rows(f32x16 &acc, const uint8_t *tile, int blk, const Owned<T, DP> &own) {
-    using G = Tile<T, DP, USE>;
     const uint32_t lane = threadIdx.x & 63u;
-    const uint8_t *p = tile + (blk * 32 + (lane & 31u)) * G::stride + (lane >> 5) * 16;
+    const uint8_t *p = tile + (blk + (lane & 31u)) * G::stride + (lane >> 5) * 16;
 #pragma unroll
     for (int s = 0; s < Owned<T, DP>::steps; s++) {
         const u32x4 x = *(const u32x4 *)(p + s * 32);
@@ -485,19 +532,17 @@ __device__ __forceinline__ i16x4 read_columns(const uint8_t *p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
 }
 
-// acc[d block][value][c] += sum over the block's rows of tile[32 blk + row][value] scores[row][c]
-template <typename T, int DP, Use USE>
-__device__ __forceinline__ void product_columns(f32x16 (&acc)[DP / 32], const uint8_t *tile, int blk,
-                                                const Scores<T> &s) {
-    using G = Tile<T, DP, USE>;
+// acc[d block][value][c] += sum over the block's rows of tile[blk + row][value] scores[row][c]
+template <typename G, typename T, int D>
+__device__ __forceinline__ void product_columns(f32x16 (&acc)[D], const uint8_t *tile, int blk, const Scores<T> &s) {
     const uint32_t lane = threadIdx.x & 63u, h = lane >> 5;
     if constexpr (sizeof(T) == 2) {
-        const uint8_t *p = tile + (blk * 32 + 4 * h + ((lane & 15u) >> 2)) * G::stride +
+        const uint8_t *p = tile + (blk + 4 * h + ((lane & 15u) >> 2)) * G::stride +
                            (16 * ((lane >> 4) & 1u) + 4 * (lane & 3u)) * 2;
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
-            for (int d = 0; d < DP / 32; d++) {
+            for (int d = 0; d < D; d++) {
                 const i16x4 lo = read_columns(p + (16 * u) * G::stride + d * 64);
                 const i16x4 hi = read_columns(p + (16 * u + 8) * G::stride + d * 64);
                 const auto x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -505,11 +550,11 @@ __device__ __forceinline__ void product_columns(f32x16 (&acc)[DP / 32], const ui
                                                                  0);
             }
     } else {
-        const uint8_t *p = tile + (blk * 32 + 4 * h) * G::stride + (lane & 31u) * 4;
+        const uint8_t *p = tile + (blk + 4 * h) * G::stride + (lane & 31u) * 4;
 #pragma unroll
         for (int r = 0; r < 16; r++)
 #pragma unroll
-            for (int d = 0; d < DP / 32; d++)
+            for (int d = 0; d < D; d++)
                 acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
                     *(const float *)(p + (8 * (r / 4) + r % 4) * G::stride + d * 128), s.x[r], acc[d], 0, 0, 0);
     }
@@ -651,9 +696,21 @@ inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Which kernels a call runs.
 enum Form { kTiles, kOne, kLists };
+#ifndef NARROW_BLOCKS
+#define NARROW_BLOCKS 128
+#endif
+constexpr uint64_t kNarrowBlocks = NARROW_BLOCKS;
+
+// Calls of tiles: narrow workgroups where sequences have 64 owned rows or fewer
+// on average, or where the others are so few that half of the card idles.
+inline bool narrow_tiles(const Attend &a, uint64_t rows, uint32_t heads) {
+    if ((a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128) * a.dtype_bytes > 256) return false;   // (LDS)
+    return rows / 64 <= a.batch || (rows / kOwned + 1) * heads <= kNarrowBlocks;
+}
 
 struct Forward {
     Form form;
+    bool narrow;
     uint32_t chunk;                      // kOne: keys of a wavefront
     uint64_t slots, most;
     size_t bytes;
@@ -669,7 +726,8 @@ inline bool short_lists(const Attend &a) { return a.k_rows / kListKeys <= a.batc
 inline Forward plan_forward(const Attend &a) {
     Forward f = {};
     if (a.q_start || a.q_len != 1) {
-        f.slots = (uint64_t)a.q_rows / kOwned + a.batch;
+        f.narrow = narrow_tiles(a, a.q_rows, a.heads);
+        f.slots = (uint64_t)a.q_rows / (f.narrow ? 32 : kOwned) + a.batch;
         f.most = INT32_MAX / a.heads;
         return f;
     }
@@ -687,7 +745,7 @@ inline Forward plan_forward(const Attend &a) {
 }
 
 struct Backward {
-    bool lists;
+    bool lists, narrow_rows, narrow_keys;
     uint32_t blocks, keep;               // kLists: workgroups; keys whose probabilities stay in LDS
     uint32_t shares;                     // shares of the first sum of bias gradients
     uint64_t q_slots, q_most, k_slots, k_most;
@@ -721,8 +779,10 @@ inline Backward plan_backward(const Attend &a) {
         p.keep = std::min<uint32_t>(kListKeys, std::min(65536u, 155648u - rest) / (4 * rows * gb * 8));
         p.parts = p.blocks;
     } else {
-        p.q_slots = (uint64_t)a.q_rows / kOwned + a.batch;
-        p.k_slots = (uint64_t)a.k_rows / kOwned + a.batch;
+        p.narrow_rows = narrow_tiles(a, a.q_rows, a.heads);
+        p.narrow_keys = narrow_tiles(a, a.k_rows, a.heads);   // (a group's heads can be spread, see split)
+        p.q_slots = (uint64_t)a.q_rows / (p.narrow_rows ? 32 : kOwned) + a.batch;
+        p.k_slots = (uint64_t)a.k_rows / (p.narrow_keys ? 32 : kOwned) + a.batch;
         p.q_most = INT32_MAX / a.heads;
         p.k_most = INT32_MAX / a.kv_heads;
         p.parts = a.q_rows ? p.q_slots : 0;
@@ -731,7 +791,7 @@ inline Backward plan_backward(const Attend &a) {
         // few for two turns of them (which causal sequences of one length need
         // to even out), a group's heads are spread over workgroups, whose
         // shares of dk and dv are summed afterwards.
-        const uint64_t tiles = ((uint64_t)a.k_rows / kOwned + 1) * a.kv_heads;
+        const uint64_t tiles = ((uint64_t)a.k_rows / (p.narrow_keys ? 32 : kOwned) + 1) * a.kv_heads;
         p.split = (uint32_t)std::min<uint64_t>(a.group, (1024 + tiles - 1) / tiles);
     }
     p.shares = p.parts > 64 ? 64 : 0;

@@ -29,31 +29,33 @@ namespace {
 // maximum's term.
 constexpr int kGaps = 192;
 
-template <typename T, int DP> constexpr uint32_t tiles_lds() {
-    return 2 * (Tile<T, DP, kByRows>::bytes + Tile<T, DP, kByColumns>::bytes) + 2 * kGaps * 4 + kMaxBuckets * 8 +
+template <typename T, int DP, bool NARROW> constexpr uint32_t tiles_lds() {
+    return (NARROW ? 1 : 2) * (Tile<T, DP, kByRows, NARROW>::bytes + Tile<T, DP, kByColumns, NARROW>::bytes) + 2 * kGaps * 4 + kMaxBuckets * 8 +
            kCells + kMaxBuckets * 4;
 }
 
-template <typename T, int DP, int POS, bool EXACT>
+template <typename T, int DP, int POS, bool EXACT, bool NARROW>
 __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
-    using G = Tile<T, DP>;
-    using KT = Tile<T, DP, kByRows>;
-    using VT = Tile<T, DP, kByColumns>;
+    using KT = Tile<T, DP, kByRows, NARROW>;
+    using VT = Tile<T, DP, kByColumns, NARROW>;
+    using G = KT;
+    using S = Span<NARROW, G::rows>;
+    const S span;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    float *extra = (float *)(lds + 2 * (KT::bytes + VT::bytes));   // [2][kGaps]: bias by gap, or positions
+    float *extra = (float *)(lds + S::buffers * (KT::bytes + VT::bytes));   // [2][kGaps]: bias by gap, or positions
     float *bias = extra + 2 * kGaps;
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
+    const uint32_t lane = threadIdx.x & 63u, col = lane & 31u;
 
     // heads of one key/value head follow each other at a distance of kv_heads:
     // workgroups that are dispatched to one XCD share keys and values
     const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
     Seq sq;
-    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, kOwned, slot, sq.tile);
+    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, S::owned, slot, sq.tile);
     sequence(a, b, sq);
-    if (sq.tile >= ((uint32_t)sq.lq + kOwned - 1) / kOwned) return;
-    const int32_t row0 = sq.tile * kOwned, row = row0 + wave * 32 + col, off = sq.lk - sq.lq;
+    if (sq.tile >= ((uint32_t)sq.lq + S::owned - 1) / S::owned) return;
+    const int32_t row0 = sq.tile * S::owned, row = row0 + (int32_t)span.own + (int32_t)col, off = sq.lk - sq.lq;
     const bool there = row < sq.lq;
 
     Owned<T, DP> q;
@@ -72,7 +74,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     }
 
     // keys [0, kend) are open to some row of the workgroup, [0, wend) of the wavefront
-    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wrow0 = row0 + (int32_t)wave * 32;
+    const int32_t last = min(row0 + S::owned, sq.lq) - 1, wrow0 = row0 + (int32_t)span.own;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
     const int32_t wend = a.causal ? min(sq.lk, min(wrow0 + 32, sq.lq) + off) : sq.lk;
     const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;   // keys open to this lane's row
@@ -83,9 +85,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     typename G::Regs kreg, vreg;
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
-        tile_load<T, DP, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
-        tile_load<T, DP, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
-        if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
+        tile_load<G, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<G, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        if constexpr (POS == 2) tile_positions<G>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
     // the gaps of the tile at k0: from least to least + owned + rows - 2
     const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
@@ -93,20 +95,20 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     const auto stage = [&](int32_t k0, int buf) {
         uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
         if constexpr (!EXACT) {
-            tile_settle<T, DP>(kreg, a.dim);
-            tile_settle<T, DP>(vreg, a.dim);
+            tile_settle<G>(kreg, a.dim);
+            tile_settle<G>(vreg, a.dim);
         }
         if constexpr (POS == 2) {
-            tile_close<T, DP>(kreg, preg);
-            tile_close<T, DP>(vreg, preg);
-            tile_store_positions<T, DP>((int32_t *)extra + buf * kGaps, preg);
+            tile_close<G>(kreg, preg);
+            tile_close<G>(vreg, preg);
+            tile_store_positions<G>((int32_t *)extra + buf * kGaps, preg);
         }
-        tile_store<T, DP, kByRows>(kt, kreg);
-        tile_store<T, DP, kByColumns>(kt + KT::bytes, vreg);
+        tile_store<KT>(kt, kreg, kend - k0);
+        tile_store<VT>(kt + KT::bytes, vreg, kend - k0);
         if constexpr (POS == 1) {
             const int32_t x = (int32_t)threadIdx.x, lo = least(k0);
             uint32_t one;
-            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) && x < kOwned + G::rows - 1)
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + S::owned + G::rows - 2, one) && x < S::owned + G::rows - 1)
                 extra[buf * kGaps + x] = bias[bucket_of(buckets.bounds, a.buckets, lo + x)];
         }
     };
@@ -124,53 +126,54 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     }
     __syncthreads();
     int buf = 0;
-    for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= 1) {
+    for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= S::buffers - 1) {
         const bool more = k0 + G::rows < kend;
         if (more) fetch(k0 + G::rows);
-        if (k0 < wend) {
+        if (k0 + (int32_t)span.take < wend) {
             const uint8_t *kt = lds + buf * (KT::bytes + VT::bytes), *vt = kt + KT::bytes;
             const float *ex = extra + buf * kGaps;
-            const bool ragged = k0 + G::rows > whole;
+            const bool ragged = k0 + (int32_t)span.take + S::rows > whole;
             float shift = 0.0f;                                // the bias where the tile has one bucket
             bool far = true, shut = false;
             if constexpr (POS == 1) {
                 uint32_t one;
-                far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + kOwned + G::rows - 2, one);
+                far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + S::owned + G::rows - 2, one);
                 if (far) shift = bias[one];
             }
-            if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[lane % G::rows] == kNoKeyFlipped);
-            f32x16 s[G::blocks];
+            if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[span.take + lane % S::rows] == kNoKeyFlipped);
+            f32x16 s[S::blocks];
             float top = -INFINITY;
 #pragma unroll
-            for (int blk = 0; blk < G::blocks; blk++) {
-                s[blk] = f32x16{};
-                product_rows<T, DP, kByRows>(s[blk], kt, blk, q);
+            for (int n = 0; n < S::blocks; n++) {
+                const int blk = span.take + n * 32;
+                s[n] = f32x16{};
+                product_rows<KT>(s[n], kt, blk, q);
                 if (POS == 1 && !far) {
-                    const float *e = ex + wave * 32 + col + (G::rows - 1) - blk * 32;
+                    const float *e = ex + span.own + col + (G::rows - 1) - blk;
 #pragma unroll
-                    for (int r = 0; r < 16; r++) s[blk][r] += e[-block_row(r)];
+                    for (int r = 0; r < 16; r++) s[n][r] += e[-block_row(r)];
                 }
                 if (POS == 2 && a.buckets) {
                     int32_t gap[16];
                     uint32_t bk[16];
 #pragma unroll
-                    for (int r = 0; r < 16; r++) gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]);
+                    for (int r = 0; r < 16; r++) gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk + block_row(r)]);
                     buckets_in(buckets, gap, bk);
 #pragma unroll
-                    for (int r = 0; r < 16; r++) s[blk][r] += bias[bk[r]];
+                    for (int r = 0; r < 16; r++) s[n][r] += bias[bk[r]];
                 }
                 if (POS == 2 && shut) {
 #pragma unroll
                     for (int r = 0; r < 16; r++)
-                        if (((const int32_t *)ex)[blk * 32 + block_row(r)] == kNoKeyFlipped) s[blk][r] = -INFINITY;
+                        if (((const int32_t *)ex)[blk + block_row(r)] == kNoKeyFlipped) s[n][r] = -INFINITY;
                 }
                 if (ragged) {
 #pragma unroll
                     for (int r = 0; r < 16; r++)
-                        if (k0 + blk * 32 + block_row(r) >= limit) s[blk][r] = -INFINITY;
+                        if (k0 + blk + block_row(r) >= limit) s[n][r] = -INFINITY;
                 }
 #pragma unroll
-                for (int r = 0; r < 16; r++) top = fmaxf(top, s[blk][r]);
+                for (int r = 0; r < 16; r++) top = fmaxf(top, s[n][r]);
             }
             top = halves_max(top) + shift;
             if (__any(top > m + behind)) {
@@ -185,22 +188,42 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
             }
             const float base = fmaf(shift, a.scale2, m == -INFINITY ? 0.0f : -m * a.scale2);
 #pragma unroll
-            for (int blk = 0; blk < G::blocks; blk++) {
+            for (int n = 0; n < S::blocks; n++) {
                 float t[16];
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
-                    t[r] = exp2_fast(fmaf(s[blk][r], a.scale2, base));
+                    t[r] = exp2_fast(fmaf(s[n][r], a.scale2, base));
                     sum += t[r];
                 }
                 Scores<T> p;
                 pack(p, t);
-                product_columns<T, DP, kByColumns>(acc, vt, blk, p);
+                product_columns<VT>(acc, vt, span.take + n * 32, p);
             }
         }
-        if (more) stage(k0 + G::rows, buf ^ 1);
+        if (NARROW && more) __syncthreads();
+        if (more) stage(k0 + G::rows, NARROW ? 0 : buf ^ 1);
         __syncthreads();
     }
     sum = halves_sum(sum);
+    if constexpr (NARROW) {
+        float *tops = (float *)lds, *sums = tops + 256;
+        tops[threadIdx.x] = m;
+        __syncthreads();
+        float top = tops[lane];
+#pragma unroll
+        for (int w = 1; w < 4; w++) top = fmaxf(top, tops[w * 64 + lane]);
+        const float f = m == top ? 1.0f : exp2_fast((m - top) * a.scale2);
+        m = top;
+        sums[threadIdx.x] = sum * f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; d++)
+#pragma unroll
+            for (int r = 0; r < 16; r++) acc[d][r] *= f;
+        __syncthreads();
+        sum = sums[lane] + sums[64 + lane] + sums[128 + lane] + sums[192 + lane];
+        join_waves<DP>(acc, sums + 256);
+        if (threadIdx.x >= 64) return;
+    }
     if (!there) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     store_owned<T, DP>((uint8_t *)a.o.p + (int64_t)(sq.q0 + row) * a.o.row + head * a.o.head, a.dim, acc, inv);
@@ -569,13 +592,13 @@ __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
 }
 
 // ---------------------------------------------------------------- launches
-template <typename T, int DP, bool EXACT>
+template <typename T, int DP, bool EXACT, bool NARROW>
 int launch_tiles(const Attend &a, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
-    const auto kernel = pos == 2   ? attend_tiles<T, DP, 2, EXACT>
-                        : pos == 1 ? attend_tiles<T, DP, 1, EXACT>
-                                   : attend_tiles<T, DP, 0, EXACT>;
-    constexpr uint32_t bytes = tiles_lds<T, DP>();
+    const auto kernel = pos == 2   ? attend_tiles<T, DP, 2, EXACT, NARROW>
+                        : pos == 1 ? attend_tiles<T, DP, 1, EXACT, NARROW>
+                                   : attend_tiles<T, DP, 0, EXACT, NARROW>;
+    constexpr uint32_t bytes = tiles_lds<T, DP, NARROW>();
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
     hipLaunchKernelGGL(kernel, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
@@ -604,15 +627,18 @@ int launch_single(const Attend &a, Form form, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
-template <typename T, int DP> int launch_form(const Attend &a, Form form, hipStream_t s) {
-    if (form != kTiles) return launch_single<T, DP>(a, form, s);
-    return exact_rows(a, a.k) && exact_rows(a, a.v) ? launch_tiles<T, DP, true>(a, s) : launch_tiles<T, DP, false>(a, s);
+template <typename T, int DP> int launch_form(const Attend &a, const Forward &f, hipStream_t s) {
+    if (f.form != kTiles) return launch_single<T, DP>(a, f.form, s);
+    if constexpr (DP * sizeof(T) <= 256)
+        if (f.narrow) return launch_tiles<T, DP, false, true>(a, s);
+    return exact_rows(a, a.k) && exact_rows(a, a.v) ? launch_tiles<T, DP, true, false>(a, s)
+                                                    : launch_tiles<T, DP, false, false>(a, s);
 }
 
-template <typename T> int launch(const Attend &a, Form form, hipStream_t s) {
-    return a.dim <= 32   ? launch_form<T, 32>(a, form, s)
-           : a.dim <= 64 ? launch_form<T, 64>(a, form, s)
-                         : launch_form<T, 128>(a, form, s);
+template <typename T> int launch(const Attend &a, const Forward &f, hipStream_t s) {
+    return a.dim <= 32   ? launch_form<T, 32>(a, f, s)
+           : a.dim <= 64 ? launch_form<T, 64>(a, f, s)
+                         : launch_form<T, 128>(a, f, s);
 }
 
 }  // namespace
@@ -642,6 +668,6 @@ extern "C" int nlb_attention(const nlb_att_call *c, const nlb_att_rows *o, float
     a.part = (float *)work;
     a.slots = (uint32_t)f.slots;
     a.chunk = f.chunk;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, f.form, (hipStream_t)stream)
-                                      : launch<float>(a, f.form, (hipStream_t)stream);
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, f, (hipStream_t)stream)
+                                      : launch<float>(a, f, (hipStream_t)stream);
 }

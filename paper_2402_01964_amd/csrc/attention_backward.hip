@@ -29,8 +29,8 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 // the pass four times as long).  Tiles whose gaps all lie in the first or the
 // last bucket add to a register.  The columns are summed at the end in a fixed
 // order into part[slot][head][bucket].
-template <typename T, int DP> constexpr uint32_t rows_lds(uint32_t buckets) {
-    return 2 * (Tile<T, DP, kBothWays>::bytes + Tile<T, DP, kByRows>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
+template <typename T, int DP, bool NARROW> constexpr uint32_t rows_lds(uint32_t buckets) {
+    return (NARROW ? 1 : 2) * (Tile<T, DP, kBothWays, NARROW>::bytes + Tile<T, DP, kByRows, NARROW>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
            kCells + kMaxBuckets * 4 + buckets * kThreads * 4;
 }
 
@@ -51,14 +51,16 @@ __device__ __forceinline__ void add_four(float *column, const uint32_t (&b)[4], 
 
 // (rows of 512 bytes leave registers for one wavefront on a SIMD, rows of 256
 // with the bias table LDS for one workgroup on a CU)
-template <typename T, int DP, int POS, bool EXACT>
+template <typename T, int DP, int POS, bool EXACT, bool NARROW>
 __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 2) void backward_rows(Attend a) {
-    using G = Tile<T, DP>;
-    using KT = Tile<T, DP, kBothWays>;
-    using VT = Tile<T, DP, kByRows>;
+    using KT = Tile<T, DP, kBothWays, NARROW>;
+    using VT = Tile<T, DP, kByRows, NARROW>;
+    using G = KT;
+    using S = Span<NARROW, G::rows>;
+    const S span;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     // [2][kGaps] bias by gap, or positions; [2][kGaps] buckets by gap
-    float *extra = (float *)(lds + 2 * (KT::bytes + VT::bytes));
+    float *extra = (float *)(lds + S::buffers * (KT::bytes + VT::bytes));
     uint32_t *code = (uint32_t *)(extra + 2 * kGaps);
     float *bias = (float *)(code + 2 * kGaps);
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
@@ -69,13 +71,13 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
     const bool want = POS != 0 && a.part;                     // the bias gradient
     Seq sq;
-    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, kOwned, slot, sq.tile);
+    const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, S::owned, slot, sq.tile);
     sequence(a, b, sq);
-    if (sq.tile >= ((uint32_t)sq.lq + kOwned - 1) / kOwned) {
+    if (sq.tile >= ((uint32_t)sq.lq + S::owned - 1) / S::owned) {
         if (want && threadIdx.x < a.buckets) a.part[((size_t)slot * a.heads + head) * a.buckets + threadIdx.x] = 0.0f;
         return;
     }
-    const int32_t row0 = sq.tile * kOwned, row = row0 + wave * 32 + col, off = sq.lk - sq.lq;
+    const int32_t row0 = sq.tile * S::owned, row = row0 + (int32_t)span.own + (int32_t)col, off = sq.lk - sq.lq;
     const bool there = row < sq.lq;
     const size_t stat = (size_t)(sq.q0 + row) * a.heads + head;
 
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         }
     }
 
-    const int32_t last = min(row0 + kOwned, sq.lq) - 1, wrow0 = row0 + (int32_t)wave * 32;
+    const int32_t last = min(row0 + S::owned, sq.lq) - 1, wrow0 = row0 + (int32_t)span.own;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
     const int32_t wend = a.causal ? min(sq.lk, min(wrow0 + 32, sq.lq) + off) : sq.lk;
     const int32_t limit = a.causal ? min(sq.lk, row + off + 1) : sq.lk;
@@ -122,29 +124,29 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     typename G::Regs kreg, vreg;
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
-        tile_load<T, DP, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
-        tile_load<T, DP, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
-        if constexpr (POS == 2) tile_positions<T, DP>(preg, a.k_pos + sq.k0 + k0, kend - k0);
+        tile_load<G, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
+        tile_load<G, EXACT>(vreg, vbase + (int64_t)k0 * a.v.row, a.v.row, kend - k0, a.dim);
+        if constexpr (POS == 2) tile_positions<G>(preg, a.k_pos + sq.k0 + k0, kend - k0);
     };
     const auto least = [&](int32_t k0) { return row0 + off - k0 - (G::rows - 1); };
     const auto stage = [&](int32_t k0, int buf) {
         uint8_t *kt = lds + buf * (KT::bytes + VT::bytes);
         if constexpr (!EXACT) {
-            tile_settle<T, DP>(kreg, a.dim);
-            tile_settle<T, DP>(vreg, a.dim);
+            tile_settle<G>(kreg, a.dim);
+            tile_settle<G>(vreg, a.dim);
         }
         if constexpr (POS == 2) {
-            tile_close<T, DP>(kreg, preg);
-            tile_close<T, DP>(vreg, preg);
-            tile_store_positions<T, DP>((int32_t *)extra + buf * kGaps, preg);
+            tile_close<G>(kreg, preg);
+            tile_close<G>(vreg, preg);
+            tile_store_positions<G>((int32_t *)extra + buf * kGaps, preg);
         }
-        tile_store<T, DP, kBothWays>(kt, kreg);
-        tile_store<T, DP, kByRows>(kt + KT::bytes, vreg);
+        tile_store<KT>(kt, kreg, kend - k0);
+        tile_store<VT>(kt + KT::bytes, vreg, kend - k0);
         if constexpr (POS == 1) {
             const int32_t x = (int32_t)threadIdx.x, lo = least(k0);
             uint32_t one;
-            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) &&
-                x < kOwned + G::rows - 1) {
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + S::owned + G::rows - 2, one) &&
+                x < S::owned + G::rows - 1) {
                 const uint32_t n = bucket_of(buckets.bounds, a.buckets, lo + x);
                 code[buf * kGaps + x] = n;
                 extra[buf * kGaps + x] = bias[n];
@@ -165,29 +167,30 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         }
         __syncthreads();
         int buf = 0;
-        for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= 1) {
+        for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= S::buffers - 1) {
             const bool more = k0 + G::rows < kend;
             if (more) fetch(k0 + G::rows);
-            if (k0 < wend) {
+            if (k0 + (int32_t)span.take < wend) {
                 const uint8_t *kt = lds + buf * (KT::bytes + VT::bytes), *vt = kt + KT::bytes;
                 const float *ex = extra + buf * kGaps;
-                const bool ragged = k0 + G::rows > whole;
+                const bool ragged = k0 + (int32_t)span.take + S::rows > whole;
                 bool far = true, shut = false;
                 uint32_t one = 0;
                 float base = -L;
                 if constexpr (POS == 1) {
-                    far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + kOwned + G::rows - 2, one);
+                    far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + S::owned + G::rows - 2, one);
                     if (far) base = fmaf(bias[one], a.scale2, base);
                 }
-                if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[lane % G::rows] == kNoKeyFlipped);
+                if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[span.take + lane % S::rows] == kNoKeyFlipped);
 #pragma unroll
-                for (int blk = 0; blk < G::blocks; blk++) {
+                for (int n = 0; n < S::blocks; n++) {
+                    const int blk = span.take + n * 32;
                     f32x16 s = {}, dp = {};
-                    product_rows<T, DP, kBothWays>(s, kt, blk, q);
-                    product_rows<T, DP, kByRows>(dp, vt, blk, dout);
+                    product_rows<KT>(s, kt, blk, q);
+                    product_rows<VT>(dp, vt, blk, dout);
                     uint32_t bk[POS == 0 ? 1 : 16];
                     if (POS == 1 && !far) {
-                        const uint32_t at = wave * 32 + col + (G::rows - 1) - blk * 32;
+                        const uint32_t at = span.own + col + (G::rows - 1) - blk;
 #pragma unroll
                         for (int r = 0; r < 16; r++) {
                             s[r] += ex[at - block_row(r)];
@@ -196,26 +199,26 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
                     }
                     if (POS == 2 && a.buckets) {
                         int32_t gap[16];
-                        uint32_t n[16];
+                        uint32_t nb[16];
 #pragma unroll
                         for (int r = 0; r < 16; r++)
-                            gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk * 32 + block_row(r)]);
-                        buckets_in(buckets, gap, n);
+                            gap[r] = gap_of(qpos, ((const int32_t *)ex)[blk + block_row(r)]);
+                        buckets_in(buckets, gap, nb);
 #pragma unroll
                         for (int r = 0; r < 16; r++) {
-                            s[r] += bias[n[r]];
-                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = n[r];
+                            s[r] += bias[nb[r]];
+                            if (!FIRST) bk[r % (POS == 0 ? 1 : 16)] = nb[r];
                         }
                     }
                     if (POS == 2 && shut) {
 #pragma unroll
                         for (int r = 0; r < 16; r++)
-                            if (((const int32_t *)ex)[blk * 32 + block_row(r)] == kNoKeyFlipped) s[r] = -INFINITY;
+                            if (((const int32_t *)ex)[blk + block_row(r)] == kNoKeyFlipped) s[r] = -INFINITY;
                     }
                     if (ragged) {
 #pragma unroll
                         for (int r = 0; r < 16; r++)
-                            if (k0 + blk * 32 + block_row(r) >= limit) s[r] = -INFINITY;
+                            if (k0 + blk + block_row(r) >= limit) s[r] = -INFINITY;
                     }
                     float ds[16];
 #pragma unroll
@@ -234,30 +237,40 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
                         } else if (want) {
 #pragma unroll
                             for (int r = 0; r < 16; r += 4) {
-                                const uint32_t n[4] = {bk[r % (POS == 0 ? 1 : 16)], bk[(r + 1) % (POS == 0 ? 1 : 16)],
+                                const uint32_t four[4] = {bk[r % (POS == 0 ? 1 : 16)], bk[(r + 1) % (POS == 0 ? 1 : 16)],
                                                        bk[(r + 2) % (POS == 0 ? 1 : 16)],
                                                        bk[(r + 3) % (POS == 0 ? 1 : 16)]};
                                 const float x[4] = {ds[r], ds[r + 1], ds[r + 2], ds[r + 3]};
-                                add_four(hist + threadIdx.x, n, x);
+                                add_four(hist + threadIdx.x, four, x);
                             }
                         }
                         Scores<T> p;
                         pack(p, ds);
-                        product_columns<T, DP, kBothWays>(acc, kt, blk, p);
+                        product_columns<KT>(acc, kt, blk, p);
                     }
                 }
             }
-            if (more) stage(k0 + G::rows, buf ^ 1);
+            if (NARROW && more) __syncthreads();
+            if (more) stage(k0 + G::rows, NARROW ? 0 : buf ^ 1);
             __syncthreads();
         }
     };
     if (want) {
         pass(std::true_type{});
         D = halves_sum(D);
+        if constexpr (NARROW) {
+            float *shares = extra;
+            shares[threadIdx.x] = D;
+            __syncthreads();
+            D = shares[lane] + shares[64 + lane] + shares[128 + lane] + shares[192 + lane];
+            __syncthreads();
+        }
     }
-    if (there && lane < 32) a.delta[stat] = D;
+    const bool first_wave = !NARROW || wave == 0;
+    if (there && lane < 32 && first_wave) a.delta[stat] = D;
     pass(std::false_type{});
-    if (there)
+    if constexpr (NARROW) join_waves<DP>(acc, (float *)lds);
+    if (there && first_wave)
         store_owned<T, DP>((uint8_t *)a.dq.p + (int64_t)(sq.q0 + row) * a.dq.row + head * a.dq.head, a.dim, acc,
                            a.scale);
     if (want) {
@@ -289,31 +302,34 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 // instead, which compute the scores twice and run two wavefronts on a SIMD
 // where the one would run one (rows of 128 bf16 values, 8095 rows in two
 // sequences, 16 heads in 4 groups: 1030 us in one launch).
-template <typename T, int DP> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
-    return 4 * Tile<T, DP, kBothWays>::bytes + 2 * (kGaps + 2 * Tile<T, DP>::rows) * 4 +
+template <typename T, int DP, bool NARROW> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
+    return (NARROW ? 2 : 4) * Tile<T, DP, kBothWays, NARROW>::bytes +
+           2 * (kGaps + 2 * Tile<T, DP, kBothWays, NARROW>::rows) * 4 +
            (bias ? kMaxBuckets * 4 * (1 + group) + kCells + kMaxBuckets * 4 : 0);
 }
 
-template <typename T, int DP, int POS, int WHAT, bool EXACT>
+template <typename T, int DP, int POS, int WHAT, bool EXACT, bool NARROW>
 __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backward_keys(Attend a) {
-    using G = Tile<T, DP, kBothWays>;
+    using G = Tile<T, DP, kBothWays, NARROW>;
+    using S = Span<NARROW, G::rows>;
+    const S span;
     constexpr bool DK = WHAT & 2, DV = WHAT & 1;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int kExtra = kGaps + 2 * G::rows;
-    float *extra = (float *)(lds + 4 * G::bytes);             // [2]: L, D of the tile's rows; bias by gap, or positions
+    float *extra = (float *)(lds + S::buffers * 2 * G::bytes);             // [2]: L, D of the tile's rows; bias by gap, or positions
     float *bias = extra + 2 * kExtra;                         // [group][buckets]
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets * a.group), (uint8_t *)(bias + kMaxBuckets * (1 + a.group)),
                        a.buckets - 1, 0};
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
+    const uint32_t lane = threadIdx.x & 63u, col = lane & 31u;
     const uint32_t kvh = blockIdx.x % a.kv_heads, share = blockIdx.x / a.kv_heads % a.split;
     const uint32_t slot = blockIdx.x / (a.kv_heads * a.split);
     // query heads of the group: this workgroup's share
     const int32_t g0 = a.group * share / a.split, g1 = a.group * (share + 1) / a.split;
     Seq sq;
-    const uint32_t b = slot_owner(a.k_start, a.k_len, a.k_rows, a.batch, kOwned, slot, sq.tile);
+    const uint32_t b = slot_owner(a.k_start, a.k_len, a.k_rows, a.batch, S::owned, slot, sq.tile);
     sequence(a, b, sq);
-    if (sq.tile >= ((uint32_t)sq.lk + kOwned - 1) / kOwned) return;
-    const int32_t key0 = sq.tile * kOwned, key = key0 + wave * 32 + col, off = sq.lk - sq.lq;
+    if (sq.tile >= ((uint32_t)sq.lk + S::owned - 1) / S::owned) return;
+    const int32_t key0 = sq.tile * S::owned, key = key0 + (int32_t)span.own + (int32_t)col, off = sq.lk - sq.lq;
     const bool there = key < sq.lk;
     int32_t kpos = 0;
     if constexpr (POS == 2) kpos = there ? flip(a.k_pos[sq.k0 + key]) : kNoKeyFlipped;
@@ -336,7 +352,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     const int32_t first = a.causal ? max(0, key0 - off) / G::rows * G::rows : 0;
     const int32_t tiles = sq.lq > first ? (sq.lq - first + G::rows - 1) / G::rows : 0;
     const int32_t seen = a.causal ? key - off : 0;            // the first row that sees this lane's key
-    const int32_t wseen = a.causal ? key0 + (int32_t)wave * 32 - off : 0;
+    const int32_t wseen = a.causal ? key0 + (int32_t)span.own - off : 0;
     const int32_t whole = a.causal ? wseen + 31 : 0;
     const bool shut = __any(!open);
 
@@ -346,8 +362,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     const auto fetch = [&](int32_t g, int32_t i0) {
         const uint32_t head = kvh * a.group + g;
         const int64_t r = sq.q0 + i0;
-        tile_load<T, DP, EXACT>(qreg, a.q.p + r * a.q.row + head * a.q.head, a.q.row, sq.lq - i0, a.dim);
-        tile_load<T, DP, EXACT>(oreg, a.dout.p + r * a.dout.row + head * a.dout.head, a.dout.row, sq.lq - i0, a.dim);
+        tile_load<G, EXACT>(qreg, a.q.p + r * a.q.row + head * a.q.head, a.q.row, sq.lq - i0, a.dim);
+        tile_load<G, EXACT>(oreg, a.dout.p + r * a.dout.row + head * a.dout.head, a.dout.row, sq.lq - i0, a.dim);
         if (threadIdx.x < G::rows) {
             const bool in = i0 + (int32_t)threadIdx.x < sq.lq;
             const size_t stat = (size_t)(r + threadIdx.x) * a.heads + head;
@@ -356,16 +372,16 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
             if (POS == 2 && a.q_pos) preg = in ? a.q_pos[r + threadIdx.x] : 0;
         }
     };
-    const auto least = [&](int32_t i0) { return i0 + off - key0 - (kOwned - 1); };
+    const auto least = [&](int32_t i0) { return i0 + off - key0 - (S::owned - 1); };
     const auto stage = [&](int32_t g, int32_t i0, int buf) {
         uint8_t *qt = lds + buf * 2 * G::bytes;
         float *e = extra + buf * kExtra;
         if constexpr (!EXACT) {
-            tile_settle<T, DP>(qreg, a.dim);
-            tile_settle<T, DP>(oreg, a.dim);
+            tile_settle<G>(qreg, a.dim);
+            tile_settle<G>(oreg, a.dim);
         }
-        tile_store<T, DP, kBothWays>(qt, qreg);
-        tile_store<T, DP, kBothWays>(qt + G::bytes, oreg);
+        tile_store<G>(qt, qreg, sq.lq - i0);
+        tile_store<G>(qt + G::bytes, oreg, sq.lq - i0);
         if (threadIdx.x < G::rows) {
             e[threadIdx.x] = -Lreg;
             if (DK) e[G::rows + threadIdx.x] = Dreg;
@@ -374,8 +390,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         if constexpr (POS == 1) {
             const int32_t x = (int32_t)threadIdx.x, lo = least(i0);
             uint32_t one;
-            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + kOwned + G::rows - 2, one) &&
-                x < kOwned + G::rows - 1)
+            if (!one_bucket(buckets.bounds, a.buckets, lo, lo + S::owned + G::rows - 2, one) &&
+                x < S::owned + G::rows - 1)
                 e[2 * G::rows + x] = bias[g * kMaxBuckets + bucket_of(buckets.bounds, a.buckets, lo + x)];
         }
     };
@@ -394,7 +410,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     __syncthreads();
     int buf = 0;
     int32_t g = g0, i0 = first;
-    for (int32_t it = 0; it < total; it++, buf ^= 1) {
+    for (int32_t it = 0; it < total; it++, buf ^= S::buffers - 1) {
         int32_t gn = g, in = i0 + G::rows;
         if (in >= sq.lq) {
             in = first;
@@ -402,46 +418,47 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         }
         const bool more = it + 1 < total;
         if (more) fetch(gn, in);
-        if (i0 + G::rows > wseen) {
+        if (i0 + (int32_t)span.take + S::rows > wseen && i0 + (int32_t)span.take < sq.lq) {
             const uint8_t *qt = lds + buf * 2 * G::bytes, *ot = qt + G::bytes;
             const float *e = extra + buf * kExtra;
-            const bool ragged = i0 < whole;
+            const bool ragged = i0 + (int32_t)span.take < whole;
             bool far = true;
             float shift = 0.0f;
             if constexpr (POS == 1) {
                 uint32_t one;
-                far = one_bucket(buckets.bounds, a.buckets, least(i0), least(i0) + kOwned + G::rows - 2, one);
+                far = one_bucket(buckets.bounds, a.buckets, least(i0), least(i0) + S::owned + G::rows - 2, one);
                 if (far) shift = bias[g * kMaxBuckets + one];
             }
 #pragma unroll
-            for (int blk = 0; blk < G::blocks; blk++) {
+            for (int n = 0; n < S::blocks; n++) {
+                    const int blk = span.take + n * 32;
                 f32x16 s = {}, dp = {};
-                product_rows<T, DP, kBothWays>(s, qt, blk, k);
-                if constexpr (DK) product_rows<T, DP, kBothWays>(dp, ot, blk, v);
+                product_rows<G>(s, qt, blk, k);
+                if constexpr (DK) product_rows<G>(dp, ot, blk, v);
                 if (POS == 1) {
                     if (far) {
 #pragma unroll
                         for (int r = 0; r < 16; r++) s[r] += shift;
                     } else {
-                        const float *x = e + 2 * G::rows + blk * 32 + (kOwned - 1) - wave * 32 - col;
+                        const float *x = e + 2 * G::rows + blk + (S::owned - 1) - span.own - col;
 #pragma unroll
                         for (int r = 0; r < 16; r++) s[r] += x[block_row(r)];
                     }
                 }
                 if (POS == 2 && a.buckets) {
                     int32_t gap[16];
-                    uint32_t n[16];
+                    uint32_t nb[16];
 #pragma unroll
                     for (int r = 0; r < 16; r++)
-                        gap[r] = gap_of(((const int32_t *)e)[2 * G::rows + blk * 32 + block_row(r)], kpos);
-                    buckets_in(buckets, gap, n);
+                        gap[r] = gap_of(((const int32_t *)e)[2 * G::rows + blk + block_row(r)], kpos);
+                    buckets_in(buckets, gap, nb);
 #pragma unroll
-                    for (int r = 0; r < 16; r++) s[r] += bias[g * kMaxBuckets + n[r]];
+                    for (int r = 0; r < 16; r++) s[r] += bias[g * kMaxBuckets + nb[r]];
                 }
                 if (ragged) {
 #pragma unroll
                     for (int r = 0; r < 16; r++)
-                        if (i0 + blk * 32 + block_row(r) < seen) s[r] = -INFINITY;
+                        if (i0 + blk + block_row(r) < seen) s[r] = -INFINITY;
                 }
                 if (shut) {
 #pragma unroll
@@ -450,25 +467,32 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
                 float p[16], ds[16];
 #pragma unroll
                 for (int r = 0; r < 16; r++) {
-                    const int ir = blk * 32 + block_row(r);
+                    const int ir = blk + block_row(r);
                     p[r] = exp2_fast(fmaf(s[r], a.scale2, e[ir]));
                     if constexpr (DK) ds[r] = p[r] * (dp[r] - e[G::rows + ir]);
                 }
                 Scores<T> w;
                 if constexpr (DV) {
                     pack(w, p);
-                    product_columns<T, DP, kBothWays>(dv, ot, blk, w);
+                    product_columns<G>(dv, ot, blk, w);
                 }
                 if constexpr (DK) {
                     pack(w, ds);
-                    product_columns<T, DP, kBothWays>(dk, qt, blk, w);
+                    product_columns<G>(dk, qt, blk, w);
                 }
             }
         }
-        if (more) stage(gn, in, buf ^ 1);
+        if (NARROW && more) __syncthreads();
+        if (more) stage(gn, in, NARROW ? 0 : buf ^ 1);
         __syncthreads();
         g = gn;
         i0 = in;
+    }
+    if constexpr (NARROW) {
+        if constexpr (DK) join_waves<DP>(dk, (float *)lds);
+        if constexpr (DK && DV) __syncthreads();
+        if constexpr (DV) join_waves<DP>(dv, (float *)lds);
+        if (threadIdx.x >= 64) return;
     }
     if (!there) return;
     const int64_t at = sq.k0 + key;
@@ -754,31 +778,61 @@ __global__ __launch_bounds__(kThreads) void sum_bias(const float *part, uint32_t
 }
 
 // ---------------------------------------------------------------- launches
-template <typename T, int DP, bool EXACT> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
+template <typename T, int DP, bool EXACT, bool NARROW>
+int launch_rows(const Attend &a, hipStream_t stream) {
     const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
-    const auto rows = pos == 2   ? backward_rows<T, DP, 2, EXACT>
-                      : pos == 1 ? backward_rows<T, DP, 1, EXACT>
-                                 : backward_rows<T, DP, 0, EXACT>;
-    constexpr bool twice = DP * sizeof(T) >= 256;
-    constexpr int A = twice ? 1 : 3, B = twice ? 2 : 3;
-    const auto keys = pos == 2   ? backward_keys<T, DP, 2, A, EXACT>
-                      : pos == 1 ? backward_keys<T, DP, 1, A, EXACT>
-                                 : backward_keys<T, DP, 0, A, EXACT>;
-    const auto more = pos == 2   ? backward_keys<T, DP, 2, B, EXACT>
-                      : pos == 1 ? backward_keys<T, DP, 1, B, EXACT>
-                                 : backward_keys<T, DP, 0, B, EXACT>;
-    const uint32_t rb = rows_lds<T, DP>(a.part ? a.buckets : 0), kb = keys_lds<T, DP>(a.group, a.buckets > 0);
-    if (!allow_lds(rows, rb) || !allow_lds(keys, kb) || !allow_lds(more, kb)) return NLB_EDEVICE;
+    const auto rows = pos == 2   ? backward_rows<T, DP, 2, EXACT, NARROW>
+                      : pos == 1 ? backward_rows<T, DP, 1, EXACT, NARROW>
+                                 : backward_rows<T, DP, 0, EXACT, NARROW>;
+    const uint32_t bytes = rows_lds<T, DP, NARROW>(a.part ? a.buckets : 0);
+    if (!allow_lds(rows, bytes)) return NLB_EDEVICE;
+    hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
+    return NLB_OK;
+}
+
+template <typename T, int DP, int WHAT, bool EXACT, bool NARROW>
+int launch_keys(const Attend &a, hipStream_t stream) {
+    const int pos = a.k_pos ? 2 : a.buckets ? 1 : 0;
+    const auto keys = pos == 2   ? backward_keys<T, DP, 2, WHAT, EXACT, NARROW>
+                      : pos == 1 ? backward_keys<T, DP, 1, WHAT, EXACT, NARROW>
+                                 : backward_keys<T, DP, 0, WHAT, EXACT, NARROW>;
+    const uint32_t bytes = keys_lds<T, DP, NARROW>(a.group, a.buckets > 0);
+    if (!allow_lds(keys, bytes)) return NLB_EDEVICE;
+    hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads * a.split), dim3(kThreads), bytes, stream, a);
+    return NLB_OK;
+}
+
+template <typename T, int DP, bool EXACT, bool NARROW> int launch_both_keys(const Attend &a, hipStream_t stream) {
+    if constexpr (DP * sizeof(T) >= 256) {
+        const int rc = launch_keys<T, DP, 1, EXACT, NARROW>(a, stream);
+        return rc != NLB_OK ? rc : launch_keys<T, DP, 2, EXACT, NARROW>(a, stream);
+    } else {
+        return launch_keys<T, DP, 3, EXACT, NARROW>(a, stream);
+    }
+}
+
+template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipStream_t stream) {
+    const bool exact = exact_rows(a, a.q) && exact_rows(a, a.k) && exact_rows(a, a.v) && exact_rows(a, a.dout);
+    int rc = NLB_OK;
     a.slots = (uint32_t)p.q_slots;
-    if (a.q_rows) hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), rb, stream, a);
+    if (a.q_rows) {
+        bool narrow = false;
+        if constexpr (DP * sizeof(T) <= 256)
+            if ((narrow = p.narrow_rows)) rc = launch_rows<T, DP, false, true>(a, stream);
+        if (!narrow)
+            rc = exact ? launch_rows<T, DP, true, false>(a, stream) : launch_rows<T, DP, false, false>(a, stream);
+    }
     a.slots = (uint32_t)p.k_slots;
-    if (a.k_rows) {
-        const dim3 grid(a.slots * a.kv_heads * a.split);
-        hipLaunchKernelGGL(keys, grid, dim3(kThreads), kb, stream, a);
-        if (twice) hipLaunchKernelGGL(more, grid, dim3(kThreads), kb, stream, a);
+    if (a.k_rows && rc == NLB_OK) {
+        bool narrow = false;
+        if constexpr (DP * sizeof(T) <= 256)
+            if ((narrow = p.narrow_keys)) rc = launch_both_keys<T, DP, false, true>(a, stream);
+        if (!narrow)
+            rc = exact ? launch_both_keys<T, DP, true, false>(a, stream)
+                       : launch_both_keys<T, DP, false, false>(a, stream);
         if (a.split > 1) hipLaunchKernelGGL((sum_heads<T>), dim3(1024, 2), dim3(kThreads), 0, stream, a);
     }
-    return NLB_OK;
+    return rc;
 }
 
 template <typename T, int DP> int launch_lists(const Attend &a, const Backward &p, hipStream_t stream) {
@@ -794,10 +848,7 @@ template <typename T, int DP> int launch_lists(const Attend &a, const Backward &
 }
 
 template <typename T, int DP> int launch_form(const Attend &a, const Backward &p, hipStream_t s) {
-    if (p.lists) return launch_lists<T, DP>(a, p, s);
-    return exact_rows(a, a.q) && exact_rows(a, a.k) && exact_rows(a, a.v) && exact_rows(a, a.dout)
-               ? launch_tiles<T, DP, true>(a, p, s)
-               : launch_tiles<T, DP, false>(a, p, s);
+    return p.lists ? launch_lists<T, DP>(a, p, s) : launch_tiles<T, DP>(a, p, s);
 }
 
 template <typename T> int launch(const Attend &a, const Backward &p, void *dbias, hipStream_t s) {
