@@ -377,17 +377,21 @@ template <int DP> __device__ __forceinline__ void join_waves(f32x16 (&acc)[DP / 
 // a test for each chunk, vector operations for them took as long as the
 // exponentials).  EXACT: a row is a whole number of chunks and a tile's rows
 // lie within 2^31 bytes.  Else a row's last chunk is loaded where the row
-// ends, and moved into place by tile_settle when it is staged.
+// ends, and moved into place by tile_settle when it is staged.  Chunks past a
+// row's end stay as tile_clear left them.
+template <typename G> __device__ __forceinline__ void tile_clear(typename G::Regs &reg) {
+#pragma unroll
+    for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
+}
+
 template <typename G, bool EXACT>
 __device__ __forceinline__ void tile_load(typename G::Regs &reg, const uint8_t *base, int64_t stride, int32_t n,
                                           uint32_t dim) {
     using T = typename G::Value;
     constexpr uint32_t N = Chunk<T>::n;
     const uint32_t c0 = threadIdx.x % G::chunks * N, r0 = threadIdx.x / G::chunks;
-    if (c0 >= dim) {
-#pragma unroll
-        for (int i = 0; i < G::per_thread; i++) reg[i] = u32x4{0, 0, 0, 0};
-    } else if (EXACT || dim >= N) {
+    if (c0 >= dim) return;
+    if (EXACT || dim >= N) {
         const uint32_t at = (EXACT ? c0 : min(c0, dim - N)) * (uint32_t)sizeof(T);
         const auto load = [&](int i) {
             const uint32_t r = min(r0 + i * G::step, (uint32_t)n - 1);
@@ -696,10 +700,7 @@ inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Which kernels a call runs.
 enum Form { kTiles, kOne, kLists };
-#ifndef NARROW_BLOCKS
-#define NARROW_BLOCKS 128
-#endif
-constexpr uint64_t kNarrowBlocks = NARROW_BLOCKS;
+constexpr uint64_t kNarrowBlocks = 128;
 
 // Calls of tiles: narrow workgroups where sequences have 64 owned rows or fewer
 // on average, or where the others are so few that half of the card idles.

@@ -83,6 +83,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
 
     typename G::Regs kreg, vreg;
+    tile_clear<G>(kreg);
+    tile_clear<G>(vreg);
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
         tile_load<G, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);

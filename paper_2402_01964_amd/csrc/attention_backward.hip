@@ -122,6 +122,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     const uint8_t *vbase = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
 
     typename G::Regs kreg, vreg;
+    tile_clear<G>(kreg);
+    tile_clear<G>(vreg);
     uint32_t preg[POS == 2 ? G::per_thread : 1];
     const auto fetch = [&](int32_t k0) {
         tile_load<G, EXACT>(kreg, kbase + (int64_t)k0 * a.k.row, a.k.row, kend - k0, a.dim);
@@ -357,6 +359,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     const bool shut = __any(!open);
 
     typename G::Regs qreg, oreg;
+    tile_clear<G>(qreg);
+    tile_clear<G>(oreg);
     float Lreg = 0.0f, Dreg = 0.0f;
     uint32_t preg = 0;
     const auto fetch = [&](int32_t g, int32_t i0) {
