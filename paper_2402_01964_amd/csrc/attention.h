@@ -57,7 +57,7 @@ struct Attend {
     Strided q, k, v, o, dout;            // o: written forward, read backward
     Strided dq, dk, dv;
     float *lse;                          // [q_rows][heads], natural
-    float *delta;                        // [q_rows][heads]
+    float2 *stats;                       // [q_rows][heads]: log2 of the sum, and D
     const int32_t *q_start, *k_start;
     uint32_t batch, q_rows, k_rows, q_len, k_len;   // *_len: rows of every sequence where *_start is null
     uint32_t heads, kv_heads, group, dim;
@@ -752,7 +752,7 @@ struct Backward {
     uint64_t q_slots, q_most, k_slots, k_most;
     uint32_t split;                      // workgroups that share a group's query heads
     uint64_t parts;                      // partial bias gradients
-    size_t delta_bytes, part_bytes, bytes;
+    size_t stat_bytes, part_bytes, bytes;
 };
 
 // Short lists with one query row take a group of lanes each; a group's heads
@@ -787,7 +787,7 @@ inline Backward plan_backward(const Attend &a) {
         p.q_most = INT32_MAX / a.heads;
         p.k_most = INT32_MAX / a.kv_heads;
         p.parts = a.q_rows ? p.q_slots : 0;
-        p.delta_bytes = align256((size_t)a.q_rows * a.heads * 4);
+        p.stat_bytes = align256((size_t)a.q_rows * a.heads * 8);
         // Two workgroups of backward_keys run on a CU.  Where key tiles are too
         // few for two turns of them (which causal sequences of one length need
         // to even out), a group's heads are spread over workgroups, whose
@@ -797,7 +797,7 @@ inline Backward plan_backward(const Attend &a) {
     }
     p.shares = p.parts > 64 ? 64 : 0;
     p.part_bytes = align256((p.parts + p.shares) * a.heads * a.buckets * 4);
-    p.bytes = p.delta_bytes + p.part_bytes;
+    p.bytes = p.stat_bytes + p.part_bytes;
     if (p.split > 1) p.bytes += 2 * p.split * (size_t)a.k_rows * a.kv_heads * ((a.dim + 3) / 4) * 16;
     return p;
 }

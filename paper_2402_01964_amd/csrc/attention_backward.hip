@@ -18,10 +18,14 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 
 // ---------------------------------------------------------------- rows
 // A workgroup owns 128 query rows of one head and streams keys and values as
-// the forward pass does.  D is do . o without a bias gradient.  With one, D is
-// summed from the probabilities in a pass of its own over the keys: a bucket's
-// gradient is a difference of large sums (all ds of a row add up to zero),
-// which the rounding of o would drown.
+// the forward pass does.  D is do . o, which is as far off as o: rounded to
+// bf16, and from probabilities rounded to bf16.  A first pass over the keys adds
+// sum_j p_j (dp_j - do . o), so that the ds of a row add up to zero as they
+// should (fp32 rows do without it unless a bias gradient is wanted, which is
+// a difference of large sums).  Without it dq and dk of 128 bf16 values are
+// 2.6e-3 to 3.1e-3 off (2-norm, relative) where rounding them and ds alone
+// makes 2.4e-3, and of a bucket that takes most of a row's weight nothing is
+// left; it takes two products of seven more.
 //
 // The bias gradient: each thread adds its ds to its own column of an LDS table
 // [buckets][threads], four at a time: reads, sums over equal buckets among the
@@ -88,9 +92,9 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     int32_t qpos = 0;
     if constexpr (POS == 2)
         if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
-    const float L = there ? row_log2(a.lse[stat]) : INFINITY;
-    float D = 0.0f;
-    if (!want) {
+    float L = there ? row_log2(a.lse[stat]) : INFINITY;
+    float D = 0.0f;                                           // do . o, corrected by the first pass
+    {
         Owned<T, DP> o;
         load_owned(o, a.o.p + (int64_t)(sq.q0 + row) * a.o.row + head * a.o.head, there, a.dim);
 #pragma unroll
@@ -103,6 +107,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         }
         D = halves_sum(D);
     }
+    float more_D = 0.0f, weight = 0.0f;
     if (POS != 0 && a.buckets) {
         stage_bias<T>(a, head, buckets.bounds, bias);
         if (want)
@@ -226,8 +231,9 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
                         const float p = exp2_fast(fmaf(s[r], a.scale2, base));
-                        if constexpr (FIRST) D = fmaf(p, dp[r], D);
+                        if constexpr (FIRST) more_D = fmaf(p, dp[r] - D, more_D);
                         else ds[r] = p * (dp[r] - D);
+                        if (FIRST && sizeof(T) == 4) weight += p;
                     }
                     if constexpr (!FIRST) {
                         if (want && POS == 1 && far) {
@@ -257,19 +263,28 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
             __syncthreads();
         }
     };
-    if (want) {
+    if (sizeof(T) == 2 || want) {
         pass(std::true_type{});
-        D = halves_sum(D);
-        if constexpr (NARROW) {
-            float *shares = extra;
-            shares[threadIdx.x] = D;
-            __syncthreads();
-            D = shares[lane] + shares[64 + lane] + shares[128 + lane] + shares[192 + lane];
-            __syncthreads();
+        const auto row_sum = [&](float x) {
+            x = halves_sum(x);
+            if constexpr (NARROW) {
+                float *shares = extra;
+                shares[threadIdx.x] = x;
+                __syncthreads();
+                x = shares[lane] + shares[64 + lane] + shares[128 + lane] + shares[192 + lane];
+                __syncthreads();
+            }
+            return x;
+        };
+        D += row_sum(more_D);
+        // fp32: lse is rounded, and a row's probabilities with it
+        if constexpr (sizeof(T) == 4) {
+            weight = row_sum(weight);
+            if (weight > 0.5f) L += log2_fast(weight);
         }
     }
     const bool first_wave = !NARROW || wave == 0;
-    if (there && lane < 32 && first_wave) a.delta[stat] = D;
+    if (there && lane < 32 && first_wave) a.stats[stat] = make_float2(L, D);
     pass(std::false_type{});
     if constexpr (NARROW) join_waves<DP>(acc, (float *)lds);
     if (there && first_wave)
@@ -371,8 +386,9 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         if (threadIdx.x < G::rows) {
             const bool in = i0 + (int32_t)threadIdx.x < sq.lq;
             const size_t stat = (size_t)(r + threadIdx.x) * a.heads + head;
-            Lreg = in ? row_log2(a.lse[stat]) : INFINITY;
-            if (DK) Dreg = in ? a.delta[stat] : 0.0f;
+            const float2 x = in ? a.stats[stat] : make_float2(INFINITY, 0.0f);
+            Lreg = x.x;
+            Dreg = x.y;
             if (POS == 2 && a.q_pos) preg = in ? a.q_pos[r + threadIdx.x] : 0;
         }
     };
@@ -577,12 +593,12 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
         Seq sq;
         sequence(a, b, sq);
         if (!there) sq.lk = 0;
-        float q[GB][N], dout[GB][N], A[GB][N], B[GB][N], lse[GB], first[GB], D[GB];
+        float q[GB][N], dout[GB][N], A[GB][N], B[GB][N], lse[GB], first[GB], D[GB], weight[GB];
 #pragma unroll
         for (int g = 0; g < GB; g++) {
             u32x4 x = {0, 0, 0, 0}, y = x;
             lse[g] = INFINITY;
-            first[g] = D[g] = 0.0f;
+            first[g] = D[g] = weight[g] = 0.0f;
             if ((uint32_t)g < a.group) {
                 x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
                 y = load_chunk<T>(a.dout.p + (int64_t)b * a.dout.row + (head0 + g) * a.dout.head, c0, a.dim);
@@ -638,6 +654,7 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
                     if constexpr (decltype(summing)::value) {
                         const float pd = p[u][g] * d[u][g];
                         D[g] += pd;
+                        weight[g] += p[u][g];
 #pragma unroll
                         for (int i = 0; i < N; i++) {
                             A[g][i] = fmaf(pd, x[i], A[g][i]);
@@ -653,12 +670,12 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
             float dk[N] = {}, dv[N] = {}, mine = 0.0f;
 #pragma unroll
             for (int g = 0; g < GB; g++) {
-                const float ds = p[g] * (d[g] - D[g]), dss = ds * a.scale;
+                const float w = p[g] * weight[g], ds = w * (d[g] - D[g]), dss = ds * a.scale;
                 if (c == (uint32_t)g) mine = ds;
 #pragma unroll
                 for (int i = 0; i < N; i++) {
                     dk[i] = fmaf(dss, q[g][i], dk[i]);
-                    dv[i] = fmaf(p[g], dout[g][i], dv[i]);
+                    dv[i] = fmaf(w, dout[g][i], dv[i]);
                 }
             }
             if (!open) return;
@@ -697,6 +714,12 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
             }
         }
         wave_lds_fence();
+        // lse is rounded, and a list's probabilities with it: they add up to one
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            weight[g] = weight[g] > 0.5f ? 1.0f / weight[g] : 1.0f;
+            D[g] *= weight[g];
+        }
         for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
             uint64_t mine = opened;
             if (__any(sq.lk > kListKeys)) {                   // (else the codes are still there)
@@ -741,7 +764,7 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
             if ((uint32_t)g >= a.group) break;
             float dq[N];
 #pragma unroll
-            for (int i = 0; i < N; i++) dq[i] = a.scale * (A[g][i] - D[g] * B[g][i]);
+            for (int i = 0; i < N; i++) dq[i] = a.scale * weight[g] * (A[g][i] - D[g] * B[g][i]);
             if (c0 < a.dim)
                 store_values<T, N>((uint8_t *)a.dq.p + (int64_t)b * a.dq.row + (head0 + g) * a.dq.head, c0, a.dim, dq);
         }
@@ -898,10 +921,10 @@ extern "C" int nlb_attention_backward(const nlb_att_call *c, const nlb_att_rows 
     CallDevice device(c->device);
     if (device.rc != NLB_OK) return device.rc;
     a.lse = const_cast<float *>(lse);
-    a.delta = (float *)work;
+    a.stats = (float2 *)work;
     a.split = p.split;
-    a.kpart = (float *)((uint8_t *)work + p.delta_bytes + p.part_bytes);
-    a.part = dbias ? (float *)((uint8_t *)work + p.delta_bytes) : nullptr;
+    a.kpart = (float *)((uint8_t *)work + p.stat_bytes + p.part_bytes);
+    a.part = dbias ? (float *)((uint8_t *)work + p.stat_bytes) : nullptr;
     return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, p, dbias, (hipStream_t)stream)
                                       : launch<float>(a, p, dbias, (hipStream_t)stream);
 }

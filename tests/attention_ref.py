@@ -11,8 +11,8 @@ terms: a probability is off by at most
 relative to itself.  Where probabilities and ds enter a product they are
 rounded to the rows' type (u more), and the product's sum of n terms is off by
 n w times the sum of its terms' magnitudes.  With a = |do| . (sum_j p_j |v_j|):
-  dp is off by dim w |do||v|; D, the row's sum of p dp, taken as do . o from
-the rounded o, by 2 u a plus the e and w terms.
+  dp is off by dim w |do||v|; D, the row's sum of p dp, by the e and w terms
+(fp32 rows without a bias take it as do . o: by 2 u a more).
 """
 import numpy as np
 
@@ -85,7 +85,7 @@ def attention(q, k, v, lq, lk, *, u, causal, scale, bias=None, bounds=None, q_po
             ds = p * (dp - dd)
             dab = np.abs(d) @ np.abs(vv).T
             a = (p * dab).sum(1, keepdims=True)
-            e_d = 2 * u * a + (p * (e + (dim + m) * W) * dab).sum(1, keepdims=True)
+            e_d = (p * (e + (dim + m) * W) * dab).sum(1, keepdims=True) + (2 * W * a if u == W else 0)
             e_ds = np.abs(ds) * (u + e) + p * (dim * W * dab + e_d + 2 * W * (np.abs(dp) + np.abs(dd)))
             gs = n * g
             out["dq"][rows, j] = ds @ kk * scale
@@ -95,8 +95,7 @@ def attention(q, k, v, lq, lk, *, u, causal, scale, bias=None, bounds=None, q_po
             out["dv"][keys, j // g] += p.T @ d
             far["dv"][keys, j // g] += (pe + gs * W * p).T @ np.abs(d)
             if bias is not None:
-                # ds unrounded, D from the probabilities themselves
-                e_d -= 2 * u * a
+                # ds unrounded
                 e_ds = np.abs(ds) * e + p * (dim * W * dab + e_d + 2 * W * (np.abs(dp) + np.abs(dd)))
                 np.add.at(out["dbias"][:, j], bk.reshape(-1), ds.reshape(-1))
                 np.add.at(far["dbias"][:, j], bk.reshape(-1), (e_ds + 256 * W * np.abs(ds)).reshape(-1))
