@@ -379,7 +379,7 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  *   Rows.  q, o: [q_rows][heads][dim], k, v: [k_rows][kv_heads][dim], of type
  * dtype, at any row and head strides (in values, 0 .. 2^31 - 1); a row's dim
  * values are contiguous, so slices of a joint projection need no copy.
- * Written rows must not overlap.
+ * Written rows must not overlap each other or what the call reads.
  *   Open keys.  causal = 1: key j is open to row i if j <= i + lk - lq (i, j
  * counted in the sequence, lq and lk its lengths): the last query row stands
  * at the last key row.  k_pos (device uint32 [k_rows] or NULL): rows with

@@ -785,17 +785,18 @@ inline Backward plan_backward(const Attend &a) {
         p.q_slots = (uint64_t)a.q_rows / (p.narrow_rows ? 32 : kOwned) + a.batch;
         p.k_slots = (uint64_t)a.k_rows / (p.narrow_keys ? 32 : kOwned) + a.batch;
         p.q_most = INT32_MAX / a.heads;
-        p.k_most = INT32_MAX / a.kv_heads;
+        p.k_most = INT32_MAX / a.heads;
         p.parts = a.q_rows ? p.q_slots : 0;
         p.stat_bytes = align256((size_t)a.q_rows * a.heads * 8);
         // Two workgroups of backward_keys run on a CU.  Where key tiles are too
         // few for two turns of them (which causal sequences of one length need
         // to even out), a group's heads are spread over workgroups, whose
         // shares of dk and dv are summed afterwards.
-        const uint64_t tiles = ((uint64_t)a.k_rows / (p.narrow_keys ? 32 : kOwned) + 1) * a.kv_heads;
+        const uint64_t tiles = p.k_slots * a.kv_heads;
         p.split = (uint32_t)std::min<uint64_t>(a.group, (1024 + tiles - 1) / tiles);
     }
-    p.shares = p.parts > 64 ? 64 : 0;
+    // (a workgroup a head sums 2048 partial gradients in 9 us; two steps take 10)
+    p.shares = p.parts > 2048 ? 64 : 0;
     p.part_bytes = align256((p.parts + p.shares) * a.heads * a.buckets * 4);
     p.bytes = p.stat_bytes + p.part_bytes;
     if (p.split > 1) p.bytes += 2 * p.split * (size_t)a.k_rows * a.kv_heads * ((a.dim + 3) / 4) * 16;

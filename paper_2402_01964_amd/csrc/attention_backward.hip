@@ -168,6 +168,9 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     // one pass over the keys: FIRST sums D, the other dq (and the bias gradient)
     const auto pass = [&](auto first_pass) {
         constexpr bool FIRST = decltype(first_pass)::value;
+        f32x16 minus_D;                                       // what the products of do and v start from
+#pragma unroll
+        for (int r = 0; r < 16; r++) minus_D[r] = -D;
         if (kend > 0) {
             fetch(0);
             stage(0, 0);
@@ -192,7 +195,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 #pragma unroll
                 for (int n = 0; n < S::blocks; n++) {
                     const int blk = span.take + n * 32;
-                    f32x16 s = {}, dp = {};
+                    f32x16 s = {}, dp = minus_D;
                     product_rows<KT>(s, kt, blk, q);
                     product_rows<VT>(dp, vt, blk, dout);
                     uint32_t bk[POS == 0 ? 1 : 16];
@@ -231,8 +234,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 #pragma unroll
                     for (int r = 0; r < 16; r++) {
                         const float p = exp2_fast(fmaf(s[r], a.scale2, base));
-                        if constexpr (FIRST) more_D = fmaf(p, dp[r] - D, more_D);
-                        else ds[r] = p * (dp[r] - D);
+                        if constexpr (FIRST) more_D = fmaf(p, dp[r], more_D);
+                        else ds[r] = p * dp[r];
                         if (FIRST && sizeof(T) == 4) weight += p;
                     }
                     if constexpr (!FIRST) {
@@ -784,21 +787,33 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
 
 // ---------------------------------------------------------------- bias gradient
 // Sums n partial tables [heads][buckets] in a fixed order: block (head, p) the
-// p-th of `outs` even shares into out[p]; the last call writes the gradient.
-// 64-bit sums: the terms cancel.
+// p-th of `outs` even shares into out[p], or the gradient itself where out is
+// null; every 16th table a wavefront.  64-bit sums: the terms cancel.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void sum_bias(const float *part, uint32_t n, uint32_t heads, uint32_t buckets,
-                                                     uint32_t outs, float *out, T *dbias) {
-    __shared__ double sums[4][64];
+__global__ __launch_bounds__(1024) void sum_bias(const float *part, uint32_t n, uint32_t heads, uint32_t buckets,
+                                                 uint32_t outs, float *out, T *dbias) {
+    __shared__ double sums[16][64];
     const uint32_t head = blockIdx.x % heads, p = blockIdx.x / heads, lane = threadIdx.x & 63u, w = threadIdx.x >> 6;
-    const uint32_t each = (n + outs - 1) / outs, lo = p * each, hi = min(n, lo + each);
+    const uint32_t each = (n + outs - 1) / outs, hi = min(n, p * each + each);
+    const size_t step = (size_t)heads * buckets;
     double x = 0.0;
-    if (lane < buckets)
-        for (uint32_t i = lo + w; i < hi; i += 4) x += (double)part[((size_t)i * heads + head) * buckets + lane];
+    if (lane < buckets) {
+        const float *t = part + (size_t)head * buckets + lane;
+        uint32_t i = p * each + w;
+        for (; i + 112 < hi; i += 128) {                      // eight loads in flight
+            float v[8];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; u++) v[u] = t[(i + 16 * u) * step];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; u++) x += (double)v[u];
+        }
+        for (; i < hi; i += 16) x += (double)t[i * step];
+    }
     sums[w][lane] = x;
     __syncthreads();
     if (w == 0 && lane < buckets) {
-        x = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+#pragma unroll
+        for (int i = 1; i < 16; i++) x += sums[i][lane];
         if (out) out[((size_t)p * heads + head) * buckets + lane] = (float)x;
         else dbias[(size_t)lane * heads + head] = (T)(float)x;
     }
@@ -888,12 +903,12 @@ template <typename T> int launch(const Attend &a, const Backward &p, void *dbias
         uint32_t n = (uint32_t)p.parts;
         if (p.shares) {
             float *mid = a.part + (size_t)n * a.heads * a.buckets;
-            hipLaunchKernelGGL((sum_bias<T>), dim3(p.shares * a.heads), dim3(kThreads), 0, s, from, n, a.heads,
+            hipLaunchKernelGGL((sum_bias<T>), dim3(p.shares * a.heads), dim3(1024), 0, s, from, n, a.heads,
                                a.buckets, p.shares, mid, (T *)nullptr);
             from = mid;
             n = p.shares;
         }
-        hipLaunchKernelGGL((sum_bias<T>), dim3(a.heads), dim3(kThreads), 0, s, from, n, a.heads, a.buckets, 1u,
+        hipLaunchKernelGGL((sum_bias<T>), dim3(a.heads), dim3(1024), 0, s, from, n, a.heads, a.buckets, 1u,
                            (float *)nullptr, (T *)dbias);
     }
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;

@@ -317,6 +317,37 @@ def test_many_lists_keep_their_heads():
         check(c, [1] * n, [7] * n, run(c, [1] * n, [7] * n, causal=False, one=True), causal=False, dtype="f32")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_heads", [1, 64, 256])
+def test_most_heads_and_buckets(dtype, kv_heads):
+    """256 heads, 64 buckets: the largest tables in LDS."""
+    import torch
+    for one, lq, lk in ((False, [40], [50]), (True, [1] * 3, [20] * 3), (True, [1], [600])):
+        c = make(dtype, lq, lk, 256, kv_heads, 32 if dtype == "bf16" else 16, bias=True, times=True, train=True)
+        c["bounds"] = torch.arange(-100, 215, 5, dtype=torch.int32)
+        c["bias"] = torch.randn(64, 256, generator=torch.Generator().manual_seed(1)).to(_dtype(dtype))
+        check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype=dtype, what=str(lk))
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 50)])
+@pytest.mark.parametrize("mode", ["plain", "places", "times"])
+def test_wide_and_narrow_workgroups(dtype, dim, mode):
+    """Calls large enough for 128 rows a workgroup, ragged ends among them."""
+    lq, lk = [300, 129, 1000, 1], [300, 700, 1000, 64]
+    c = make(dtype, lq, lk, 16, 4, dim, bias=mode != "plain", times=mode == "times", train=True)
+    for causal in (False, True):
+        check(c, lq, lk, run(c, lq, lk, causal=causal), causal=causal, dtype=dtype)
+
+
+def test_longer_and_shorter_than_a_tile_together():
+    """Hundreds of sequences whose starts lie anywhere in the tiles' slots."""
+    rng = np.random.default_rng(3)
+    lq = [int(x) for x in rng.integers(0, 70, 300)]
+    lk = [int(x) for x in rng.integers(0, 70, 300)]
+    c = make("f32", lq, lk, 2, 2, 16, bias=True, train=True)
+    check(c, lq, lk, run(c, lq, lk, causal=True), causal=True, dtype="f32")
+
+
 def test_gradients_against_differences():
     """dq, dk, dv and dbias against differences of the forward pass itself."""
     import torch
@@ -375,14 +406,15 @@ def test_gradient_rows_outside_the_sequences_stay():
         assert (t[:10] == 7).all() and (t[90:] == 7).all() and (t[10:90] != 7).flatten(1).any(-1).all()
 
 
-@pytest.mark.parametrize("one", [False, True])
-def test_captured_training_step(one):
+@pytest.mark.parametrize("one,dim", [(False, 64), (False, 128), (True, 64)])
+def test_captured_training_step(one, dim):
     """Forward and backward captured with their working memory, replayed with
-    new inputs, eager calls between."""
+    new inputs, eager calls between (128 values: kernels with over 64 KiB of
+    LDS)."""
     import torch
     import paper_2402_01964_amd as nlb
-    lq, lk = ([1] * 40, [20] * 40) if one else ([100, 33], [100, 70])
-    cs = [make("bf16", lq, lk, 4, 2, 64, bias=True, times=True, train=True, seed=s) for s in range(2)]
+    lq, lk = ([1] * 40, [20] * 40) if one else ([100, 33], [100, 70]) if dim == 64 else ([700] * 6, [700] * 6)
+    cs = [make("bf16", lq, lk, 4, 2, dim, bias=True, times=True, train=True, seed=s) for s in range(2)]
     how = dict(batch=len(lq), bounds=cs[0]["bounds"].cuda())
     if not one:
         how.update(q_start=torch.from_numpy(ref.starts(lq)).cuda(), k_start=torch.from_numpy(ref.starts(lk)).cuda())
