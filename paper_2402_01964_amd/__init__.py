@@ -562,8 +562,14 @@ def attention(q, k, v, *, batch=None, q_start=None, k_start=None, causal=False, 
     if lse is None:
         lse = q.new_empty(q.shape[:2], dtype=torch.float32)
     o = _AttRows(*_att_rows(out, q, q.shape, "out"))
+    args = c, o, _lse(lse, q)
+    if work is None:                                          # most calls need none: ask only where one is refused
+        rc = lib.nlb_attention(*args, None, 0, _current_stream(q.device))
+        if rc != NLB_ESCRATCH:
+            _check(rc, "nlb_attention")
+            return out, lse
     keep, p, size = _work(lib.nlb_attention_work, c, (0,), work, q, "nlb_attention")
-    _check(lib.nlb_attention(c, o, _lse(lse, q), p, size, _current_stream(q.device)), "nlb_attention")
+    _check(lib.nlb_attention(*args, p, size, _current_stream(q.device)), "nlb_attention")
     return out, lse
 
 

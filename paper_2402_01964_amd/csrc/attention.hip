@@ -64,15 +64,6 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     int32_t qpos = 0;
     if constexpr (POS == 2)
         if (there && a.q_pos) qpos = flip(a.q_pos[sq.q0 + row]);
-    if (POS != 0 && a.buckets) {
-        stage_bias<T>(a, head, buckets.bounds, bias);
-        int32_t *ends = (int32_t *)(buckets.cells + kCells);
-        __syncthreads();
-        if constexpr (POS == 2) {
-            fill_cells(buckets, ends);
-        }
-    }
-
     // keys [0, kend) are open to some row of the workgroup, [0, wend) of the wavefront
     const int32_t last = min(row0 + S::owned, sq.lq) - 1, wrow0 = row0 + (int32_t)span.own;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
@@ -122,10 +113,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
     float m = -INFINITY, sum = 0.0f;
     const float behind = 8.0f / a.scale2;
 
-    if (kend > 0) {
-        fetch(0);
-        stage(0, 0);
+    if (kend > 0) fetch(0);                                    // (in flight beside the bias tables' loads)
+    if (POS != 0 && a.buckets) {
+        stage_bias<T>(a, head, buckets.bounds, bias);
+        int32_t *ends = (int32_t *)(buckets.cells + kCells);
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, ends);
+        }
     }
+    if (kend > 0) stage(0, 0);
     __syncthreads();
     int buf = 0;
     for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= S::buffers - 1) {

@@ -35,7 +35,7 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 // order into part[slot][head][bucket].
 template <typename T, int DP, bool NARROW> constexpr uint32_t rows_lds(uint32_t buckets) {
     return (NARROW ? 1 : 2) * (Tile<T, DP, kBothWays, NARROW>::bytes + Tile<T, DP, kByRows, NARROW>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
-           kCells + kMaxBuckets * 4 + buckets * kThreads * 4;
+           kCells + kMaxBuckets * 4 + (1 + buckets) * kThreads * 4;
 }
 
 __device__ __forceinline__ void add_four(float *column, const uint32_t (&b)[4], const float (&x)[4]) {
@@ -69,7 +69,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     float *bias = (float *)(code + 2 * kGaps);
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets), (uint8_t *)(bias + 2 * kMaxBuckets), a.buckets - 1, 0};
     int32_t *cell_ends = (int32_t *)(buckets.cells + kCells);
-    float *hist = (float *)(cell_ends + kMaxBuckets);         // [buckets][threads]
+    float *shares = (float *)(cell_ends + kMaxBuckets);       // [threads]
+    float *hist = shares + kThreads;                          // [buckets][threads]
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
     const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
@@ -108,16 +109,6 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         D = halves_sum(D);
     }
     float more_D = 0.0f, weight = 0.0f;
-    if (POS != 0 && a.buckets) {
-        stage_bias<T>(a, head, buckets.bounds, bias);
-        if (want)
-            for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
-        __syncthreads();
-        if constexpr (POS == 2) {
-            fill_cells(buckets, cell_ends);
-        }
-    }
-
     const int32_t last = min(row0 + S::owned, sq.lq) - 1, wrow0 = row0 + (int32_t)span.own;
     const int32_t kend = a.causal ? min(sq.lk, last + off + 1) : sq.lk;
     const int32_t wend = a.causal ? min(sq.lk, min(wrow0 + 32, sq.lq) + off) : sq.lk;
@@ -161,6 +152,19 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         }
     };
 
+    if (kend > 0) fetch(0);                                    // (in flight beside the bias tables' loads)
+    if (POS != 0 && a.buckets) {
+        stage_bias<T>(a, head, buckets.bounds, bias);
+        if (want)
+            for (uint32_t i = 0; i < a.buckets; i++) hist[i * kThreads + threadIdx.x] = 0.0f;
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, cell_ends);
+        }
+    }
+    if (kend > 0) stage(0, 0);
+    __syncthreads();
+
     f32x16 acc[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; d++) acc[d] = f32x16{};
@@ -171,11 +175,6 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
         f32x16 minus_D;                                       // what the products of do and v start from
 #pragma unroll
         for (int r = 0; r < 16; r++) minus_D[r] = -D;
-        if (kend > 0) {
-            fetch(0);
-            stage(0, 0);
-        }
-        __syncthreads();
         int buf = 0;
         for (int32_t k0 = 0; k0 < kend; k0 += G::rows, buf ^= S::buffers - 1) {
             const bool more = k0 + G::rows < kend;
@@ -268,10 +267,14 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     };
     if (sizeof(T) == 2 || want) {
         pass(std::true_type{});
+        if (kend > G::rows) {                                 // (else the one tile is still there)
+            fetch(0);
+            stage(0, 0);
+        }
+        __syncthreads();
         const auto row_sum = [&](float x) {
             x = halves_sum(x);
             if constexpr (NARROW) {
-                float *shares = extra;
                 shares[threadIdx.x] = x;
                 __syncthreads();
                 x = shares[lane] + shares[64 + lane] + shares[128 + lane] + shares[192 + lane];
@@ -358,16 +361,6 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     load_owned(k, a.k.p + (int64_t)(sq.k0 + key) * a.k.row + kvh * a.k.head, open, a.dim);
     if constexpr (DK) load_owned(v, a.v.p + (int64_t)(sq.k0 + key) * a.v.row + kvh * a.v.head, open, a.dim);
     sign_owned(k, a.scale);
-    if (POS != 0 && a.buckets) {
-        for (uint32_t g = 0; g < a.group; g++)
-            stage_bias<T>(a, kvh * a.group + g, g ? nullptr : buckets.bounds, bias + g * kMaxBuckets);
-        int32_t *cell_ends = (int32_t *)(buckets.cells + kCells);
-        __syncthreads();
-        if constexpr (POS == 2) {
-            fill_cells(buckets, cell_ends);
-        }
-    }
-
     // rows from `first` on see a key of the workgroup, from `whole` on all of the wavefront's
     const int32_t first = a.causal ? max(0, key0 - off) / G::rows * G::rows : 0;
     const int32_t tiles = sq.lq > first ? (sq.lq - first + G::rows - 1) / G::rows : 0;
@@ -426,10 +419,17 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         if constexpr (DV) dv[d] = f32x16{};
     }
     const int32_t total = tiles * (g1 - g0);
-    if (total > 0) {
-        fetch(g0, first);
-        stage(g0, first, 0);
+    if (total > 0) fetch(g0, first);                           // (in flight beside the bias tables' loads)
+    if (POS != 0 && a.buckets) {
+        for (uint32_t g = 0; g < a.group; g++)
+            stage_bias<T>(a, kvh * a.group + g, g ? nullptr : buckets.bounds, bias + g * kMaxBuckets);
+        int32_t *cell_ends = (int32_t *)(buckets.cells + kCells);
+        __syncthreads();
+        if constexpr (POS == 2) {
+            fill_cells(buckets, cell_ends);
+        }
     }
+    if (total > 0) stage(g0, first, 0);
     __syncthreads();
     int buf = 0;
     int32_t g = g0, i0 = first;
