@@ -593,27 +593,35 @@ template <typename T, int DP> struct Lanes {
 };
 constexpr int kListKeys = 64;            // keys of a list whose open ones are looked up at once
 
-// The open keys among j0 .. j0 + 63 of each lane group's list, as a bit mask
-// in each of its lanes, and their buckets in codes[group][64].  A lane looks
-// up every per_row-th key, so each bucket is searched once.
-template <int PER>
-__device__ __forceinline__ uint64_t open_keys(const Attend &a, const int32_t *bounds, uint8_t *codes, uint32_t k0,
-                                              int32_t lk, int32_t j0, int32_t qpos) {
+// The positions of KEYS (64 at most) keys from j0 on of each lane group's list:
+// a lane loads every PER-th.
+template <int PER, int KEYS> struct ListPositions {
+    uint32_t pos[KEYS / PER];
+    __device__ __forceinline__ void load(const Attend &a, uint32_t k0, int32_t lk, int32_t j0) {
+        const int32_t c = threadIdx.x % PER;
+#pragma unroll
+        for (int i = 0; i < KEYS / PER; i++) {
+            const int32_t j = j0 + i * PER + c;
+            pos[i] = j < lk ? (uint32_t)j : kNoKey;
+            if (a.k_pos && j < lk) pos[i] = a.k_pos[k0 + j];
+        }
+    }
+};
+
+// The open keys among them as a bit mask in each lane of the group, and their
+// buckets in codes[group][64]: each is searched once.
+template <int PER, int KEYS>
+__device__ __forceinline__ uint64_t open_keys(const Attend &a, const int32_t *bounds, uint8_t *codes,
+                                              const ListPositions<PER, KEYS> &at, int32_t lk, int32_t j0, int32_t qpos) {
     const uint32_t lane = threadIdx.x & 63u, c = lane % PER, base = lane - c;
     uint64_t mine = 0;
 #pragma unroll
-    for (int i = 0; i < kListKeys / PER; i++) {
+    for (int i = 0; i < KEYS / PER; i++) {
         if (!__any(j0 + i * PER < lk)) break;
-        const int32_t j = j0 + i * PER + c;
-        uint32_t pos = j;
-        bool open = j < lk;
-        if (a.k_pos && open) {
-            pos = a.k_pos[k0 + j];
-            open = pos != kNoKey;
-        }
-        const uint64_t m = __ballot(open);
+        const uint64_t m = __ballot(at.pos[i] != kNoKey);
         mine |= ((m >> base) & ((1ull << PER) - 1)) << (i * PER);
-        if (a.buckets) codes[base / PER * kListKeys + i * PER + c] = bucket_of(bounds, a.buckets, gap_of(qpos, flip(pos)));
+        if (a.buckets)
+            codes[base / PER * kListKeys + i * PER + c] = bucket_of(bounds, a.buckets, gap_of(qpos, flip(at.pos[i])));
     }
     return mine;
 }
@@ -755,13 +763,16 @@ struct Backward {
     size_t stat_bytes, part_bytes, bytes;
 };
 
-// Short lists with one query row take a group of lanes each; a group's heads
-// are in registers there, four at most.  Everything else, single rows over
-// long histories among it, goes through tiles, whose second kernel spreads
-// over the keys.
+// Short lists with one query row, and longer ones where they are many, take a
+// group of lanes each; a group's heads are in registers there, four at most.
+// Everything else, single rows over long histories among it, goes through
+// tiles, whose second kernel spreads over the keys.
+constexpr uint64_t kManyLists = 16384;
+
 inline Backward plan_backward(const Attend &a) {
     Backward p = {};
-    p.lists = !a.q_start && a.q_len == 1 && a.group <= 4 && short_lists(a);
+    p.lists = !a.q_start && a.q_len == 1 && a.group <= 4 &&
+              (short_lists(a) || (a.k_rows / 1024 <= a.batch && (uint64_t)a.batch * a.kv_heads >= kManyLists));
     if (p.lists) {
         const uint32_t n = a.dtype_bytes == 2 ? 8 : 4, dp = a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128;
         const uint32_t rows = 64 / (dp / n), gb = a.group > 2 ? 4 : a.group;

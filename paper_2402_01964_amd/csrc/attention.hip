@@ -470,6 +470,7 @@ template <typename T, int DP, int GB>
 __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
     using L = Lanes<T, DP>;
     constexpr int N = Chunk<T>::n, U = 4;
+    constexpr int K = std::min(kListKeys, 4 * L::per_row);    // (more positions in registers cost a wavefront)
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     int32_t *bounds = (int32_t *)lds;
     float *bias = (float *)(bounds + kMaxBuckets);            // [buckets][heads]
@@ -493,13 +494,20 @@ __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
         Seq sq;
         sequence(a, b, sq);
         if (!there) sq.lk = 0;
+        // (the first positions are in flight with q)
+        u32x4 raw[GB];
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            raw[g] = u32x4{0, 0, 0, 0};
+            if ((uint32_t)g < ng)
+                raw[g] = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
+        }
+        ListPositions<L::per_row, K> keys;
+        keys.load(a, sq.k0, sq.lk, 0);
         float q[GB][N], acc[GB][N], m[GB], sum[GB];
 #pragma unroll
         for (int g = 0; g < GB; g++) {
-            u32x4 x = {0, 0, 0, 0};
-            if ((uint32_t)g < ng)
-                x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
-            unpack<T>(x, q[g]);
+            unpack<T>(raw[g], q[g]);
 #pragma unroll
             for (int i = 0; i < N; i++) {
                 q[g][i] *= a.signed2;
@@ -511,9 +519,10 @@ __global__ __launch_bounds__(kThreads) void attend_lists(Attend a) {
         const int32_t qpos = a.buckets ? (a.q_pos ? flip(a.q_pos[b]) : flip((uint32_t)sq.lk - 1)) : 0;
         const uint8_t *kp = a.k.p + (int64_t)sq.k0 * a.k.row + kvh * a.k.head;
         const uint8_t *vp = a.v.p + (int64_t)sq.k0 * a.v.row + kvh * a.v.head;
-        for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
+        for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += K) {
+            if (j0) keys.load(a, sq.k0, sq.lk, j0);
             wave_lds_fence();
-            uint64_t mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+            uint64_t mine = open_keys(a, bounds, codes, keys, sq.lk, j0, qpos);
             wave_lds_fence();
             while (__any(mine != 0)) {
                 u32x4 k[U], v[U];

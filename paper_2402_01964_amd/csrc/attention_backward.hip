@@ -596,19 +596,27 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
         Seq sq;
         sequence(a, b, sq);
         if (!there) sq.lk = 0;
+        // (the first positions are in flight with q and do)
+        u32x4 rawq[GB], rawo[GB];
         float q[GB][N], dout[GB][N], A[GB][N], B[GB][N], lse[GB], first[GB], D[GB], weight[GB];
 #pragma unroll
         for (int g = 0; g < GB; g++) {
-            u32x4 x = {0, 0, 0, 0}, y = x;
-            lse[g] = INFINITY;
-            first[g] = D[g] = weight[g] = 0.0f;
+            rawq[g] = rawo[g] = u32x4{0, 0, 0, 0};
+            lse[g] = -INFINITY;
             if ((uint32_t)g < a.group) {
-                x = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
-                y = load_chunk<T>(a.dout.p + (int64_t)b * a.dout.row + (head0 + g) * a.dout.head, c0, a.dim);
-                lse[g] = row_log2(a.lse[(size_t)b * a.heads + head0 + g]);
+                rawq[g] = load_chunk<T>(a.q.p + (int64_t)b * a.q.row + (head0 + g) * a.q.head, c0, a.dim);
+                rawo[g] = load_chunk<T>(a.dout.p + (int64_t)b * a.dout.row + (head0 + g) * a.dout.head, c0, a.dim);
+                lse[g] = a.lse[(size_t)b * a.heads + head0 + g];
             }
-            unpack<T>(x, q[g]);
-            unpack<T>(y, dout[g]);
+        }
+        ListPositions<L::per_row, kListKeys> keys;
+        keys.load(a, sq.k0, sq.lk, 0);
+#pragma unroll
+        for (int g = 0; g < GB; g++) {
+            lse[g] = row_log2(lse[g]);
+            first[g] = D[g] = weight[g] = 0.0f;
+            unpack<T>(rawq[g], q[g]);
+            unpack<T>(rawo[g], dout[g]);
 #pragma unroll
             for (int i = 0; i < N; i++) A[g][i] = B[g][i] = 0.0f;
         }
@@ -693,8 +701,9 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
 
         uint64_t opened = 0;                                  // of the list's first 64 keys
         for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
+            if (j0) keys.load(a, sq.k0, sq.lk, j0);
             wave_lds_fence();
-            uint64_t mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+            uint64_t mine = open_keys(a, bounds, codes, keys, sq.lk, j0, qpos);
             wave_lds_fence();
             if (j0 == 0) opened = mine;
             while (__any(mine != 0)) {
@@ -726,8 +735,9 @@ __global__ __launch_bounds__(kThreads) void backward_lists(Attend a, uint32_t ke
         for (int32_t j0 = 0; __any(j0 < sq.lk); j0 += kListKeys) {
             uint64_t mine = opened;
             if (__any(sq.lk > kListKeys)) {                   // (else the codes are still there)
+                keys.load(a, sq.k0, sq.lk, j0);
                 wave_lds_fence();
-                mine = open_keys<L::per_row>(a, bounds, codes, sq.k0, sq.lk, j0, qpos);
+                mine = open_keys(a, bounds, codes, keys, sq.lk, j0, qpos);
                 wave_lds_fence();
             }
             // rows of closed keys
