@@ -342,7 +342,8 @@ template <typename T, int DP, Use USE, bool NARROW> struct Tile {
 // next tile is staged in a second buffer.  A NARROW workgroup owns 32 rows;
 // tiles have 128 rows, a wavefront takes every fourth 32 of them, and their
 // results are joined at the end: for sequences of few rows, and for calls of
-// few workgroups, whose time is that of one workgroup's way along its tiles.
+// few workgroups, whose time is that of one workgroup's way along its tiles (37
+// sequences of up to 1000 keys, two fp32 heads of 50: 207 and 62 us).
 template <bool NARROW, int ROWS> struct Span {
     static constexpr int owned = NARROW ? 32 : kOwned;
     static constexpr int buffers = NARROW ? 1 : 2;
@@ -612,7 +613,8 @@ template <int PER, int KEYS> struct ListPositions {
 // buckets in codes[group][64]: each is searched once.
 template <int PER, int KEYS>
 __device__ __forceinline__ uint64_t open_keys(const Attend &a, const int32_t *bounds, uint8_t *codes,
-                                              const ListPositions<PER, KEYS> &at, int32_t lk, int32_t j0, int32_t qpos) {
+                                              const ListPositions<PER, KEYS> &at, int32_t lk, int32_t j0,
+                                              int32_t qpos) {
     const uint32_t lane = threadIdx.x & 63u, c = lane % PER, base = lane - c;
     uint64_t mine = 0;
 #pragma unroll
@@ -711,7 +713,8 @@ enum Form { kTiles, kOne, kLists };
 constexpr uint64_t kNarrowBlocks = 128;
 
 // Calls of tiles: narrow workgroups where sequences have 64 owned rows or fewer
-// on average, or where the others are so few that half of the card idles.
+// on average, or where the others are so few that half of the card idles (480
+// of the others, 8 sequences of 128 to 2048 rows: 49 us, narrow 62).
 inline bool narrow_tiles(const Attend &a, uint64_t rows, uint32_t heads) {
     if ((a.dim <= 32 ? 32 : a.dim <= 64 ? 64 : 128) * a.dtype_bytes > 256) return false;   // (LDS)
     return rows / 64 <= a.batch || (rows / kOwned + 1) * heads <= kNarrowBlocks;
@@ -725,11 +728,15 @@ struct Forward {
     size_t bytes;
 };
 
-// One query row per sequence.  Short lists, many of them, take a group of
-// lanes each (kLists).  Else a wavefront takes a list (kOne), or where lists
+// One query row per sequence.  Many short lists take a group of lanes each
+// (kLists).  Else a wavefront takes a list (kOne), or where lists
 // are too few to fill the card (8 wavefronts on each of 1024 SIMDs) a chunk of
 // its keys, of 256 rows at least, so that what a chunk writes stays below a
 // hundredth of what it reads.
+// Lists times key/value heads from which a group of lanes each fills the card
+// (4000 lists of 63 slots in two heads, bf16: 37 us, a wavefront each 28; 8000:
+// 44 and 49; 6000 of 10 slots: 14 and 18).
+constexpr uint64_t kManyLists = 8192;
 inline bool short_lists(const Attend &a) { return a.k_rows / kListKeys <= a.batch; }
 
 inline Forward plan_forward(const Attend &a) {
@@ -743,7 +750,7 @@ inline Forward plan_forward(const Attend &a) {
     f.most = INT32_MAX;
     f.slots = a.batch;
     f.form = kLists;
-    if (short_lists(a)) return f;
+    if (short_lists(a) && (uint64_t)a.batch * a.kv_heads >= kManyLists) return f;
     f.form = kOne;
     const uint64_t even = ((uint64_t)a.k_rows * a.kv_heads + 8191) / 8192;
     f.chunk = (uint32_t)(((even < 256 ? 256 : even) + 63) / 64 * 64);
@@ -767,8 +774,6 @@ struct Backward {
 // group of lanes each; a group's heads are in registers there, four at most.
 // Everything else, single rows over long histories among it, goes through
 // tiles, whose second kernel spreads over the keys.
-constexpr uint64_t kManyLists = 16384;
-
 inline Backward plan_backward(const Attend &a) {
     Backward p = {};
     p.lists = !a.q_start && a.q_len == 1 && a.group <= 4 &&

@@ -33,8 +33,13 @@ __device__ __forceinline__ float row_log2(float lse) { return lse == -INFINITY ?
 // the pass four times as long).  Tiles whose gaps all lie in the first or the
 // last bucket add to a register.  The columns are summed at the end in a fixed
 // order into part[slot][head][bucket].
+//
+// Measured: 8095 causal rows in two sequences, 16 heads of 128 bf16 values: 365
+// us for five products (920 TFLOP/s); 7584 rows in 8 sequences, 8 heads of 64
+// with the bias and its gradient 108 us, 523 with atomics on its table.
 template <typename T, int DP, bool NARROW> constexpr uint32_t rows_lds(uint32_t buckets) {
-    return (NARROW ? 1 : 2) * (Tile<T, DP, kBothWays, NARROW>::bytes + Tile<T, DP, kByRows, NARROW>::bytes) + 2 * kGaps * 8 + kMaxBuckets * 8 +
+    return (NARROW ? 1 : 2) * (Tile<T, DP, kBothWays, NARROW>::bytes + Tile<T, DP, kByRows, NARROW>::bytes) +
+           2 * kGaps * 8 + kMaxBuckets * 8 +
            kCells + kMaxBuckets * 4 + (1 + buckets) * kThreads * 4;
 }
 
@@ -190,7 +195,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
                     far = one_bucket(buckets.bounds, a.buckets, least(k0), least(k0) + S::owned + G::rows - 2, one);
                     if (far) base = fmaf(bias[one], a.scale2, base);
                 }
-                if constexpr (POS == 2) shut = __any(((const int32_t *)ex)[span.take + lane % S::rows] == kNoKeyFlipped);
+                if constexpr (POS == 2)
+                    shut = __any(((const int32_t *)ex)[span.take + lane % S::rows] == kNoKeyFlipped);
 #pragma unroll
                 for (int n = 0; n < S::blocks; n++) {
                     const int blk = span.take + n * 32;
@@ -247,9 +253,9 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
                         } else if (want) {
 #pragma unroll
                             for (int r = 0; r < 16; r += 4) {
-                                const uint32_t four[4] = {bk[r % (POS == 0 ? 1 : 16)], bk[(r + 1) % (POS == 0 ? 1 : 16)],
-                                                       bk[(r + 2) % (POS == 0 ? 1 : 16)],
-                                                       bk[(r + 3) % (POS == 0 ? 1 : 16)]};
+                                constexpr int kept = POS == 0 ? 1 : 16;
+                                const uint32_t four[4] = {bk[r % kept], bk[(r + 1) % kept], bk[(r + 2) % kept],
+                                                          bk[(r + 3) % kept]};
                                 const float x[4] = {ds[r], ds[r + 1], ds[r + 2], ds[r + 3]};
                                 add_four(hist + threadIdx.x, four, x);
                             }
@@ -323,8 +329,10 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
 // WHAT: 1 dv, 2 dk, 3 both.  Both at once keep k, v, dk and dv of a
 // wavefront's keys in registers: rows of 256 bytes and more take two launches
 // instead, which compute the scores twice and run two wavefronts on a SIMD
-// where the one would run one (rows of 128 bf16 values, 8095 rows in two
-// sequences, 16 heads in 4 groups: 1030 us in one launch).
+// where the one would run one.  Measured (8095 causal rows in two sequences, 16
+// heads in 4 groups of 128 bf16 values, a group's heads on four workgroups): 185
+// and 245 us for two and three products, 24 for the sum of the heads; in one
+// launch 565 us, and with a group on one workgroup 1030.
 template <typename T, int DP, bool NARROW> constexpr uint32_t keys_lds(uint32_t group, bool bias) {
     return (NARROW ? 2 : 4) * Tile<T, DP, kBothWays, NARROW>::bytes +
            2 * (kGaps + 2 * Tile<T, DP, kBothWays, NARROW>::rows) * 4 +
@@ -339,7 +347,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     constexpr bool DK = WHAT & 2, DV = WHAT & 1;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int kExtra = kGaps + 2 * G::rows;
-    float *extra = (float *)(lds + S::buffers * 2 * G::bytes);             // [2]: L, D of the tile's rows; bias by gap, or positions
+    // [2]: L, D of the tile's rows; bias by gap, or positions
+    float *extra = (float *)(lds + S::buffers * 2 * G::bytes);
     float *bias = extra + 2 * kExtra;                         // [group][buckets]
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets * a.group), (uint8_t *)(bias + kMaxBuckets * (1 + a.group)),
                        a.buckets - 1, 0};
@@ -559,7 +568,8 @@ template <typename T> __global__ __launch_bounds__(kThreads) void sum_heads(Atte
 // and ds_j = p_j (d_j - D'), so dk_j = scale ds_j q and dv_j = p_j do need
 // neither k nor v again: p_j and d_j of the list's first `keep` keys wait in
 // LDS, a longer list is read again for the others.  Bound by reading k and v
-// and writing dk and dv once.
+// and writing dk and dv once.  Measured: 12 000 lists of 20 slots, two heads of 50
+// fp32 values (0.33 GB): 96 us, 3.4 TB/s.
 struct PD {
     float p, d;
 };
