@@ -44,6 +44,7 @@ constexpr int32_t kNoKeyFlipped = INT32_MAX;
 constexpr int kThreads = 256;            // four wavefronts, everywhere
 constexpr int kOwned = 128;              // rows that a tiled workgroup owns, 32 per wavefront
 constexpr int kMaxBuckets = NLB_ATT_MAX_BUCKETS;
+constexpr uint32_t kMostRows = INT32_MAX - 1023;   // a tile past any row still has a 32-bit place
 static_assert(kMaxBuckets == 64, "bucket_of takes six steps");
 constexpr float kBiasCloses = -0x1p100f; // bias values at or below this close their bucket
 
@@ -291,7 +292,7 @@ __device__ __forceinline__ void fill_cells(Buckets &t, int32_t *ends) {
         if (ends[below + step - 1] < c) below += step;
         if (ends[upto + step - 1] <= c) upto += step;
     }
-    t.cells[c] = (uint8_t)below;
+    t.cells[c] = (uint8_t)min(below, t.last);                 // (also where bounds do not increase)
     uint32_t in = upto - below;
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) in = max(in, (uint32_t)__shfl_xor((int)in, w));
@@ -657,7 +658,7 @@ inline int fill_call(const nlb_att_call *c, Attend &a) {
     const float size = std::fabs(c->scale);
     if (!(size == 0.0f || (size >= 0x1p-20f && size <= 0x1p20f))) return NLB_EINVAL;
     if (c->causal != 0 && c->causal != 1) return NLB_EINVAL;
-    if (c->batch < 1 || c->batch > INT32_MAX / NLB_ATT_MAX_HEADS || c->q_rows > INT32_MAX || c->k_rows > INT32_MAX)
+    if (c->batch < 1 || c->batch > INT32_MAX / NLB_ATT_MAX_HEADS || c->q_rows > kMostRows || c->k_rows > kMostRows)
         return NLB_EINVAL;
     if ((!c->q_start && c->q_rows % c->batch) || (!c->k_start && c->k_rows % c->batch)) return NLB_EINVAL;
     if (c->buckets < 0 || c->buckets > NLB_ATT_MAX_BUCKETS) return NLB_EINVAL;

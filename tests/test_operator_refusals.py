@@ -26,7 +26,7 @@ ROWS = nlb._AttRows(P, 256, 64)
 BAD_CALLS = [
     dict(dtype=2), dict(heads=0), dict(heads=257, kv_heads=257), dict(kv_heads=0), dict(kv_heads=3), dict(dim=0),
     dict(dim=129), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=2.0**21), dict(scale=2.0**-21), dict(causal=2), dict(batch=0), dict(batch=2**31),
-    dict(q_rows=2**31), dict(k_rows=2**31), dict(q_rows=11), dict(k_rows=11), dict(buckets=-1), dict(buckets=65, bias=P,
+    dict(q_rows=2**31), dict(k_rows=2**31), dict(q_rows=2**31 - 1023, q_start=P), dict(k_rows=2**31 - 1023, k_start=P), dict(q_rows=11), dict(k_rows=11), dict(buckets=-1), dict(buckets=65, bias=P,
                                                                                                      bounds=P),
     dict(buckets=4), dict(bias=P), dict(buckets=4, bias=P), dict(buckets=4, bias=P, bounds=P + 2),
     dict(buckets=4, bias=P + 1, bounds=P), dict(q_pos=P), dict(q_start=P + 1), dict(k_start=P + 2), dict(k_pos=P + 1),
@@ -69,7 +69,7 @@ def test_attention_work_is_checked():
 
 def test_attention_grid_limit():
     lib = nlb.load_library()
-    c = _call(heads=256, kv_heads=256, q_rows=2**31 - 1, q_start=P)
+    c = _call(heads=256, kv_heads=256, q_rows=2**31 - 1024, q_start=P)
     assert lib.nlb_attention(ctypes.byref(c), ROWS, None, None, 0, None) == nlb.NLB_EINVAL
 
 
@@ -105,7 +105,7 @@ def test_attention_backward_work_is_checked():
         assert n.value > 0
         for work, size in ((P, n.value - 1), (None, n.value), (None, 0)):
             assert _backward(lib, c, work=work, size=size) == nlb.NLB_ESCRATCH
-    c = _call(heads=256, kv_heads=256, k_rows=2**31 - 1, k_start=P)
+    c = _call(heads=256, kv_heads=256, k_rows=2**31 - 1024, k_start=P)
     assert _backward(lib, c, work=P, size=1 << 50) == nlb.NLB_EINVAL      # more workgroups than a grid has
 
 
