@@ -212,6 +212,30 @@ def test_bias_that_closes_a_bucket(dtype, one, low):
         check(c, lq, lk, run(c, lq, lk, causal=True, one=one), causal=True, dtype=dtype, what=str(shut))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode", ["places", "times"])
+@pytest.mark.parametrize("one", [False, True])
+def test_bounds_that_do_not_increase(dtype, mode, one):
+    """Equal bounds have empty buckets between them.  Falling ones leave open
+    which bucket a gap is in, but it is one of them: with the same bias in all
+    of them that is the one answer."""
+    import torch
+    lq, lk = ([1] * 5, [300, 1, 70, 0, 33]) if one else ([200, 33], [260, 70])
+    c = make(dtype, lq, lk, 4, 2, 32, bias=True, times=mode == "times", train=True)
+    c["bounds"] = torch.tensor([-5, 0, 0, 0, 4, 4, 30, 30], dtype=torch.int32)
+    check(c, lq, lk, run(c, lq, lk, causal=False, one=one), causal=False, dtype=dtype, what="equal")
+    c["bias"] = c["bias"][:1].expand(9, 4).contiguous()
+    got = run(dict(c, bounds=torch.tensor([100, 30, 9, 4, 2, 1, 0, -5], dtype=torch.int32)), lq, lk, causal=False,
+              one=one)
+    assert torch.isfinite(got.pop("dbias")).all()
+    want, far = ref.attention(*(_f64(c[n]) for n in "qkv"), lq, lk, u=HALF_STEP[dtype], causal=False,
+                              scale=32 ** -0.5, bias=_f64(c["bias"]), bounds=BOUNDS, q_pos=_u32(c["q_pos"]),
+                              k_pos=_u32(c["k_pos"]), do=_f64(c["do"]))
+    for n, x in got.items():
+        fine = np.isfinite(want[n])
+        assert (np.abs(x.double().cpu().numpy()[fine] - want[n][fine]) <= far[n][fine]).all(), n
+
+
 def test_gaps_of_unsigned_positions_are_clamped():
     """Positions over the whole unsigned range; gaps beyond int32."""
     import torch
