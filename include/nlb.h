@@ -388,11 +388,11 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  * some rows only must hold finite values, or those rows may become NaN.
  *   scale: 0, or of a magnitude from 2^-20 to 2^20.
  *   Bias.  buckets = 0: none (bias NULL).  Else bias is a device array
- * [buckets][heads] of dtype, bounds a device int32 [buckets - 1], none below the
- * one before it, and bucket(x) the number of bounds <= x.  Positions are q_pos (device uint32
- * [q_rows]) and k_pos, whose difference is clamped to int32 (as nlb_sample's
- * tq and ts go in), or without either the places i + lk - lq and j.  A bias at
- * or below -2^100 closes its bucket.
+ * [buckets][heads] of dtype, bounds a device int32 [buckets - 1], none
+ * below the one before it, and bucket(x) the number of bounds <= x.  Positions
+ * are q_pos (device uint32 [q_rows]) and k_pos, whose difference is clamped to
+ * int32 (as nlb_sample's tq and ts go in), or without either the places
+ * i + lk - lq and j.  A bias at or below -2^100 closes its bucket.
  *   Numerics.  Sums, the softmax's maximum and sum, and lse are fp32.  bf16
  * rows: products of bf16 values are exact in fp32, softmax weights enter the
  * second product as bf16 (in the single-row form as fp32), o is rounded once.
