@@ -403,8 +403,9 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  * may be NULL where no backward pass follows.  Only enqueues kernels: may be
  * captured in a HIP graph.  No table is involved; device names the device of
  * the arrays and the stream (-1: the current one).  Errors: NLB_EINVAL (as
- * above; more than 2^31 - 1024 rows; sizes whose grid passes 2^31 - 1
- * workgroups), NLB_ESCRATCH (work_bytes too few), NLB_EDEVICE. */
+ * above; more than 2^31 - 1024 rows; more than 2^31 - 1 workgroups, of which
+ * a head takes one for each sequence and each 32 or 128 rows),
+ * NLB_ESCRATCH (work_bytes too few), NLB_EDEVICE. */
 #define NLB_ATT_MAX_DIM 128
 #define NLB_ATT_MAX_HEADS 256
 #define NLB_ATT_MAX_BUCKETS 64

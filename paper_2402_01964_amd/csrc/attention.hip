@@ -57,7 +57,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_tiles(Attend a) {
 
     // heads of one key/value head follow each other at a distance of kv_heads:
     // workgroups that are dispatched to one XCD share keys and values
-    const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
+    const uint32_t id = a.first + blockIdx.x, hid = id % a.heads, slot = a.slots - 1 - id / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
     Seq sq;
     const uint32_t b = slot_owner(a.q_start, a.q_len, a.q_rows, a.batch, S::owned, slot, sq.tile);
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(kThreads) void attend_one(Attend a) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void attend_join(Attend a) {
     __shared__ float tops[4], sums[4], values[4][128];
-    const uint32_t b = blockIdx.x / a.heads, head = blockIdx.x % a.heads;
+    const uint32_t id = a.first + blockIdx.x, b = id / a.heads, head = id % a.heads;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     Seq sq;
     sequence(a, b, sq);
@@ -623,7 +623,7 @@ int launch_tiles(const Attend &a, hipStream_t stream) {
                                    : attend_tiles<T, DP, 0, EXACT, NARROW>;
     constexpr uint32_t bytes = tiles_lds<T, DP, NARROW>();
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
-    hipLaunchKernelGGL(kernel, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
+    enqueue_blocks(kernel, a, (uint64_t)a.slots * a.heads, bytes, stream);
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
@@ -646,8 +646,7 @@ int launch_single(const Attend &a, Form form, hipStream_t stream) {
         if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
         const uint64_t need = ((uint64_t)a.slots * a.kv_heads * parts + 3) / 4;
         hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(need, 256 * 8)), dim3(kThreads), bytes, stream, a);
-        if (a.slots != a.batch)
-            hipLaunchKernelGGL((attend_join<T>), dim3(a.batch * a.heads), dim3(kThreads), 0, stream, a);
+        if (a.slots != a.batch) enqueue_blocks(attend_join<T>, a, (uint64_t)a.batch * a.heads, 0, stream);
     }
     return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }

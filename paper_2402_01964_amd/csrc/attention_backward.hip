@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > (POS ? 128 : 256) ? 1 : 
     float *shares = (float *)(cell_ends + kMaxBuckets);       // [threads]
     float *hist = shares + kThreads;                          // [buckets][threads]
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = lane & 31u;
-    const uint32_t hid = blockIdx.x % a.heads, slot = a.slots - 1 - blockIdx.x / a.heads;
+    const uint32_t id = a.first + blockIdx.x, hid = id % a.heads, slot = a.slots - 1 - id / a.heads;
     const uint32_t kvh = hid % a.kv_heads, head = kvh * a.group + hid / a.kv_heads;
     const bool want = POS != 0 && a.part;                     // the bias gradient
     Seq sq;
@@ -353,8 +353,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
     Buckets buckets = {(int32_t *)(bias + kMaxBuckets * a.group), (uint8_t *)(bias + kMaxBuckets * (1 + a.group)),
                        a.buckets - 1, 0};
     const uint32_t lane = threadIdx.x & 63u, col = lane & 31u;
-    const uint32_t kvh = blockIdx.x % a.kv_heads, share = blockIdx.x / a.kv_heads % a.split;
-    const uint32_t slot = blockIdx.x / (a.kv_heads * a.split);
+    const uint32_t id = a.first + blockIdx.x, kvh = id % a.kv_heads, share = id / a.kv_heads % a.split;
+    const uint32_t slot = id / (a.kv_heads * a.split);
     // query heads of the group: this workgroup's share
     const int32_t g0 = a.group * share / a.split, g1 = a.group * (share + 1) / a.split;
     Seq sq;
@@ -848,7 +848,7 @@ int launch_rows(const Attend &a, hipStream_t stream) {
                                  : backward_rows<T, DP, 0, EXACT, NARROW>;
     const uint32_t bytes = rows_lds<T, DP, NARROW>(a.part ? a.buckets : 0);
     if (!allow_lds(rows, bytes)) return NLB_EDEVICE;
-    hipLaunchKernelGGL(rows, dim3(a.slots * a.heads), dim3(kThreads), bytes, stream, a);
+    enqueue_blocks(rows, a, (uint64_t)a.slots * a.heads, bytes, stream);
     return NLB_OK;
 }
 
@@ -860,7 +860,7 @@ int launch_keys(const Attend &a, hipStream_t stream) {
                                  : backward_keys<T, DP, 0, WHAT, EXACT, NARROW>;
     const uint32_t bytes = keys_lds<T, DP, NARROW>(a.group, a.buckets > 0);
     if (!allow_lds(keys, bytes)) return NLB_EDEVICE;
-    hipLaunchKernelGGL(keys, dim3(a.slots * a.kv_heads * a.split), dim3(kThreads), bytes, stream, a);
+    enqueue_blocks(keys, a, (uint64_t)a.slots * a.kv_heads * a.split, bytes, stream);
     return NLB_OK;
 }
 
