@@ -705,18 +705,23 @@ inline bool exact_rows(const Attend &a, const Strided &r) {
 // Kernels that take more LDS than 64 KiB need to be allowed it.
 template <typename K> bool allow_lds(K kernel, uint32_t bytes) {
     if (bytes <= 65536) return true;
-    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
+        return true;
+    (void)hipGetLastError();
+    return false;
 }
 
 // Starts `blocks` (2^31 - 1 at most) workgroups.  A launch holds fewer than
 // 2^32 work items, so more than 2^24 - 1 workgroups (a million sequences with
 // 16 heads) take several launches, each of which is told its first one.
-template <typename K> void enqueue_blocks(K kernel, Attend a, uint64_t blocks, uint32_t lds, hipStream_t stream) {
+inline int enqueue_blocks(void (*kernel)(Attend), Attend a, uint64_t blocks, uint32_t lds, hipStream_t stream) {
     constexpr uint64_t most = (1ull << 32) / kThreads - 1;
     for (uint64_t first = 0; first < blocks; first += most) {
         a.first = (uint32_t)first;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(most, blocks - first)), dim3(kThreads), lds, stream, a);
+        const int rc = enqueue(kernel, (uint32_t)std::min(most, blocks - first), kThreads, lds, stream, a);
+        if (rc != NLB_OK) return rc;
     }
+    return NLB_OK;
 }
 
 inline size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }

@@ -623,8 +623,7 @@ int launch_tiles(const Attend &a, hipStream_t stream) {
                                    : attend_tiles<T, DP, 0, EXACT, NARROW>;
     constexpr uint32_t bytes = tiles_lds<T, DP, NARROW>();
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
-    enqueue_blocks(kernel, a, (uint64_t)a.slots * a.heads, bytes, stream);
-    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+    return enqueue_blocks(kernel, a, (uint64_t)a.slots * a.heads, bytes, stream);
 }
 
 template <typename T, int DP>
@@ -640,15 +639,15 @@ int launch_single(const Attend &a, Form form, hipStream_t stream) {
         bytes += rows * kListKeys;
         if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
         const uint64_t need = ((uint64_t)a.batch * a.kv_heads * parts + rows - 1) / rows;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(need, 256 * 8)), dim3(kThreads), bytes, stream, a);
+        return enqueue(kernel, (uint32_t)std::min<uint64_t>(need, 256 * 8), kThreads, bytes, stream, a);
     } else {
         const auto kernel = gb == 4 ? attend_one<T, DP, 4> : gb == 2 ? attend_one<T, DP, 2> : attend_one<T, DP, 1>;
         if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
         const uint64_t need = ((uint64_t)a.slots * a.kv_heads * parts + 3) / 4;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min<uint64_t>(need, 256 * 8)), dim3(kThreads), bytes, stream, a);
-        if (a.slots != a.batch) enqueue_blocks(attend_join<T>, a, (uint64_t)a.batch * a.heads, 0, stream);
+        const int rc = enqueue(kernel, (uint32_t)std::min<uint64_t>(need, 256 * 8), kThreads, bytes, stream, a);
+        if (rc != NLB_OK || a.slots == a.batch) return rc;
+        return enqueue_blocks(attend_join<T>, a, (uint64_t)a.batch * a.heads, 0, stream);
     }
-    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
 }
 
 template <typename T, int DP> int launch_form(const Attend &a, const Forward &f, hipStream_t s) {

@@ -848,8 +848,7 @@ int launch_rows(const Attend &a, hipStream_t stream) {
                                  : backward_rows<T, DP, 0, EXACT, NARROW>;
     const uint32_t bytes = rows_lds<T, DP, NARROW>(a.part ? a.buckets : 0);
     if (!allow_lds(rows, bytes)) return NLB_EDEVICE;
-    enqueue_blocks(rows, a, (uint64_t)a.slots * a.heads, bytes, stream);
-    return NLB_OK;
+    return enqueue_blocks(rows, a, (uint64_t)a.slots * a.heads, bytes, stream);
 }
 
 template <typename T, int DP, int WHAT, bool EXACT, bool NARROW>
@@ -860,8 +859,7 @@ int launch_keys(const Attend &a, hipStream_t stream) {
                                  : backward_keys<T, DP, 0, WHAT, EXACT, NARROW>;
     const uint32_t bytes = keys_lds<T, DP, NARROW>(a.group, a.buckets > 0);
     if (!allow_lds(keys, bytes)) return NLB_EDEVICE;
-    enqueue_blocks(keys, a, (uint64_t)a.slots * a.kv_heads * a.split, bytes, stream);
-    return NLB_OK;
+    return enqueue_blocks(keys, a, (uint64_t)a.slots * a.kv_heads * a.split, bytes, stream);
 }
 
 template <typename T, int DP, bool EXACT, bool NARROW> int launch_both_keys(const Attend &a, hipStream_t stream) {
@@ -892,7 +890,7 @@ template <typename T, int DP> int launch_tiles(Attend a, const Backward &p, hipS
         if (!narrow)
             rc = exact ? launch_both_keys<T, DP, true, false>(a, stream)
                        : launch_both_keys<T, DP, false, false>(a, stream);
-        if (a.split > 1) hipLaunchKernelGGL((sum_heads<T>), dim3(1024, 2), dim3(kThreads), 0, stream, a);
+        if (a.split > 1 && rc == NLB_OK) rc = enqueue(sum_heads<T>, dim3(1024, 2), kThreads, 0, stream, a);
     }
     return rc;
 }
@@ -905,8 +903,7 @@ template <typename T, int DP> int launch_lists(const Attend &a, const Backward &
     const uint32_t bytes = kMaxBuckets * 4 + a.buckets * a.heads * 4 + 8 + groups * p.keep * gb * 8 +
                            (a.part ? a.buckets * gb * groups * 4 : 0) + groups * kListKeys;
     if (!allow_lds(kernel, bytes)) return NLB_EDEVICE;
-    hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(kThreads), bytes, stream, a, p.keep);
-    return NLB_OK;
+    return enqueue(kernel, p.blocks, kThreads, bytes, stream, a, p.keep);
 }
 
 template <typename T, int DP> int launch_form(const Attend &a, const Backward &p, hipStream_t s) {
@@ -914,24 +911,20 @@ template <typename T, int DP> int launch_form(const Attend &a, const Backward &p
 }
 
 template <typename T> int launch(const Attend &a, const Backward &p, void *dbias, hipStream_t s) {
-    const int rc = a.dim <= 32   ? launch_form<T, 32>(a, p, s)
-                   : a.dim <= 64 ? launch_form<T, 64>(a, p, s)
-                                 : launch_form<T, 128>(a, p, s);
-    if (rc != NLB_OK) return rc;
-    if (dbias) {
-        const float *from = a.part;
-        uint32_t n = (uint32_t)p.parts;
-        if (p.shares) {
-            float *mid = a.part + (size_t)n * a.heads * a.buckets;
-            hipLaunchKernelGGL((sum_bias<T>), dim3(p.shares * a.heads), dim3(1024), 0, s, from, n, a.heads,
-                               a.buckets, p.shares, mid, (T *)nullptr);
-            from = mid;
-            n = p.shares;
-        }
-        hipLaunchKernelGGL((sum_bias<T>), dim3(a.heads), dim3(1024), 0, s, from, n, a.heads, a.buckets, 1u,
-                           (float *)nullptr, (T *)dbias);
+    int rc = a.dim <= 32   ? launch_form<T, 32>(a, p, s)
+             : a.dim <= 64 ? launch_form<T, 64>(a, p, s)
+                           : launch_form<T, 128>(a, p, s);
+    if (rc != NLB_OK || !dbias) return rc;
+    const float *from = a.part;
+    uint32_t n = (uint32_t)p.parts;
+    if (p.shares) {
+        float *mid = a.part + (size_t)n * a.heads * a.buckets;
+        rc = enqueue(sum_bias<T>, p.shares * a.heads, 1024, 0, s, from, n, a.heads, a.buckets, p.shares, mid, nullptr);
+        if (rc != NLB_OK) return rc;
+        from = mid;
+        n = p.shares;
     }
-    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+    return enqueue(sum_bias<T>, a.heads, 1024, 0, s, from, n, a.heads, a.buckets, 1u, nullptr, (T *)dbias);
 }
 
 }  // namespace

@@ -1,5 +1,5 @@
-// call_device.h -- the device of a call that no table belongs to.  Private to
-// libnlb.so.
+// call_device.h -- the device of a call that no table belongs to, and its
+// launches.  Private to libnlb.so.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -34,5 +34,18 @@ class CallDevice {
     int prev_ = -1;
     bool set_ = false;
 };
+
+// Starts a kernel.  What it returns is this launch's own: kernels that read
+// what it leaves are not started after a failure, and an error that an earlier
+// call of the program left is not taken for one.
+template <typename T> struct Given { typedef T type; };
+template <typename... P>
+int enqueue(void (*kernel)(P...), dim3 blocks, uint32_t threads, uint32_t lds, hipStream_t stream,
+            typename Given<P>::type... args) {
+    void *p[] = {(void *)&args...};
+    if (hipLaunchKernel((const void *)kernel, blocks, dim3(threads), p, lds, stream) == hipSuccess) return NLB_OK;
+    (void)hipGetLastError();
+    return NLB_EDEVICE;
+}
 
 }  // namespace

@@ -357,8 +357,7 @@ template <typename T> int launch(const Norm &a, hipStream_t s) {
     return with_shape<T>(a.width, [&](auto n, auto c) {
         constexpr int N = decltype(n)::value, C = decltype(c)::value;
         const uint32_t per = 256 / N, blocks = (a.rows + per - 1) / per;
-        hipLaunchKernelGGL((norm_rows<T, N, C>), dim3(blocks < 2048 ? blocks : 2048), dim3(256), 0, s, a);
-        return NLB_OK;
+        return enqueue(norm_rows<T, N, C>, blocks < 2048 ? blocks : 2048, 256, 0, s, a);
     });
 }
 
@@ -366,11 +365,9 @@ template <typename T> int launch_backward(const Norm &a, float *dw, float *db, h
     return with_shape<T>(a.width, [&](auto n, auto c) {
         constexpr int N = decltype(n)::value, C = decltype(c)::value;
         const uint32_t blocks = backward_blocks(a.rows, 256 / N);
-        hipLaunchKernelGGL((norm_rows_backward<T, N, C>), dim3(blocks), dim3(256), 0, s, a);
-        if (a.part)
-            hipLaunchKernelGGL(sum_shares, dim3((2 * a.width + 63) / 64), dim3(1024), 0, s, a.part, blocks, a.width, dw,
-                               db);
-        return NLB_OK;
+        const int rc = enqueue(norm_rows_backward<T, N, C>, blocks, 256, 0, s, a);
+        if (rc != NLB_OK || !a.part) return rc;
+        return enqueue(sum_shares, (2 * a.width + 63) / 64, 1024, 0, s, a.part, blocks, a.width, dw, db);
     });
 }
 
@@ -390,9 +387,7 @@ extern "C" int nlb_layer_norm(const nlb_norm_call *c, const float *b, float eps,
     a.eps = eps;
     a.out = (uint8_t *)y;
     a.out_row = y_stride * (c->dtype == NLB_DTYPE_BF16 ? 2 : 4);
-    rc = c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, (hipStream_t)stream) : launch<float>(a, (hipStream_t)stream);
-    if (rc != NLB_OK) return rc;
-    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16>(a, (hipStream_t)stream) : launch<float>(a, (hipStream_t)stream);
 }
 
 extern "C" int nlb_layer_norm_work(const nlb_norm_call *c, size_t *bytes) {
@@ -422,8 +417,6 @@ extern "C" int nlb_layer_norm_backward(const nlb_norm_call *c, const void *dy, i
     a.out = (uint8_t *)dx;
     a.out_row = dx_stride * e;
     a.part = dw || db ? (float *)work : nullptr;
-    rc = c->dtype == NLB_DTYPE_BF16 ? launch_backward<__bf16>(a, dw, db, (hipStream_t)stream)
-                                    : launch_backward<float>(a, dw, db, (hipStream_t)stream);
-    if (rc != NLB_OK) return rc;
-    return hipGetLastError() == hipSuccess ? NLB_OK : NLB_EDEVICE;
+    return c->dtype == NLB_DTYPE_BF16 ? launch_backward<__bf16>(a, dw, db, (hipStream_t)stream)
+                                      : launch_backward<float>(a, dw, db, (hipStream_t)stream);
 }

@@ -91,3 +91,38 @@ c = _call(heads=256, kv_heads=1, batch=2**23 - 1, q_rows=2**23 - 1, k_rows=2**31
 assert forward(c) == nlb.NLB_OK
 check("join", (2**23 - 1) * 256)
 """)
+
+
+def test_nothing_follows_a_launch_that_fails(stand_in):
+    """A call whose first, second, ... launch is refused returns NLB_EDEVICE
+    and starts none after it: those would read what the missing one leaves.
+    An error that an earlier call of the program left is not this call's."""
+    run(stand_in, """
+at = ctypes.c_int.in_dll(hip, "fail_at")
+bias = dict(buckets=4, bias=P, bounds=P)
+million = dict(heads=16, batch=1_050_000, q_rows=4_200_000, k_rows=4_200_000, q_start=P, k_start=P)
+calls = {
+    "tiles": (lambda: forward(_call()), 1),
+    "tiles in pieces": (lambda: forward(_call(**million)), 2),
+    "lists": (lambda: forward(_call(batch=9000, q_rows=9000, k_rows=90_000)), 1),
+    "chunks": (lambda: forward(_call(q_rows=2, k_rows=2000)), 2),
+    "backward": (lambda: backward(_call()), 3),               # rows, keys, the sum of a group's heads
+    "backward, wide rows": (lambda: backward(_call(dim=128)), 4),
+    "backward, pieces": (lambda: backward(_call(**million)), 3),
+    "backward, bias": (lambda: backward(_call(**bias), dbias=P), 4),
+    "backward, bias of many": (lambda: backward(_call(q_rows=600_000, **bias), dbias=P), 5),
+    "backward, lists": (lambda: backward(_call(q_rows=2, k_rows=20, **bias), dbias=P), 2),
+    "norm": (lambda: lib.nlb_layer_norm(_norm(), None, 1e-5, P, 100, None), 1),
+    "norm, backward": (lambda: lib.nlb_layer_norm_backward(_norm(), P, 100, P, 100, P, P, P, 1 << 40, None), 2),
+}
+for what, (call, n) in calls.items():
+    hip.leave_error(1)
+    assert call() == nlb.NLB_OK, what
+    assert hip.launched() == n, (what, hip.launched())
+    hip.forget()
+    for at.value in range(n):
+        assert call() == nlb.NLB_EDEVICE, (what, at.value)
+        assert hip.launched() == at.value + 1, (what, at.value, hip.launched())
+        hip.forget()
+    at.value = -1
+""")
