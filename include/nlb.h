@@ -392,11 +392,17 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  * below the one before it, and bucket(x) the number of bounds <= x.  Positions
  * are q_pos (device uint32 [q_rows]) and k_pos, whose difference is clamped to
  * int32 (as nlb_sample's tq and ts go in), or without either the places
- * i + lk - lq and j.  A bias at or below -2^100 closes its bucket.
+ * i + lk - lq and j.  A bias at or below -2^100 closes its bucket; any other
+ * beyond 2^20 in magnitude counts as 2^20 (with its sign): a mask of -1e9 takes
+ * all weight from its keys, and a row that has no other keys spreads it over
+ * them by their scores.
  *   Numerics.  Sums, the softmax's maximum and sum, and lse are fp32.  bf16
  * rows: products of bf16 values are exact in fp32, softmax weights enter the
  * second product as bf16 (in the single-row form as fp32), o is rounded once.
- * fp32 rows: fp32 products throughout.  The same call gives the same bits.
+ * fp32 rows: fp32 products throughout.  Scores are fp32 too: where a row's
+ * scores reach a magnitude of x, its weights (and what the backward pass makes
+ * of lse) are off by some 2^-22 x of themselves.  The same call gives the same
+ * bits.
  *   Working memory: nlb_attention_work bytes of device memory (16-byte
  * aligned, may be NULL if that is 0), used by the call's kernels only; calls
  * that may overlap in time need one each.  lse (device fp32 [q_rows][heads])

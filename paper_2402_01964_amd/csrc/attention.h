@@ -47,6 +47,7 @@ constexpr int kMaxBuckets = NLB_ATT_MAX_BUCKETS;
 constexpr uint32_t kMostRows = INT32_MAX - 1023;   // a tile past any row still has a 32-bit place
 static_assert(kMaxBuckets == 64, "bucket_of takes six steps");
 constexpr float kBiasCloses = -0x1p100f; // bias values at or below this close their bucket
+constexpr float kBiasMost = 0x1p20f;     // others count as at most this in magnitude (see bias2_of)
 
 struct Strided {
     const uint8_t *p;
@@ -235,10 +236,16 @@ __device__ __forceinline__ uint32_t bucket_of(const int32_t *bounds, uint32_t bu
     return min(n, buckets - 1);
 }
 
-// One head's bias in powers of two.
+// One head's bias in powers of two.  Scores and lse are fp32, so a row whose
+// scores are of magnitude x has weights that are off by some 2^-22 x of
+// themselves: at 2^20 by a quarter, at 2^31 (a mask of -1e9 is 2^30) by factors
+// that no longer fit, and the row, with the gradients of all of its keys, would
+// be infinite or zero.  So biases are held within 2^20: a row's weights change
+// only where two of them beyond that lead it, or where all of its keys have one.
 template <typename T> __device__ __forceinline__ float bias2_of(const Attend &a, uint32_t b, uint32_t head) {
     const float x = (float)((const T *)a.bias)[(size_t)b * a.heads + head];
-    return x <= kBiasCloses ? -INFINITY : x * kLog2e;
+    const float most = x > kBiasMost ? kBiasMost : x < -kBiasMost ? -kBiasMost : x;   // (NaN stays)
+    return x <= kBiasCloses ? -INFINITY : most * kLog2e;
 }
 
 // The bounds of a workgroup's buckets and one head's bias as tiled kernels add
