@@ -478,6 +478,12 @@ def _vector(t, n, like, dtypes, name):
     return t.data_ptr()
 
 
+def _sizes(*sizes):
+    """Sizes that 32 bits hold (a structure's fields would keep what is left of others)."""
+    if min(sizes) < 0 or max(sizes) >= 2**31:
+        raise ValueError("sizes must be below 2^31, and not negative")
+
+
 def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos):
     import torch
     dtype = _float_dtype(q, "q")
@@ -501,6 +507,7 @@ def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_p
     elif bounds is not None:
         raise ValueError("bounds without bias")
     words = (torch.int32, torch.uint32)
+    _sizes(batch, q_rows, k_rows, heads, kv_heads, dim, buckets)
     return _AttCall(q.device.index, dtype, heads, kv_heads, dim, 1 if causal else 0, buckets,
                     dim ** -0.5 if scale is None and dim else scale or 0.0, batch, q_rows, k_rows,
                     _vector(q_start, batch + 1, q, ints, "q_start"), _vector(k_start, batch + 1, q, ints, "k_start"),
@@ -632,6 +639,7 @@ def _norm_call(x, w, mean, rstd):
     width = x.shape[-1]
     rows = x.numel() // max(1, width)
     fp32 = (torch.float32,)
+    _sizes(rows, width)
     return _NormCall(x.device.index, dtype, rows, width, *_norm_rows(x, x, "x"), _vector(w, width, x, fp32, "w"),
                      _vector(mean, rows, x, fp32, "mean"), _vector(rstd, rows, x, fp32, "rstd"))
 
