@@ -478,6 +478,17 @@ def _vector(t, n, like, dtypes, name):
     return t.data_ptr()
 
 
+def _no_graph(what, *inputs):
+    """Refuses inputs whose gradients autograd would be asked for: the result has none."""
+    import torch
+    if not torch.is_grad_enabled():
+        return
+    for t in inputs:
+        if getattr(t, "requires_grad", False):
+            raise RuntimeError(f"{what} keeps no autograd graph: call it under torch.no_grad() or in a "
+                               f"torch.autograd.Function, with {what}_backward for the gradients")
+
+
 def _sizes(*sizes):
     """Sizes that 32 bits hold (a structure's fields would keep what is left of others)."""
     if min(sizes) < 0 or max(sizes) >= 2**31:
@@ -556,10 +567,13 @@ def attention(q, k, v, *, batch=None, q_start=None, k_start=None, causal=False, 
     ``q_pos`` and ``k_pos`` (a ts answer goes in as k_pos with its tq as
     q_pos) or, without them, between places.  ``scale`` defaults to
     dim ** -0.5.  ``work``: working memory of attention_work bytes, allocated
-    if None.  Returns (or fills) out (as q) and lse, fp32 [q_rows, heads]."""
+    if None.  Returns (or fills) out (as q) and lse, fp32 [q_rows, heads].  No
+    autograd graph is kept: inputs that require gradients are refused unless
+    gradients are off (torch.no_grad, a torch.autograd.Function)."""
     import torch
     lib = load_library()
     c = _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos)
+    _no_graph("attention", q, k, v, bias)
     if stream is not None:
         with _on(stream, q.device):
             return attention(q, k, v, batch=batch, q_start=q_start, k_start=k_start, causal=causal, scale=scale,
@@ -648,10 +662,11 @@ def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rst
     """Layer norm over the last dimension (nlb_layer_norm): ``x`` float32 or
     bfloat16, two-dimensional with any row stride or contiguous; ``w``, ``b``
     float32 or None.  Returns (or fills) out (as x), mean and rstd (float32,
-    one per row)."""
+    one per row).  No autograd graph is kept, as in ``attention``."""
     import torch
     lib = load_library()
     _float_dtype(x, "x")
+    _no_graph("layer_norm", x, w, b)
     if stream is not None:
         with _on(stream, x.device):
             return layer_norm(x, w, b, eps, out=out, mean=mean, rstd=rstd)
