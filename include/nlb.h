@@ -452,13 +452,24 @@ int nlb_attention(const nlb_att_call *call, const nlb_att_rows *o, float *lse, v
  *   dbias[b][h] = the sum of ds_ij over the pairs of bucket b
  * dk and dv sum over the query heads of a key/value head.  All rows of the
  * sequences are written (zeros for closed keys and for rows without open
- * keys), rows outside them are not.  dbias: device [buckets][heads] of dtype,
- * or NULL where it is not wanted (with it, D_i comes from a pass over the keys
- * of its own, else from o).  Numerics: as nlb_attention; ds enters the
- * products as bf16 for bf16 rows (not in the single-row form), dbias sums it
- * in fp32 and fp64, rounded once.  No atomics on results: the same call gives
- * the same bits.  Work, capture and errors: as nlb_attention (NLB_EINVAL also
- * for dbias without buckets). */
+ * keys), rows outside them are not.  q and dout hold finite values in all rows
+ * of the sequences, those without open keys too.  dbias: device
+ * [buckets][heads] of dtype, or NULL where it is not wanted.
+ *   Single rows have a form of their own here where they are lists: at most 4
+ * query heads on a key/value head, and up to 64 keys a list on average (up to
+ * 1024 for 8192 lists times key/value heads and more).  All other calls, single
+ * rows over longer histories and larger groups of heads among them, take the
+ * form for rows of any number: right, but slow for single rows (200 000 lists
+ * of 10 bf16 rows, 8 heads on one: 33 ms; 4 heads on one: 0.6).
+ *   Numerics.  As nlb_attention; in the form for rows of any number softmax
+ * weights and ds enter the second products as bf16 for bf16 rows, in that for
+ * lists as fp32.  D_i: in the form for lists its own sum (o is not read); else
+ * dout . o, corrected by a pass over the keys for bf16 rows, and for fp32 rows
+ * where dbias is wanted.  dbias sums ds in fp32 and fp64, rounded once.  No
+ * atomics on results: the same call gives the same bits.
+ *   Work, capture and errors: as nlb_attention (NLB_EINVAL also for dbias
+ * without buckets).  dbias takes 4 heads x buckets bytes for each sequence and
+ * each 32 or 128 query rows (in the form for lists, of 2048 workgroups at most). */
 int nlb_attention_backward(const nlb_att_call *call, const nlb_att_rows *o, const float *lse,
                            const nlb_att_rows *dout, const nlb_att_rows *dq, const nlb_att_rows *dk,
                            const nlb_att_rows *dv, void *dbias, void *work, size_t work_bytes, void *stream);
