@@ -375,7 +375,14 @@ int nlb_rnn_update_noalloc(nlb_table *h, const int32_t *src, const int32_t *dst,
  * the last sequence are neither read nor written.  Starts outside [0, rows]
  * are taken as the nearest end, so no call reads or writes outside its rows.
  * With q_start NULL and q_rows == batch (a retrieved list per query, or one
- * new token per sequence) the call runs in a form made for single rows.
+ * new token per sequence) the call runs in a form made for single rows.  The
+ * host sees the average length only: of lists of 64 keys or fewer on average
+ * (8192 and more, times key/value heads; the gradients' lists likewise) each is
+ * one lane group's, however long, and the call waits for the longest (10 000
+ * lists of 30 keys, one of them of 10 000: 3.6 ms and 12 for the gradients,
+ * where it has 30 too 0.03 and 0.07).  With q_start given, 0 .. batch, single
+ * rows take the form for rows of any number instead (0.3 and 1.0 ms; 0.17 and
+ * 0.7 for short lists).
  *   Rows.  q, o: [q_rows][heads][dim], k, v: [k_rows][kv_heads][dim], of type
  * dtype, at any row and head strides (in values, 0 .. 2^31 - 1); a row's dim
  * values are contiguous, so slices of a joint projection need no copy.

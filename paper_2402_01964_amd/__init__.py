@@ -25,8 +25,8 @@ MAX_SLOTS = 1024
 # Symbols declared in include/nlb.h.
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
                "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
-               "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward", "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status",
-               "nlb_strerror")
+               "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward",
+               "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status", "nlb_strerror")
 AGG_HIDDEN = 64
 RNN_MAX_DIM = 1024
 DTYPE_F32, DTYPE_BF16 = 0, 1

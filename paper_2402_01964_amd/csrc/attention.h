@@ -754,10 +754,13 @@ struct Forward {
 };
 
 // One query row per sequence.  Many short lists take a group of lanes each
-// (kLists).  Else a wavefront takes a list (kOne), or where lists
-// are too few to fill the card (8 wavefronts on each of 1024 SIMDs) a chunk of
-// its keys, of 256 rows at least, so that what a chunk writes stays below a
-// hundredth of what it reads.
+// (kLists), however long it is: the host knows the average length only, and a
+// call waits for its longest list (see the header).  Else a wavefront takes a
+// list (kOne), or where lists are too few to fill the card (8 wavefronts on each
+// of 1024 SIMDs) a chunk of its keys, of 256 rows at least.  A chunk writes a
+// group's heads of fp32 values, which the join reads again, for 512 rows of
+// keys and values that it reads: group / 256 of the bytes for bf16, group / 512
+// for fp32 rows, so 1.6 % at 4 heads on one, a quarter at 64.
 // Lists times key/value heads from which a group of lanes each fills the card
 // (4000 lists of 63 slots in two heads, bf16: 37 us, a wavefront each 28; 8000:
 // 44 and 49; 6000 of 10 slots: 14 and 18).
@@ -798,7 +801,9 @@ struct Backward {
 // Short lists with one query row, and longer ones where they are many, take a
 // group of lanes each; a group's heads are in registers there, four at most.
 // Everything else, single rows over long histories among it, goes through
-// tiles, whose second kernel spreads over the keys.
+// tiles.  Their second kernel spreads over the keys; the first gives a row and
+// head to one workgroup, which walks all keys (bf16 rows twice) and sets the
+// time where rows are few.
 inline Backward plan_backward(const Attend &a) {
     Backward p = {};
     p.lists = !a.q_start && a.q_len == 1 && a.group <= 4 &&

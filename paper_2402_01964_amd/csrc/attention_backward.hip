@@ -427,6 +427,8 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
         if constexpr (DK) dk[d] = f32x16{};
         if constexpr (DV) dv[d] = f32x16{};
     }
+    // (below 2^31: tiles have 32 rows and more, and lse and stats, 12 bytes a row
+    // and head, of 2^36 rows times heads fit no memory)
     const int32_t total = tiles * (g1 - g0);
     if (total > 0) fetch(g0, first);                           // (in flight beside the bias tables' loads)
     if (POS != 0 && a.buckets) {
@@ -463,7 +465,7 @@ __global__ __launch_bounds__(kThreads, DP * sizeof(T) > 256 ? 1 : 2) void backwa
             }
 #pragma unroll
             for (int n = 0; n < S::blocks; n++) {
-                    const int blk = span.take + n * 32;
+                const int blk = span.take + n * 32;
                 f32x16 s = {}, dp = {};
                 product_rows<G>(s, qt, blk, k);
                 if constexpr (DK) product_rows<G>(dp, ot, blk, v);
