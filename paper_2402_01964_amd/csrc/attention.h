@@ -19,7 +19,7 @@
 // owned row (running maximum, sum, log of the sum) is one value per lane.
 // bf16 inputs run on 32x32x16 products, fp32 inputs on 32x32x2 fp32 products;
 // sums are fp32.  The bf16 kernels round p and ds to bf16 for the products
-// that contract over them (a relative 2^-9 of each term, like the rounding of
+// that contract over them (up to 2^-8 of each term, like the rounding of
 // the result itself); sums and statistics take them unrounded.
 #pragma once
 
