@@ -481,18 +481,13 @@ def _vector(t, n, like, dtypes, name):
 def _no_graph(what, *inputs):
     """Refuses inputs whose gradients autograd would be asked for: the result has none."""
     import torch
-    if not torch.is_grad_enabled():
-        return
     for t in inputs:
-        if getattr(t, "requires_grad", False):
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise RuntimeError(f"{what} keeps no autograd graph: call it under torch.no_grad() or in a "
                                f"torch.autograd.Function, with {what}_backward for the gradients")
 
 
-def _sizes(*sizes):
-    """Sizes that 32 bits hold (a structure's fields would keep what is left of others)."""
-    if min(sizes) < 0 or max(sizes) >= 2**31:
-        raise ValueError("sizes must be below 2^31, and not negative")
+_SIZES = "sizes must be below 2^31, and not negative"        # (a structure's fields would keep what is left of others)
 
 
 def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_pos, k_pos):
@@ -518,7 +513,8 @@ def _att_call(q, k, v, batch, q_start, k_start, causal, scale, bias, bounds, q_p
     elif bounds is not None:
         raise ValueError("bounds without bias")
     words = (torch.int32, torch.uint32)
-    _sizes(batch, q_rows, k_rows, heads, kv_heads, dim, buckets)
+    if (batch | q_rows | k_rows | heads | kv_heads | dim | buckets) >> 31:
+        raise ValueError(_SIZES)
     return _AttCall(q.device.index, dtype, heads, kv_heads, dim, 1 if causal else 0, buckets,
                     dim ** -0.5 if scale is None and dim else scale or 0.0, batch, q_rows, k_rows,
                     _vector(q_start, batch + 1, q, ints, "q_start"), _vector(k_start, batch + 1, q, ints, "k_start"),
@@ -653,7 +649,8 @@ def _norm_call(x, w, mean, rstd):
     width = x.shape[-1]
     rows = x.numel() // max(1, width)
     fp32 = (torch.float32,)
-    _sizes(rows, width)
+    if (rows | width) >> 31:
+        raise ValueError(_SIZES)
     return _NormCall(x.device.index, dtype, rows, width, *_norm_rows(x, x, "x"), _vector(w, width, x, fp32, "w"),
                      _vector(mean, rows, x, fp32, "mean"), _vector(rstd, rows, x, fp32, "rstd"))
 
@@ -666,7 +663,6 @@ def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rst
     import torch
     lib = load_library()
     _float_dtype(x, "x")
-    _no_graph("layer_norm", x, w, b)
     if stream is not None:
         with _on(stream, x.device):
             return layer_norm(x, w, b, eps, out=out, mean=mean, rstd=rstd)
@@ -677,6 +673,7 @@ def layer_norm(x, w=None, b=None, eps: float = 1e-5, *, out=None, mean=None, rst
     if rstd is None:
         rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
     c = _norm_call(x, w, mean, rstd)
+    _no_graph("layer_norm", x, w, b)
     _check(lib.nlb_layer_norm(c, _vector(b, c.width, x, (torch.float32,), "b"), eps, *_norm_rows(out, x, "out"),
                               _current_stream(x.device)), "nlb_layer_norm")
     return out, mean, rstd
