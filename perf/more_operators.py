@@ -1,0 +1,513 @@
+"""The operators that train a layer over retrieved lists and histories, as cases
+to be timed: what they compute in plain torch, and the library's calls.
+
+  lookup, lookup_train   rows of a table by id, times a scale, and the table's
+                         gradient: whole (dense) or of the rows that occur
+                         (listed), in ascending order of their ids
+      out_i = scale table[id_i]      (0 where the id is none of the table's)
+      dtable_r = scale sum over the i with id_i = r of dout_i
+
+  scan, scan_train       a gated linear recurrence over packed sequences
+      z_t = sigmoid(g_t),  h_t = z_t h_{t-1} + (1 - z_t) x_t
+  from each sequence's h0 (or 0) to its last state, and its gradients
+
+  rotate, rotate_train   norm of each head's queries and keys, and their
+                         rotation by position, in one pass, and its gradients
+      u = x (mean(x^2) + eps)^-1/2 w,  m frequencies f,  a_i = pos f_i
+      y_i = u_i cos a_i - u_{m+i} sin a_i,  y_{m+i} = u_{m+i} cos a_i + u_i sin a_i
+  for i < m, y = u behind the 2 m rotated values; a row at position 0xFFFFFFFF
+  (an empty slot) gives zeros and takes no part in gradients
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+EPS = 1e-5
+
+
+def _lookup(name, kind, dtype, n, rows, width, fill=1.0, listed=False, even=False, gap=0):
+    """n ids into `rows` rows of `width` values; fill: the share of ids that
+    are rows, the others being -1; even: all rows as likely, else popular ones
+    (the i-th with a share of 1 / i).  gap: values between a row's end and the
+    next row."""
+    c = {"kind": kind, "dtype": dtype, "n": n, "rows": rows, "width": width, "fill": fill, "listed": listed,
+         "even": even, "gap": gap}
+    return {"name": name, **c} if name else c
+
+
+def _scan(name, kind, dtype, batch, lo, hi, width, first=True, joint=True, mix=1):
+    """batch sequences of lo to hi rows; first: they begin at given states;
+    joint: x and g are halves of one projection's output."""
+    c = {"kind": kind, "dtype": dtype, "batch": batch, "lo": lo, "hi": hi, "width": width, "first": first,
+         "joint": joint, "mix": mix}
+    return {"name": name, **c} if name else c
+
+
+def _rotate(name, kind, dtype, q_rows, k_rows, heads, kv_heads, dim, rot, fill=1.0, times=True, weights=True):
+    """k_rows 0: queries and keys are heads of the same rows of one
+    projection's output.  rot: values of a head that are rotated.  times:
+    positions are timestamps, else places.  fill: the share of keys that are
+    not empty slots."""
+    c = {"kind": kind, "dtype": dtype, "q_rows": q_rows, "k_rows": k_rows, "heads": heads, "kv_heads": kv_heads,
+         "dim": dim, "rot": rot, "fill": fill, "times": times, "weights": weights}
+    return {"name": name, **c} if name else c
+
+
+def listed():
+    return [
+        # The rows of a small batch's queries: launch latency.
+        _lookup("lookup-small", "lookup", "f32", 600, 1000, 100),
+        # The rows of a large sparse batch's retrieved lists, a third of the
+        # slots empty.
+        _lookup("lookup-large", "lookup", "bf16", 3_000_000, 10_000_000, 128, fill=0.66),
+        # Their gradient: the rows that occur, a few of them thousands of times.
+        _lookup("lookup-train-listed", "lookup_train", "bf16", 3_000_000, 20_000_000, 128, fill=0.66, listed=True),
+        # The gradient of a small table of fp32 statuses, whole.
+        _lookup("lookup-train-dense", "lookup_train", "f32", 240_000, 17_000, 100, fill=0.9),
+        # One event each for 512 nodes that keep their states.
+        _scan("scan-token", "scan", "bf16", 512, 1, 1, 1024),
+        # One history of a million events.
+        _scan("scan-long", "scan", "bf16", 1, 1_000_000, 1_000_000, 128, first=False, joint=False),
+        # A training step over a batch of histories of very different lengths.
+        _scan("scan-train-packed", "scan_train", "bf16", 48, 16, 4096, 1024),
+        # A training step over many short histories of fp32 statuses.
+        _scan("scan-train-short-f32", "scan_train", "f32", 20_000, 1, 60, 100, joint=False),
+        # One new token each for 16 sequences.
+        _rotate("rotate-token", "rotate", "bf16", 16, 0, 32, 8, 128, 128, times=False),
+        # The queries and keys of a large batch of histories.
+        _rotate("rotate-large", "rotate", "bf16", 131_072, 0, 16, 4, 128, 128, times=False),
+        # A training step over packed histories, half of each head rotated.
+        _rotate("rotate-train-packed", "rotate_train", "bf16", 32_768, 0, 8, 2, 64, 32),
+        # A training step over retrieved lists of 20 slots, fp32 statuses of
+        # width 100 in two heads, rotated by timestamps.
+        _rotate("rotate-train-lists-f32", "rotate_train", "f32", 12_000, 240_000, 2, 2, 50, 50, fill=0.7),
+    ]
+
+
+def draw(rng):
+    """A case of the same ranges: lookups of 1 to 2 000 000 ids in tables of 10
+    to 10 000 000 rows of 1 to 1030 values; scans of 1 to 20 000 sequences of 1
+    to 500 000 rows, 1 to 2048 wide; rotations of 1 to 200 000 rows of 1 to 16
+    heads of 2 to 128 values."""
+    def log(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+    kind = rng.choice(["lookup", "lookup_train", "lookup_train", "scan", "scan_train", "scan_train", "rotate",
+                       "rotate_train", "rotate_train"])
+    dtype = rng.choice(["bf16", "f32"])
+    if kind.startswith("lookup"):
+        width = rng.choice([log(1, 1030), log(1, 1030), 64, 100, 128, 172, 256])
+        n = log(1, min(2_000_000, 300_000_000 // width))
+        rows = log(10, 2_000_000_000 // width if kind == "lookup" else 200_000_000 // width)
+        return _lookup("", kind, dtype, n, min(rows, 10_000_000), width, fill=rng.choice([1.0, rng.uniform(0.1, 1.0)]),
+                       listed=kind == "lookup_train" and rng.random() < 0.5, even=rng.random() < 0.3,
+                       gap=rng.choice([0, 0, 1, 8]))
+    if kind.startswith("scan"):
+        width = rng.choice([log(1, 2048), log(1, 2048), 64, 100, 128, 1024])
+        most = min(500_000, 100_000_000 // width)                # rows of the call
+        hi = rng.choice([1, log(1, most), log(1, most)])
+        lo = rng.choice([1, max(1, hi // 8), hi])
+        return _scan("", kind, dtype, log(1, max(1, min(20_000, most // hi))), lo, hi, width,
+                     first=rng.random() < 0.5, joint=rng.random() < 0.5, mix=rng.randint(1, 1 << 20))
+    kv_heads = rng.choice([1, 2, 4])
+    heads = kv_heads * rng.choice([1, 1, 2, 4])
+    dim = rng.choice([25, 32, 50, 64, 64, 128, 128, rng.randint(2, 128)])
+    rot = rng.choice([dim // 2 * 2, dim // 2 * 2, dim // 4 * 2, 0])
+    q_rows = log(1, min(200_000, 100_000_000 // (dim * heads)))
+    k_rows = rng.choice([0, 0, log(1, min(400_000, 100_000_000 // (dim * kv_heads)))])
+    return _rotate("", kind, dtype, q_rows, k_rows, heads, kv_heads, dim, rot,
+                   fill=1.0 if not k_rows else rng.uniform(0.2, 1.0), times=rng.random() < 0.6,
+                   weights=rng.random() < 0.8)
+
+
+# ------------------------------------------------------------------ inputs
+def _lengths(c):
+    r = random.Random(c["mix"])
+    lo, hi = math.log(c["lo"]), math.log(c["hi"])
+    n = [int(round(math.exp(r.uniform(lo, hi)))) for _ in range(c["batch"])]
+    n[0] = c["hi"]
+    return n
+
+
+def prepare(case, seed):
+    c = case
+    gen = torch.Generator(device="cuda").manual_seed(int(seed) * 6131 + 29)
+    dtype = DTYPES[c["dtype"]]
+
+    def randn(*shape, t=None):
+        return torch.randn(shape, device="cuda", generator=gen, dtype=t or dtype)
+
+    def rand(n):
+        return torch.rand(n, device="cuda", generator=gen, dtype=torch.float64)
+
+    if c["kind"].startswith("lookup"):
+        n, rows, d = c["n"], c["rows"], c["width"]
+        if c["even"]:
+            ids = (rand(n) * rows).long()
+        else:                                                 # by rank, the ranks spread over the table
+            ids = torch.pow(float(rows + 1), rand(n)).long().sub_(1).clamp_(0, rows - 1)
+            ids = ids.mul_(1_000_003).remainder_(rows)
+        ids = ids.to(torch.int32)
+        if c["fill"] < 1:
+            ids.masked_fill_(rand(n) >= c["fill"], -1)
+        st = {"case": c, "ids": ids, "scale": d ** 0.5}
+        if c["kind"] == "lookup":
+            st["table"] = randn(rows, d + c["gap"])[:, :d]
+        else:
+            st["dout"] = randn(n, d + c["gap"])[:, :d]
+            if c["listed"]:                                   # buffers that the program keeps; behind the last row, zeros
+                st["grads"] = torch.zeros((n, d), device="cuda", dtype=dtype)
+        return st
+    if c["kind"].startswith("scan"):
+        lengths = _lengths(c)
+        t, d = sum(lengths), c["width"]
+        if c["joint"]:
+            both = randn(t, 2 * d)
+            x, g = both[:, :d], both[:, d:]
+        else:
+            x, g = randn(t, d), randn(t, d)
+        g.mul_(2.0).add_(2.0)                                 # gates around 0.9: states that remember
+        start = None
+        if c["lo"] < c["hi"]:
+            start = torch.tensor([0] + lengths, dtype=torch.int64).cumsum(0).to(torch.int32).cuda()
+        st = {"case": c, "x": x, "g": g, "start": start, "longest": max(lengths),
+              "h0": randn(c["batch"], d, t=torch.float32) if c["first"] else None}
+        if c["kind"] == "scan_train":
+            st["dh"] = randn(t, d)
+            st["dlast"] = randn(c["batch"], d, t=torch.float32) if c["first"] else None
+        return st
+    nq, nk, h, hk, d = c["q_rows"], c["k_rows"], c["heads"], c["kv_heads"], c["dim"]
+
+    def pair():
+        if nk:
+            return randn(nq, h, d), randn(nk, hk, d)
+        both = randn(nq, h + 2 * hk, d)
+        return both[:, :h], both[:, h:h + hk]
+
+    q, k = pair()
+    m = c["rot"] // 2
+    if c["times"]:
+        def times(n):
+            return (rand(n) * (1 << 28)).to(torch.int32)
+        freq = torch.pow(10.0, -9.0 * torch.arange(m, device="cuda", dtype=torch.float64) / max(1, m - 1)).float()
+        q_pos = times(nq)
+        k_pos = times(nk) if nk else q_pos
+    else:
+        freq = torch.pow(10.0, -4.0 * torch.arange(m, device="cuda", dtype=torch.float64) / max(1, m)).float()
+        q_pos = torch.arange(nq, device="cuda", dtype=torch.int32)
+        k_pos = torch.arange(nk, device="cuda", dtype=torch.int32) if nk else q_pos
+    if c["fill"] < 1:
+        k_pos = k_pos.masked_fill(rand(nk) >= c["fill"], -1)
+    st = {"case": c, "q": q, "k": k, "freq": freq if m else None, "q_pos": q_pos, "k_pos": k_pos, "wq": None,
+          "wk": None}
+    if c["weights"]:
+        st["wq"], st["wk"] = (1.0 + 0.1 * randn(d, t=torch.float32) for _ in range(2))
+    if c["kind"] == "rotate_train":
+        st["dq"], st["dk"] = pair()
+    return st
+
+
+# ------------------------------------------------------------------ the plain form
+def _plain_lookup(st):
+    c, ids = st["case"], st["ids"].long()
+    there = (ids >= 0) & (ids < c["rows"])
+    if "table" in st:
+        out = (st["table"][ids.clamp(0, c["rows"] - 1)].float() * st["scale"]).masked_fill_(~there[:, None], 0)
+        return {"out": out.to(st["table"].dtype)}
+    dout = st["dout"]
+    ids, order = torch.sort(torch.where(there, ids, c["rows"]), stable=True)
+    found, many = torch.unique_consecutive(ids, return_counts=True)
+    ends = many.cumsum(0)
+    # sums over each id's stretch as differences of running sums, which are
+    # long: in 64 bits
+    sums = torch.zeros((c["width"], c["n"] + 1), dtype=torch.float64, device=ids.device)
+    torch.cumsum(dout[order].T.double(), 1, out=sums[:, 1:])
+    sums = ((sums[:, ends] - sums[:, ends - many]) * st["scale"]).T.to(dout.dtype)
+    in_table = found < c["rows"]
+    found, sums = found[in_table], sums[in_table]
+    if not c["listed"]:
+        out = torch.zeros((c["rows"], c["width"]), dtype=dout.dtype, device=ids.device)
+        out[found] = sums
+        return {"dtable": out}
+    n = found.numel()
+    out = {"grads": torch.zeros((c["n"], c["width"]), dtype=dout.dtype, device=ids.device),
+           "ids": torch.full((c["n"],), -1, dtype=torch.int32, device=ids.device),
+           "count": torch.tensor([n], dtype=torch.int32, device=ids.device)}
+    out["grads"][:n], out["ids"][:n] = sums, found.to(torch.int32)
+    return out
+
+
+def _combine(a, b, longest):
+    """h_t = a_t h_{t-1} + b_t over dimension 0, by doubling: a step joins what
+    two neighbouring stretches do.  a is 0 where a sequence begins."""
+    step = 1
+    while step < longest:
+        b = torch.cat([b[:step], b[step:] + a[step:] * b[:-step]])
+        a = torch.cat([a[:step], a[step:] * a[:-step]])
+        step *= 2
+    return b
+
+
+def _ends(st):
+    """First and last rows of the sequences."""
+    if st["start"] is not None:
+        return st["start"][:-1].long(), st["start"][1:].long() - 1
+    n = st["case"]["hi"]
+    first = torch.arange(st["case"]["batch"], device=st["x"].device) * n
+    return first, first + n - 1
+
+
+def _plain_scan(st):
+    x, g = st["x"].float(), st["g"].float()
+    z, one_less = torch.sigmoid(g), torch.sigmoid(-g)
+    first, last = _ends(st)
+    a, b = z.clone(), one_less * x
+    a[first] = 0
+    if st["h0"] is not None:
+        b[first] += z[first] * st["h0"]
+    h = _combine(a, b, st["longest"])
+    out = {"h": h.to(st["x"].dtype), "last": h[last]}
+    if "dh" not in st:
+        return out
+    before = torch.cat([h[:1], h[:-1]])
+    before[first] = st["h0"] if st["h0"] is not None else 0.0
+    # backwards: d_t = dh_t + z_{t+1} d_{t+1}
+    d = st["dh"].float()
+    if st["dlast"] is not None:
+        d[last] += st["dlast"]
+    a = torch.cat([z[1:], z[:1]])
+    a[last] = 0
+    d = _combine(a.flip(0), d.flip(0), st["longest"]).flip(0)
+    dtype = st["x"].dtype
+    out.update(dx=(one_less * d).to(dtype), dg=(z * one_less * d * (before - x)).to(dtype))
+    if st["h0"] is not None:
+        out["dh0"] = z[first] * d[first]
+    return out
+
+
+def _plain_rotate_rows(x, pos, freq, w, dy=None):
+    dtype, d = x.dtype, x.shape[2]
+    pos = pos.long() & 0xFFFFFFFF
+    there = (pos != 0xFFFFFFFF)[:, None, None]
+    x = x.float().masked_fill(~there, 0)
+    r = torch.rsqrt((x * x).mean(2, keepdim=True) + EPS)
+    xh = x * r
+    u = xh * w if w is not None else xh
+    m = 0 if freq is None else freq.numel()
+    if m:
+        angle = pos.double()[:, None] * freq.double()
+        cos, sin = angle.cos().float()[:, None], angle.sin().float()[:, None]
+        lo, hi = u[..., :m], u[..., m:2 * m]
+        u = torch.cat([lo * cos - hi * sin, hi * cos + lo * sin, u[..., 2 * m:]], 2)
+    y = u.to(dtype)
+    if dy is None:
+        return y, None, None
+    g = dy.float().masked_fill(~there, 0)
+    if m:
+        lo, hi = g[..., :m], g[..., m:2 * m]
+        g = torch.cat([lo * cos + hi * sin, hi * cos - lo * sin, g[..., 2 * m:]], 2)
+    dw = (g * xh).sum((0, 1), dtype=torch.float64).float()
+    if w is not None:
+        g = g * w
+    dx = r * (g - xh * (g * xh).mean(2, keepdim=True))
+    return y, dx.to(dtype), dw
+
+
+def _plain_rotate(st):
+    yq, dq, dwq = _plain_rotate_rows(st["q"], st["q_pos"], st["freq"], st["wq"], st.get("dq"))
+    yk, dk, dwk = _plain_rotate_rows(st["k"], st["k_pos"], st["freq"], st["wk"], st.get("dk"))
+    out = {"q": yq, "k": yk}
+    if "dq" in st:
+        out.update(dq=dq, dk=dk, dwq=dwq, dwk=dwk)
+    return out
+
+
+# ------------------------------------------------------------------ one pass
+def run(state):
+    c = state["case"]
+    kind = c["kind"].split("_")[0]
+    if not own:
+        return {"lookup": _plain_lookup, "scan": _plain_scan, "rotate": _plain_rotate}[kind](state)
+    import paper_2402_01964_amd as nlb
+    if kind == "lookup":
+        if "table" in state:
+            return {"out": nlb.lookup(state["table"], state["ids"], state["scale"])}
+        if not c["listed"]:
+            return {"dtable": nlb.lookup_backward(state["dout"], state["ids"], c["rows"], state["scale"])}
+        grads, ids, count = nlb.lookup_backward_listed(state["dout"], state["ids"], c["rows"], state["scale"],
+                                                       grads=state["grads"])
+        return {"grads": grads, "ids": ids, "count": count}
+    if kind == "scan":
+        how = dict(batch=c["batch"], start=state["start"], h0=state["h0"])
+        x, g = state["x"], state["g"]
+        if "dh" not in state:
+            h, last, _ = nlb.gated_scan(x, g, need_states=False, **how)
+            return {"h": h, "last": last}
+        h, last, states = nlb.gated_scan(x, g, **how)
+        dx, dg, dh0 = nlb.gated_scan_backward(state["dh"], x, g, states, dlast=state["dlast"], **how)
+        out = {"h": h, "last": last, "dx": dx, "dg": dg}
+        if dh0 is not None:
+            out["dh0"] = dh0
+        return out
+    args = (state["q"], state["k"], state["freq"], state["q_pos"], state["k_pos"], state["wq"], state["wk"], EPS)
+    q, k = nlb.norm_rotate(*args)
+    out = {"q": q, "k": k}
+    if "dq" in state:
+        out["dq"], out["dk"], out["dwq"], out["dwk"] = nlb.norm_rotate_backward(state["dq"], state["dk"], *args)
+    return out
+
+
+# ------------------------------------------------------------------ in 64 bits
+def _exact_lookup(c, st):
+    ids = st["ids"].long()
+    if c["kind"] == "lookup":
+        padded = torch.where((ids >= 0) & (ids < c["rows"]), ids, torch.full_like(ids, c["rows"]))
+        out = torch.empty((c["n"], c["width"]), dtype=torch.float64, device="cuda")
+        for a in range(0, c["n"], 1 << 20):                   # (in pieces: fp64 rows take room)
+            i = padded[a:a + (1 << 20)]
+            rows = st["table"][i.clamp(max=c["rows"] - 1)].double() * st["scale"]
+            out[a:a + (1 << 20)] = torch.where((i < c["rows"])[:, None], rows, torch.zeros_like(rows))
+        return {"out": out}
+    i = ((ids >= 0) & (ids < c["rows"])).nonzero()[:, 0]
+    if not c["listed"]:
+        out = torch.zeros((c["rows"], c["width"]), dtype=torch.float64, device="cuda")
+        return {"dtable": out.index_add_(0, ids[i], st["dout"][i].double()) * st["scale"]}
+    to = torch.unique(ids[i], return_inverse=True)[1]
+    out = torch.zeros((c["n"], c["width"]), dtype=torch.float64, device="cuda")
+    return {"grads": out.index_add_(0, to, st["dout"][i].double()) * st["scale"], "ids": None, "count": None}
+
+
+def _exact_chain(a, b):
+    """h_t = a_t h_{t-1} + b_t in fp64: stretches of rows one row after the
+    other, all stretches side by side, then their starts one after the other."""
+    t, d = b.shape
+    n = max(1, math.isqrt(t))
+    m = -(-t // n)                                            # n stretches of m rows
+    a = torch.cat([a, torch.zeros((n * m - t, d), dtype=a.dtype, device=a.device)]).view(n, m, d)
+    b = torch.cat([b, torch.zeros((n * m - t, d), dtype=a.dtype, device=a.device)]).view(n, m, d)
+    h, p = torch.empty_like(b), torch.empty_like(a)
+    s, q = torch.zeros_like(b[:, 0]), torch.ones_like(b[:, 0])
+    for i in range(m):
+        s, q = a[:, i] * s + b[:, i], q * a[:, i]
+        h[:, i], p[:, i] = s, q
+    into, s = torch.zeros_like(b[:, 0]), torch.zeros_like(b[0, 0])
+    for j in range(n):
+        into[j] = s
+        s = h[j, -1] + p[j, -1] * s
+    return (h + p * into[:, None]).reshape(n * m, d)[:t]
+
+
+def _exact_scan(c, st):
+    lengths = torch.tensor(_lengths(c), device="cuda")
+    last = lengths.cumsum(0) - 1
+    first = last - lengths + 1
+    x, g = st["x"].double(), st["g"].double()
+    z, y = 1 / (1 + torch.exp(-g)), 1 / (1 + torch.exp(g))
+    h0 = st["h0"].double() if st["h0"] is not None else torch.zeros((c["batch"], c["width"]), dtype=torch.float64,
+                                                                    device="cuda")
+    a, b = z.clone(), y * x
+    a[first] = 0
+    b[first] += z[first] * h0
+    h = _exact_chain(a, b)
+    out = {"h": h, "last": h[last]}
+    if "dh" in st:
+        d = st["dh"].double()
+        if st["dlast"] is not None:
+            d[last] += st["dlast"].double()
+        a = torch.roll(z, -1, 0)
+        a[last] = 0
+        d = _exact_chain(a.flip(0), d.flip(0)).flip(0)
+        h = torch.roll(h, 1, 0)
+        h[first] = h0
+        out.update(dx=y * d, dg=z * y * d * (h - x))
+        if st["h0"] is not None:
+            out["dh0"] = (z * d)[first]
+    return out
+
+
+def _exact_rotate(c, st):
+    out = {}
+    for name, x, pos, w in (("q", st["q"], st["q_pos"], st["wq"]), ("k", st["k"], st["k_pos"], st["wk"])):
+        n, h, d = x.shape
+        pos = pos.long() & 0xFFFFFFFF
+        w = torch.ones(d, dtype=torch.float64, device="cuda") if w is None else w.double()
+        # the rotation as a complex factor of the values i and m + i
+        m = c["rot"] // 2
+        turn = torch.polar(torch.ones((n, 1, m), dtype=torch.float64, device="cuda"),
+                           (pos.double()[:, None] * st["freq"].double())[:, None] if m else
+                           torch.zeros((n, 1, 0), dtype=torch.float64, device="cuda"))
+        y = torch.zeros((n, h, d), dtype=torch.float64, device="cuda")
+        dx, dw = torch.zeros_like(y), torch.zeros(d, dtype=torch.float64, device="cuda")
+        dy = st["d" + name] if "dq" in st else None
+        step = max(1, (1 << 26) // (h * d))
+        for a in range(0, n, step):
+            v = x[a:a + step].double()
+            v = torch.where((pos[a:a + step] == 0xFFFFFFFF)[:, None, None], torch.zeros_like(v), v)
+            r = (v.square().sum(2, keepdim=True) / d + EPS) ** -0.5
+            xh = v * r
+            u = xh * w
+            pair = torch.complex(u[..., :m], u[..., m:2 * m]) * turn[a:a + step]
+            y[a:a + step] = torch.cat([pair.real, pair.imag, u[..., 2 * m:]], 2)
+            if dy is None:
+                continue
+            gy = dy[a:a + step].double()
+            gy = torch.where((pos[a:a + step] == 0xFFFFFFFF)[:, None, None], torch.zeros_like(gy), gy)
+            pair = torch.complex(gy[..., :m], gy[..., m:2 * m]) * turn[a:a + step].conj()
+            du = torch.cat([pair.real, pair.imag, gy[..., 2 * m:]], 2)
+            dw += (du * xh).sum((0, 1))
+            g = du * w
+            dx[a:a + step] = r * (g - xh * (g * xh).sum(2, keepdim=True) / d)
+        out[name] = y
+        if dy is not None:
+            out["d" + name], out["dw" + name] = dx, dw
+    if "dq" in st:                                            # in run()'s order
+        out = {k: out[k] for k in ("q", "k", "dq", "dk", "dwq", "dwk")}
+    return out
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    return {"lookup": _exact_lookup, "scan": _exact_scan, "rotate": _exact_rotate}[case["kind"].split("_")[0]](case, st)
+
+
+# ------------------------------------------------------------------ what it cannot do without
+def work(case):
+    c = case
+    e = 2 if c["dtype"] == "bf16" else 4
+    train = c["kind"].endswith("_train")
+    if c["kind"].startswith("lookup"):
+        n, rows, d = c["n"], c["rows"], c["width"]
+        some = n * c["fill"]
+        # rows that occur: the expected number of distinct ids
+        if c["even"]:
+            found = -rows * math.expm1(-some / rows)
+        else:
+            top, found = math.log(rows + 1), 0.0
+            for i in range(200):                              # ranks from e^lo to e^hi
+                lo, hi = top * i / 200, top * (i + 1) / 200
+                size = math.exp(hi) - math.exp(lo)
+                found -= size * math.expm1(-some * (hi - lo) / top / size)
+        found = min(found, some, rows)
+        if not train:
+            return {"bytes": 4.0 * n + e * d * (found + n), "flops": float(n * d)}
+        out = found if c["listed"] else rows
+        return {"bytes": 4.0 * n + e * d * (some + out) + (4.0 * n if c["listed"] else 0.0), "flops": some * d}
+    if c["kind"].startswith("scan"):
+        values, states = sum(_lengths(c)) * c["width"], 4 * c["batch"] * c["width"]
+        size, flops = 3 * e * values + states * (2 if c["first"] else 1), 8 * values
+        if train:
+            size, flops = size + 5 * e * values + states * (3 if c["first"] else 0), flops + 20 * values
+        return {"bytes": float(size), "flops": float(flops)}
+    q = c["q_rows"] * c["heads"] * c["dim"]
+    all_k = (c["k_rows"] or c["q_rows"]) * c["kv_heads"] * c["dim"]
+    k = all_k * c["fill"]
+    size = e * (q + k) + e * (q + all_k) + 4 * (c["q_rows"] + c["k_rows"])
+    flops = 7.0 * (q + k)
+    if train:
+        size += e * 2 * (q + k) + e * (q + all_k) + 4 * (c["q_rows"] + c["k_rows"])
+        flops += 16.0 * (q + k)
+    return {"bytes": float(size), "flops": float(flops)}
