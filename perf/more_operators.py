@@ -276,7 +276,7 @@ def _plain_scan(st):
     before = torch.cat([h[:1], h[:-1]])
     before[first] = st["h0"] if st["h0"] is not None else 0.0
     # backwards: d_t = dh_t + z_{t+1} d_{t+1}
-    d = st["dh"].float()
+    d = st["dh"].to(torch.float32, copy=True)
     if st["dlast"] is not None:
         d[last] += st["dlast"]
     a = torch.cat([z[1:], z[:1]])
