@@ -521,6 +521,65 @@ int nlb_layer_norm_work(const nlb_norm_call *call, size_t *bytes);
 int nlb_layer_norm_backward(const nlb_norm_call *call, const void *dy, int64_t dy_stride, void *dx,
                             int64_t dx_stride, float *dw, float *db, void *work, size_t work_bytes, void *stream);
 
+/* A gated linear recurrence over packed sequences, channel by channel: a state
+ * for each node's history that a scan makes for all its events at once, or that
+ * one event moves on (a sequence of one row).
+ *   z_t = sigmoid(g_t),  h_t = z_t h_{t-1} + (1 - z_t) x_t
+ * from h0[b] (NULL: zeros) before sequence b's first row; last[b] is the state
+ * behind its last row (h0[b] where it has none).
+ *   Sequences.  Sequence b has the rows start[b] .. start[b + 1] - 1 (device
+ * int32 [batch + 1], non-decreasing; lengths may be zero, the host need not
+ * know them).  start NULL: rows / batch rows each (no rest).  Starts outside
+ * [0, rows] are taken as the nearest end.  Rows before the first and behind the
+ * last sequence are neither read nor written.
+ *   Rows.  x, g, h: [rows][width] of dtype, at any row stride (in values,
+ * 0 .. 2^31 - 1); a row's values are contiguous.  h may be x.  h0, last: device
+ * fp32 [batch][width], contiguous; last may be NULL, and may be h0 where start
+ * is NULL and rows == batch (else arrays that overlap are refused).  states
+ * (device fp32 [rows / NLB_SCAN_STATE_ROWS, rounded up][width]) is what a
+ * backward pass starts from; NULL where none follows.
+ *   Numerics.  Gates, states and products are fp32 (1 - z is not formed by
+ * subtraction), h is rounded once.  Gates beyond 80 in magnitude count as 80.
+ * Maps of 16 rows and more are joined in a fixed tree: the same call gives the
+ * same bits.  What one sequence holds (NaN, infinities) does not reach another.
+ *   nlb_gated_scan_backward, from the same call, states as written, the gradient
+ * dh of h and that of last (dlast, NULL: zeros):
+ *   d_t = dh_t + z_{t+1} d_{t+1}  (behind the last row: dlast)
+ *   dx = (1 - z) d,  dg = z (1 - z) d (h_{t-1} - x),  dh0[b] = z d of the first row
+ * (dlast[b] where a sequence has no rows).  h is made again in fp32, not read.
+ * dx, dg: rows as x; dx may be dh.  dh0: device fp32 [batch][width] or NULL.
+ *   Work: nlb_gated_scan_work bytes of device memory (16-byte aligned, may be
+ * NULL if that is 0) for either pass, used by the call's kernels only.  Only
+ * enqueues kernels: may be captured in a HIP graph.  Written rows must not
+ * overlap each other.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
+#define NLB_SCAN_MAX_WIDTH 65536
+#define NLB_SCAN_MAX_ROWS 2147480000u
+#define NLB_SCAN_STATE_ROWS 64
+
+typedef struct nlb_scan_rows {
+    void *data;
+    int64_t row_stride;      /* values */
+} nlb_scan_rows;
+
+typedef struct nlb_scan_call {
+    int32_t device;          /* HIP device ordinal, -1 = current */
+    int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: x, g, h and their gradients */
+    uint32_t rows, batch;
+    int32_t width;           /* 1 .. NLB_SCAN_MAX_WIDTH */
+    const int32_t *start;
+    const float *h0;
+    nlb_scan_rows x, g;      /* not written */
+} nlb_scan_call;
+
+int nlb_gated_scan_work(const nlb_scan_call *call, size_t *bytes);
+
+int nlb_gated_scan(const nlb_scan_call *call, const nlb_scan_rows *h, float *last, float *states, void *work,
+                   size_t work_bytes, void *stream);
+
+int nlb_gated_scan_backward(const nlb_scan_call *call, const float *states, const nlb_scan_rows *dh,
+                            const float *dlast, const nlb_scan_rows *dx, const nlb_scan_rows *dg, float *dh0,
+                            void *work, size_t work_bytes, void *stream);
+
 /* Free the table's device memory after synchronising its device.  NULL is a
  * no-op.  Borrowed buffers are not touched. */
 int nlb_destroy(nlb_table *h);

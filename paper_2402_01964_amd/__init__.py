@@ -26,6 +26,7 @@ MAX_SLOTS = 1024
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
                "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
                "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward",
+               "nlb_gated_scan", "nlb_gated_scan_work", "nlb_gated_scan_backward",
                "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status", "nlb_strerror")
 AGG_HIDDEN = 64
 RNN_MAX_DIM = 1024
@@ -33,6 +34,7 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 RNN_FORM_NONE, RNN_FORM_TILED, RNN_FORM_WEIGHT_STATIONARY = 0, 1, 2
 ATT_MAX_DIM, ATT_MAX_HEADS, ATT_MAX_BUCKETS = 128, 256, 64
 NORM_MAX_WIDTH = 8192
+SCAN_MAX_WIDTH, SCAN_MAX_ROWS, SCAN_STATE_ROWS = 65536, 2147480000, 64
 EID_LAST_BATCH = 2**64 - 1   # first_eid of rnn_update: the links inserted last (device count)
 
 
@@ -85,6 +87,17 @@ class _NormCall(ctypes.Structure):
     _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_uint32),
                 ("width", ctypes.c_int32), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64)] + \
                [(k, ctypes.c_void_p) for k in ("w", "mean", "rstd")]
+
+
+class _ScanRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64)]
+
+
+class _ScanCall(ctypes.Structure):                            # (x, g: nlb_scan_rows each)
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_uint32),
+                ("batch", ctypes.c_uint32), ("width", ctypes.c_int32), ("start", ctypes.c_void_p),
+                ("h0", ctypes.c_void_p)] + \
+               [(t + f, c) for t in ("x", "g") for f, c in (("", ctypes.c_void_p), ("_row", ctypes.c_int64))]
 
 
 class _Info(ctypes.Structure):
@@ -146,6 +159,13 @@ def load_library(path: str | None = None):
     lib.nlb_layer_norm_work.restype = I
     lib.nlb_layer_norm_backward.argtypes = [N, P, I64, P, I64, P, P, P, S, P]
     lib.nlb_layer_norm_backward.restype = I
+    G, GR = ctypes.POINTER(_ScanCall), ctypes.POINTER(_ScanRows)
+    lib.nlb_gated_scan_work.argtypes = [G, ctypes.POINTER(S)]
+    lib.nlb_gated_scan_work.restype = I
+    lib.nlb_gated_scan.argtypes = [G, GR, P, P, P, S, P]
+    lib.nlb_gated_scan.restype = I
+    lib.nlb_gated_scan_backward.argtypes = [G, P, GR, P, GR, GR, P, P, S, P]
+    lib.nlb_gated_scan_backward.restype = I
     lib.nlb_destroy.argtypes = [P]
     lib.nlb_destroy.restype = I
     lib.nlb_get_info.argtypes = [P, ctypes.POINTER(_Info)]
@@ -698,3 +718,121 @@ def layer_norm_backward(dy, x, w, mean, rstd, *, dx=None, dw=None, db=None, work
                                        _vector(dw, c.width, x, fp32, "dw"), _vector(db, c.width, x, fp32, "db"), p,
                                        size, _current_stream(x.device)), "nlb_layer_norm_backward")
     return dx, dw, db
+
+
+def _scan_rows(t, x, name):
+    """A tensor [rows, width] with contiguous values as (pointer, row stride)."""
+    if t.dtype != x.dtype or t.device != x.device:
+        raise TypeError(f"{name} must have x's type and device")
+    if t.shape != x.shape:
+        raise ValueError(f"{name} must be {list(x.shape)}, not {list(t.shape)}")
+    s = t.stride()
+    if s[1] != 1 and x.shape[1] > 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return t.data_ptr(), s[0]
+
+
+def _scan_call(x, g, batch, start, h0):
+    import torch
+    dtype = _float_dtype(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x and g must be [rows, width]")
+    rows, width = x.shape
+    if batch is None:
+        batch = 1 if start is None else start.numel() - 1
+    if (batch | rows | width) >> 31:
+        raise ValueError(_SIZES)
+    return _ScanCall(x.device.index, dtype, rows, batch, width, _vector(start, batch + 1, x, (torch.int32,), "start"),
+                     _states(h0, batch, x, "h0"), *_scan_rows(x, x, "x"), *_scan_rows(g, x, "g"))
+
+
+def _states(t, batch, x, name):
+    import torch
+    if t is not None and t.shape != (batch, x.shape[1]):
+        raise ValueError(f"{name} must be [batch, width]")
+    return _vector(t, batch * x.shape[1], x, (torch.float32,), name)
+
+
+def gated_scan_work(x, g, *, batch=None, start=None, h0=None) -> int:
+    """Bytes of working memory that such a call takes (``work=``), forward or
+    backward."""
+    n = ctypes.c_size_t()
+    _check(load_library().nlb_gated_scan_work(_scan_call(x, g, batch, start, h0), n), "nlb_gated_scan_work")
+    return n.value
+
+
+def gated_scan(x, g, *, batch=None, start=None, h0=None, need_states=True, out=None, last=None, states=None, work=None,
+               stream=None):
+    """Gated linear recurrence over packed sequences (nlb_gated_scan): ``x``,
+    ``g`` [rows, width], float32 or bfloat16, any row stride; h = z h' + (1 -
+    z) x with z = sigmoid(g) and h' the state before.  ``start``: int32
+    [batch + 1] first rows, or None for rows / batch each.  ``h0``: float32
+    [batch, width] first states, or None for zeros; ``last`` may be h0 itself
+    where each sequence is one row.  Returns (or fills) out (as x), last
+    (float32 [batch, width]) and the states that gated_scan_backward starts
+    from (float32 [ceil(rows / SCAN_STATE_ROWS), width]; None with
+    need_states=False).  ``work``: gated_scan_work bytes, allocated if None.
+    No autograd graph is kept, as in ``attention``."""
+    import torch
+    lib = load_library()
+    c = _scan_call(x, g, batch, start, h0)
+    _no_graph("gated_scan", x, g, h0)
+    if stream is not None:
+        with _on(stream, x.device):
+            return gated_scan(x, g, batch=batch, start=start, h0=h0, need_states=need_states, out=out, last=last,
+                              states=states, work=work)
+    if out is None:
+        out = x.new_empty(x.shape)
+    if last is None:
+        last = x.new_empty((c.batch, c.width), dtype=torch.float32)
+    shape = (-(-c.rows // SCAN_STATE_ROWS), c.width)
+    if not need_states:
+        states = None
+    elif states is None:
+        states = x.new_empty(shape, dtype=torch.float32)
+    elif states.shape != shape:
+        raise ValueError(f"states must be {list(shape)}, not {list(states.shape)}")
+    h = _ScanRows(*_scan_rows(out, x, "out"))
+    args = c, h, _states(last, c.batch, x, "last"), _vector(states, shape[0] * shape[1], x, (torch.float32,), "states")
+    if work is None:                                          # asked for only where one is needed
+        rc = lib.nlb_gated_scan(*args, None, 0, _current_stream(x.device))
+        if rc != NLB_ESCRATCH:
+            _check(rc, "nlb_gated_scan")
+            return out, last, states
+    keep, p, size = _work(lib.nlb_gated_scan_work, c, (), work, x, "nlb_gated_scan")
+    _check(lib.nlb_gated_scan(*args, p, size, _current_stream(x.device)), "nlb_gated_scan")
+    return out, last, states
+
+
+def gated_scan_backward(dout, x, g, states, *, dlast=None, batch=None, start=None, h0=None, dx=None, dg=None, dh0=None,
+                        need_dh0=True, work=None, stream=None):
+    """Gradients of ``gated_scan`` (nlb_gated_scan_backward) from the same
+    arguments, its ``states``, the gradient ``dout`` of its result and that of
+    its last states (``dlast``, float32, None for zeros).  Returns (or fills)
+    dx, dg (as x) and dh0 (float32; None without h0, or with need_dh0=False)."""
+    import torch
+    lib = load_library()
+    c = _scan_call(x, g, batch, start, h0)
+    if stream is not None:
+        with _on(stream, x.device):
+            return gated_scan_backward(dout, x, g, states, dlast=dlast, batch=batch, start=start, h0=h0, dx=dx, dg=dg,
+                                       dh0=dh0, need_dh0=need_dh0, work=work)
+    shape = (-(-c.rows // SCAN_STATE_ROWS), c.width)
+    if states.shape != shape:
+        raise ValueError(f"states must be {list(shape)}, not {list(states.shape)}")
+    dx, dg = (x.new_empty(x.shape) if t is None else t for t in (dx, dg))
+    if h0 is None or not need_dh0:
+        dh0 = None
+    elif dh0 is None:
+        dh0 = x.new_empty((c.batch, c.width), dtype=torch.float32)
+    rows = [_ScanRows(*_scan_rows(t, x, name)) for t, name in ((dout, "dout"), (dx, "dx"), (dg, "dg"))]
+    args = (c, _vector(states, shape[0] * shape[1], x, (torch.float32,), "states"), rows[0],
+            _states(dlast, c.batch, x, "dlast"), rows[1], rows[2], _states(dh0, c.batch, x, "dh0"))
+    if work is None:
+        rc = lib.nlb_gated_scan_backward(*args, None, 0, _current_stream(x.device))
+        if rc != NLB_ESCRATCH:
+            _check(rc, "nlb_gated_scan_backward")
+            return dx, dg, dh0
+    keep, p, size = _work(lib.nlb_gated_scan_work, c, (), work, x, "nlb_gated_scan_backward")
+    _check(lib.nlb_gated_scan_backward(*args, p, size, _current_stream(x.device)), "nlb_gated_scan_backward")
+    return dx, dg, dh0
