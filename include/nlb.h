@@ -521,6 +521,57 @@ int nlb_layer_norm_work(const nlb_norm_call *call, size_t *bytes);
 int nlb_layer_norm_backward(const nlb_norm_call *call, const void *dy, int64_t dy_stride, void *dx,
                             int64_t dx_stride, float *dw, float *db, void *work, size_t work_bytes, void *stream);
 
+/* RMS norm of each head's queries and keys and their rotation by position, in
+ * one pass, between the projections and the attention:
+ *   u = x (sum x^2 / dim + eps)^-1/2 w,  a_i = pos freq[i]  for i < m = freqs
+ *   y_i = u_i cos a_i - u_{m+i} sin a_i,  y_{m+i} = u_{m+i} cos a_i + u_i sin a_i
+ *   y = u  behind the first 2 m values of a head
+ * so that the product of a query and a key depends on the gap of their
+ * positions alone: by places, or by timestamps with the frequencies of a time
+ * encoding (nlb_sample's tq and ts go in as they are).
+ *   Rows.  q: [q_rows][heads][dim], k: [k_rows][kv_heads][dim] of dtype, as for
+ * nlb_attention, and so the results (which may be q and k themselves); k_rows
+ * = 0: no keys.  q_pos, k_pos: device uint32, one for each row (NULL: 0, where
+ * freqs is 0).  A row at position 0xFFFFFFFF is an empty slot, as nlb_sample's
+ * ts marks it: it is not read, its result and gradient are zeros and it takes
+ * no part in dwq and dwk.  freq: device fp32 [freqs]; wq, wk: device fp32 [dim],
+ * NULL for ones.
+ *   Numerics.  Angles are formed and reduced in 64 bits: their error is some
+ * 2^-24 and |a| 2^-51.  Sums and products are fp32, each row's values are read
+ * once and rounded once.
+ *   nlb_norm_rotate_backward, from the same call (q and k as they went in) and
+ * the gradients dq_out, dk_out of the results: with du = the gradient rotated
+ * by -a, g = du w, r = the norm's factor,
+ *   dq = r (g - x r^2 sum(g x) / dim),  dwq = sum over rows and heads of du x r
+ * and so for k.  dq, dk may be dq_out, dk_out.  dwq, dwk: device fp32 [dim],
+ * written (not added to), each may be NULL; with both NULL no work is needed,
+ * else nlb_norm_rotate_work bytes of device memory (16-byte aligned) that the
+ * call's kernels use.  Their sums are fp32 within a workgroup, then fp64, in a
+ * fixed order: the same call gives the same bits.
+ *   Only enqueues kernels: may be captured in a HIP graph.  Written rows must
+ * not overlap each other.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
+typedef struct nlb_rotate_call {
+    int32_t device;          /* HIP device ordinal, -1 = current */
+    int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: q, k, the results and their gradients */
+    int32_t dim;             /* 1 .. NLB_ATT_MAX_DIM */
+    int32_t freqs;           /* 0 .. dim / 2 */
+    int32_t heads, kv_heads; /* 1 (kv_heads without keys: 0) .. NLB_ATT_MAX_HEADS */
+    uint32_t q_rows, k_rows;
+    float eps;
+    const float *freq;
+    const uint32_t *q_pos, *k_pos;
+    const float *wq, *wk;
+    nlb_att_rows q, k;       /* not written */
+} nlb_rotate_call;
+
+int nlb_norm_rotate(const nlb_rotate_call *call, const nlb_att_rows *q_out, const nlb_att_rows *k_out, void *stream);
+
+int nlb_norm_rotate_work(const nlb_rotate_call *call, size_t *bytes);
+
+int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq_out, const nlb_att_rows *dk_out,
+                             const nlb_att_rows *dq, const nlb_att_rows *dk, float *dwq, float *dwk, void *work,
+                             size_t work_bytes, void *stream);
+
 /* A gated linear recurrence over packed sequences, channel by channel: a state
  * for each node's history that a scan makes for all its events at once, or that
  * one event moves on (a sequence of one row).

@@ -26,6 +26,7 @@ MAX_SLOTS = 1024
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
                "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
                "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward",
+               "nlb_norm_rotate", "nlb_norm_rotate_work", "nlb_norm_rotate_backward",
                "nlb_gated_scan", "nlb_gated_scan_work", "nlb_gated_scan_backward",
                "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status", "nlb_strerror")
 AGG_HIDDEN = 64
@@ -87,6 +88,14 @@ class _NormCall(ctypes.Structure):
     _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_uint32),
                 ("width", ctypes.c_int32), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64)] + \
                [(k, ctypes.c_void_p) for k in ("w", "mean", "rstd")]
+
+
+class _RotateCall(ctypes.Structure):                          # (q, k: nlb_att_rows each)
+    _fields_ = [(k, ctypes.c_int32) for k in ("device", "dtype", "dim", "freqs", "heads", "kv_heads")] + \
+               [("q_rows", ctypes.c_uint32), ("k_rows", ctypes.c_uint32), ("eps", ctypes.c_float)] + \
+               [(k, ctypes.c_void_p) for k in ("freq", "q_pos", "k_pos", "wq", "wk")] + \
+               [(t + f, c) for t in ("q", "k")
+                for f, c in (("", ctypes.c_void_p), ("_row", ctypes.c_int64), ("_head", ctypes.c_int64))]
 
 
 class _ScanRows(ctypes.Structure):
@@ -159,6 +168,13 @@ def load_library(path: str | None = None):
     lib.nlb_layer_norm_work.restype = I
     lib.nlb_layer_norm_backward.argtypes = [N, P, I64, P, I64, P, P, P, S, P]
     lib.nlb_layer_norm_backward.restype = I
+    T = ctypes.POINTER(_RotateCall)
+    lib.nlb_norm_rotate.argtypes = [T, R, R, P]
+    lib.nlb_norm_rotate.restype = I
+    lib.nlb_norm_rotate_work.argtypes = [T, ctypes.POINTER(S)]
+    lib.nlb_norm_rotate_work.restype = I
+    lib.nlb_norm_rotate_backward.argtypes = [T, R, R, R, R, P, P, P, S, P]
+    lib.nlb_norm_rotate_backward.restype = I
     G, GR = ctypes.POINTER(_ScanCall), ctypes.POINTER(_ScanRows)
     lib.nlb_gated_scan_work.argtypes = [G, ctypes.POINTER(S)]
     lib.nlb_gated_scan_work.restype = I
@@ -718,6 +734,96 @@ def layer_norm_backward(dy, x, w, mean, rstd, *, dx=None, dw=None, db=None, work
                                        _vector(dw, c.width, x, fp32, "dw"), _vector(db, c.width, x, fp32, "db"), p,
                                        size, _current_stream(x.device)), "nlb_layer_norm_backward")
     return dx, dw, db
+
+
+def _rotate_call(q, k, freq, q_pos, k_pos, wq, wk, eps):
+    import torch
+    dtype = _float_dtype(q, "q")
+    if q.dim() != 3 or (k is not None and k.dim() != 3):
+        raise ValueError("q and k must be [rows, heads, dim]")
+    q_rows, heads, dim = q.shape
+    k_rows, kv_heads = (0, 0) if k is None else k.shape[:2]
+    if (q_rows | k_rows | heads | kv_heads | dim) >> 31:
+        raise ValueError(_SIZES)
+    fp32, words = (torch.float32,), (torch.int32, torch.uint32)
+    m = 0 if freq is None else freq.numel()
+    if m and (q_pos is None or (k is not None and k_pos is None)):
+        raise ValueError("a rotation needs positions")
+    if k is None and (k_pos is not None or wk is not None):
+        raise ValueError("k_pos and wk need k")
+    if 2 * m > dim:
+        raise ValueError("freq must have at most dim / 2 elements")
+    return _RotateCall(q.device.index, dtype, dim, m, heads, kv_heads, q_rows, k_rows, eps,
+                       _vector(freq, m, q, fp32, "freq"), _vector(q_pos, q_rows, q, words, "q_pos"),
+                       _vector(k_pos, k_rows, q, words, "k_pos"), _vector(wq, dim, q, fp32, "wq"),
+                       _vector(wk, dim, q, fp32, "wk"), *_att_rows(q, q, q.shape, "q"),
+                       *((None, 0, 0) if k is None else _att_rows(k, q, (k_rows, kv_heads, dim), "k")))
+
+
+def _rotated(t, like, q, name):
+    """A result for `like`'s rows (allocated if None) and its structure."""
+    if like is None:
+        if t is not None:
+            raise ValueError(f"{name} without k")
+        return None, None
+    t = q.new_empty(like.shape) if t is None else t
+    return t, _AttRows(*_att_rows(t, q, like.shape, name))
+
+
+def norm_rotate(q, k, freq, q_pos, k_pos, wq=None, wk=None, eps: float = 1e-5, *, q_out=None, k_out=None, stream=None):
+    """RMS norm of each head's queries and keys and their rotation by position
+    (nlb_norm_rotate): ``q`` [q_rows, heads, dim], ``k`` [k_rows, kv_heads,
+    dim] or None, float32 or bfloat16, any row and head strides; ``freq``
+    float32 [m] turns the pairs (i, m + i) by pos * freq[i], None: no rotation;
+    ``q_pos``, ``k_pos`` one int32 or uint32 for each row (places, or tq and ts:
+    rows at 0xFFFFFFFF, empty slots, give zeros); ``wq``, ``wk`` float32 [dim]
+    or None.  Returns (or fills) q_out and k_out, which may be q and k.  No
+    autograd graph is kept, as in ``attention``."""
+    lib = load_library()
+    c = _rotate_call(q, k, freq, q_pos, k_pos, wq, wk, eps)
+    _no_graph("norm_rotate", q, k, freq, wq, wk)
+    if stream is not None:
+        with _on(stream, q.device):
+            return norm_rotate(q, k, freq, q_pos, k_pos, wq, wk, eps, q_out=q_out, k_out=k_out)
+    q_out, a = _rotated(q_out, q, q, "q_out")
+    k_out, b = _rotated(k_out, k, q, "k_out")
+    _check(lib.nlb_norm_rotate(c, a, b, _current_stream(q.device)), "nlb_norm_rotate")
+    return q_out, k_out
+
+
+def norm_rotate_backward(dq_out, dk_out, q, k, freq, q_pos, k_pos, wq=None, wk=None, eps: float = 1e-5, *, dq=None,
+                         dk=None, dwq=None, dwk=None, need_dw=True, work=None, stream=None):
+    """Gradients of ``norm_rotate`` (nlb_norm_rotate_backward) from the same
+    arguments (q and k as they went in) and the gradients ``dq_out``,
+    ``dk_out`` of its results.  Returns (or fills) dq, dk (which may be dq_out
+    and dk_out) and dwq, dwk (float32 [dim]; None with need_dw=False, and what
+    belongs to k without it)."""
+    import torch
+    lib = load_library()
+    c = _rotate_call(q, k, freq, q_pos, k_pos, wq, wk, eps)
+    if stream is not None:
+        with _on(stream, q.device):
+            return norm_rotate_backward(dq_out, dk_out, q, k, freq, q_pos, k_pos, wq, wk, eps, dq=dq, dk=dk, dwq=dwq,
+                                        dwk=dwk, need_dw=need_dw, work=work)
+    if k is None and (dk_out is not None or dwk is not None):
+        raise ValueError("dk_out and dwk need k")
+    gq = _AttRows(*_att_rows(dq_out, q, q.shape, "dq_out"))
+    gk = None if k is None else _AttRows(*_att_rows(dk_out, q, k.shape, "dk_out"))
+    dq, a = _rotated(dq, q, q, "dq")
+    dk, b = _rotated(dk, k, q, "dk")
+    fp32 = (torch.float32,)
+    if not need_dw:
+        dwq = dwk = None
+    else:
+        dwq = q.new_empty(c.dim, dtype=torch.float32) if dwq is None else dwq
+        if k is not None and dwk is None:
+            dwk = q.new_empty(c.dim, dtype=torch.float32)
+    keep, p, size = _work(lib.nlb_norm_rotate_work, c, (), work, q, "nlb_norm_rotate_backward") if need_dw \
+        else (None, None, 0)
+    _check(lib.nlb_norm_rotate_backward(c, gq, gk, a, b, _vector(dwq, c.dim, q, fp32, "dwq"),
+                                        _vector(dwk, c.dim, q, fp32, "dwk"), p, size, _current_stream(q.device)),
+           "nlb_norm_rotate_backward")
+    return dq, dk, dwq, dwk
 
 
 def _scan_rows(t, x, name):
