@@ -521,6 +521,47 @@ int nlb_layer_norm_work(const nlb_norm_call *call, size_t *bytes);
 int nlb_layer_norm_backward(const nlb_norm_call *call, const void *dy, int64_t dy_stride, void *dx,
                             int64_t dx_stride, float *dw, float *db, void *work, size_t work_bytes, void *stream);
 
+/* Rows of a learned table by id, and the table's gradient: the rows that
+ * nlb_sample gathers as nfeat and self are those of its nbr and node ids, so
+ * that a table can be trained through them.
+ *   nlb_lookup: out_i = scale table[ids[i]], zeros where ids[i] is none of 0 ..
+ * rows - 1 (nbr's -1, an empty slot).  table: device [rows][width], out: device
+ * [n][width] of dtype, at any row stride (in values, 0 .. 2^31 - 1); a row's
+ * values are contiguous.  Rounded once.
+ *   nlb_lookup_backward, from the same call and the gradient dout of out:
+ *   dtable_r = scale (sum of dout_i over the i with ids[i] = r)
+ * list and count NULL: the whole gradient, [rows][width], zeros for rows that
+ * do not occur.  Else the rows that occur: list (device int32 [n]) gets their
+ * ids, ascending, and -1 behind them, count (device uint32) their number, and
+ * the first `count` rows of dtable ([n][width]) their gradients; the rows behind
+ * them stay as they are.  The ids are sorted; a row's gradients are added up in
+ * fp32 in an order that the ids alone set, no atomics on results: the same call
+ * gives the same bits.  Rows of ids outside the table are not read.
+ *   Work: nlb_lookup_work bytes of device memory (16-byte aligned; listed = 0
+ * for the whole gradient, 1 for the rows that occur), used by the call's kernels
+ * only.  Only enqueues kernels: may be captured in a HIP graph.  Written rows
+ * must not overlap each other or what is read.  Errors: NLB_EINVAL,
+ * NLB_ESCRATCH, NLB_EDEVICE. */
+#define NLB_LOOKUP_MAX_WIDTH 65536
+
+typedef struct nlb_lookup_call {
+    int32_t device;          /* HIP device ordinal, -1 = current */
+    int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: table, out and their gradients */
+    uint32_t n, rows;        /* ids (0 .. 2^31 - 1); rows of the table (1 .. 2^31 - 1) */
+    int32_t width;           /* 1 .. NLB_LOOKUP_MAX_WIDTH */
+    float scale;             /* finite */
+    const int32_t *ids;
+} nlb_lookup_call;
+
+int nlb_lookup(const nlb_lookup_call *call, const void *table, int64_t table_stride, void *out, int64_t out_stride,
+               void *stream);
+
+int nlb_lookup_work(const nlb_lookup_call *call, int32_t listed, size_t *bytes);
+
+int nlb_lookup_backward(const nlb_lookup_call *call, const void *dout, int64_t dout_stride, void *dtable,
+                        int64_t dtable_stride, int32_t *list, uint32_t *count, void *work, size_t work_bytes,
+                        void *stream);
+
 /* RMS norm of each head's queries and keys and their rotation by position, in
  * one pass, between the projections and the attention:
  *   u = x (sum x^2 / dim + eps)^-1/2 w,  a_i = pos freq[i]  for i < m = freqs

@@ -26,6 +26,7 @@ MAX_SLOTS = 1024
 ABI_SYMBOLS = ("nlb_create", "nlb_insert_batch", "nlb_sample", "nlb_sample_hop2", "nlb_time_encode", "nlb_aggregate",
                "nlb_rnn_update", "nlb_rnn_update_noalloc", "nlb_attention_work", "nlb_attention",
                "nlb_attention_backward", "nlb_layer_norm", "nlb_layer_norm_work", "nlb_layer_norm_backward",
+               "nlb_lookup", "nlb_lookup_work", "nlb_lookup_backward",
                "nlb_norm_rotate", "nlb_norm_rotate_work", "nlb_norm_rotate_backward",
                "nlb_gated_scan", "nlb_gated_scan_work", "nlb_gated_scan_backward",
                "nlb_destroy", "nlb_get_info", "nlb_export", "nlb_status", "nlb_strerror")
@@ -35,6 +36,7 @@ DTYPE_F32, DTYPE_BF16 = 0, 1
 RNN_FORM_NONE, RNN_FORM_TILED, RNN_FORM_WEIGHT_STATIONARY = 0, 1, 2
 ATT_MAX_DIM, ATT_MAX_HEADS, ATT_MAX_BUCKETS = 128, 256, 64
 NORM_MAX_WIDTH = 8192
+LOOKUP_MAX_WIDTH = 65536
 SCAN_MAX_WIDTH, SCAN_MAX_ROWS, SCAN_STATE_ROWS = 65536, 2147480000, 64
 EID_LAST_BATCH = 2**64 - 1   # first_eid of rnn_update: the links inserted last (device count)
 
@@ -88,6 +90,12 @@ class _NormCall(ctypes.Structure):
     _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rows", ctypes.c_uint32),
                 ("width", ctypes.c_int32), ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64)] + \
                [(k, ctypes.c_void_p) for k in ("w", "mean", "rstd")]
+
+
+class _LookupCall(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n", ctypes.c_uint32),
+                ("rows", ctypes.c_uint32), ("width", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("ids", ctypes.c_void_p)]
 
 
 class _RotateCall(ctypes.Structure):                          # (q, k: nlb_att_rows each)
@@ -168,6 +176,13 @@ def load_library(path: str | None = None):
     lib.nlb_layer_norm_work.restype = I
     lib.nlb_layer_norm_backward.argtypes = [N, P, I64, P, I64, P, P, P, S, P]
     lib.nlb_layer_norm_backward.restype = I
+    L = ctypes.POINTER(_LookupCall)
+    lib.nlb_lookup.argtypes = [L, P, I64, P, I64, P]
+    lib.nlb_lookup.restype = I
+    lib.nlb_lookup_work.argtypes = [L, ctypes.c_int32, ctypes.POINTER(S)]
+    lib.nlb_lookup_work.restype = I
+    lib.nlb_lookup_backward.argtypes = [L, P, I64, P, I64, P, P, P, S, P]
+    lib.nlb_lookup_backward.restype = I
     T = ctypes.POINTER(_RotateCall)
     lib.nlb_norm_rotate.argtypes = [T, R, R, P]
     lib.nlb_norm_rotate.restype = I
@@ -734,6 +749,118 @@ def layer_norm_backward(dy, x, w, mean, rstd, *, dx=None, dw=None, db=None, work
                                        _vector(dw, c.width, x, fp32, "dw"), _vector(db, c.width, x, fp32, "db"), p,
                                        size, _current_stream(x.device)), "nlb_layer_norm_backward")
     return dx, dw, db
+
+
+def _table_rows(t, like, rows, width, name):
+    """A tensor [rows, width] with contiguous values as (pointer, row stride)."""
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError(f"{name} must have {like.dtype} values, on the other tensors' device")
+    if t.dim() != 2 or t.shape != (rows, width):
+        raise ValueError(f"{name} must be {[rows, width]}, not {list(t.shape)}")
+    s = t.stride()
+    if s[1] != 1 and width > 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    return t.data_ptr(), s[0]
+
+
+def _lookup_call(like, ids, rows, width, scale, name):
+    import torch
+    dtype = _float_dtype(like, name)
+    if not isinstance(ids, torch.Tensor):
+        raise TypeError("ids must be a tensor")
+    n, rows = ids.numel(), int(rows)
+    if (n | rows | width) >> 31:
+        raise ValueError(_SIZES)
+    return _LookupCall(like.device.index, dtype, n, rows, width, scale, _vector(ids, n, like, (torch.int32,), "ids"))
+
+
+def lookup(table, ids, scale: float = 1.0, *, out=None, stream=None):
+    """Rows of ``table`` [rows, width] (float32 or bfloat16, any row stride) by
+    ``ids`` (int32, contiguous, any shape), times ``scale`` (nlb_lookup); zeros
+    for ids outside the table, as ``sample``'s nbr marks empty slots.  Returns
+    (or fills) out [*ids.shape, width].  No autograd graph is kept, as in
+    ``attention``."""
+    lib = load_library()
+    _float_dtype(table, "table")
+    if table.dim() != 2:
+        raise ValueError("table must be [rows, width]")
+    rows, width = table.shape
+    c = _lookup_call(table, ids, rows, width, scale, "table")
+    _no_graph("lookup", table)
+    if stream is not None:
+        with _on(stream, table.device):
+            return lookup(table, ids, scale, out=out)
+    if out is None:
+        out = table.new_empty((*ids.shape, width))
+    elif out.shape != (*ids.shape, width):
+        raise ValueError(f"out must be {[*ids.shape, width]}, not {list(out.shape)}")
+    flat = out if out.dim() == 2 else out.view(c.n, width)
+    _check(lib.nlb_lookup(c, *_table_rows(table, table, rows, width, "table"),
+                          *_table_rows(flat, table, c.n, width, "out"), _current_stream(table.device)), "nlb_lookup")
+    return out
+
+
+def _lookup_gradient(dout, ids, rows, scale):
+    """dout as [n, width] and the call."""
+    if dout.dim() < 1 or dout.shape[:-1] != ids.shape:
+        raise ValueError("dout must be [*ids.shape, width]")
+    width = dout.shape[-1]
+    c = _lookup_call(dout, ids, rows, width, scale, "dout")
+    return (dout if dout.dim() == 2 else dout.reshape(c.n, width)), c
+
+
+def lookup_work(dout, ids, rows: int, scale: float = 1.0, *, listed=False) -> int:
+    """Bytes of working memory that lookup_backward (or, with ``listed``,
+    lookup_backward_listed) of these takes (``work=``)."""
+    n = ctypes.c_size_t()
+    _check(load_library().nlb_lookup_work(_lookup_gradient(dout, ids, rows, scale)[1], int(bool(listed)), n),
+           "nlb_lookup_work")
+    return n.value
+
+
+def lookup_backward(dout, ids, rows: int, scale: float = 1.0, *, dtable=None, work=None, stream=None):
+    """The gradient of ``lookup``'s table of ``rows`` rows (nlb_lookup_backward)
+    from its ids and scale and the gradient ``dout`` of its result.  Returns (or
+    fills) dtable [rows, width].  ``work``: lookup_work bytes, allocated if
+    None."""
+    lib = load_library()
+    d, c = _lookup_gradient(dout, ids, rows, scale)
+    if stream is not None:
+        with _on(stream, dout.device):
+            return lookup_backward(dout, ids, rows, scale, dtable=dtable, work=work)
+    if dtable is None:
+        dtable = dout.new_empty((c.rows, c.width))
+    keep, p, size = _work(lib.nlb_lookup_work, c, (0,), work, dout, "nlb_lookup_backward")
+    _check(lib.nlb_lookup_backward(c, *_table_rows(d, dout, c.n, c.width, "dout"),
+                                   *_table_rows(dtable, dout, c.rows, c.width, "dtable"), None, None, p, size,
+                                   _current_stream(dout.device)), "nlb_lookup_backward")
+    return dtable
+
+
+def lookup_backward_listed(dout, ids, rows: int, scale: float = 1.0, *, grads=None, row_ids=None, count=None,
+                           work=None, stream=None):
+    """The same for the rows that occur, for tables too large for a whole
+    gradient.  Returns (or fills) grads [n, width] (n: the number of ids), of
+    which the first rows are the gradients and the others stay as they are,
+    row_ids int32 [n], the rows' ids in ascending order, -1 behind them, and
+    count int32 [1], their number (on the device: nothing is waited for)."""
+    import torch
+    lib = load_library()
+    d, c = _lookup_gradient(dout, ids, rows, scale)
+    if stream is not None:
+        with _on(stream, dout.device):
+            return lookup_backward_listed(dout, ids, rows, scale, grads=grads, row_ids=row_ids, count=count, work=work)
+    ints = (torch.int32,)
+    if grads is None:
+        grads = dout.new_empty((c.n, c.width))
+    row_ids = dout.new_empty(c.n, dtype=torch.int32) if row_ids is None else row_ids
+    count = dout.new_empty(1, dtype=torch.int32) if count is None else count
+    keep, p, size = _work(lib.nlb_lookup_work, c, (1,), work, dout, "nlb_lookup_backward")
+    _check(lib.nlb_lookup_backward(c, *_table_rows(d, dout, c.n, c.width, "dout"),
+                                   *_table_rows(grads, dout, c.n, c.width, "grads"),
+                                   _vector(row_ids, c.n, dout, ints, "row_ids"), _vector(count, 1, dout, ints, "count"),
+                                   p, size, _current_stream(dout.device)), "nlb_lookup_backward")
+    return grads, row_ids, count
 
 
 def _rotate_call(q, k, freq, q_pos, k_pos, wq, wk, eps):

@@ -1,0 +1,679 @@
+// lookup.hip -- rows of a table by id, and the table's gradient by sorted ids.
+//   out_i = scale table[id_i],  dtable_r = scale sum over id_i = r of dout_i
+// Forward: bound by reading rows at random places and writing them in order.
+// Backward: the places i are sorted by id (radix passes over pairs of id and
+// place, ids that are no rows left out by the first), so that each row's
+// gradients stand together and are summed in the order of their places, without
+// atomics; bound by reading dout's rows at random places.
+//   The sorted places are split into runs of equal length, a group of lanes each.
+// A group sums the rows that begin in its run, into the next run where a row ends
+// there; one that goes further (a popular id) is split: every run that it
+// touches leaves its part's sum, and a last launch joins them in order.
+#include <type_traits>
+
+#include "call_device.h"
+#include "nlb_internal.h"
+
+namespace {
+
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+constexpr int kThreads = 256, kItems = 16, kWaves = kThreads / 64;
+constexpr uint32_t kTile = kThreads * kItems;              // entries a workgroup sorts
+constexpr uint32_t kMaxBits = 9, kMaxDigits = 1u << kMaxBits;
+
+template <typename T> struct Chunk { static constexpr int n = 16 / sizeof(T); };
+
+// 16 bytes of values from c on of a row of `width`, zeros past its end.
+template <typename T> __device__ __forceinline__ u32x4 load_chunk(const uint8_t *row, uint32_t c, uint32_t width) {
+    constexpr uint32_t n = Chunk<T>::n;
+    const uint8_t *p = row + (size_t)c * sizeof(T);
+    u32x4 x = {0, 0, 0, 0};
+    if (c + n <= width) {
+        x = *(const u32x4_any *)p;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < n - 1; i++)
+            if (c + i < width) {
+                if constexpr (sizeof(T) == 4) x[i] = ((const uint32_t *)p)[i];
+                else x[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (16 * (i % 2));
+            }
+    }
+    return x;
+}
+template <typename T> __device__ __forceinline__ void store_chunk(uint8_t *row, uint32_t c, uint32_t width, u32x4 x) {
+    constexpr uint32_t n = Chunk<T>::n;
+    uint8_t *p = row + (size_t)c * sizeof(T);
+    if (c + n <= width) {
+        *(u32x4_any *)p = x;
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < n - 1; i++)
+            if (c + i < width) {
+                if constexpr (sizeof(T) == 4) ((uint32_t *)p)[i] = x[i];
+                else ((uint16_t *)p)[i] = (uint16_t)(x[i / 2] >> (16 * (i % 2)));
+            }
+    }
+}
+template <typename T> __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Chunk<T>::n]) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if constexpr (sizeof(T) == 4) {
+            f[i] = __uint_as_float(x[i]);
+        } else {
+            f[2 * i] = __uint_as_float(x[i] << 16);
+            f[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+        }
+    }
+}
+template <typename T> __device__ __forceinline__ u32x4 packed(const float (&f)[Chunk<T>::n], float scale) {
+    T v[Chunk<T>::n];
+#pragma unroll
+    for (int i = 0; i < Chunk<T>::n; i++) v[i] = (T)(f[i] * scale);
+    u32x4 u;
+    __builtin_memcpy(&u, v, 16);
+    return u;
+}
+
+// ---------------------------------------------------------------- rows
+struct Rows {
+    const uint8_t *table;
+    uint8_t *out;
+    int64_t table_row, out_row;                            // bytes
+    const int32_t *ids;
+    uint32_t n, rows, width, chunks, per;                  // chunks of a row, rows of a tile
+    uint64_t magic;                                        // division by chunks
+    float scale;
+};
+
+// A workgroup takes `per` rows at a time, a thread four of their chunks.  FILL:
+// zeros for all rows of `out`, without a table.
+template <typename T, bool FILL> __global__ __launch_bounds__(kThreads) void copy_rows(Rows a) {
+    const uint32_t tiles = (a.n + a.per - 1) / a.per;
+    for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t first = tile * a.per, all = min(a.per, a.n - first) * a.chunks;
+        for (uint32_t l0 = threadIdx.x; l0 < all; l0 += 4 * kThreads) {
+            uint32_t row[4], c[4];
+            int32_t id[4];
+            u32x4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t l = l0 + i * kThreads, r = nlb_div(l, a.magic);
+                row[i] = first + r;
+                c[i] = (l - r * a.chunks) * Chunk<T>::n;
+                id[i] = -1;
+                if (!FILL && l < all) id[i] = a.ids[row[i]];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                x[i] = u32x4{0, 0, 0, 0};
+                if (!FILL && (uint32_t)id[i] < a.rows)
+                    x[i] = load_chunk<T>(a.table + (int64_t)id[i] * a.table_row, c[i], a.width);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (l0 + i * kThreads >= all) continue;
+                if constexpr (!FILL) {
+                    float f[Chunk<T>::n];
+                    unpack<T>(x[i], f);
+                    if ((uint32_t)id[i] < a.rows) x[i] = packed<T>(f, a.scale);
+                }
+                store_chunk<T>(a.out + (int64_t)row[i] * a.out_row, c[i], a.width, x[i]);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- sorting
+struct Sort {
+    const int32_t *ids;
+    const uint64_t *from;                                  // id in the upper half, place in the lower
+    uint64_t *to;
+    uint32_t *hist, *totals, *valid;                       // [digits][tiles], [digits], one word
+    uint32_t n, rows, tiles, shift, bits;
+};
+
+template <bool FIRST> __device__ __forceinline__ uint64_t entry(const Sort &a, uint32_t i, uint32_t n) {
+    if constexpr (FIRST) {
+        const int32_t id = i < n ? a.ids[i] : -1;
+        return (uint32_t)id < a.rows ? (uint64_t)(uint32_t)id << 32 | i : ~0ull;
+    } else {
+        return i < n ? a.from[i] : ~0ull;
+    }
+}
+__device__ __forceinline__ uint32_t digit_of(const Sort &a, uint64_t e) {
+    return (uint32_t)(e >> (32 + a.shift)) & ((1u << a.bits) - 1);
+}
+
+// How many of a tile's entries have each digit.
+template <bool FIRST> __global__ __launch_bounds__(kThreads) void count_digits(Sort a) {
+    __shared__ uint32_t count[kMaxDigits];
+    const uint32_t digits = 1u << a.bits, n = FIRST ? a.n : *a.valid;
+    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
+    __syncthreads();
+    uint64_t e[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; i++) e[i] = entry<FIRST>(a, blockIdx.x * kTile + i * kThreads + threadIdx.x, n);
+#pragma unroll
+    for (int i = 0; i < kItems; i++)
+        if (e[i] != ~0ull) atomicAdd(&count[digit_of(a, e[i])], 1u);
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) a.hist[(size_t)d * a.tiles + blockIdx.x] = count[d];
+}
+
+// The sum of x over the workgroup's threads before this one; `all` that of all.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t &all, uint32_t *lds) {
+    const uint32_t lane = threadIdx.x % 64, waves = blockDim.x / 64;
+    uint32_t s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t y = __shfl_up(s, o);
+        if (lane >= (uint32_t)o) s += y;
+    }
+    __syncthreads();
+    if (lane == 63) lds[threadIdx.x / 64] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+    for (uint32_t w = 0; w < waves; w++) {
+        if (w == threadIdx.x / 64) before = all;
+        all += lds[w];
+    }
+    return before + s - x;
+}
+
+// A digit's counts become those of the tiles before each; their sum goes to totals.
+__global__ __launch_bounds__(kThreads) void scan_digits(Sort a) {
+    __shared__ uint32_t lds[kWaves];
+    uint32_t *h = a.hist + (size_t)blockIdx.x * a.tiles;
+    uint32_t before = 0;
+    for (uint32_t t0 = 0; t0 < a.tiles; t0 += 4 * kThreads) {
+        uint32_t x[4], sum = 0, all;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) {
+            const uint32_t t = t0 + 4 * threadIdx.x + i;
+            x[i] = t < a.tiles ? h[t] : 0;
+            sum += x[i];
+        }
+        uint32_t at = before + sum_before(sum, all, lds);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; i++) {
+            const uint32_t t = t0 + 4 * threadIdx.x + i;
+            if (t < a.tiles) h[t] = at;
+            at += x[i];
+        }
+        before += all;
+    }
+    if (threadIdx.x == 0) a.totals[blockIdx.x] = before;
+}
+
+// Each entry of a tile to its place: behind all of lower digits, the earlier
+// tiles' of its own and the earlier of its own in the tile.  The tile is put in
+// order in LDS first, so that neighbours go out together.
+template <bool FIRST> __global__ __launch_bounds__(kThreads) void scatter(Sort a) {
+    __shared__ uint64_t items[kTile];
+    __shared__ uint32_t waves[kWaves][kMaxDigits], start[kMaxDigits], base[kMaxDigits], lds[kWaves];
+    const uint32_t digits = 1u << a.bits, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint32_t n = FIRST ? a.n : *a.valid;
+    if (!FIRST && blockIdx.x * kTile >= n) return;
+    for (uint32_t d = threadIdx.x; d < kWaves * kMaxDigits; d += kThreads) waves[d / kMaxDigits][d % kMaxDigits] = 0;
+    uint64_t e[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; i++)
+        e[i] = entry<FIRST>(a, blockIdx.x * kTile + (wave * kItems + i) * 64 + lane, n);
+    __syncthreads();
+    uint32_t rank[kItems];                                 // in the wavefront's entries of the digit
+#pragma unroll
+    for (int i = 0; i < kItems; i++) {
+        const bool there = e[i] != ~0ull;
+        const uint32_t d = there ? digit_of(a, e[i]) : 0;
+        uint64_t same = __ballot(there);
+        for (uint32_t b = 0; b < a.bits; b++) {
+            const uint64_t one = __ballot(d >> b & 1);
+            same &= d >> b & 1 ? one : ~one;
+        }
+        const uint32_t before = __popcll(same & ((1ull << lane) - 1));
+        volatile uint32_t *count = &waves[wave][d];
+        const uint32_t c = there ? *count : 0;
+        rank[i] = c + before;
+        if (there && before == 0) *count = c + __popcll(same);
+    }
+    __syncthreads();
+    // two digits a thread: their counts' sums over wavefronts, digits and tiles
+    uint32_t sum[2], all, total[2], total_all;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const uint32_t d = 2 * threadIdx.x + i;
+        sum[i] = total[i] = 0;
+        if (d >= digits) continue;
+        for (int w = 0; w < kWaves; w++) {
+            const uint32_t c = waves[w][d];
+            waves[w][d] = sum[i];
+            sum[i] += c;
+        }
+        total[i] = a.totals[d];
+    }
+    uint32_t at = sum_before(sum[0] + sum[1], all, lds), to = sum_before(total[0] + total[1], total_all, lds);
+    if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *a.valid = total_all;
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const uint32_t d = 2 * threadIdx.x + i;
+        if (d >= digits) continue;
+        start[d] = at;
+        base[d] = to + a.hist[(size_t)d * a.tiles + blockIdx.x] - at;
+        at += sum[i];
+        to += total[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kItems; i++) {
+        if (e[i] == ~0ull) continue;
+        const uint32_t d = digit_of(a, e[i]);
+        items[start[d] + waves[wave][d] + rank[i]] = e[i];
+    }
+    __syncthreads();
+    for (uint32_t p = threadIdx.x; p < all; p += kThreads) {
+        const uint64_t x = items[p];
+        a.to[base[digit_of(a, x)] + p] = x;
+    }
+}
+
+// ---------------------------------------------------------------- sums
+struct Sums {
+    const uint8_t *dout;
+    uint8_t *out;
+    int64_t dout_row, out_row;                             // bytes
+    const uint64_t *sorted;
+    const uint32_t *valid;
+    float *part;                                           // [runs][2][width]
+    int32_t *list;                                         // NULL: rows go to their ids
+    uint32_t *heads;                                       // [runs + 1]: rows that begin in the runs before
+    uint32_t *count;
+    uint32_t n, width, lanes, run, runs;
+    float scale;
+};
+
+__device__ __forceinline__ uint32_t id_at(const Sums &a, uint32_t i) { return (uint32_t)(a.sorted[i] >> 32); }
+
+// How many rows begin in each run: 16 lanes a run.
+__global__ __launch_bounds__(kThreads) void count_heads(Sums a) {
+    const uint32_t n = *a.valid, r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16, lane = threadIdx.x % 16;
+    uint32_t k = 0;
+    for (uint32_t i = lane; i < a.run && r < a.runs; i += 16) {
+        const uint32_t j = r * a.run + i;
+        if (j < n && (j == 0 || id_at(a, j) != id_at(a, j - 1))) k++;
+    }
+    for (int o = 8; o; o /= 2) k += __shfl_xor(k, o);
+    if (r < a.runs && lane == 0) a.heads[r] = k;
+}
+
+// They become those of the runs before each, and behind the last all of them.
+__global__ __launch_bounds__(1024) void scan_heads(Sums a) {
+    __shared__ uint32_t lds[16];
+    uint32_t before = 0;
+    for (uint32_t r0 = 0; r0 < a.runs; r0 += 8 * 1024) {
+        uint32_t x[8], sum = 0, all;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) {
+            const uint32_t r = r0 + 8 * threadIdx.x + i;
+            x[i] = r < a.runs ? a.heads[r] : 0;
+            sum += x[i];
+        }
+        uint32_t at = before + sum_before(sum, all, lds);
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) {
+            const uint32_t r = r0 + 8 * threadIdx.x + i;
+            if (r < a.runs) a.heads[r] = at;
+            at += x[i];
+        }
+        before += all;
+    }
+    if (threadIdx.x == 0) {
+        a.heads[a.runs] = before;
+        *a.count = before;
+    }
+}
+
+// Whether the row at place i goes on behind the run after i's run `r`, so that
+// it is summed in parts: `first` is where that run ends.
+__device__ __forceinline__ bool goes_on(const Sums &a, uint32_t id, uint32_t at, uint32_t n) {
+    return at < n && id_at(a, at) == id;
+}
+
+template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums a) {
+    constexpr int N = Chunk<T>::n, U = 8;
+    const uint32_t n = *a.valid, lane = threadIdx.x % a.lanes;
+    const uint32_t r = blockIdx.x * (kThreads / a.lanes) + threadIdx.x / a.lanes;
+    const uint32_t c = (blockIdx.y * a.lanes + lane) * N;
+    if (r >= a.runs) return;
+    const uint32_t begin = r * a.run, end = min(begin + a.run, n);
+    uint32_t slot = 0;
+    if (a.list) {
+        slot = a.heads[r];
+        if (blockIdx.y == 0)                               // behind the last row's id
+            for (uint32_t i = begin + lane; i < begin + a.run && i < a.n; i += a.lanes)
+                if (i >= a.heads[a.runs]) a.list[i] = -1;
+    }
+    if (begin >= n) return;
+    uint32_t id = id_at(a, begin), i = begin, stop = end;
+    bool head = begin > 0 && id_at(a, begin - 1) == id, tail = false;
+    if (head) {
+        const bool parts = goes_on(a, id, end, n) && end == begin + a.run;
+        if (!parts && !(begin > a.run && id_at(a, begin - a.run - 1) == id)) {
+            // the run before has summed it to its end
+            for (uint32_t step = end - i; step;) {         // the first place behind it
+                const uint32_t half = step / 2;
+                if (id_at(a, i + half) == id) i += half + 1, step -= half + 1;
+                else step = half;
+            }
+            head = false;
+        }
+    }
+    if (i >= end) return;
+    const uint32_t last = id_at(a, end - 1);
+    if (goes_on(a, last, end, n) && !(head && last == id)) {
+        const uint32_t far = min(end + a.run, n);
+        tail = far == end + a.run && goes_on(a, last, far, n);
+        if (!tail) {
+            stop = end;
+            for (uint32_t step = far - end; step;) {
+                const uint32_t half = step / 2;
+                if (id_at(a, stop + half) == last) stop += half + 1, step -= half + 1;
+                else step = half;
+            }
+        }
+    }
+    float sum[N];
+#pragma unroll
+    for (int k = 0; k < N; k++) sum[k] = 0.0f;
+    id = id_at(a, i);
+    const auto leave_part = [&](int which) {
+        float *p = a.part + ((size_t)r * 2 + which) * a.width;
+#pragma unroll
+        for (int k = 0; k < N; k++)
+            if (c + k < a.width) p[c + k] = sum[k];
+    };
+    const auto leave = [&](uint32_t id) {
+        if (c < a.width)
+            store_chunk<T>(a.out + (int64_t)(a.list ? slot : id) * a.out_row, c, a.width, packed<T>(sum, a.scale));
+        if (a.list) {
+            if (c == 0) a.list[slot] = (int32_t)id;
+            slot++;
+        }
+    };
+    for (; i < stop; i += U) {
+        uint64_t e[U];
+        u32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) e[u] = a.sorted[min(i + u, stop - 1)];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            x[u] = u32x4{0, 0, 0, 0};
+            if (i + u < stop && c < a.width) x[u] = load_chunk<T>(a.dout + (int64_t)(uint32_t)e[u] * a.dout_row, c, a.width);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const uint32_t now = (uint32_t)(e[u] >> 32);
+            if (now != id) {
+                if (head) leave_part(0);
+                else leave(id);
+                head = false;
+                id = now;
+#pragma unroll
+                for (int k = 0; k < N; k++) sum[k] = 0.0f;
+            }
+            float f[N];
+            unpack<T>(x[u], f);
+            if (i + u < stop)
+#pragma unroll
+                for (int k = 0; k < N; k++) sum[k] += f[k];
+        }
+    }
+    if (head) leave_part(0);
+    else if (tail) leave_part(1);
+    else leave(id);
+}
+
+// Rows that were summed in parts: a workgroup looks at 256 runs and joins the
+// rows that begin in them, one after the other, its groups of lanes a stretch of
+// the parts each.
+template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(Sums a) {
+    constexpr int N = Chunk<T>::n, U = 4;
+    __shared__ uint32_t found[kThreads], number, reach;
+    __shared__ float sums[kThreads][N + 1];
+    const uint32_t n = *a.valid, r = blockIdx.x * kThreads + threadIdx.x;
+    if (threadIdx.x == 0) number = 0;
+    __syncthreads();
+    if (r < a.runs && (uint64_t)(r + 2) * a.run < n) {
+        const uint32_t begin = r * a.run, end = begin + a.run, id = id_at(a, end - 1);
+        const bool from_before = id_at(a, begin) == id && begin > 0 && id_at(a, begin - 1) == id;
+        if (!from_before && id_at(a, end) == id && id_at(a, end + a.run) == id) found[atomicAdd(&number, 1u)] = r;
+    }
+    __syncthreads();
+    const uint32_t lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kThreads / a.lanes;
+    const uint32_t c = (blockIdx.y * a.lanes + lane) * N;
+    for (uint32_t k = 0; k < number; k++) {
+        const uint32_t first = found[k], id = id_at(a, first * a.run + a.run - 1);
+        // the last run that holds it: runs that begin with it, 256 tried at once
+        uint32_t last = first + 1, step = (a.runs - first + kThreads - 1) / kThreads;
+        for (;; step = (step + kThreads - 1) / kThreads) {
+            if (threadIdx.x == 0) reach = 0;
+            __syncthreads();
+            const uint64_t q = (uint64_t)last + (uint64_t)step * threadIdx.x;
+            if (q < a.runs && q * a.run < n && id_at(a, (uint32_t)q * a.run) == id) atomicMax(&reach, threadIdx.x);
+            __syncthreads();
+            last += step * reach;
+            __syncthreads();
+            if (step == 1) break;
+        }
+        // parts: the first run's second, then the others' first
+        const uint32_t parts = last - first + 1, per = (parts + groups - 1) / groups;
+        const uint32_t p0 = group * per, p1 = min(p0 + per, parts);
+        float sum[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) sum[i] = 0.0f;
+        for (uint32_t p = p0; p < p1; p += U) {
+            float x[U][N];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const float *f = a.part + ((size_t)(first + p + u) * 2 + (p + u == 0)) * a.width;
+#pragma unroll
+                for (int i = 0; i < N; i++) x[u][i] = p + u < p1 && c + i < a.width ? f[c + i] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int i = 0; i < N; i++) sum[i] += x[u][i];
+        }
+#pragma unroll
+        for (int i = 0; i < N; i++) sums[threadIdx.x][i] = sum[i];
+        __syncthreads();
+        if (group == 0 && c < a.width) {
+            for (uint32_t g = 1; g < groups; g++)
+#pragma unroll
+                for (int i = 0; i < N; i++) sum[i] += sums[g * a.lanes + lane][i];
+            const uint32_t row = a.list ? a.heads[first + 1] - 1 : id;
+            store_chunk<T>(a.out + (int64_t)row * a.out_row, c, a.width, packed<T>(sum, a.scale));
+            if (a.list && c == 0) a.list[row] = (int32_t)id;
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- host
+uint32_t chunks_of(uint32_t width, int32_t dtype) {
+    const uint32_t n = dtype == NLB_DTYPE_BF16 ? 8 : 4;
+    return (width + n - 1) / n;
+}
+
+// Passes and the bits of each for ids below `rows`.
+void passes_of(uint32_t rows, uint32_t &passes, uint32_t &bits) {
+    uint32_t all = 1;
+    while (all < 31 && (1ull << all) < rows) all++;
+    passes = (all + kMaxBits - 1) / kMaxBits;
+    bits = (all + passes - 1) / passes;
+}
+
+uint32_t run_of(uint32_t n) {
+    uint32_t run = 16;
+    while (run < 256 && run < n / 16384) run *= 2;
+    return run;
+}
+
+size_t align16z(size_t n) { return (n + 15) & ~(size_t)15; }
+
+struct Work {                                              // places in the working memory
+    size_t pairs[2], hist, totals, valid, heads, part, all;
+    uint32_t tiles, passes, bits, run, runs;
+    Work(const nlb_lookup_call *c, bool listed) {
+        passes_of(c->rows, passes, bits);
+        tiles = (uint32_t)(((uint64_t)c->n + kTile - 1) / kTile);
+        run = run_of(c->n);
+        runs = (uint32_t)(((uint64_t)c->n + run - 1) / run);
+        size_t at = 0;
+        const auto take = [&](size_t n) {
+            const size_t p = at;
+            at += align16z(n);
+            return p;
+        };
+        for (size_t &p : pairs) p = take((size_t)c->n * 8);
+        hist = take(((size_t)tiles << bits) * 4);
+        totals = take(4ull << bits);
+        valid = take(4);
+        heads = take(listed ? ((size_t)runs + 1) * 4 : 0);
+        part = take((size_t)runs * 2 * c->width * 4);
+        all = at;
+    }
+};
+
+int check(const nlb_lookup_call *c) {
+    if (!c || (c->dtype != NLB_DTYPE_F32 && c->dtype != NLB_DTYPE_BF16)) return NLB_EINVAL;
+    if (c->width < 1 || c->width > NLB_LOOKUP_MAX_WIDTH || c->n > INT32_MAX || c->rows < 1 || c->rows > INT32_MAX)
+        return NLB_EINVAL;
+    if ((c->n && !c->ids) || (uintptr_t)c->ids % 4 || !std::isfinite(c->scale)) return NLB_EINVAL;
+    return NLB_OK;
+}
+
+bool bad_rows(const void *p, int64_t stride, bool some, int32_t dtype) {
+    return (some && !p) || (uintptr_t)p % (dtype == NLB_DTYPE_BF16 ? 2 : 4) || stride < 0 || stride > INT32_MAX;
+}
+
+Rows rows_of(const nlb_lookup_call *c, void *out, int64_t out_stride, uint32_t n) {
+    Rows a = {};
+    a.out = (uint8_t *)out;
+    a.out_row = out_stride * (c->dtype == NLB_DTYPE_BF16 ? 2 : 4);
+    a.ids = c->ids;
+    a.n = n;
+    a.rows = c->rows;
+    a.width = (uint32_t)c->width;
+    a.chunks = chunks_of(a.width, c->dtype);
+    a.per = a.chunks < 4 * kThreads ? 4 * kThreads / a.chunks : 1;
+    a.magic = nlb_div_magic(a.chunks);
+    a.scale = c->scale;
+    return a;
+}
+
+template <bool FILL> int copy(const Rows &a, int32_t dtype, hipStream_t s) {
+    const uint32_t tiles = (uint32_t)(((uint64_t)a.n + a.per - 1) / a.per), blocks = tiles < 1u << 20 ? tiles : 1u << 20;
+    if (!blocks) return NLB_OK;
+    return enqueue(dtype == NLB_DTYPE_BF16 ? copy_rows<__bf16, FILL> : copy_rows<float, FILL>, blocks, kThreads, 0, s, a);
+}
+
+// Sorts; *sorted is where the pairs end up.
+int sort(const nlb_lookup_call *c, const Work &w, uint8_t *work, const uint64_t **sorted, hipStream_t s) {
+    Sort a = {};
+    a.ids = c->ids;
+    a.hist = (uint32_t *)(work + w.hist);
+    a.totals = (uint32_t *)(work + w.totals);
+    a.valid = (uint32_t *)(work + w.valid);
+    a.n = c->n;
+    a.rows = c->rows;
+    a.tiles = w.tiles;
+    a.bits = w.bits;
+    for (uint32_t p = 0; p < w.passes; p++) {
+        a.shift = p * w.bits;
+        a.from = (const uint64_t *)(work + w.pairs[(p + 1) % 2]);
+        a.to = (uint64_t *)(work + w.pairs[p % 2]);
+        int rc = enqueue(p ? count_digits<false> : count_digits<true>, w.tiles, kThreads, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(scan_digits, 1u << w.bits, kThreads, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(p ? scatter<false> : scatter<true>, w.tiles, kThreads, 0, s, a);
+        if (rc != NLB_OK) return rc;
+        *sorted = a.to;
+    }
+    return NLB_OK;
+}
+
+}  // namespace
+
+extern "C" int nlb_lookup(const nlb_lookup_call *c, const void *table, int64_t table_stride, void *out,
+                          int64_t out_stride, void *stream) {
+    const int rc = check(c);
+    if (rc != NLB_OK) return rc;
+    if (bad_rows(table, table_stride, c->n, c->dtype) || bad_rows(out, out_stride, c->n, c->dtype)) return NLB_EINVAL;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
+    Rows a = rows_of(c, out, out_stride, c->n);
+    a.table = (const uint8_t *)table;
+    a.table_row = table_stride * (c->dtype == NLB_DTYPE_BF16 ? 2 : 4);
+    return copy<false>(a, c->dtype, (hipStream_t)stream);
+}
+
+extern "C" int nlb_lookup_work(const nlb_lookup_call *c, int32_t listed, size_t *bytes) {
+    if (!bytes) return NLB_EINVAL;
+    const int rc = check(c);
+    if (rc != NLB_OK) return rc;
+    *bytes = Work(c, listed != 0).all;
+    return NLB_OK;
+}
+
+extern "C" int nlb_lookup_backward(const nlb_lookup_call *c, const void *dout, int64_t dout_stride, void *dtable,
+                                   int64_t dtable_stride, int32_t *list, uint32_t *count, void *work, size_t work_bytes,
+                                   void *stream) {
+    int rc = check(c);
+    if (rc != NLB_OK) return rc;
+    const bool listed = list || count;
+    if (bad_rows(dout, dout_stride, c->n, c->dtype) || bad_rows(dtable, dtable_stride, !listed || c->n, c->dtype))
+        return NLB_EINVAL;
+    if (listed && ((c->n && !list) || !count)) return NLB_EINVAL;
+    if (((uintptr_t)list | (uintptr_t)count) % 4 || (uintptr_t)work % 16) return NLB_EINVAL;
+    const Work w(c, listed);
+    if (w.all && (!work || work_bytes < w.all)) return NLB_ESCRATCH;
+    CallDevice device(c->device);
+    if (device.rc != NLB_OK) return device.rc;
+    const hipStream_t s = (hipStream_t)stream;
+    if (!listed) {
+        rc = copy<true>(rows_of(c, dtable, dtable_stride, c->rows), c->dtype, s);
+        if (rc != NLB_OK || !c->n) return rc;
+    }
+    Sums a = {};
+    a.dout = (const uint8_t *)dout;
+    a.out = (uint8_t *)dtable;
+    a.dout_row = dout_stride * (c->dtype == NLB_DTYPE_BF16 ? 2 : 4);
+    a.out_row = dtable_stride * (c->dtype == NLB_DTYPE_BF16 ? 2 : 4);
+    uint8_t *m = (uint8_t *)work;
+    a.valid = (const uint32_t *)(m + w.valid);
+    a.part = (float *)(m + w.part);
+    a.list = list;
+    a.heads = (uint32_t *)(m + w.heads);
+    a.count = count;
+    a.n = c->n;
+    a.width = (uint32_t)c->width;
+    a.lanes = 4;
+    const uint32_t chunks = chunks_of(a.width, c->dtype);
+    while (a.lanes < 64 && a.lanes < chunks) a.lanes *= 2;
+    a.run = w.run;
+    a.runs = w.runs;
+    a.scale = c->scale;
+    if (c->n) rc = sort(c, w, m, &a.sorted, s);
+    if (rc == NLB_OK && listed) {
+        if (c->n) rc = enqueue(count_heads, (w.runs + 15) / 16, kThreads, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(scan_heads, 1, 1024, 0, s, a);
+    }
+    if (rc != NLB_OK || !c->n) return rc;
+    const bool bf16 = c->dtype == NLB_DTYPE_BF16;
+    const uint32_t groups = kThreads / a.lanes, columns = (chunks + a.lanes - 1) / a.lanes;
+    rc = enqueue(bf16 ? sum_runs<__bf16> : sum_runs<float>, dim3((w.runs + groups - 1) / groups, columns), kThreads, 0, s, a);
+    if (rc != NLB_OK) return rc;
+    return enqueue(bf16 ? join_parts<__bf16> : join_parts<float>, dim3((w.runs + kThreads - 1) / kThreads, columns),
+                   kThreads, 0, s, a);
+}
