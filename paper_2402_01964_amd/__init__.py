@@ -795,8 +795,8 @@ def lookup(table, ids, scale: float = 1.0, *, out=None, stream=None):
     elif out.shape != (*ids.shape, width):
         raise ValueError(f"out must be {[*ids.shape, width]}, not {list(out.shape)}")
     flat = out if out.dim() == 2 else out.view(c.n, width)
-    _check(lib.nlb_lookup(c, *_table_rows(table, table, rows, width, "table"),
-                          *_table_rows(flat, table, c.n, width, "out"), _current_stream(table.device)), "nlb_lookup")
+    args = *_table_rows(table, table, rows, width, "table"), *_table_rows(flat, table, c.n, width, "out")
+    _check(lib.nlb_lookup(c, *args, _current_stream(table.device)), "nlb_lookup")
     return out
 
 
@@ -812,9 +812,9 @@ def _lookup_gradient(dout, ids, rows, scale):
 def lookup_work(dout, ids, rows: int, scale: float = 1.0, *, listed=False) -> int:
     """Bytes of working memory that lookup_backward (or, with ``listed``,
     lookup_backward_listed) of these takes (``work=``)."""
+    c = _lookup_gradient(dout, ids, rows, scale)[1]
     n = ctypes.c_size_t()
-    _check(load_library().nlb_lookup_work(_lookup_gradient(dout, ids, rows, scale)[1], int(bool(listed)), n),
-           "nlb_lookup_work")
+    _check(load_library().nlb_lookup_work(c, int(bool(listed)), n), "nlb_lookup_work")
     return n.value
 
 
@@ -989,8 +989,9 @@ def _states(t, batch, x, name):
 def gated_scan_work(x, g, *, batch=None, start=None, h0=None) -> int:
     """Bytes of working memory that such a call takes (``work=``), forward or
     backward."""
+    c = _scan_call(x, g, batch, start, h0)
     n = ctypes.c_size_t()
-    _check(load_library().nlb_gated_scan_work(_scan_call(x, g, batch, start, h0), n), "nlb_gated_scan_work")
+    _check(load_library().nlb_gated_scan_work(c, n), "nlb_gated_scan_work")
     return n.value
 
 

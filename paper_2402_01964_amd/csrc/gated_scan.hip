@@ -583,8 +583,7 @@ bool overlap(const Scan &a, const float *p, const float *q) {
     return p && q && p < q + n && q < p + n;
 }
 
-template <typename T, bool BACKWARD> int launch(Scan &a, void *work, size_t work_bytes, hipStream_t s) {
-    if (work_bytes < work_of(a) || (work_of(a) && !work)) return NLB_ESCRATCH;
+template <typename T, bool BACKWARD> int launch(Scan &a, void *work, hipStream_t s) {
     const uint32_t groups = groups_of(a, Lane<T>::n);
     // (a call of no rows still has states to pass on)
     const dim3 grid(a.chunks ? a.chunks : 1, groups);
@@ -621,14 +620,15 @@ extern "C" int nlb_gated_scan(const nlb_scan_call *c, const nlb_scan_rows *h, fl
         return NLB_EINVAL;
     // a sequence's last state may be written before another workgroup reads its first
     if (overlap(a, a.h0, last) && !(a.h0 == last && !a.start && a.len == 1)) return NLB_EINVAL;
+    if (work_of(a) && (!work || work_bytes < work_of(a))) return NLB_ESCRATCH;
     a.h = (uint8_t *)h->data;
     a.h_row = h->row_stride * e;
     a.last = last;
     a.states = states;
     CallDevice device(c->device);
     if (device.rc != NLB_OK) return device.rc;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, false>(a, work, work_bytes, (hipStream_t)stream)
-                                      : launch<float, false>(a, work, work_bytes, (hipStream_t)stream);
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, false>(a, work, (hipStream_t)stream)
+                                      : launch<float, false>(a, work, (hipStream_t)stream);
 }
 
 extern "C" int nlb_gated_scan_backward(const nlb_scan_call *c, const float *states, const nlb_scan_rows *dh,
@@ -643,6 +643,7 @@ extern "C" int nlb_gated_scan_backward(const nlb_scan_call *c, const float *stat
     if ((c->rows && !states) || ((uintptr_t)states | (uintptr_t)dlast | (uintptr_t)dh0) % 4 || (uintptr_t)work % 16)
         return NLB_EINVAL;
     if (overlap(a, dlast, dh0) || overlap(a, a.h0, dh0)) return NLB_EINVAL;
+    if (work_of(a) && (!work || work_bytes < work_of(a))) return NLB_ESCRATCH;
     a.states = (float *)states;
     a.dh = (const uint8_t *)dh->data;
     a.dx = (uint8_t *)dx->data;
@@ -654,6 +655,6 @@ extern "C" int nlb_gated_scan_backward(const nlb_scan_call *c, const float *stat
     a.dh0 = dh0;
     CallDevice device(c->device);
     if (device.rc != NLB_OK) return device.rc;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, true>(a, work, work_bytes, (hipStream_t)stream)
-                                      : launch<float, true>(a, work, work_bytes, (hipStream_t)stream);
+    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, true>(a, work, (hipStream_t)stream)
+                                      : launch<float, true>(a, work, (hipStream_t)stream);
 }
