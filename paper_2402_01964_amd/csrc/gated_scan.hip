@@ -13,6 +13,7 @@
 // A workgroup walks a chunk of the rows tile by tile.  Where there are several
 // chunks, a first launch makes their maps (it reads x and g once more, but only
 // from the last first row in the chunk on), a second joins them.
+#include <algorithm>
 #include <type_traits>
 
 #include "call_device.h"
@@ -37,51 +38,63 @@ struct Scan {
     uint32_t lanes, chunk_rows, chunks;
 };
 
-// Values c and c + 1 of a row (fp32: c), 0 past its end.
-template <typename T> struct Lane;
-template <> struct Lane<float> {
+// A lane's channels of a row: one fp32 value, or two bf16 ones in a word.  The
+// last bf16 value of an odd width comes in the upper half of the word that ends
+// with it, and goes out by itself; a width of one has a type of its own.
+struct OneBf16 {};
+template <typename T> struct Piece;
+template <> struct Piece<float> {
     static constexpr int n = 1;
-    static __device__ __forceinline__ uint32_t load(const uint8_t *row, uint32_t c, uint32_t) {
-        return ((const uint32_t *)row)[c];
-    }
-    static __device__ __forceinline__ void unpack(uint32_t w, float (&f)[1]) { f[0] = __uint_as_float(w); }
-    static __device__ __forceinline__ void store(uint8_t *row, uint32_t c, uint32_t, const float (&f)[1]) {
-        ((float *)row)[c] = f[0];
-    }
+    uint32_t off;
+    bool there;
+    __device__ __forceinline__ Piece(uint32_t c, uint32_t width) : off(c < width ? 4 * c : 0), there(c < width) {}
+    __device__ __forceinline__ uint32_t load(const uint8_t *row) const { return *(const uint32_t *)(row + off); }
+    __device__ __forceinline__ void unpack(uint32_t w, float (&f)[1]) const { f[0] = __uint_as_float(w); }
+    __device__ __forceinline__ void store(uint8_t *row, const float (&f)[1]) const { *(float *)(row + off) = f[0]; }
 };
-template <> struct Lane<__bf16> {
+template <> struct Piece<__bf16> {
     static constexpr int n = 2;
-    static __device__ __forceinline__ uint32_t load(const uint8_t *row, uint32_t c, uint32_t width) {
-        const uint8_t *p = row + 2 * c;
-        return c + 1 < width ? *(const u32_any *)p : *(const uint16_t *)p;
+    uint32_t off, shift;
+    bool there;
+    __device__ __forceinline__ Piece(uint32_t c, uint32_t width) : there(c < width) {
+        shift = c + 1 == width ? 16 : 0;
+        off = there ? 2 * c - (shift ? 2 : 0) : 0;
     }
-    static __device__ __forceinline__ void unpack(uint32_t w, float (&f)[2]) {
+    __device__ __forceinline__ uint32_t load(const uint8_t *row) const { return *(const u32_any *)(row + off); }
+    __device__ __forceinline__ void unpack(uint32_t w, float (&f)[2]) const {
+        w >>= shift;
         f[0] = __uint_as_float(w << 16);
         f[1] = __uint_as_float(w & 0xFFFF0000u);
     }
-    static __device__ __forceinline__ void store(uint8_t *row, uint32_t c, uint32_t width, const float (&f)[2]) {
+    __device__ __forceinline__ void store(uint8_t *row, const float (&f)[2]) const {
         __bf16 v[2] = {(__bf16)f[0], (__bf16)f[1]};
         uint32_t w;
         __builtin_memcpy(&w, v, 4);
-        uint8_t *p = row + 2 * c;
-        if (c + 1 < width) *(u32_any *)p = w;
-        else *(uint16_t *)p = (uint16_t)w;
+        if (!shift) *(u32_any *)(row + off) = w;
+        else *(uint16_t *)(row + off + 2) = (uint16_t)w;
     }
 };
+template <> struct Piece<OneBf16> {
+    static constexpr int n = 1;
+    bool there;
+    __device__ __forceinline__ Piece(uint32_t c, uint32_t width) : there(c < width) {}
+    __device__ __forceinline__ uint32_t load(const uint8_t *row) const { return *(const uint16_t *)row; }
+    __device__ __forceinline__ void unpack(uint32_t w, float (&f)[1]) const { f[0] = __uint_as_float(w << 16); }
+    __device__ __forceinline__ void store(uint8_t *row, const float (&f)[1]) const { *(__bf16 *)row = (__bf16)f[0]; }
+};
 
-// z = sigmoid(g) and 1 - z, each with its own relative error of some 2^-22:
-// from e = exp(-|g|), the larger of them 1 / (1 + e) and the smaller e times
-// that.  e is 2^(t + lo) with t + lo = -|g| / ln 2 in two words.  Gates beyond
-// 80 in magnitude (e below 2^-115) count as 80.
+// z = sigmoid(g) = 1 / (1 + e) and 1 - z = e z with e = exp(-g), each with its
+// own relative error of some 2^-21.  e = 2^t (1 + lo) where t = -g / ln 2 is
+// rounded and lo = -g - t ln 2 what that left.  Gates beyond 80 in magnitude
+// count as 80 (e up to 2^115).
 __device__ __forceinline__ void gate(float g, float &z, float &y) {
-    const float m = fabsf(g) > 80.0f ? 80.0f : fabsf(g);      // (a NaN stays one)
-    const float t = m * -1.44269504f;
-    const float lo = fmaf(m, -1.92596299e-8f, fmaf(m, -1.44269504f, -t));
+    g = fabsf(g) > 80.0f ? copysignf(80.0f, g) : g;           // (a NaN stays one)
+    const float t = g * -1.44269504f;
+    const float lo = fmaf(t, -0.693147181f, -g);
     float e = __builtin_amdgcn_exp2f(t);
-    e = fmaf(e, lo * 0.693147181f, e);
-    const float big = __builtin_amdgcn_rcpf(1.0f + e), small = e * big;
-    z = g < 0.0f ? small : big;
-    y = g < 0.0f ? big : small;
+    e = fmaf(e, lo, e);
+    z = __builtin_amdgcn_rcpf(1.0f + e);
+    y = e * z;
 }
 
 // The map h -> a h + b of a stretch of rows.  A stretch that holds a first row
@@ -101,69 +114,77 @@ constexpr float kForgets = -0.0f;
 struct Edges {                                             // of a tile's sequences, in LDS
     uint32_t begins[kThreads / 8], ends[kThreads / 8];     // a bit for each row, a word for a thread's rows
     int32_t begin[kThreads / 8 * kRows], end[kThreads / 8 * kRows];   // their sequences
+    uint32_t next;
 };
 
-// Rows that sequences have: first to last.
-__device__ __forceinline__ uint32_t clamped(const int32_t *start, uint32_t b, uint32_t rows) {
-    const int32_t s = start[b];
-    return s < 0 ? 0u : (uint32_t)s < rows ? (uint32_t)s : rows;
+// The first row of sequence b, the rows' end for b = batch.
+__device__ __forceinline__ uint32_t start_of(const Scan &a, uint32_t b) {
+    if (!a.start) return b * a.len;
+    const int32_t s = a.start[b];
+    return s < 0 ? 0u : (uint32_t)s < a.rows ? (uint32_t)s : a.rows;
 }
 
 // The last sequence that begins at row r or before it (0 if none does): a
 // wavefront tries 64 of them at once.
-__device__ __forceinline__ uint32_t find_sequence(const int32_t *start, uint32_t batch, uint32_t r) {
-    uint32_t lo = 0, n = batch;
+__device__ __forceinline__ uint32_t find_sequence(const Scan &a, uint32_t r) {
+    if (!a.start) return r / a.len;
+    uint32_t lo = 0, n = a.batch;
     const uint32_t lane = threadIdx.x % 64;
     for (;;) {
         const uint32_t step = (n + 63) / 64, i = lane * step;
-        const bool before = i < n && start[lo + i] <= (int32_t)r;
+        const bool before = i < n && a.start[lo + i] <= (int32_t)r;
         const uint32_t k = __popcll(__ballot(before));
         if (k > 1) lo += (k - 1) * step, n -= (k - 1) * step;
-        if (step == 1) return lo;
+        if (step == 1) return __builtin_amdgcn_readfirstlane(lo);
         n = n < step ? n : step;
     }
 }
 
-// Fills `edges` for the rows r0 .. r0 + n - 1; two barriers, so that what was
-// read before it may be written, and what it writes may be read.
-template <int R> __device__ __forceinline__ void find_edges(const Scan &a, uint32_t r0, uint32_t n, Edges &edges) {
-    if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
-    __syncthreads();
-    if (!a.start) {
-        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
-            const uint32_t b = (r0 + i) / a.len, at = r0 + i - b * a.len;
-            if (r0 + i >= a.rows) break;
-            if (at == 0) {
-                atomicOr(&edges.begins[i / R], 1u << (i % R));
-                edges.begin[i] = b;
-            }
-            if (at == a.len - 1) {
-                atomicOr(&edges.ends[i / R], 1u << (i % R));
-                edges.end[i] = b;
-            }
-        }
-        __syncthreads();
-        return;
+// Walks the sequences along with the tiles (BACK: from the last one on).  b is
+// the last sequence that begins at the tile's first row (BACK: its last row) or
+// before it, s and e its rows; where they go beyond the tile to both sides, no
+// edge is in it, and the tile needs no barrier for them.
+template <int R, bool BACK> struct Cursor {
+    uint32_t b, s, e;
+    __device__ __forceinline__ void at(const Scan &a, uint32_t to) {
+        b = to;
+        s = __builtin_amdgcn_readfirstlane(start_of(a, b));
+        e = __builtin_amdgcn_readfirstlane(start_of(a, b + 1));
     }
-    uint32_t b = find_sequence(a.start, a.batch, r0) + threadIdx.x;
-    for (;; b += kThreads) {
-        bool more = false;
-        if (b < a.batch) {
-            const uint32_t s = clamped(a.start, b, a.rows), e = clamped(a.start, b + 1, a.rows);
-            more = s < r0 + n;                                // rows end before 2^31
-            if (s < e && s - r0 < n) {
-                atomicOr(&edges.begins[(s - r0) / R], 1u << ((s - r0) % R));
-                edges.begin[s - r0] = b;
-            }
-            if (s < e && e - 1 - r0 < n) {
-                atomicOr(&edges.ends[(e - 1 - r0) / R], 1u << ((e - 1 - r0) % R));
-                edges.end[e - 1 - r0] = b;
-            }
-        }
-        if (threadIdx.x != kThreads - 1) more = false;
-        if (!__syncthreads_or(more)) return;
+    __device__ __forceinline__ bool plain(uint32_t r0, uint32_t n) const { return s < r0 && e > r0 + n; }
+    // this thread's share of the sequences that may have edges in the tile
+    __device__ __forceinline__ void look(const Scan &a, uint32_t &i, uint32_t &is, uint32_t &ie) const {
+        i = BACK ? b - threadIdx.x : b + threadIdx.x;
+        is = ie = 0;
+        if (i < a.batch) is = start_of(a, i), ie = start_of(a, i + 1);
     }
-}
+    // Fills `edges`, whose words are 0 and whose `next` is 0, for the rows r0 ..
+    // r0 + n - 1, and moves on to the next tile; ends with a barrier.
+    __device__ __forceinline__ void find(const Scan &a, uint32_t r0, uint32_t n, uint32_t i, uint32_t is, uint32_t ie,
+                                         Edges &edges) {
+        for (;;) {
+            bool more = false;
+            if (i < a.batch) {
+                if (is < ie && is - r0 < n) {
+                    atomicOr(&edges.begins[(is - r0) / R], 1u << ((is - r0) % R));
+                    edges.begin[is - r0] = i;
+                }
+                if (is < ie && ie - 1 - r0 < n) {
+                    atomicOr(&edges.ends[(ie - 1 - r0) / R], 1u << ((ie - 1 - r0) % R));
+                    edges.end[ie - 1 - r0] = i;
+                }
+                // where the next tile begins to look, and whether that is further on
+                if (BACK ? is < r0 : is <= r0 + n) atomicMax(&edges.next, i);
+                more = threadIdx.x == kThreads - 1 && (BACK ? is >= r0 : is < r0 + n);
+            }
+            if (!__syncthreads_or(more)) break;
+            i = BACK ? i - kThreads : i + kThreads;
+            is = ie = 0;
+            if (i < a.batch) is = start_of(a, i), ie = start_of(a, i + 1);
+        }
+        at(a, __builtin_amdgcn_readfirstlane(edges.next));
+    }
+};
 
 // Joins the maps of the workgroup's stretches (`own`, a thread's rows each): returns
 // that of all stretches before this one (REVERSE: behind it), `all` that of
@@ -199,7 +220,7 @@ __device__ __forceinline__ void join(const Map (&own)[C], uint32_t lanes, Map (&
 #pragma unroll
     for (int i = 0; i < C; i++) {
         Map up = {1.0f, 0.0f}, sum = {1.0f, 0.0f};
-#pragma unroll
+#pragma unroll 2
         for (uint32_t k = 0; k < kThreads / 64; k++) {
             const uint32_t w = REVERSE ? kThreads / 64 - 1 - k : k;
             if (w == wave) up = sum;
@@ -210,122 +231,195 @@ __device__ __forceinline__ void join(const Map (&own)[C], uint32_t lanes, Map (&
     }
 }
 
-// Where a thread's rows and channels are.
-struct Place {
+// Where a thread's rows and channels are.  ONE: a wavefront holds one stretch
+// of rows, so that rows and what is asked of them are the wavefront's.
+template <int R, bool ONE> struct Place {
     uint32_t sub, c, tile;                                 // its stretch in a tile, its first channel, rows of a tile
     uint32_t first, last;                                  // rows that sequences have
-    __device__ __forceinline__ Place(const Scan &a, int n, int rows) {
-        sub = threadIdx.x / a.lanes;
+    __device__ __forceinline__ Place(const Scan &a, int n) {
+        sub = ONE ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / a.lanes;
         c = (blockIdx.y * a.lanes + threadIdx.x % a.lanes) * n;
-        tile = kThreads / a.lanes * rows;
-        first = a.start ? clamped(a.start, 0, a.rows) : 0;
-        last = a.start ? clamped(a.start, a.batch, a.rows) : a.rows;
+        tile = kThreads / a.lanes * R;
+        first = __builtin_amdgcn_readfirstlane(start_of(a, 0));
+        last = __builtin_amdgcn_readfirstlane(start_of(a, a.batch));
+    }
+    __device__ __forceinline__ bool none() const { return first >= last; }
+    __device__ __forceinline__ bool there(uint32_t r) const { return r >= first && r < last; }
+    __device__ __forceinline__ bool all_there(uint32_t r) const { return r >= first && r + R <= last; }
+    __device__ __forceinline__ uint32_t word(const uint32_t *words) const {
+        return ONE ? __builtin_amdgcn_readfirstlane(words[sub]) : words[sub];
     }
 };
 
-template <typename T, int R>
-__device__ __forceinline__ void load_rows(const uint8_t *p, int64_t stride, uint32_t r, const Place &at, uint32_t width,
-                                          uint32_t (&raw)[R]) {
+// The words of a thread's rows.  IN: all of them are rows of sequences; else the
+// nearest of those are read where they are not.  (No choice within the loop: each
+// load would be waited for before the next.)
+template <bool IN, typename T, int R, bool ONE>
+__device__ __forceinline__ void load_rows(const uint8_t *p, int64_t stride, uint32_t r, const Place<R, ONE> &at,
+                                          const Piece<T> &piece, uint32_t (&raw)[R]) {
+    if constexpr (IN) {
+        p += (int64_t)r * stride;
 #pragma unroll
-    for (int i = 0; i < R; i++) {
-        raw[i] = 0;
-        if (at.c < width && r + i >= at.first && r + i < at.last)
-            raw[i] = Lane<T>::load(p + (int64_t)(r + i) * stride, at.c, width);
+        for (int i = 0; i < R; i++, p += stride) raw[i] = piece.load(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < R; i++) raw[i] = piece.load(p + (int64_t)min(max(r + i, at.first), at.last - 1) * stride);
     }
+}
+template <typename T, int R, bool ONE>
+__device__ __forceinline__ void store_rows(uint8_t *p, int64_t stride, uint32_t r, const Place<R, ONE> &at,
+                                           const Piece<T> &piece, bool whole, const float (&f)[R][Piece<T>::n]) {
+    p += (int64_t)r * stride;
+    if (!piece.there) return;
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < R; i++, p += stride) piece.store(p, f[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < R; i++, p += stride)
+            if (at.there(r + i)) piece.store(p, f[i]);
+    }
+}
+
+// Values c on of row b of an fp32 array [batch][width], zeros without one.
+template <int C>
+__device__ __forceinline__ void load_state(const Scan &a, const float *p, uint32_t b, uint32_t c, float (&f)[C]) {
+#pragma unroll
+    for (int i = 0; i < C; i++) f[i] = p && c + i < a.width ? p[(size_t)b * a.width + c + i] : 0.0f;
+}
+template <int C>
+__device__ __forceinline__ void store_state(const Scan &a, float *p, uint32_t b, uint32_t c, const float (&f)[C]) {
+#pragma unroll
+    for (int i = 0; i < C; i++)
+        if (c + i < a.width) p[(size_t)b * a.width + c + i] = f[i];
 }
 
 // Sequences without rows, which no tile holds: their states go through.
-__device__ __forceinline__ void pass_on(const Scan &a, const float *from, float *to, uint32_t c, int n) {
+template <int C> __device__ __forceinline__ void pass_on(const Scan &a, const float *from, float *to, uint32_t c) {
     if (!to || (!a.start && a.len)) return;
     for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
-        if (a.start && clamped(a.start, b, a.rows) < clamped(a.start, b + 1, a.rows)) continue;
-        if (threadIdx.x < a.lanes)
-            for (int i = 0; i < n; i++)
-                if (c + i < a.width)
-                    to[(size_t)b * a.width + c + i] = from ? from[(size_t)b * a.width + c + i] : 0.0f;
+        if (start_of(a, b) < start_of(a, b + 1) || threadIdx.x >= a.lanes) continue;
+        float f[C];
+        load_state(a, from, b, c, f);
+        store_state(a, to, b, c, f);
     }
 }
 
+// Has the compiler unpack the words again behind it, instead of keeping what they
+// held in registers of its own.
+template <int R> __device__ __forceinline__ void forget(uint32_t (&raw)[R]) {
+#pragma unroll
+    for (int k = 0; k < R; k++) asm volatile("" : "+v"(raw[k]));
+}
+// Keeps the compiler from starting what follows among what comes before: that
+// would take more registers than there are.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
 // APPLY = false: the chunks' maps; true: h, the last states and the states
 // that the backward pass starts from.
-template <typename T, bool APPLY>
+template <typename T, bool ONE, bool APPLY>
 __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
-    constexpr int C = Lane<T>::n, R = kRows;
+    constexpr int C = Piece<T>::n, R = kRows;
     __shared__ Edges edges;
     __shared__ Map lds[kThreads / 64][64 * C];
-    const Place at(a, C, R);
+    const Place<R, ONE> at(a, C);
+    const Piece<T> piece(at.c, a.width);
     const uint32_t from = blockIdx.x * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
     float state[C];
     Map chunk[C];
+    load_state(a, APPLY ? a.into : nullptr, blockIdx.x, at.c, state);
 #pragma unroll
-    for (int i = 0; i < C; i++) {
-        chunk[i] = {1.0f, 0.0f};
-        state[i] = APPLY && a.into && at.c + i < a.width ? a.into[(size_t)blockIdx.x * a.width + at.c + i] : 0.0f;
-    }
+    for (int i = 0; i < C; i++) chunk[i] = {1.0f, 0.0f};
+    if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
+    if (threadIdx.x == 0) edges.next = 0;
+    __syncthreads();
     uint32_t r0 = from;
-    if constexpr (!APPLY) {
-        // rows before the last first row in the chunk do not matter
-        const uint32_t b = a.start ? find_sequence(a.start, a.batch, to - 1) : (to - 1) / a.len;
-        const uint32_t s = a.start ? clamped(a.start, b, a.rows) : b * a.len;
-        if (s > from) r0 = from + (s - from) / at.tile * at.tile;
+    Cursor<R, false> cursor;
+    if (from < to && !at.none()) {
+        if constexpr (!APPLY) {                            // rows before the last first row in the chunk do not matter
+            cursor.at(a, find_sequence(a, to - 1));
+            if (cursor.s > from) r0 = from + (cursor.s - from) / at.tile * at.tile;
+        }
+        cursor.at(a, find_sequence(a, r0));
     }
+    if (at.none()) r0 = to;
     for (; r0 < to; r0 += at.tile) {
         const uint32_t r = r0 + at.sub * R;
-        uint32_t rx[R], rg[R];
-        load_rows<T, R>(a.x, a.x_row, r, at, a.width, rx);
-        load_rows<T, R>(a.g, a.g_row, r, at, a.width, rg);
-        find_edges<R>(a, r0, at.tile, edges);
-        const uint32_t begins = edges.begins[at.sub], ends = APPLY ? edges.ends[at.sub] : 0;
-        float z[R][C], y[R][C];
+        const bool plain = cursor.plain(r0, at.tile);
+        uint32_t rx[R], rg[R], b, bs, be, begins = 0, ends = 0;
+        if (!plain) cursor.look(a, b, bs, be);
+        const bool whole = plain || at.all_there(r);
+        if (whole) {
+            load_rows<true>(a.x, a.x_row, r, at, piece, rx);
+            load_rows<true>(a.g, a.g_row, r, at, piece, rg);
+        } else {
+            load_rows<false>(a.x, a.x_row, r, at, piece, rx);
+            load_rows<false>(a.g, a.g_row, r, at, piece, rg);
+        }
+        if (!plain) {
+            cursor.find(a, r0, at.tile, b, bs, be, edges);
+            begins = at.word(edges.begins);
+            if constexpr (APPLY) ends = at.word(edges.ends);
+        }
+        float z[APPLY ? R : 1][C], y[APPLY ? R : 1][C];
         Map own[C], before[C], all[C];
 #pragma unroll
         for (int i = 0; i < C; i++) own[i] = {1.0f, 0.0f};
+        phase();
 #pragma unroll
         for (int k = 0; k < R; k++) {
-            float x[C], g[C];
-            Lane<T>::unpack(rx[k], x);
-            Lane<T>::unpack(rg[k], g);
-            const bool there = r + k >= at.first && r + k < at.last;
+            constexpr int one = APPLY ? 1 : 0;
+            float x[C], g[C], (&zk)[C] = z[one * k], (&yk)[C] = y[one * k];
+            piece.unpack(rx[k], x);
+            piece.unpack(rg[k], g);
 #pragma unroll
             for (int i = 0; i < C; i++) {
-                gate(g[i], z[k][i], y[k][i]);
-                y[k][i] *= x[i];
-                if (!there) z[k][i] = 1.0f, y[k][i] = 0.0f;
+                gate(g[i], zk[i], yk[i]);
+                yk[i] *= x[i];
+                if (!whole && !at.there(r + k)) zk[i] = 1.0f, yk[i] = 0.0f;
             }
             if (begins >> k & 1) {
-                const int32_t b = edges.begin[at.sub * R + k];
+                float h0[C];
+                load_state(a, a.h0, edges.begin[at.sub * R + k], at.c, h0);
 #pragma unroll
                 for (int i = 0; i < C; i++) {
-                    const float h0 = a.h0 && at.c + i < a.width ? a.h0[(size_t)b * a.width + at.c + i] : 0.0f;
-                    y[k][i] = fmaf(z[k][i], h0, y[k][i]);
-                    z[k][i] = kForgets;
+                    yk[i] = fmaf(zk[i], h0[i], yk[i]);
+                    zk[i] = kForgets;
+                    own[i] = {kForgets, yk[i]};
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < C; i++) {                // (a forgetting map's -0 stays one times z)
+                    own[i].a *= zk[i];
+                    own[i].b = fmaf(zk[i], own[i].b, yk[i]);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < C; i++) own[i] = Map{z[k][i], y[k][i]}.after(own[i]);
+            if (k % 4 == 3) phase();
         }
         join<C, false>(own, a.lanes, before, all, lds);
+        if (!plain && threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
+        if (!plain && threadIdx.x == 0) edges.next = 0;
         if constexpr (APPLY) {
             float h[C];
 #pragma unroll
             for (int i = 0; i < C; i++) h[i] = before[i].of(state[i]);
-            if (a.states && r % kStateRows == 0 && r < a.rows)
+            if (a.states && r % kStateRows == 0 && r < a.rows) store_state(a, a.states, r / kStateRows, at.c, h);
+            if (!begins) {
 #pragma unroll
-                for (int i = 0; i < C; i++)
-                    if (at.c + i < a.width) a.states[(size_t)(r / kStateRows) * a.width + at.c + i] = h[i];
+                for (int k = 0; k < R; k++)
 #pragma unroll
-            for (int k = 0; k < R; k++) {
+                    for (int i = 0; i < C; i++) y[k][i] = h[i] = fmaf(z[k][i], h[i], y[k][i]);
+            } else {
 #pragma unroll
-                for (int i = 0; i < C; i++) h[i] = Map{z[k][i], y[k][i]}.of(h[i]);
-                if (at.c < a.width && r + k >= at.first && r + k < at.last) {
-                    Lane<T>::store(a.h + (int64_t)(r + k) * a.h_row, at.c, a.width, h);
-                    if (a.last && (ends >> k & 1)) {
-                        const int32_t b = edges.end[at.sub * R + k];
+                for (int k = 0; k < R; k++)
 #pragma unroll
-                        for (int i = 0; i < C; i++)
-                            if (at.c + i < a.width) a.last[(size_t)b * a.width + at.c + i] = h[i];
-                    }
-                }
+                    for (int i = 0; i < C; i++) y[k][i] = h[i] = Map{z[k][i], y[k][i]}.of(h[i]);
+            }
+            store_rows<T>(a.h, a.h_row, r, at, piece, whole, y);
+            if (a.last && ends) {
+#pragma unroll
+                for (int k = 0; k < R; k++)
+                    if (ends >> k & 1) store_state(a, a.last, edges.end[at.sub * R + k], at.c, y[k]);
             }
 #pragma unroll
             for (int i = 0; i < C; i++) state[i] = all[i].of(state[i]);
@@ -336,7 +430,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
         __syncthreads();
     }
     if constexpr (APPLY) {
-        pass_on(a, a.h0, a.last, at.c, C);
+        pass_on<C>(a, a.h0, a.last, at.c);
     } else if (threadIdx.x < a.lanes) {
         float *m = a.maps + (size_t)blockIdx.x * 2 * a.width;
 #pragma unroll
@@ -346,65 +440,95 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
 }
 
 // The same backwards: APPLY = false: the chunks' maps of e; true: the gradients.
-template <typename T, bool APPLY>
-__global__ __launch_bounds__(kThreads, 2) void scan_rows_backward(Scan a) {
-    constexpr int C = Lane<T>::n, R = kRowsBack;
+template <typename T, bool ONE, bool APPLY>
+__global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
+    constexpr int C = Piece<T>::n, R = kRowsBack;
     __shared__ Edges edges;
     __shared__ Map lds[2][kThreads / 64][64 * C];
-    const Place at(a, C, R);
+    const Place<R, ONE> at(a, C);
+    const Piece<T> piece(at.c, a.width);
     const uint32_t from = blockIdx.x * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
     float state[C];
     Map chunk[C];
+    load_state(a, APPLY ? a.into : nullptr, blockIdx.x, at.c, state);
 #pragma unroll
-    for (int i = 0; i < C; i++) {
-        chunk[i] = {1.0f, 0.0f};
-        state[i] = APPLY && a.into && at.c + i < a.width ? a.into[(size_t)blockIdx.x * a.width + at.c + i] : 0.0f;
-    }
+    for (int i = 0; i < C; i++) chunk[i] = {1.0f, 0.0f};
+    if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
+    if (threadIdx.x == 0) edges.next = 0;
+    __syncthreads();
     uint32_t tiles = (to - from + at.tile - 1) / at.tile;
-    if constexpr (!APPLY) {
-        // rows behind the first last row in the chunk do not matter
-        const uint32_t b = a.start ? find_sequence(a.start, a.batch, from) : from / a.len;
-        const uint32_t e = a.start ? clamped(a.start, b + 1, a.rows) : (b + 1) * a.len;
-        if (e > from && e <= to) tiles = min(tiles, (e - from + at.tile - 1) / at.tile);
+    Cursor<R, true> cursor;
+    if (at.none()) tiles = 0;
+    if (tiles) {
+        if constexpr (!APPLY) {                            // rows behind the first last row in the chunk do not matter
+            cursor.at(a, find_sequence(a, from));
+            if (cursor.e > from && cursor.e <= to) tiles = (cursor.e - from + at.tile - 1) / at.tile;
+        }
+        cursor.at(a, find_sequence(a, min(from + tiles * at.tile, a.rows) - 1));
     }
     for (uint32_t t = tiles; t-- > 0;) {
         const uint32_t r0 = from + t * at.tile, r = r0 + at.sub * R;
-        uint32_t rx[R], rg[R], rd[R];
-        load_rows<T, R>(a.g, a.g_row, r, at, a.width, rg);
-        load_rows<T, R>(a.dh, a.dh_row, r, at, a.width, rd);
-        if constexpr (APPLY) load_rows<T, R>(a.x, a.x_row, r, at, a.width, rx);
+        const bool plain = cursor.plain(r0, at.tile);
+        uint32_t rx[R], rg[R], rd[R], b, bs, be, begins = 0, ends = 0;
+        if (!plain) cursor.look(a, b, bs, be);
+        const bool whole = plain || at.all_there(r);
+        if (whole) {
+            load_rows<true>(a.g, a.g_row, r, at, piece, rg);
+            load_rows<true>(a.dh, a.dh_row, r, at, piece, rd);
+            if constexpr (APPLY) load_rows<true>(a.x, a.x_row, r, at, piece, rx);
+        } else {
+            load_rows<false>(a.g, a.g_row, r, at, piece, rg);
+            load_rows<false>(a.dh, a.dh_row, r, at, piece, rd);
+            if constexpr (APPLY) load_rows<false>(a.x, a.x_row, r, at, piece, rx);
+        }
         float h[C];
-#pragma unroll
-        for (int i = 0; i < C; i++)
-            h[i] = APPLY && at.c + i < a.width ? a.states[(size_t)(r0 / kStateRows) * a.width + at.c + i] : 0.0f;
-        find_edges<R>(a, r0, at.tile, edges);
-        const uint32_t begins = APPLY ? edges.begins[at.sub] : 0, ends = edges.ends[at.sub];
-        float z[R][C], y[R][C], d[R][C];
+        load_state(a, APPLY ? a.states : nullptr, r0 / kStateRows, at.c, h);
+        if (!plain) {
+            cursor.find(a, r0, at.tile, b, bs, be, edges);
+            ends = at.word(edges.ends);
+            if constexpr (APPLY) begins = at.word(edges.begins);
+        }
+        float z[R][C], y[R][C];
         Map own[C], before[C], all[C];
+#pragma unroll
+        for (int k = 0; k < R; k++) {
+            float g[C];
+            piece.unpack(rg[k], g);
+#pragma unroll
+            for (int i = 0; i < C; i++) gate(g[i], z[k][i], y[k][i]);
+            if (k % 4 == 3) phase();
+        }
+        if (!whole) {
+#pragma unroll
+            for (int k = 0; k < R; k++)
+#pragma unroll
+                for (int i = 0; i < C; i++)
+                    if (!at.there(r + k)) z[k][i] = 1.0f, y[k][i] = 0.0f;
+        }
 #pragma unroll
         for (int i = 0; i < C; i++) own[i] = {1.0f, 0.0f};
 #pragma unroll
         for (int k = R - 1; k >= 0; k--) {
-            float g[C];
-            Lane<T>::unpack(rg[k], g);
-            Lane<T>::unpack(rd[k], d[k]);
-            const bool there = r + k >= at.first && r + k < at.last, end = ends >> k & 1;
+            float d[C];
+            piece.unpack(rd[k], d);
+            if (ends >> k & 1) {
+                float last[C];
+                load_state(a, a.dlast, edges.end[at.sub * R + k], at.c, last);
 #pragma unroll
-            for (int i = 0; i < C; i++) {
-                gate(g[i], z[k][i], y[k][i]);
-                if (!there) z[k][i] = 1.0f, y[k][i] = 0.0f;
+                for (int i = 0; i < C; i++) own[i] = {kForgets, z[k][i] * (d[i] + last[i])};
+            } else {
+#pragma unroll
+                for (int i = 0; i < C; i++) {                // (a forgetting map's -0 stays one times z)
+                    own[i].a *= z[k][i];
+                    own[i].b = fmaf(z[k][i], own[i].b, z[k][i] * d[i]);
+                }
             }
-            if (end && a.dlast) {
-                const int32_t b = edges.end[at.sub * R + k];
-#pragma unroll
-                for (int i = 0; i < C; i++)
-                    if (at.c + i < a.width) d[k][i] += a.dlast[(size_t)b * a.width + at.c + i];
-            }
-#pragma unroll
-            for (int i = 0; i < C; i++)
-                own[i] = Map{end ? kForgets : z[k][i], z[k][i] * d[k][i]}.after(own[i]);
         }
+        phase();
         join<C, true>(own, a.lanes, before, all, lds[0]);
+        phase();
+        if (!plain && threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
+        if (!plain && threadIdx.x == 0) edges.next = 0;
         float e[C];
 #pragma unroll
         for (int i = 0; i < C; i++) {
@@ -414,72 +538,102 @@ __global__ __launch_bounds__(kThreads, 2) void scan_rows_backward(Scan a) {
         }
         if constexpr (APPLY) {
             // h before each row again: forward maps from the state that was kept
-            const auto forward = [&](int k, int i, const float (&x)[C]) {
-                Map m = {z[k][i], y[k][i] * x[i]};
-                if (begins >> k & 1) {
-                    const float h0 = a.h0 && at.c + i < a.width
-                                         ? a.h0[(size_t)edges.begin[at.sub * R + k] * a.width + at.c + i] : 0.0f;
-                    m = {kForgets, fmaf(m.a, h0, m.b)};
-                }
-                return m;
-            };
+            float w[R][C];
 #pragma unroll
             for (int i = 0; i < C; i++) own[i] = {1.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < R; k++) {
                 float x[C];
-                Lane<T>::unpack(rx[k], x);
+                piece.unpack(rx[k], x);
+                if (begins >> k & 1) {
+                    load_state(a, a.h0, edges.begin[at.sub * R + k], at.c, w[k]);
 #pragma unroll
-                for (int i = 0; i < C; i++) own[i] = forward(k, i, x).after(own[i]);
+                    for (int i = 0; i < C; i++) own[i] = {kForgets, fmaf(z[k][i], w[k][i], y[k][i] * x[i])};
+                } else {
+#pragma unroll
+                    for (int i = 0; i < C; i++) {
+                        own[i].a *= z[k][i];
+                        own[i].b = fmaf(z[k][i], own[i].b, y[k][i] * x[i]);
+                    }
+                }
             }
+            phase();
             join<C, false>(own, a.lanes, before, all, lds[1]);
-            float w[R][C];                               // h before the row
+            forget(rx);
+            phase();
 #pragma unroll
             for (int i = 0; i < C; i++) h[i] = before[i].of(h[i]);
 #pragma unroll
             for (int k = 0; k < R; k++) {
                 float x[C];
-                Lane<T>::unpack(rx[k], x);
+                piece.unpack(rx[k], x);
+                if (!(begins >> k & 1)) {
 #pragma unroll
-                for (int i = 0; i < C; i++) {
-                    w[k][i] = h[i];
-                    if (begins >> k & 1)
-                        w[k][i] = a.h0 && at.c + i < a.width
-                                      ? a.h0[(size_t)edges.begin[at.sub * R + k] * a.width + at.c + i] : 0.0f;
-                    h[i] = forward(k, i, x).of(h[i]);
+                    for (int i = 0; i < C; i++) w[k][i] = h[i];
                 }
+#pragma unroll
+                for (int i = 0; i < C; i++) h[i] = fmaf(z[k][i], w[k][i], y[k][i] * x[i]);
+                if (k % 4 == 3) phase();
             }
+            forget(rx);
+            forget(rd);
+            phase();
+            // y becomes dx, w dg, z what goes on to the row before
 #pragma unroll
             for (int k = R - 1; k >= 0; k--) {
-                float x[C], dx[C], dg[C];
-                Lane<T>::unpack(rx[k], x);
+                float x[C], d[C];
+                piece.unpack(rx[k], x);
+                piece.unpack(rd[k], d);
+                if (ends >> k & 1) load_state(a, a.dlast, edges.end[at.sub * R + k], at.c, e);
 #pragma unroll
                 for (int i = 0; i < C; i++) {
-                    const float q = (ends >> k & 1) ? d[k][i] : d[k][i] + e[i];
-                    dx[i] = y[k][i] * q;
-                    e[i] = z[k][i] * q;
-                    dg[i] = dx[i] * z[k][i] * (w[k][i] - x[i]);
+                    const float q = d[i] + e[i];
+                    y[k][i] *= q;
+                    w[k][i] = y[k][i] * z[k][i] * (w[k][i] - x[i]);
+                    e[i] = z[k][i] *= q;
                 }
-                if (at.c >= a.width || r + k < at.first || r + k >= at.last) continue;
-                Lane<T>::store(a.dx + (int64_t)(r + k) * a.dx_row, at.c, a.width, dx);
-                Lane<T>::store(a.dg + (int64_t)(r + k) * a.dg_row, at.c, a.width, dg);
-                if (a.dh0 && (begins >> k & 1)) {
-                    const int32_t b = edges.begin[at.sub * R + k];
+                if (k % 4 == 0) phase();
+            }
+            store_rows<T>(a.dx, a.dx_row, r, at, piece, whole, y);
+            store_rows<T>(a.dg, a.dg_row, r, at, piece, whole, w);
+            if (a.dh0 && begins) {
 #pragma unroll
-                    for (int i = 0; i < C; i++)
-                        if (at.c + i < a.width) a.dh0[(size_t)b * a.width + at.c + i] = e[i];
-                }
+                for (int k = 0; k < R; k++)
+                    if (begins >> k & 1) store_state(a, a.dh0, edges.begin[at.sub * R + k], at.c, z[k]);
             }
         }
         __syncthreads();
     }
     if constexpr (APPLY) {
-        pass_on(a, a.dlast, a.dh0, at.c, C);
+        pass_on<C>(a, a.dlast, a.dh0, at.c);
     } else if (threadIdx.x < a.lanes) {
         float *m = a.maps + (size_t)blockIdx.x * 2 * a.width;
 #pragma unroll
         for (int i = 0; i < C; i++)
             if (at.c + i < a.width) m[at.c + i] = chunk[i].a, m[a.width + at.c + i] = chunk[i].b;
+    }
+}
+
+// One row a sequence, as it comes: a thread a few channels of one row.
+template <typename T> __global__ __launch_bounds__(256) void single_rows(Scan a) {
+    constexpr int C = Piece<T>::n;
+    const uint32_t pieces = (a.width + C - 1) / C;
+    const uint64_t all = (uint64_t)a.rows * pieces, step = (uint64_t)gridDim.x * 256;
+    for (uint64_t l = (uint64_t)blockIdx.x * 256 + threadIdx.x; l < all; l += step) {
+        const uint32_t r = (uint32_t)(l / pieces), c = (uint32_t)(l - (uint64_t)r * pieces) * C;
+        const Piece<T> piece(c, a.width);
+        float x[C], g[C], h[C];
+        piece.unpack(piece.load(a.x + (int64_t)r * a.x_row), x);
+        piece.unpack(piece.load(a.g + (int64_t)r * a.g_row), g);
+        load_state(a, a.h0, r, c, h);
+#pragma unroll
+        for (int i = 0; i < C; i++) {
+            float z, y;
+            gate(g[i], z, y);
+            h[i] = fmaf(z, h[i], y * x[i]);
+        }
+        piece.store(a.h + (int64_t)r * a.h_row, h);
+        if (a.last) store_state(a, a.last, r, c, h);
     }
 }
 
@@ -583,20 +737,30 @@ bool overlap(const Scan &a, const float *p, const float *q) {
     return p && q && p < q + n && q < p + n;
 }
 
-template <typename T, bool BACKWARD> int launch(Scan &a, void *work, hipStream_t s) {
-    const uint32_t groups = groups_of(a, Lane<T>::n);
+template <typename T, bool ONE, bool BACKWARD> int launch(Scan &a, void *work, hipStream_t s) {
     // (a call of no rows still has states to pass on)
-    const dim3 grid(a.chunks ? a.chunks : 1, groups);
+    const dim3 grid(a.chunks ? a.chunks : 1, groups_of(a, Piece<T>::n));
     if (carried(a)) {
         a.maps = (float *)work;
         float *into = (float *)((uint8_t *)work + align16z((size_t)a.chunks * 2 * a.width * 4));
-        int rc = enqueue(BACKWARD ? scan_rows_backward<T, false> : scan_rows<T, false>, grid, kThreads, 0, s, a);
+        int rc = enqueue(BACKWARD ? scan_rows_backward<T, ONE, false> : scan_rows<T, ONE, false>, grid, kThreads, 0, s, a);
         if (rc != NLB_OK) return rc;
         a.into = into;
         rc = enqueue(join_chunks<BACKWARD>, (a.width + 15) / 16, 1024, 0, s, a);
         if (rc != NLB_OK) return rc;
     }
-    return enqueue(BACKWARD ? scan_rows_backward<T, true> : scan_rows<T, true>, grid, kThreads, 0, s, a);
+    return enqueue(BACKWARD ? scan_rows_backward<T, ONE, true> : scan_rows<T, ONE, true>, grid, kThreads, 0, s, a);
+}
+template <typename T, bool BACKWARD> int launch(Scan &a, void *work, hipStream_t s) {
+    if (!BACKWARD && !a.start && a.len == 1 && !a.states) {
+        const uint64_t pieces = (uint64_t)a.rows * ((a.width + Piece<T>::n - 1) / Piece<T>::n);
+        return enqueue(single_rows<T>, (uint32_t)std::min<uint64_t>((pieces + 255) / 256, 1u << 20), 256, 0, s, a);
+    }
+    return a.lanes == 64 ? launch<T, true, BACKWARD>(a, work, s) : launch<T, false, BACKWARD>(a, work, s);
+}
+
+template <bool BACKWARD> int launch_bf16(Scan &a, void *work, hipStream_t s) {
+    return a.width == 1 ? launch<OneBf16, false, BACKWARD>(a, work, s) : launch<__bf16, BACKWARD>(a, work, s);
 }
 
 }  // namespace
@@ -627,7 +791,7 @@ extern "C" int nlb_gated_scan(const nlb_scan_call *c, const nlb_scan_rows *h, fl
     a.states = states;
     CallDevice device(c->device);
     if (device.rc != NLB_OK) return device.rc;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, false>(a, work, (hipStream_t)stream)
+    return c->dtype == NLB_DTYPE_BF16 ? launch_bf16<false>(a, work, (hipStream_t)stream)
                                       : launch<float, false>(a, work, (hipStream_t)stream);
 }
 
@@ -655,6 +819,6 @@ extern "C" int nlb_gated_scan_backward(const nlb_scan_call *c, const float *stat
     a.dh0 = dh0;
     CallDevice device(c->device);
     if (device.rc != NLB_OK) return device.rc;
-    return c->dtype == NLB_DTYPE_BF16 ? launch<__bf16, true>(a, work, (hipStream_t)stream)
+    return c->dtype == NLB_DTYPE_BF16 ? launch_bf16<true>(a, work, (hipStream_t)stream)
                                       : launch<float, true>(a, work, (hipStream_t)stream);
 }

@@ -18,8 +18,9 @@ namespace {
 
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
-constexpr int kThreads = 256, kItems = 16, kWaves = kThreads / 64;
-constexpr uint32_t kTile = kThreads * kItems;              // entries a workgroup sorts
+constexpr int kThreads = 256;
+constexpr int kSortThreads = 512, kItems = 8, kWaves = kSortThreads / 64;
+constexpr uint32_t kTile = kSortThreads * kItems;          // entries a workgroup sorts
 constexpr uint32_t kMaxBits = 9, kMaxDigits = 1u << kMaxBits;
 
 template <typename T> struct Chunk { static constexpr int n = 16 / sizeof(T); };
@@ -129,7 +130,7 @@ struct Sort {
     const int32_t *ids;
     const uint64_t *from;                                  // id in the upper half, place in the lower
     uint64_t *to;
-    uint32_t *hist, *totals, *valid;                       // [digits][tiles], [digits], one word
+    uint32_t *hist, *totals, *valid;                       // [tiles][digits], [digits], one word
     uint32_t n, rows, tiles, shift, bits;
 };
 
@@ -146,19 +147,19 @@ __device__ __forceinline__ uint32_t digit_of(const Sort &a, uint64_t e) {
 }
 
 // How many of a tile's entries have each digit.
-template <bool FIRST> __global__ __launch_bounds__(kThreads) void count_digits(Sort a) {
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void count_digits(Sort a) {
     __shared__ uint32_t count[kMaxDigits];
     const uint32_t digits = 1u << a.bits, n = FIRST ? a.n : *a.valid;
-    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
+    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
     __syncthreads();
     uint64_t e[kItems];
 #pragma unroll
-    for (int i = 0; i < kItems; i++) e[i] = entry<FIRST>(a, blockIdx.x * kTile + i * kThreads + threadIdx.x, n);
+    for (int i = 0; i < kItems; i++) e[i] = entry<FIRST>(a, blockIdx.x * kTile + i * kSortThreads + threadIdx.x, n);
 #pragma unroll
     for (int i = 0; i < kItems; i++)
         if (e[i] != ~0ull) atomicAdd(&count[digit_of(a, e[i])], 1u);
     __syncthreads();
-    for (uint32_t d = threadIdx.x; d < digits; d += kThreads) a.hist[(size_t)d * a.tiles + blockIdx.x] = count[d];
+    for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.hist[((size_t)blockIdx.x << a.bits) + d] = count[d];
 }
 
 // The sum of x over the workgroup's threads before this one; `all` that of all.
@@ -173,54 +174,71 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t &all, uint32
     __syncthreads();
     if (lane == 63) lds[threadIdx.x / 64] = s;
     __syncthreads();
-    uint32_t before = 0;
-    all = 0;
-    for (uint32_t w = 0; w < waves; w++) {
-        if (w == threadIdx.x / 64) before = all;
-        all += lds[w];
+    uint32_t w = lane < waves ? lds[lane] : 0;             // of wavefronts, at most 16
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) {
+        const uint32_t y = __shfl_up(w, o);
+        if (lane >= (uint32_t)o) w += y;
     }
+    all = __shfl(w, waves - 1);
+    const uint32_t before = threadIdx.x / 64 ? __shfl(w, threadIdx.x / 64 - 1) : 0;
     return before + s - x;
 }
 
-// A digit's counts become those of the tiles before each; their sum goes to totals.
-__global__ __launch_bounds__(kThreads) void scan_digits(Sort a) {
-    __shared__ uint32_t lds[kWaves];
-    uint32_t *h = a.hist + (size_t)blockIdx.x * a.tiles;
-    uint32_t before = 0;
-    for (uint32_t t0 = 0; t0 < a.tiles; t0 += 4 * kThreads) {
-        uint32_t x[4], sum = 0, all;
+// A digit's counts become those of the tiles before each; their sum goes to
+// totals.  16 digits a workgroup, 64 threads each, a stretch of the tiles a thread.
+__global__ __launch_bounds__(1024) void scan_digits(Sort a) {
+    __shared__ uint32_t sums[64][17];
+    const uint32_t c = threadIdx.x % 16, t = threadIdx.x / 16, d = blockIdx.x * 16 + c, digits = 1u << a.bits;
+    const uint32_t per = (a.tiles + 63) / 64, t0 = min(t * per, a.tiles), t1 = d < digits ? min(t0 + per, a.tiles) : t0;
+    uint32_t *h = a.hist + d;
+    uint32_t sum = 0;
+    for (uint32_t k = t0; k < t1; k += 8) {
+        uint32_t x[8];
 #pragma unroll
-        for (uint32_t i = 0; i < 4; i++) {
-            const uint32_t t = t0 + 4 * threadIdx.x + i;
-            x[i] = t < a.tiles ? h[t] : 0;
-            sum += x[i];
-        }
-        uint32_t at = before + sum_before(sum, all, lds);
+        for (uint32_t i = 0; i < 8; i++) x[i] = k + i < t1 ? h[(size_t)(k + i) << a.bits] : 0;
 #pragma unroll
-        for (uint32_t i = 0; i < 4; i++) {
-            const uint32_t t = t0 + 4 * threadIdx.x + i;
-            if (t < a.tiles) h[t] = at;
+        for (uint32_t i = 0; i < 8; i++) sum += x[i];
+    }
+    sums[t][c] = sum;
+    __syncthreads();
+    uint32_t at = 0, all = 0;
+#pragma unroll 16
+    for (uint32_t i = 0; i < 64; i++) {
+        const uint32_t x = sums[i][c];
+        at += i < t ? x : 0;
+        all += x;
+    }
+    for (uint32_t k = t0; k < t1; k += 8) {
+        uint32_t x[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) x[i] = k + i < t1 ? h[(size_t)(k + i) << a.bits] : 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 8; i++) {
+            if (k + i < t1) h[(size_t)(k + i) << a.bits] = at;
             at += x[i];
         }
-        before += all;
     }
-    if (threadIdx.x == 0) a.totals[blockIdx.x] = before;
+    if (t == 0 && d < digits) a.totals[d] = all;
 }
 
 // Each entry of a tile to its place: behind all of lower digits, the earlier
 // tiles' of its own and the earlier of its own in the tile.  The tile is put in
 // order in LDS first, so that neighbours go out together.
-template <bool FIRST> __global__ __launch_bounds__(kThreads) void scatter(Sort a) {
+template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void scatter(Sort a) {
     __shared__ uint64_t items[kTile];
-    __shared__ uint32_t waves[kWaves][kMaxDigits], start[kMaxDigits], base[kMaxDigits], lds[kWaves];
+    __shared__ uint16_t waves[kWaves][kMaxDigits];
+    __shared__ uint32_t start[kMaxDigits], base[kMaxDigits], lds[kWaves];
     const uint32_t digits = 1u << a.bits, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const uint32_t n = FIRST ? a.n : *a.valid;
     if (!FIRST && blockIdx.x * kTile >= n) return;
-    for (uint32_t d = threadIdx.x; d < kWaves * kMaxDigits; d += kThreads) waves[d / kMaxDigits][d % kMaxDigits] = 0;
+    for (uint32_t d = threadIdx.x; d < kWaves * kMaxDigits; d += kSortThreads) waves[d / kMaxDigits][d % kMaxDigits] = 0;
     uint64_t e[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; i++)
         e[i] = entry<FIRST>(a, blockIdx.x * kTile + (wave * kItems + i) * 64 + lane, n);
+    const uint32_t total = threadIdx.x < digits ? a.totals[threadIdx.x] : 0;
+    const uint32_t earlier = threadIdx.x < digits ? a.hist[((size_t)blockIdx.x << a.bits) + threadIdx.x] : 0;
     __syncthreads();
     uint32_t rank[kItems];                                 // in the wavefront's entries of the digit
 #pragma unroll
@@ -233,36 +251,28 @@ template <bool FIRST> __global__ __launch_bounds__(kThreads) void scatter(Sort a
             same &= d >> b & 1 ? one : ~one;
         }
         const uint32_t before = __popcll(same & ((1ull << lane) - 1));
-        volatile uint32_t *count = &waves[wave][d];
+        volatile uint16_t *count = &waves[wave][d];
         const uint32_t c = there ? *count : 0;
         rank[i] = c + before;
-        if (there && before == 0) *count = c + __popcll(same);
+        if (there && before == 0) *count = (uint16_t)(c + __popcll(same));
     }
     __syncthreads();
-    // two digits a thread: their counts' sums over wavefronts, digits and tiles
-    uint32_t sum[2], all, total[2], total_all;
+    // a digit a thread: its counts' sums over wavefronts, digits and tiles
+    uint32_t sum = 0, all, total_all;
+    const uint32_t mine = threadIdx.x;
+    if (mine < digits) {
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const uint32_t d = 2 * threadIdx.x + i;
-        sum[i] = total[i] = 0;
-        if (d >= digits) continue;
         for (int w = 0; w < kWaves; w++) {
-            const uint32_t c = waves[w][d];
-            waves[w][d] = sum[i];
-            sum[i] += c;
+            const uint32_t c = waves[w][mine];
+            waves[w][mine] = (uint16_t)sum;
+            sum += c;
         }
-        total[i] = a.totals[d];
     }
-    uint32_t at = sum_before(sum[0] + sum[1], all, lds), to = sum_before(total[0] + total[1], total_all, lds);
+    const uint32_t at = sum_before(sum, all, lds), to = sum_before(total, total_all, lds);
     if (FIRST && blockIdx.x == 0 && threadIdx.x == 0) *a.valid = total_all;
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const uint32_t d = 2 * threadIdx.x + i;
-        if (d >= digits) continue;
-        start[d] = at;
-        base[d] = to + a.hist[(size_t)d * a.tiles + blockIdx.x] - at;
-        at += sum[i];
-        to += total[i];
+    if (mine < digits) {
+        start[mine] = at;
+        base[mine] = to + earlier - at;
     }
     __syncthreads();
 #pragma unroll
@@ -272,7 +282,7 @@ template <bool FIRST> __global__ __launch_bounds__(kThreads) void scatter(Sort a
         items[start[d] + waves[wave][d] + rank[i]] = e[i];
     }
     __syncthreads();
-    for (uint32_t p = threadIdx.x; p < all; p += kThreads) {
+    for (uint32_t p = threadIdx.x; p < all; p += kSortThreads) {
         const uint64_t x = items[p];
         a.to[base[digit_of(a, x)] + p] = x;
     }
@@ -287,7 +297,7 @@ struct Sums {
     const uint32_t *valid;
     float *part;                                           // [runs][2][width]
     int32_t *list;                                         // NULL: rows go to their ids
-    uint32_t *heads;                                       // [runs + 1]: rows that begin in the runs before
+    uint32_t *heads, *blocks;                              // [runs], [their blocks + 1]: rows that begin before
     uint32_t *count;
     uint32_t n, width, lanes, run, runs;
     float scale;
@@ -295,43 +305,56 @@ struct Sums {
 
 __device__ __forceinline__ uint32_t id_at(const Sums &a, uint32_t i) { return (uint32_t)(a.sorted[i] >> 32); }
 
-// How many rows begin in each run: 16 lanes a run.
-__global__ __launch_bounds__(kThreads) void count_heads(Sums a) {
-    const uint32_t n = *a.valid, r = blockIdx.x * (kThreads / 16) + threadIdx.x / 16, lane = threadIdx.x % 16;
+// How many rows begin in the runs before each, within the workgroup's 64 runs
+// (16 lanes each), and in all of those.
+constexpr uint32_t kBlock = 64;
+__global__ __launch_bounds__(1024) void count_heads(Sums a) {
+    __shared__ uint32_t count[kBlock];
+    const uint32_t n = *a.valid, r = blockIdx.x * kBlock + threadIdx.x / 16, lane = threadIdx.x % 16;
     uint32_t k = 0;
+#pragma unroll 4
     for (uint32_t i = lane; i < a.run && r < a.runs; i += 16) {
         const uint32_t j = r * a.run + i;
         if (j < n && (j == 0 || id_at(a, j) != id_at(a, j - 1))) k++;
     }
     for (int o = 8; o; o /= 2) k += __shfl_xor(k, o);
-    if (r < a.runs && lane == 0) a.heads[r] = k;
+    if (lane == 0) count[threadIdx.x / 16] = k;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    k = count[threadIdx.x];
+    uint32_t sum = k;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const uint32_t y = __shfl_up(sum, o);
+        if (threadIdx.x >= (uint32_t)o) sum += y;
+    }
+    const uint32_t at = blockIdx.x * kBlock + threadIdx.x;
+    if (at < a.runs) a.heads[at] = sum - k;
+    if (threadIdx.x == 63) a.blocks[blockIdx.x] = sum;
 }
 
-// They become those of the runs before each, and behind the last all of them.
-__global__ __launch_bounds__(1024) void scan_heads(Sums a) {
+// The blocks' counts become those of the blocks before each; behind the last,
+// all of them.
+__global__ __launch_bounds__(1024) void scan_blocks(Sums a) {
     __shared__ uint32_t lds[16];
+    const uint32_t blocks = (a.runs + kBlock - 1) / kBlock;
     uint32_t before = 0;
-    for (uint32_t r0 = 0; r0 < a.runs; r0 += 8 * 1024) {
-        uint32_t x[8], sum = 0, all;
-#pragma unroll
-        for (uint32_t i = 0; i < 8; i++) {
-            const uint32_t r = r0 + 8 * threadIdx.x + i;
-            x[i] = r < a.runs ? a.heads[r] : 0;
-            sum += x[i];
-        }
-        uint32_t at = before + sum_before(sum, all, lds);
-#pragma unroll
-        for (uint32_t i = 0; i < 8; i++) {
-            const uint32_t r = r0 + 8 * threadIdx.x + i;
-            if (r < a.runs) a.heads[r] = at;
-            at += x[i];
-        }
+    for (uint32_t b0 = 0; b0 < blocks; b0 += 1024) {
+        const uint32_t b = b0 + threadIdx.x, x = b < blocks ? a.blocks[b] : 0;
+        uint32_t all;
+        const uint32_t at = before + sum_before(x, all, lds);
+        if (b < blocks) a.blocks[b] = at;
         before += all;
     }
     if (threadIdx.x == 0) {
-        a.heads[a.runs] = before;
+        a.blocks[blocks] = before;
         *a.count = before;
     }
+}
+
+// Rows that begin in the runs before r (all of them behind the last run).
+__device__ __forceinline__ uint32_t heads_before(const Sums &a, uint32_t r) {
+    return r < a.runs ? a.heads[r] + a.blocks[r / kBlock] : a.blocks[(a.runs + kBlock - 1) / kBlock];
 }
 
 // Whether the row at place i goes on behind the run after i's run `r`, so that
@@ -349,10 +372,11 @@ template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums 
     const uint32_t begin = r * a.run, end = min(begin + a.run, n);
     uint32_t slot = 0;
     if (a.list) {
-        slot = a.heads[r];
+        slot = heads_before(a, r);
+        const uint32_t all = heads_before(a, a.runs);
         if (blockIdx.y == 0)                               // behind the last row's id
             for (uint32_t i = begin + lane; i < begin + a.run && i < a.n; i += a.lanes)
-                if (i >= a.heads[a.runs]) a.list[i] = -1;
+                if (i >= all) a.list[i] = -1;
     }
     if (begin >= n) return;
     uint32_t id = id_at(a, begin), i = begin, stop = end;
@@ -434,57 +458,103 @@ template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums 
     else leave(id);
 }
 
-// Rows that were summed in parts: a workgroup looks at 256 runs and joins the
-// rows that begin in them, one after the other, its groups of lanes a stretch of
-// the parts each.
-template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(Sums a) {
-    constexpr int N = Chunk<T>::n, U = 4;
-    __shared__ uint32_t found[kThreads], number, reach;
-    __shared__ float sums[kThreads][N + 1];
-    const uint32_t n = *a.valid, r = blockIdx.x * kThreads + threadIdx.x;
-    if (threadIdx.x == 0) number = 0;
+// Rows that were summed in parts: a workgroup looks at 32 runs and joins the
+// rows that begin in them: a wavefront each those of up to 64 parts more, all of
+// them together the longer ones; groups of lanes take a stretch of the parts
+// each, whose sums are added in order.
+constexpr uint32_t kLook = 32, kJoinThreads = 1024;
+
+// The sum over parts p0 to p1 - 1 of the row that begins in run `first`: the
+// run's second part, then the first ones of the runs behind it.
+template <int N>
+__device__ __forceinline__ void add_parts(const Sums &a, uint32_t first, uint32_t p0, uint32_t p1, uint32_t c,
+                                          float (&sum)[N]) {
+    constexpr int U = 8;
+#pragma unroll
+    for (int i = 0; i < N; i++) sum[i] = 0.0f;
+    for (uint32_t p = p0; p < p1; p += U) {
+        float x[U][N];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const float *f = a.part + ((size_t)(first + p + u) * 2 + (p + u == 0)) * a.width + c;
+            if (c + N <= a.width) {
+#pragma unroll
+                for (int i = 0; i < N; i += 4) {
+                    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+                    if (p + u < p1) v = *(const f32x4_at4 *)(f + i);
+                    x[u][i] = v[0], x[u][i + 1] = v[1], x[u][i + 2] = v[2], x[u][i + 3] = v[3];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; i++) x[u][i] = p + u < p1 && c + i < a.width ? f[i] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int i = 0; i < N; i++) sum[i] += x[u][i];
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void join_parts(Sums a) {
+    constexpr int N = Chunk<T>::n;
+    __shared__ uint32_t found[kLook], number, large[kLook], larges, reach;
+    __shared__ float sums[kJoinThreads][N + 1];
+    const uint32_t n = *a.valid, r = blockIdx.x * kLook + threadIdx.x;
+    if (blockIdx.x * kLook * a.run >= n) return;
+    if (threadIdx.x == 0) number = larges = 0;
     __syncthreads();
-    if (r < a.runs && (uint64_t)(r + 2) * a.run < n) {
+    if (threadIdx.x < kLook && r < a.runs && (uint64_t)(r + 2) * a.run < n) {
         const uint32_t begin = r * a.run, end = begin + a.run, id = id_at(a, end - 1);
         const bool from_before = id_at(a, begin) == id && begin > 0 && id_at(a, begin - 1) == id;
         if (!from_before && id_at(a, end) == id && id_at(a, end + a.run) == id) found[atomicAdd(&number, 1u)] = r;
     }
     __syncthreads();
-    const uint32_t lane = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes, groups = kThreads / a.lanes;
-    const uint32_t c = (blockIdx.y * a.lanes + lane) * N;
-    for (uint32_t k = 0; k < number; k++) {
-        const uint32_t first = found[k], id = id_at(a, first * a.run + a.run - 1);
-        // the last run that holds it: runs that begin with it, 256 tried at once
-        uint32_t last = first + 1, step = (a.runs - first + kThreads - 1) / kThreads;
-        for (;; step = (step + kThreads - 1) / kThreads) {
+    const uint32_t lane = threadIdx.x % a.lanes, c = (blockIdx.y * a.lanes + lane) * N;
+    const auto leave = [&](uint32_t first, uint32_t id, const float (&sum)[N]) {
+        const uint32_t row = a.list ? heads_before(a, first + 1) - 1 : id;
+        store_chunk<T>(a.out + (int64_t)row * a.out_row, c, a.width, packed<T>(sum, a.scale));
+        if (a.list && c == 0) a.list[row] = (int32_t)id;
+    };
+    const auto in_run = [&](uint64_t q, uint32_t id) {
+        return q < a.runs && q * a.run < n && id_at(a, (uint32_t)q * a.run) == id;
+    };
+    for (uint32_t k = threadIdx.x / 64; k < number; k += kJoinThreads / 64) {
+        const uint32_t first = found[k], id = id_at(a, first * a.run + a.run - 1), in_wave = threadIdx.x % 64;
+        const uint32_t more = __popcll(__ballot(in_run((uint64_t)first + 1 + in_wave, id)));
+        if (more == 64) {
+            if (in_wave == 0) large[atomicAdd(&larges, 1u)] = first;
+            continue;
+        }
+        const uint32_t groups = 64 / a.lanes, per = (more + groups) / groups, p0 = in_wave / a.lanes * per;
+        float sum[N];
+        add_parts<N>(a, first, min(p0, more + 1), min(p0 + per, more + 1), c, sum);
+        for (uint32_t g = 1; g < groups; g++)
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const float x = __shfl(sum[i], (in_wave + g * a.lanes) % 64);
+                if (in_wave < a.lanes) sum[i] += x;
+            }
+        if (in_wave < a.lanes && c < a.width) leave(first, id, sum);
+    }
+    __syncthreads();
+    const uint32_t group = threadIdx.x / a.lanes, groups = kJoinThreads / a.lanes;
+    for (uint32_t k = 0; k < larges; k++) {
+        const uint32_t first = large[k], id = id_at(a, first * a.run + a.run - 1);
+        // the last run that holds it, as many tried at once as there are threads
+        uint32_t last = first + 1, step = (a.runs - first + kJoinThreads - 1) / kJoinThreads;
+        for (;; step = (step + kJoinThreads - 1) / kJoinThreads) {
             if (threadIdx.x == 0) reach = 0;
             __syncthreads();
-            const uint64_t q = (uint64_t)last + (uint64_t)step * threadIdx.x;
-            if (q < a.runs && q * a.run < n && id_at(a, (uint32_t)q * a.run) == id) atomicMax(&reach, threadIdx.x);
+            if (in_run((uint64_t)last + (uint64_t)step * threadIdx.x, id)) atomicMax(&reach, threadIdx.x);
             __syncthreads();
             last += step * reach;
             __syncthreads();
             if (step == 1) break;
         }
-        // parts: the first run's second, then the others' first
         const uint32_t parts = last - first + 1, per = (parts + groups - 1) / groups;
-        const uint32_t p0 = group * per, p1 = min(p0 + per, parts);
         float sum[N];
-#pragma unroll
-        for (int i = 0; i < N; i++) sum[i] = 0.0f;
-        for (uint32_t p = p0; p < p1; p += U) {
-            float x[U][N];
-#pragma unroll
-            for (int u = 0; u < U; u++) {
-                const float *f = a.part + ((size_t)(first + p + u) * 2 + (p + u == 0)) * a.width;
-#pragma unroll
-                for (int i = 0; i < N; i++) x[u][i] = p + u < p1 && c + i < a.width ? f[c + i] : 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < U; u++)
-#pragma unroll
-                for (int i = 0; i < N; i++) sum[i] += x[u][i];
-        }
+        add_parts<N>(a, first, min(group * per, parts), min(group * per + per, parts), c, sum);
 #pragma unroll
         for (int i = 0; i < N; i++) sums[threadIdx.x][i] = sum[i];
         __syncthreads();
@@ -492,9 +562,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void join_parts(Sum
             for (uint32_t g = 1; g < groups; g++)
 #pragma unroll
                 for (int i = 0; i < N; i++) sum[i] += sums[g * a.lanes + lane][i];
-            const uint32_t row = a.list ? a.heads[first + 1] - 1 : id;
-            store_chunk<T>(a.out + (int64_t)row * a.out_row, c, a.width, packed<T>(sum, a.scale));
-            if (a.list && c == 0) a.list[row] = (int32_t)id;
+            leave(first, id, sum);
         }
         __syncthreads();
     }
@@ -516,14 +584,14 @@ void passes_of(uint32_t rows, uint32_t &passes, uint32_t &bits) {
 
 uint32_t run_of(uint32_t n) {
     uint32_t run = 16;
-    while (run < 256 && run < n / 16384) run *= 2;
+    while (run < 64 && run < n / 4096) run *= 2;
     return run;
 }
 
 size_t align16z(size_t n) { return (n + 15) & ~(size_t)15; }
 
 struct Work {                                              // places in the working memory
-    size_t pairs[2], hist, totals, valid, heads, part, all;
+    size_t pairs[2], hist, totals, valid, heads, blocks, part, all;
     uint32_t tiles, passes, bits, run, runs;
     Work(const nlb_lookup_call *c, bool listed) {
         passes_of(c->rows, passes, bits);
@@ -540,7 +608,8 @@ struct Work {                                              // places in the work
         hist = take(((size_t)tiles << bits) * 4);
         totals = take(4ull << bits);
         valid = take(4);
-        heads = take(listed ? ((size_t)runs + 1) * 4 : 0);
+        heads = take(listed ? (size_t)runs * 4 : 0);
+        blocks = take(listed ? ((runs + kBlock - 1) / kBlock + 1) * 4ull : 0);
         part = take((size_t)runs * 2 * c->width * 4);
         all = at;
     }
@@ -594,9 +663,9 @@ int sort(const nlb_lookup_call *c, const Work &w, uint8_t *work, const uint64_t 
         a.shift = p * w.bits;
         a.from = (const uint64_t *)(work + w.pairs[(p + 1) % 2]);
         a.to = (uint64_t *)(work + w.pairs[p % 2]);
-        int rc = enqueue(p ? count_digits<false> : count_digits<true>, w.tiles, kThreads, 0, s, a);
-        if (rc == NLB_OK) rc = enqueue(scan_digits, 1u << w.bits, kThreads, 0, s, a);
-        if (rc == NLB_OK) rc = enqueue(p ? scatter<false> : scatter<true>, w.tiles, kThreads, 0, s, a);
+        int rc = enqueue(p ? count_digits<false> : count_digits<true>, w.tiles, kSortThreads, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(scan_digits, ((1u << w.bits) + 15) / 16, 1024, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(p ? scatter<false> : scatter<true>, w.tiles, kSortThreads, 0, s, a);
         if (rc != NLB_OK) return rc;
         *sorted = a.to;
     }
@@ -655,6 +724,7 @@ extern "C" int nlb_lookup_backward(const nlb_lookup_call *c, const void *dout, i
     a.part = (float *)(m + w.part);
     a.list = list;
     a.heads = (uint32_t *)(m + w.heads);
+    a.blocks = (uint32_t *)(m + w.blocks);
     a.count = count;
     a.n = c->n;
     a.width = (uint32_t)c->width;
@@ -666,14 +736,14 @@ extern "C" int nlb_lookup_backward(const nlb_lookup_call *c, const void *dout, i
     a.scale = c->scale;
     if (c->n) rc = sort(c, w, m, &a.sorted, s);
     if (rc == NLB_OK && listed) {
-        if (c->n) rc = enqueue(count_heads, (w.runs + 15) / 16, kThreads, 0, s, a);
-        if (rc == NLB_OK) rc = enqueue(scan_heads, 1, 1024, 0, s, a);
+        if (c->n) rc = enqueue(count_heads, (w.runs + kBlock - 1) / kBlock, 1024, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(scan_blocks, 1, 1024, 0, s, a);
     }
     if (rc != NLB_OK || !c->n) return rc;
     const bool bf16 = c->dtype == NLB_DTYPE_BF16;
     const uint32_t groups = kThreads / a.lanes, columns = (chunks + a.lanes - 1) / a.lanes;
     rc = enqueue(bf16 ? sum_runs<__bf16> : sum_runs<float>, dim3((w.runs + groups - 1) / groups, columns), kThreads, 0, s, a);
     if (rc != NLB_OK) return rc;
-    return enqueue(bf16 ? join_parts<__bf16> : join_parts<float>, dim3((w.runs + kThreads - 1) / kThreads, columns),
-                   kThreads, 0, s, a);
+    return enqueue(bf16 ? join_parts<__bf16> : join_parts<float>, dim3((w.runs + kLook - 1) / kLook, columns),
+                   kJoinThreads, 0, s, a);
 }
