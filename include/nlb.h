@@ -646,7 +646,7 @@ int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq
  * overlap each other.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
 #define NLB_SCAN_MAX_WIDTH 65536
 #define NLB_SCAN_MAX_ROWS 2147480000u
-#define NLB_SCAN_STATE_ROWS 64
+#define NLB_SCAN_STATE_ROWS 32
 
 typedef struct nlb_scan_rows {
     void *data;

@@ -37,7 +37,7 @@ RNN_FORM_NONE, RNN_FORM_TILED, RNN_FORM_WEIGHT_STATIONARY = 0, 1, 2
 ATT_MAX_DIM, ATT_MAX_HEADS, ATT_MAX_BUCKETS = 128, 256, 64
 NORM_MAX_WIDTH = 8192
 LOOKUP_MAX_WIDTH = 65536
-SCAN_MAX_WIDTH, SCAN_MAX_ROWS, SCAN_STATE_ROWS = 65536, 2147480000, 64
+SCAN_MAX_WIDTH, SCAN_MAX_ROWS, SCAN_STATE_ROWS = 65536, 2147480000, 32
 EID_LAST_BATCH = 2**64 - 1   # first_eid of rnn_update: the links inserted last (device count)
 
 

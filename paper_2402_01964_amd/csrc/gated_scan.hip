@@ -8,7 +8,7 @@
 // rows, in which a sequence's first row forgets what came before it, so that
 // neither their number nor their lengths matter to how the work is split.
 //   A thread holds 16 (backward: 8) rows of its channels in registers, a workgroup's
-// 8 wavefronts stand one below the other: maps of those rows are joined over the
+// 4 wavefronts stand one below the other: maps of those rows are joined over the
 // workgroup through LDS, then every thread walks its rows again, in registers.
 // A workgroup walks a chunk of the rows tile by tile.  Where there are several
 // chunks, a first launch makes their maps (it reads x and g once more, but only
@@ -23,8 +23,8 @@ namespace {
 
 typedef uint32_t u32_any __attribute__((aligned(2)));
 
-constexpr int kThreads = 512, kRows = 16, kRowsBack = 8;   // rows a thread holds
-constexpr uint32_t kStateRows = NLB_SCAN_STATE_ROWS;
+constexpr int kThreads = 256, kRows = 16, kRowsBack = 8;   // rows a thread holds
+constexpr uint32_t kStateRows = NLB_SCAN_STATE_ROWS, kChunks = 1024;
 
 struct Scan {
     const uint8_t *x, *g, *dh;
@@ -83,16 +83,50 @@ template <> struct Piece<OneBf16> {
     __device__ __forceinline__ void store(uint8_t *row, const float (&f)[1]) const { *(__bf16 *)row = (__bf16)f[0]; }
 };
 
-// z = sigmoid(g) = 1 / (1 + e) and 1 - z = e z with e = exp(-g), each with its
-// own relative error of some 2^-21.  e = 2^t (1 + lo) where t = -g / ln 2 is
-// rounded and lo = -g - t ln 2 what that left.  Gates beyond 80 in magnitude
-// count as 80 (e up to 2^115).
-__device__ __forceinline__ void gate(float g, float &z, float &y) {
-    g = fabsf(g) > 80.0f ? copysignf(80.0f, g) : g;           // (a NaN stays one)
+// Gates beyond 80 in magnitude become 80 (NaN stays): few calls have one, so a
+// wavefront looks at the largest of its words' magnitudes first.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <typename T, int R> __device__ __forceinline__ void limit(uint32_t (&raw)[R]) {
+    if constexpr (std::is_same<T, float>::value) {
+        float most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < R; k++) most = fmaxf(most, fabsf(__uint_as_float(raw[k])));
+        if (!__any(most > 80.0f)) return;
+#pragma unroll
+        for (int k = 0; k < R; k++) {
+            const float g = __uint_as_float(raw[k]);
+            if (fabsf(g) > 80.0f) raw[k] = __float_as_uint(copysignf(80.0f, g));
+        }
+    } else {
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int k = 0; k < R; k++) {
+            const uint32_t w = raw[k] & 0x7FFF7FFFu;
+            u16x2 v;
+            __builtin_memcpy(&v, &w, 4);
+            most = __builtin_elementwise_max(most, v);
+        }
+        if (!__any(most[0] > 0x42A0 || most[1] > 0x42A0)) return;
+#pragma unroll
+        for (int k = 0; k < R; k++)
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) {
+                const uint32_t m = raw[k] >> i & 0x7FFF;
+                if (m > 0x42A0 && m <= 0x7F80) raw[k] = (raw[k] & ~(0x7FFFu << i)) | 0x42A0u << i;
+            }
+    }
+}
+
+// z = sigmoid(g) = 1 / (1 + e) and 1 - z = e z with e = exp(-g) = 2^t, t = -g / ln
+// 2, |g| up to 80.  EXACT: e (1 + lo) with what t's rounding left, lo = -g - t ln 2,
+// so that both have relative errors of some 2^-21.  Without it, for bf16 gates, e
+// and 1 - z are off by |g| 2^-24 more of themselves (z by less than 2^-24: where e
+// is off, z is near 1): below the rounding of what they go into, and two operations
+// of 14 less.
+template <bool EXACT> __device__ __forceinline__ void gate(float g, float &z, float &y) {
     const float t = g * -1.44269504f;
-    const float lo = fmaf(t, -0.693147181f, -g);
     float e = __builtin_amdgcn_exp2f(t);
-    e = fmaf(e, lo, e);
+    if constexpr (EXACT) e = fmaf(e, fmaf(t, -0.693147181f, -g), e);
     z = __builtin_amdgcn_rcpf(1.0f + e);
     y = e * z;
 }
@@ -264,6 +298,7 @@ __device__ __forceinline__ void load_rows(const uint8_t *p, int64_t stride, uint
     } else {
 #pragma unroll
         for (int i = 0; i < R; i++) raw[i] = piece.load(p + (int64_t)min(max(r + i, at.first), at.last - 1) * stride);
+        asm volatile("");                                  // (keeps the two kinds of loads apart)
     }
 }
 template <typename T, int R, bool ONE>
@@ -320,6 +355,7 @@ __device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 template <typename T, bool ONE, bool APPLY>
 __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
     constexpr int C = Piece<T>::n, R = kRows;
+    constexpr bool EXACT = std::is_same<T, float>::value;
     __shared__ Edges edges;
     __shared__ Map lds[kThreads / 64][64 * C];
     const Place<R, ONE> at(a, C);
@@ -361,6 +397,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
             begins = at.word(edges.begins);
             if constexpr (APPLY) ends = at.word(edges.ends);
         }
+        limit<T>(rg);
         float z[APPLY ? R : 1][C], y[APPLY ? R : 1][C];
         Map own[C], before[C], all[C];
 #pragma unroll
@@ -374,7 +411,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
             piece.unpack(rg[k], g);
 #pragma unroll
             for (int i = 0; i < C; i++) {
-                gate(g[i], zk[i], yk[i]);
+                gate<EXACT>(g[i], zk[i], yk[i]);
                 yk[i] *= x[i];
                 if (!whole && !at.there(r + k)) zk[i] = 1.0f, yk[i] = 0.0f;
             }
@@ -443,6 +480,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
 template <typename T, bool ONE, bool APPLY>
 __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
     constexpr int C = Piece<T>::n, R = kRowsBack;
+    constexpr bool EXACT = std::is_same<T, float>::value;
     __shared__ Edges edges;
     __shared__ Map lds[2][kThreads / 64][64 * C];
     const Place<R, ONE> at(a, C);
@@ -488,6 +526,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
             ends = at.word(edges.ends);
             if constexpr (APPLY) begins = at.word(edges.begins);
         }
+        limit<T>(rg);
         float z[R][C], y[R][C];
         Map own[C], before[C], all[C];
 #pragma unroll
@@ -495,7 +534,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
             float g[C];
             piece.unpack(rg[k], g);
 #pragma unroll
-            for (int i = 0; i < C; i++) gate(g[i], z[k][i], y[k][i]);
+            for (int i = 0; i < C; i++) gate<EXACT>(g[i], z[k][i], y[k][i]);
             if (k % 4 == 3) phase();
         }
         if (!whole) {
@@ -617,6 +656,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
 // One row a sequence, as it comes: a thread a few channels of one row.
 template <typename T> __global__ __launch_bounds__(256) void single_rows(Scan a) {
     constexpr int C = Piece<T>::n;
+    constexpr bool EXACT = std::is_same<T, float>::value;
     const uint32_t pieces = (a.width + C - 1) / C;
     const uint64_t all = (uint64_t)a.rows * pieces, step = (uint64_t)gridDim.x * 256;
     for (uint64_t l = (uint64_t)blockIdx.x * 256 + threadIdx.x; l < all; l += step) {
@@ -624,12 +664,14 @@ template <typename T> __global__ __launch_bounds__(256) void single_rows(Scan a)
         const Piece<T> piece(c, a.width);
         float x[C], g[C], h[C];
         piece.unpack(piece.load(a.x + (int64_t)r * a.x_row), x);
-        piece.unpack(piece.load(a.g + (int64_t)r * a.g_row), g);
+        uint32_t w[1] = {piece.load(a.g + (int64_t)r * a.g_row)};
+        limit<T>(w);
+        piece.unpack(w[0], g);
         load_state(a, a.h0, r, c, h);
 #pragma unroll
         for (int i = 0; i < C; i++) {
             float z, y;
-            gate(g[i], z, y);
+            gate<EXACT>(g[i], z, y);
             h[i] = fmaf(z, h[i], y * x[i]);
         }
         piece.store(a.h + (int64_t)r * a.h_row, h);
@@ -690,7 +732,7 @@ void split(Scan &a, int n) {
     a.lanes = 8;
     while (a.lanes < 64 && a.lanes * n < a.width) a.lanes *= 2;
     const uint32_t tile = kThreads / a.lanes * kRows, tiles = (a.rows + tile - 1) / tile;
-    const uint32_t groups = groups_of(a, n), most = groups < 1024 ? 1024 / groups : 1;
+    const uint32_t groups = groups_of(a, n), most = groups < kChunks ? kChunks / groups : 1;
     const uint32_t per = (tiles + most - 1) / most;
     a.chunk_rows = per * tile;
     a.chunks = per ? (tiles + per - 1) / per : 0;
