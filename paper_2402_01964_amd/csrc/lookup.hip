@@ -19,8 +19,10 @@ namespace {
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kThreads = 256;
-constexpr int kSortThreads = 512, kItems = 8, kWaves = kSortThreads / 64;
-constexpr uint32_t kTile = kSortThreads * kItems;          // entries a workgroup sorts
+constexpr int kSortThreads = 512, kWaves = kSortThreads / 64;
+// Entries that a workgroup sorts: 8 a thread, 2 where that leaves CUs idle (a
+// pass of few tiles takes as long as one does: 240 000 ids 11 us with 8).
+constexpr uint32_t tile_of(uint32_t n) { return kSortThreads * (n < 1u << 20 ? 2 : 8); }
 constexpr uint32_t kMaxBits = 9, kMaxDigits = 1u << kMaxBits;
 
 template <typename T> struct Chunk { static constexpr int n = 16 / sizeof(T); };
@@ -147,7 +149,8 @@ __device__ __forceinline__ uint32_t digit_of(const Sort &a, uint64_t e) {
 }
 
 // How many of a tile's entries have each digit.
-template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void count_digits(Sort a) {
+template <bool FIRST, int kItems> __global__ __launch_bounds__(kSortThreads) void count_digits(Sort a) {
+    constexpr uint32_t kTile = kSortThreads * kItems;
     __shared__ uint32_t count[kMaxDigits];
     const uint32_t digits = 1u << a.bits, n = FIRST ? a.n : *a.valid;
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) count[d] = 0;
@@ -225,7 +228,8 @@ __global__ __launch_bounds__(1024) void scan_digits(Sort a) {
 // Each entry of a tile to its place: behind all of lower digits, the earlier
 // tiles' of its own and the earlier of its own in the tile.  The tile is put in
 // order in LDS first, so that neighbours go out together.
-template <bool FIRST> __global__ __launch_bounds__(kSortThreads) void scatter(Sort a) {
+template <bool FIRST, int kItems> __global__ __launch_bounds__(kSortThreads) void scatter(Sort a) {
+    constexpr uint32_t kTile = kSortThreads * kItems;
     __shared__ uint64_t items[kTile];
     __shared__ uint16_t waves[kWaves][kMaxDigits];
     __shared__ uint32_t start[kMaxDigits], base[kMaxDigits], lds[kWaves];
@@ -425,16 +429,20 @@ template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums 
             slot++;
         }
     };
+    uint64_t e[U], ahead[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) ahead[u] = a.sorted[min(i + u, stop - 1)];
     for (; i < stop; i += U) {
-        uint64_t e[U];
         u32x4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; u++) e[u] = a.sorted[min(i + u, stop - 1)];
+        for (int u = 0; u < U; u++) e[u] = ahead[u];
 #pragma unroll
         for (int u = 0; u < U; u++) {
             x[u] = u32x4{0, 0, 0, 0};
             if (i + u < stop && c < a.width) x[u] = load_chunk<T>(a.dout + (int64_t)(uint32_t)e[u] * a.dout_row, c, a.width);
         }
+#pragma unroll
+        for (int u = 0; u < U; u++) ahead[u] = a.sorted[min(i + U + u, stop - 1)];
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const uint32_t now = (uint32_t)(e[u] >> 32);
@@ -584,7 +592,7 @@ void passes_of(uint32_t rows, uint32_t &passes, uint32_t &bits) {
 
 uint32_t run_of(uint32_t n) {
     uint32_t run = 16;
-    while (run < 64 && run < n / 4096) run *= 2;
+    while (run < 64 && run < n / 8192) run *= 2;
     return run;
 }
 
@@ -595,7 +603,7 @@ struct Work {                                              // places in the work
     uint32_t tiles, passes, bits, run, runs;
     Work(const nlb_lookup_call *c, bool listed) {
         passes_of(c->rows, passes, bits);
-        tiles = (uint32_t)(((uint64_t)c->n + kTile - 1) / kTile);
+        tiles = (uint32_t)(((uint64_t)c->n + tile_of(c->n) - 1) / tile_of(c->n));
         run = run_of(c->n);
         runs = (uint32_t)(((uint64_t)c->n + run - 1) / run);
         size_t at = 0;
@@ -649,7 +657,7 @@ template <bool FILL> int copy(const Rows &a, int32_t dtype, hipStream_t s) {
 }
 
 // Sorts; *sorted is where the pairs end up.
-int sort(const nlb_lookup_call *c, const Work &w, uint8_t *work, const uint64_t **sorted, hipStream_t s) {
+template <int ITEMS> int sort(const nlb_lookup_call *c, const Work &w, uint8_t *work, const uint64_t **sorted, hipStream_t s) {
     Sort a = {};
     a.ids = c->ids;
     a.hist = (uint32_t *)(work + w.hist);
@@ -663,9 +671,9 @@ int sort(const nlb_lookup_call *c, const Work &w, uint8_t *work, const uint64_t 
         a.shift = p * w.bits;
         a.from = (const uint64_t *)(work + w.pairs[(p + 1) % 2]);
         a.to = (uint64_t *)(work + w.pairs[p % 2]);
-        int rc = enqueue(p ? count_digits<false> : count_digits<true>, w.tiles, kSortThreads, 0, s, a);
+        int rc = enqueue(p ? count_digits<false, ITEMS> : count_digits<true, ITEMS>, w.tiles, kSortThreads, 0, s, a);
         if (rc == NLB_OK) rc = enqueue(scan_digits, ((1u << w.bits) + 15) / 16, 1024, 0, s, a);
-        if (rc == NLB_OK) rc = enqueue(p ? scatter<false> : scatter<true>, w.tiles, kSortThreads, 0, s, a);
+        if (rc == NLB_OK) rc = enqueue(p ? scatter<false, ITEMS> : scatter<true, ITEMS>, w.tiles, kSortThreads, 0, s, a);
         if (rc != NLB_OK) return rc;
         *sorted = a.to;
     }
@@ -734,7 +742,7 @@ extern "C" int nlb_lookup_backward(const nlb_lookup_call *c, const void *dout, i
     a.run = w.run;
     a.runs = w.runs;
     a.scale = c->scale;
-    if (c->n) rc = sort(c, w, m, &a.sorted, s);
+    if (c->n) rc = tile_of(c->n) == 2 * kSortThreads ? sort<2>(c, w, m, &a.sorted, s) : sort<8>(c, w, m, &a.sorted, s);
     if (rc == NLB_OK && listed) {
         if (c->n) rc = enqueue(count_heads, (w.runs + kBlock - 1) / kBlock, 1024, 0, s, a);
         if (rc == NLB_OK) rc = enqueue(scan_blocks, 1, 1024, 0, s, a);

@@ -52,27 +52,43 @@ __device__ __forceinline__ void sincos_turns(double turns, float &s, float &c) {
     c = (k + 1) & 2 ? -b : b;
 }
 
-// A lane's pairs: V of them, from V j on where the halves are whole chunks
-// (VEC), else every L-th.  Pair p is the values lo(p) and hi(p) of a head; the
-// last pair behind the rotated ones may lack the second.
-template <typename T, int L, bool VEC> struct Pairs {
+// A lane's pairs: V of them, side by side where both halves can be read in whole
+// chunks (kWhole; kOverlap: where the last chunk of the rotated pairs, or of those
+// behind them, is not full, it is moved back over the one before, and the first
+// `skip` of its pairs belong to that), else every L-th (kStrided).  Pair p is the
+// values lo(p) and hi(p) of a head; the last pair behind the rotated ones may lack
+// the second.
+constexpr int kWhole = 0, kOverlap = 1, kStrided = 2;
+template <typename T, int L, int MODE> struct Pairs {
     static constexpr int V = 16 / sizeof(T);
-    uint32_t j;
-    __device__ __forceinline__ uint32_t pair(int i) const { return VEC ? j * V + i : i * L + j; }
+    uint32_t j, p0, skip;
+    bool some;
+    __device__ __forceinline__ Pairs(const Rotate &a, uint32_t lane) : j(lane), p0(0), skip(0), some(true) {
+        if constexpr (MODE != kStrided) {
+            const uint32_t turned = (a.m + V - 1) / V, in = j < turned ? j : j - turned;
+            const uint32_t n = j < turned ? a.m : a.rest;
+            some = in * V < n;
+            p0 = in * V;
+            if (some && p0 + V > n) skip = p0 + V - n, p0 = n - V;
+            p0 += j < turned ? 0 : a.m;
+        }
+    }
+    __device__ __forceinline__ uint32_t pair(int i) const { return MODE != kStrided ? p0 + i : i * L + j; }
     static __device__ __forceinline__ uint32_t lo(const Rotate &a, uint32_t p) { return p < a.m ? p : a.m + p; }
     static __device__ __forceinline__ uint32_t hi(const Rotate &a, uint32_t p) {
         return p < a.m ? a.m + p : a.m + a.rest + p;
     }
-    __device__ __forceinline__ bool has_lo(const Rotate &a, uint32_t p) const { return p < a.m + a.rest; }
+    // whether pair(i) is this lane's to add up
+    __device__ __forceinline__ bool own(int i) const { return MODE != kOverlap || i >= (int)skip; }
+    __device__ __forceinline__ bool has_lo(const Rotate &a, uint32_t p) const { return some && p < a.m + a.rest; }
     __device__ __forceinline__ bool has_hi(const Rotate &a, uint32_t p) const {
-        return p < a.m + a.rest && hi(a, p) < a.dim;
+        return some && p < a.m + a.rest && hi(a, p) < a.dim;
     }
     // the values of one half, HI or not
     template <bool HI> __device__ __forceinline__ void load(const Rotate &a, const uint8_t *x, u32x4 &raw) const {
         raw = u32x4{0, 0, 0, 0};
-        if constexpr (VEC) {
-            const uint32_t p = j * V;
-            if (p < a.m + a.rest) raw = *(const u32x4_any *)(x + (HI ? hi(a, p) : lo(a, p)) * sizeof(T));
+        if constexpr (MODE != kStrided) {
+            if (some) raw = *(const u32x4_any *)(x + (HI ? hi(a, p0) : lo(a, p0)) * sizeof(T));
         } else {
 #pragma unroll
             for (int i = 0; i < V; i++) {
@@ -95,15 +111,16 @@ template <typename T, int L, bool VEC> struct Pairs {
             }
         }
     }
+    // (pairs of two chunks are written twice, the same values: a head's lanes are
+    // in one wavefront, and all have read before any writes)
     template <bool HI> __device__ __forceinline__ void store(const Rotate &a, uint8_t *y, const float (&f)[V]) const {
         T v[V];
 #pragma unroll
         for (int i = 0; i < V; i++) v[i] = (T)f[i];
-        if constexpr (VEC) {
-            const uint32_t p = j * V;
+        if constexpr (MODE != kStrided) {
             u32x4 u;
             __builtin_memcpy(&u, v, 16);
-            if (p < a.m + a.rest) *(u32x4_any *)(y + (HI ? hi(a, p) : lo(a, p)) * sizeof(T)) = u;
+            if (some) *(u32x4_any *)(y + (HI ? hi(a, p0) : lo(a, p0)) * sizeof(T)) = u;
         } else {
 #pragma unroll
             for (int i = 0; i < V; i++) {
@@ -138,14 +155,14 @@ template <int L> __device__ __forceinline__ float head_sum(float x) {
 
 // A task is a row's `per` heads (the last task's may be fewer); L lanes take
 // one, the workgroup's groups of lanes tasks side by side.
-template <typename T, int L, bool VEC, bool BACK>
+template <typename T, int L, int MODE, bool BACK>
 __global__ __launch_bounds__(kThreads) void rotate_heads(Rotate a) {
-    typedef Pairs<T, L, VEC> P;
+    typedef Pairs<T, L, MODE> P;
     constexpr int V = P::V, U = BACK ? 2 : 4;              // heads whose loads are in flight at once
     const uint32_t is_k = blockIdx.x >= a.side[0].blocks;
     const Side &s = a.side[is_k];
     const uint32_t block = blockIdx.x - (is_k ? a.side[0].blocks : 0);
-    const P pairs = {threadIdx.x % L};
+    const P pairs(a, threadIdx.x % L);
     const float inv = 1.0f / a.dim;
     float wlo[V], whi[V];
     pairs.template weights<false>(a, s.w, 1.0f, wlo);
@@ -200,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void rotate_heads(Rotate a) {
                 P::unpack(xl[u], lo);
                 P::unpack(xh[u], hi);
 #pragma unroll
-                for (int i = 0; i < V; i++) sq = fmaf(hi[i], hi[i], fmaf(lo[i], lo[i], sq));
+                for (int i = 0; i < V; i++) sq += pairs.own(i) ? fmaf(hi[i], hi[i], lo[i] * lo[i]) : 0.0f;
                 float ol[V], oh[V];
                 const float r = __builtin_amdgcn_rsqf(fmaf(head_sum<L>(sq), inv, a.eps));
                 if constexpr (!BACK) {
@@ -220,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void rotate_heads(Rotate a) {
                         dwlo[i] = fmaf(dl, lo[i] * r, dwlo[i]);
                         dwhi[i] = fmaf(dh, hi[i] * r, dwhi[i]);
                         ol[i] = dl * wlo[i], oh[i] = dh * whi[i];
-                        sg = fmaf(oh[i], hi[i], fmaf(ol[i], lo[i], sg));
+                        sg += pairs.own(i) ? fmaf(oh[i], hi[i], ol[i] * lo[i]) : 0.0f;
                     }
                     const float mean = head_sum<L>(sg) * inv * r * r;
 #pragma unroll
@@ -246,9 +263,9 @@ __global__ __launch_bounds__(kThreads) void rotate_heads(Rotate a) {
     __syncthreads();
     for (uint32_t k = threadIdx.x; k < 2 * L * V; k += kThreads) {
         const uint32_t half = k / (L * V), at = k % (L * V);
-        const P other = {at % L};
+        const P other(a, at % L);
         const uint32_t p = other.pair(at / L);
-        if (half ? !other.has_hi(a, p) : !other.has_lo(a, p)) continue;
+        if (!other.own(at / L) || (half ? !other.has_hi(a, p) : !other.has_lo(a, p))) continue;
         float x = 0.0f;
 #pragma unroll 8
         for (int g = 0; g < G; g++) x += sums[half][g][at];
@@ -264,19 +281,32 @@ __global__ __launch_bounds__(1024) void sum_shares(const float *part, uint32_t q
     const uint32_t at = threadIdx.x / 16, c = blockIdx.x * 16 + threadIdx.x % 16;
     const uint32_t first = blockIdx.y ? q_blocks : 0, n = blockIdx.y ? k_blocks : q_blocks;
     double x = 0.0;
-    if (c < dim)
-        for (uint32_t i = at; i < n; i += 64) x += (double)part[(size_t)(first + i) * dim + c];
+    for (uint32_t i = at; i < n && c < dim; i += 512) {     // eight loads in flight
+        float v[8];
+#pragma unroll
+        for (uint32_t u = 0; u < 8; u++) v[u] = i + 64 * u < n ? part[(size_t)(first + i + 64 * u) * dim + c] : 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; u++) x += (double)v[u];
+    }
     sums[at][threadIdx.x % 16] = x;
     __syncthreads();
     float *dw = blockIdx.y ? dwk : dwq;
     if (at || c >= dim || !dw) return;
+#pragma unroll 9
     for (int i = 1; i < 64; i++) x += sums[i][threadIdx.x];
     dw[c] = (float)x;
 }
 
 // ---------------------------------------------------------------- host
+template <typename T> int mode_of(const Rotate &a) {
+    const uint32_t v = 16 / sizeof(T), rest = a.dim - 2 * a.m;
+    if (a.m % v == 0 && rest % (2 * v) == 0) return kWhole;
+    // half a chunk's lanes idle at most, and pairs of both halves
+    return rest % 2 == 0 && (a.m == 0 || a.m >= v) && (rest == 0 || rest >= 2 * v) ? kOverlap : kStrided;
+}
 template <typename T> uint32_t lanes_of(const Rotate &a) {
-    const uint32_t need = (a.m + a.rest + 16 / sizeof(T) - 1) / (16 / sizeof(T));
+    const uint32_t v = 16 / sizeof(T);
+    const uint32_t need = mode_of<T>(a) == kStrided ? (a.m + a.rest + v - 1) / v : (a.m + v - 1) / v + (a.rest + v - 1) / v;
     uint32_t l = 2;
     while (l < need) l *= 2;
     return l;
@@ -344,22 +374,26 @@ int fill(const nlb_rotate_call *c, Rotate &a) {
 
 size_t work_of(const Rotate &a) { return (size_t)(a.side[0].blocks + a.side[1].blocks) * a.dim * 4; }
 
-template <typename T, bool BACK, bool VEC> int launch(const Rotate &a, hipStream_t s) {
+template <typename T, bool BACK, int MODE> int launch(const Rotate &a, hipStream_t s) {
     const uint32_t blocks = a.side[0].blocks + a.side[1].blocks;
     switch (lanes_of<T>(a)) {
-        case 2: return enqueue(rotate_heads<T, 2, VEC, BACK>, blocks, kThreads, 0, s, a);
-        case 4: return enqueue(rotate_heads<T, 4, VEC, BACK>, blocks, kThreads, 0, s, a);
-        case 8: return enqueue(rotate_heads<T, 8, VEC, BACK>, blocks, kThreads, 0, s, a);
-        case 16: if constexpr (sizeof(T) == 4) return enqueue(rotate_heads<T, 16, VEC, BACK>, blocks, kThreads, 0, s, a);
+        case 2: return enqueue(rotate_heads<T, 2, MODE, BACK>, blocks, kThreads, 0, s, a);
+        case 4: return enqueue(rotate_heads<T, 4, MODE, BACK>, blocks, kThreads, 0, s, a);
+        case 8: return enqueue(rotate_heads<T, 8, MODE, BACK>, blocks, kThreads, 0, s, a);
+        case 16: return enqueue(rotate_heads<T, 16, MODE, BACK>, blocks, kThreads, 0, s, a);
     }
     return NLB_EINVAL;
 }
+template <typename T, bool BACK> int launch(const Rotate &a, hipStream_t s) {
+    switch (mode_of<T>(a)) {
+        case kWhole: return launch<T, BACK, kWhole>(a, s);
+        case kOverlap: return launch<T, BACK, kOverlap>(a, s);
+    }
+    return launch<T, BACK, kStrided>(a, s);
+}
 template <bool BACK> int launch(const Rotate &a, int32_t dtype, hipStream_t s) {
     if (!(a.side[0].blocks + a.side[1].blocks)) return NLB_OK;
-    const uint32_t v = dtype == NLB_DTYPE_BF16 ? 8 : 4;
-    const bool vec = a.m % v == 0 && (a.dim - 2 * a.m) % (2 * v) == 0;
-    if (dtype == NLB_DTYPE_BF16) return vec ? launch<__bf16, BACK, true>(a, s) : launch<__bf16, BACK, false>(a, s);
-    return vec ? launch<float, BACK, true>(a, s) : launch<float, BACK, false>(a, s);
+    return dtype == NLB_DTYPE_BF16 ? launch<__bf16, BACK>(a, s) : launch<float, BACK>(a, s);
 }
 
 }  // namespace
