@@ -35,7 +35,7 @@ struct Scan {
     float *last, *dh0, *states;
     float *maps, *into;                                    // [chunks][2][width], [chunks][width]
     uint32_t rows, width, batch, len;
-    uint32_t lanes, chunk_rows, chunks;
+    uint32_t lanes, chunk_rows, chunks, groups;            // lanes of a row, groups of them for all its channels
 };
 
 // A lane's channels of a row: one fp32 value, or two bf16 ones in a word.  The
@@ -148,7 +148,7 @@ constexpr float kForgets = -0.0f;
 struct Edges {                                             // of a tile's sequences, in LDS
     uint32_t begins[kThreads / 8], ends[kThreads / 8];     // a bit for each row, a word for a thread's rows
     int32_t begin[kThreads / 8 * kRows], end[kThreads / 8 * kRows];   // their sequences
-    uint32_t next;
+    uint32_t next, s[kThreads], e[kThreads];               // the next tile's sequence; rows of those looked at
 };
 
 // The first row of sequence b, the rows' end for b = batch.
@@ -186,37 +186,51 @@ template <int R, bool BACK> struct Cursor {
         e = __builtin_amdgcn_readfirstlane(start_of(a, b + 1));
     }
     __device__ __forceinline__ bool plain(uint32_t r0, uint32_t n) const { return s < r0 && e > r0 + n; }
-    // this thread's share of the sequences that may have edges in the tile
-    __device__ __forceinline__ void look(const Scan &a, uint32_t &i, uint32_t &is, uint32_t &ie) const {
-        i = BACK ? b - threadIdx.x : b + threadIdx.x;
-        is = ie = 0;
-        if (i < a.batch) is = start_of(a, i), ie = start_of(a, i + 1);
+    // This thread's share of the sequences that may have edges in the tile, a
+    // workgroup of them from `from` on, and the last of these.
+    struct Look {
+        uint32_t from, i, s, e, last;
+        bool more;
+    };
+    __device__ __forceinline__ void look(const Scan &a, uint32_t from, Look &l) const {
+        l.from = from;
+        l.i = BACK ? from - threadIdx.x : from + threadIdx.x;
+        l.s = l.e = 0;
+        if (l.i < a.batch) l.s = start_of(a, l.i), l.e = start_of(a, l.i + 1);
+        l.more = from < a.batch && (BACK ? from >= kThreads - 1 : from + (kThreads - 1) < a.batch);
+        l.last = l.more ? start_of(a, BACK ? from - (kThreads - 1) : from + (kThreads - 1)) : 0;
     }
     // Fills `edges`, whose words are 0 and whose `next` is 0, for the rows r0 ..
     // r0 + n - 1, and moves on to the next tile; ends with a barrier.
-    __device__ __forceinline__ void find(const Scan &a, uint32_t r0, uint32_t n, uint32_t i, uint32_t is, uint32_t ie,
-                                         Edges &edges) {
+    __device__ __forceinline__ void find(const Scan &a, uint32_t r0, uint32_t n, Look &l, Edges &edges) {
         for (;;) {
-            bool more = false;
-            if (i < a.batch) {
-                if (is < ie && is - r0 < n) {
-                    atomicOr(&edges.begins[(is - r0) / R], 1u << ((is - r0) % R));
-                    edges.begin[is - r0] = i;
+            if (l.i < a.batch) {
+                if (l.s < l.e && l.s - r0 < n) {
+                    atomicOr(&edges.begins[(l.s - r0) / R], 1u << ((l.s - r0) % R));
+                    edges.begin[l.s - r0] = l.i;
                 }
-                if (is < ie && ie - 1 - r0 < n) {
-                    atomicOr(&edges.ends[(ie - 1 - r0) / R], 1u << ((ie - 1 - r0) % R));
-                    edges.end[ie - 1 - r0] = i;
+                if (l.s < l.e && l.e - 1 - r0 < n) {
+                    atomicOr(&edges.ends[(l.e - 1 - r0) / R], 1u << ((l.e - 1 - r0) % R));
+                    edges.end[l.e - 1 - r0] = l.i;
                 }
-                // where the next tile begins to look, and whether that is further on
-                if (BACK ? is < r0 : is <= r0 + n) atomicMax(&edges.next, i);
-                more = threadIdx.x == kThreads - 1 && (BACK ? is >= r0 : is < r0 + n);
+                // where the next tile begins to look
+                if (BACK ? l.s < r0 : l.s <= r0 + n) atomicMax(&edges.next, l.i);
+                edges.s[threadIdx.x] = l.s;
+                edges.e[threadIdx.x] = l.e;
             }
-            if (!__syncthreads_or(more)) break;
-            i = BACK ? i - kThreads : i + kThreads;
-            is = ie = 0;
-            if (i < a.batch) is = start_of(a, i), ie = start_of(a, i + 1);
+            __syncthreads();
+            if (!(l.more && (BACK ? l.last >= r0 : l.last < r0 + n))) break;
+            look(a, BACK ? l.from - kThreads : l.from + kThreads, l);
+            if (l.from >= a.batch) break;                  // (BACK: below the first)
         }
-        at(a, __builtin_amdgcn_readfirstlane(edges.next));
+        b = __builtin_amdgcn_readfirstlane(edges.next);
+        const uint32_t at_ = BACK ? l.from - b : b - l.from;
+        if (l.from < a.batch && at_ < kThreads) {
+            s = __builtin_amdgcn_readfirstlane(edges.s[at_]);
+            e = __builtin_amdgcn_readfirstlane(edges.e[at_]);
+        } else {
+            at(a, b);
+        }
     }
 };
 
@@ -267,12 +281,18 @@ __device__ __forceinline__ void join(const Map (&own)[C], uint32_t lanes, Map (&
 
 // Where a thread's rows and channels are.  ONE: a wavefront holds one stretch
 // of rows, so that rows and what is asked of them are the wavefront's.
+//   The groups of a chunk's channels are eight workgroups apart, so that the same
+// XCD takes them, side by side: rows that do not begin at a cache line share
+// lines between groups (288 654 rows of 100 fp32 values, a training step: 385 us
+// with the groups one after the other, 366 so).
 template <int R, bool ONE> struct Place {
-    uint32_t sub, c, tile;                                 // its stretch in a tile, its first channel, rows of a tile
+    uint32_t chunk, sub, c, tile;                          // its stretch in a tile, its first channel, rows of a tile
     uint32_t first, last;                                  // rows that sequences have
     __device__ __forceinline__ Place(const Scan &a, int n) {
+        const uint32_t in = blockIdx.x % (8 * a.groups);
+        chunk = blockIdx.x / (8 * a.groups) * 8 + in % 8;
         sub = ONE ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / a.lanes;
-        c = (blockIdx.y * a.lanes + threadIdx.x % a.lanes) * n;
+        c = (in / 8 * a.lanes + threadIdx.x % a.lanes) * n;
         tile = kThreads / a.lanes * R;
         first = __builtin_amdgcn_readfirstlane(start_of(a, 0));
         last = __builtin_amdgcn_readfirstlane(start_of(a, a.batch));
@@ -330,9 +350,10 @@ __device__ __forceinline__ void store_state(const Scan &a, float *p, uint32_t b,
 }
 
 // Sequences without rows, which no tile holds: their states go through.
-template <int C> __device__ __forceinline__ void pass_on(const Scan &a, const float *from, float *to, uint32_t c) {
+template <int C>
+__device__ __forceinline__ void pass_on(const Scan &a, const float *from, float *to, uint32_t chunk, uint32_t c) {
     if (!to || (!a.start && a.len)) return;
-    for (uint32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    for (uint32_t b = chunk; b < a.batch; b += max(a.chunks, 1u)) {
         if (start_of(a, b) < start_of(a, b + 1) || threadIdx.x >= a.lanes) continue;
         float f[C];
         load_state(a, from, b, c, f);
@@ -360,10 +381,11 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
     __shared__ Map lds[kThreads / 64][64 * C];
     const Place<R, ONE> at(a, C);
     const Piece<T> piece(at.c, a.width);
-    const uint32_t from = blockIdx.x * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
+    if (at.chunk >= max(a.chunks, 1u)) return;
+    const uint32_t from = at.chunk * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
     float state[C];
     Map chunk[C];
-    load_state(a, APPLY ? a.into : nullptr, blockIdx.x, at.c, state);
+    load_state(a, APPLY ? a.into : nullptr, at.chunk, at.c, state);
 #pragma unroll
     for (int i = 0; i < C; i++) chunk[i] = {1.0f, 0.0f};
     if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
@@ -382,8 +404,9 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
     for (; r0 < to; r0 += at.tile) {
         const uint32_t r = r0 + at.sub * R;
         const bool plain = cursor.plain(r0, at.tile);
-        uint32_t rx[R], rg[R], b, bs, be, begins = 0, ends = 0;
-        if (!plain) cursor.look(a, b, bs, be);
+        uint32_t rx[R], rg[R], begins = 0, ends = 0;
+        typename Cursor<R, false>::Look look;
+        if (!plain) cursor.look(a, cursor.b, look);
         const bool whole = plain || at.all_there(r);
         if (whole) {
             load_rows<true>(a.x, a.x_row, r, at, piece, rx);
@@ -393,7 +416,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
             load_rows<false>(a.g, a.g_row, r, at, piece, rg);
         }
         if (!plain) {
-            cursor.find(a, r0, at.tile, b, bs, be, edges);
+            cursor.find(a, r0, at.tile, look, edges);
             begins = at.word(edges.begins);
             if constexpr (APPLY) ends = at.word(edges.ends);
         }
@@ -467,9 +490,9 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
         __syncthreads();
     }
     if constexpr (APPLY) {
-        pass_on<C>(a, a.h0, a.last, at.c);
+        pass_on<C>(a, a.h0, a.last, at.chunk, at.c);
     } else if (threadIdx.x < a.lanes) {
-        float *m = a.maps + (size_t)blockIdx.x * 2 * a.width;
+        float *m = a.maps + (size_t)at.chunk * 2 * a.width;
 #pragma unroll
         for (int i = 0; i < C; i++)
             if (at.c + i < a.width) m[at.c + i] = chunk[i].a, m[a.width + at.c + i] = chunk[i].b;
@@ -485,10 +508,11 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
     __shared__ Map lds[2][kThreads / 64][64 * C];
     const Place<R, ONE> at(a, C);
     const Piece<T> piece(at.c, a.width);
-    const uint32_t from = blockIdx.x * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
+    if (at.chunk >= max(a.chunks, 1u)) return;
+    const uint32_t from = at.chunk * a.chunk_rows, to = min(a.rows, from + a.chunk_rows);
     float state[C];
     Map chunk[C];
-    load_state(a, APPLY ? a.into : nullptr, blockIdx.x, at.c, state);
+    load_state(a, APPLY ? a.into : nullptr, at.chunk, at.c, state);
 #pragma unroll
     for (int i = 0; i < C; i++) chunk[i] = {1.0f, 0.0f};
     if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
@@ -507,8 +531,9 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
     for (uint32_t t = tiles; t-- > 0;) {
         const uint32_t r0 = from + t * at.tile, r = r0 + at.sub * R;
         const bool plain = cursor.plain(r0, at.tile);
-        uint32_t rx[R], rg[R], rd[R], b, bs, be, begins = 0, ends = 0;
-        if (!plain) cursor.look(a, b, bs, be);
+        uint32_t rx[R], rg[R], rd[R], begins = 0, ends = 0;
+        typename Cursor<R, true>::Look look;
+        if (!plain) cursor.look(a, cursor.b, look);
         const bool whole = plain || at.all_there(r);
         if (whole) {
             load_rows<true>(a.g, a.g_row, r, at, piece, rg);
@@ -522,7 +547,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
         float h[C];
         load_state(a, APPLY ? a.states : nullptr, r0 / kStateRows, at.c, h);
         if (!plain) {
-            cursor.find(a, r0, at.tile, b, bs, be, edges);
+            cursor.find(a, r0, at.tile, look, edges);
             ends = at.word(edges.ends);
             if constexpr (APPLY) begins = at.word(edges.begins);
         }
@@ -644,9 +669,9 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
         __syncthreads();
     }
     if constexpr (APPLY) {
-        pass_on<C>(a, a.dlast, a.dh0, at.c);
+        pass_on<C>(a, a.dlast, a.dh0, at.chunk, at.c);
     } else if (threadIdx.x < a.lanes) {
-        float *m = a.maps + (size_t)blockIdx.x * 2 * a.width;
+        float *m = a.maps + (size_t)at.chunk * 2 * a.width;
 #pragma unroll
         for (int i = 0; i < C; i++)
             if (at.c + i < a.width) m[at.c + i] = chunk[i].a, m[a.width + at.c + i] = chunk[i].b;
@@ -724,15 +749,14 @@ template <bool REVERSE> __global__ __launch_bounds__(1024) void join_chunks(Scan
 }
 
 // ---------------------------------------------------------------- host
-uint32_t groups_of(const Scan &a, int n) { return (a.width + a.lanes * n - 1) / (a.lanes * n); }
-
 // Lanes that share a row: a power of two from 8 to 64 that holds the channels.
 // Chunks: as many workgroups as the card holds twice, of whole tiles.
 void split(Scan &a, int n) {
     a.lanes = 8;
     while (a.lanes < 64 && a.lanes * n < a.width) a.lanes *= 2;
     const uint32_t tile = kThreads / a.lanes * kRows, tiles = (a.rows + tile - 1) / tile;
-    const uint32_t groups = groups_of(a, n), most = groups < kChunks ? kChunks / groups : 1;
+    a.groups = (a.width + a.lanes * n - 1) / (a.lanes * n);
+    const uint32_t most = a.groups < kChunks ? kChunks / a.groups : 1;
     const uint32_t per = (tiles + most - 1) / most;
     a.chunk_rows = per * tile;
     a.chunks = per ? (tiles + per - 1) / per : 0;
@@ -781,7 +805,7 @@ bool overlap(const Scan &a, const float *p, const float *q) {
 
 template <typename T, bool ONE, bool BACKWARD> int launch(Scan &a, void *work, hipStream_t s) {
     // (a call of no rows still has states to pass on)
-    const dim3 grid(a.chunks ? a.chunks : 1, groups_of(a, Piece<T>::n));
+    const uint32_t grid = (a.chunks ? (a.chunks + 7) / 8 : 1) * 8 * a.groups;
     if (carried(a)) {
         a.maps = (float *)work;
         float *into = (float *)((uint8_t *)work + align16z((size_t)a.chunks * 2 * a.width * 4));
