@@ -794,6 +794,8 @@ def lookup(table, ids, scale: float = 1.0, *, out=None, stream=None):
         out = table.new_empty((*ids.shape, width))
     elif out.shape != (*ids.shape, width):
         raise ValueError(f"out must be {[*ids.shape, width]}, not {list(out.shape)}")
+    if out.dim() != 2 and not out.is_contiguous():
+        raise ValueError("out must be contiguous, or of two dimensions")
     flat = out if out.dim() == 2 else out.view(c.n, width)
     args = *_table_rows(table, table, rows, width, "table"), *_table_rows(flat, table, c.n, width, "out")
     _check(lib.nlb_lookup(c, *args, _current_stream(table.device)), "nlb_lookup")
