@@ -391,21 +391,18 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
     if (threadIdx.x < kThreads / 8) edges.begins[threadIdx.x] = edges.ends[threadIdx.x] = 0;
     if (threadIdx.x == 0) edges.next = 0;
     __syncthreads();
-    uint32_t r0 = from;
-    Cursor<R, false> cursor;
-    if (from < to && !at.none()) {
-        if constexpr (!APPLY) {                            // rows before the last first row in the chunk do not matter
-            cursor.at(a, find_sequence(a, to - 1));
-            if (cursor.s > from) r0 = from + (cursor.s - from) / at.tile * at.tile;
-        }
-        cursor.at(a, find_sequence(a, r0));
+    uint32_t tiles = at.none() ? 0 : (to - from + at.tile - 1) / at.tile, t0 = 0;
+    Cursor<R, !APPLY> cursor;
+    if (tiles) {
+        cursor.at(a, find_sequence(a, APPLY ? from : to - 1));
+        // rows before the last first row in the chunk do not matter
+        if (!APPLY && cursor.s > from) t0 = (cursor.s - from) / at.tile;
     }
-    if (at.none()) r0 = to;
-    for (; r0 < to; r0 += at.tile) {
-        const uint32_t r = r0 + at.sub * R;
+    for (uint32_t n = t0; n < tiles; n++) {
+        const uint32_t t = APPLY ? n : tiles - 1 - (n - t0), r0 = from + t * at.tile, r = r0 + at.sub * R;
         const bool plain = cursor.plain(r0, at.tile);
         uint32_t rx[R], rg[R], begins = 0, ends = 0;
-        typename Cursor<R, false>::Look look;
+        typename Cursor<R, !APPLY>::Look look;
         if (!plain) cursor.look(a, cursor.b, look);
         const bool whole = plain || at.all_there(r);
         if (whole) {
@@ -485,7 +482,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows(Scan a) {
             for (int i = 0; i < C; i++) state[i] = all[i].of(state[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < C; i++) chunk[i] = all[i].after(chunk[i]);
+            for (int i = 0; i < C; i++) chunk[i] = chunk[i].after(all[i]);
         }
         __syncthreads();
     }
@@ -519,20 +516,18 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
     if (threadIdx.x == 0) edges.next = 0;
     __syncthreads();
     uint32_t tiles = (to - from + at.tile - 1) / at.tile;
-    Cursor<R, true> cursor;
+    Cursor<R, APPLY> cursor;
     if (at.none()) tiles = 0;
     if (tiles) {
-        if constexpr (!APPLY) {                            // rows behind the first last row in the chunk do not matter
-            cursor.at(a, find_sequence(a, from));
-            if (cursor.e > from && cursor.e <= to) tiles = (cursor.e - from + at.tile - 1) / at.tile;
-        }
-        cursor.at(a, find_sequence(a, min(from + tiles * at.tile, a.rows) - 1));
+        cursor.at(a, find_sequence(a, APPLY ? to - 1 : from));
+        // rows behind the first last row in the chunk do not matter
+        if (!APPLY && cursor.e > from && cursor.e <= to) tiles = (cursor.e - from + at.tile - 1) / at.tile;
     }
-    for (uint32_t t = tiles; t-- > 0;) {
-        const uint32_t r0 = from + t * at.tile, r = r0 + at.sub * R;
+    for (uint32_t n = 0; n < tiles; n++) {
+        const uint32_t t = APPLY ? tiles - 1 - n : n, r0 = from + t * at.tile, r = r0 + at.sub * R;
         const bool plain = cursor.plain(r0, at.tile);
         uint32_t rx[R], rg[R], rd[R], begins = 0, ends = 0;
-        typename Cursor<R, true>::Look look;
+        typename Cursor<R, APPLY>::Look look;
         if (!plain) cursor.look(a, cursor.b, look);
         const bool whole = plain || at.all_there(r);
         if (whole) {
@@ -598,7 +593,7 @@ __global__ __launch_bounds__(kThreads, 4) void scan_rows_backward(Scan a) {
         for (int i = 0; i < C; i++) {
             e[i] = before[i].of(state[i]);
             if constexpr (APPLY) state[i] = all[i].of(state[i]);
-            else chunk[i] = all[i].after(chunk[i]);
+            else chunk[i] = chunk[i].after(all[i]);
         }
         if constexpr (APPLY) {
             // h before each row again: forward maps from the state that was kept

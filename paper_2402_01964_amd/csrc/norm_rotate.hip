@@ -288,13 +288,15 @@ __global__ __launch_bounds__(1024) void sum_shares(const float *part, uint32_t q
 #pragma unroll
         for (int u = 0; u < 8; u++) x += (double)v[u];
     }
-    sums[at][threadIdx.x % 16] = x;
-    __syncthreads();
+    const uint32_t col = threadIdx.x % 16;
+    sums[at][col] = x;
+    for (uint32_t o = 32; o; o /= 2) {
+        __syncthreads();
+        if (at < o) sums[at][col] += sums[at + o][col];
+    }
     float *dw = blockIdx.y ? dwk : dwq;
     if (at || c >= dim || !dw) return;
-#pragma unroll 9
-    for (int i = 1; i < 64; i++) x += sums[i][threadIdx.x];
-    dw[c] = (float)x;
+    dw[c] = (float)sums[0][col];
 }
 
 // ---------------------------------------------------------------- host
