@@ -324,10 +324,11 @@ void split(Side &s, uint32_t lanes, uint32_t most) {
     s.blocks = need < most ? (uint32_t)need : most;
 }
 
-// Workgroups in all: eight on each of 256 CUs; queries and keys share them by
-// their values.
-template <typename T> void split(Rotate &a) {
-    const uint32_t lanes = lanes_of<T>(a), most = 2048;
+// Workgroups in all, of which queries and keys have shares by their values:
+// eight on each of 256 CUs forward; backward, where each leaves a share of dw, as
+// many as the CUs hold at once (registers: three for bf16 rows, four for fp32).
+template <typename T> void split(Rotate &a, bool back) {
+    const uint32_t lanes = lanes_of<T>(a), most = !back ? 2048 : sizeof(T) == 2 ? 768 : 1024;
     const uint64_t q = (uint64_t)a.side[0].rows * a.side[0].heads, k = (uint64_t)a.side[1].rows * a.side[1].heads;
     uint32_t for_q = q + k ? (uint32_t)((double)most * q / (q + k)) : 0;
     for_q = for_q < 64 ? 64 : for_q > most - 64 ? most - 64 : for_q;
@@ -340,7 +341,7 @@ bool bad_rows(const nlb_att_rows &r, uint32_t rows, int64_t e) {
            r.head_stride < 0 || r.head_stride > INT32_MAX;
 }
 
-int fill(const nlb_rotate_call *c, Rotate &a) {
+int fill(const nlb_rotate_call *c, Rotate &a, bool back) {
     a = {};
     if (!c || (c->dtype != NLB_DTYPE_F32 && c->dtype != NLB_DTYPE_BF16)) return NLB_EINVAL;
     if (c->dim < 1 || c->dim > NLB_ATT_MAX_DIM || c->freqs < 0 || 2 * c->freqs > c->dim) return NLB_EINVAL;
@@ -369,8 +370,8 @@ int fill(const nlb_rotate_call *c, Rotate &a) {
         s.rows = i ? c->k_rows : c->q_rows;
         s.heads = (uint32_t)(i ? c->kv_heads : c->heads);
     }
-    if (c->dtype == NLB_DTYPE_BF16) split<__bf16>(a);
-    else split<float>(a);
+    if (c->dtype == NLB_DTYPE_BF16) split<__bf16>(a, back);
+    else split<float>(a, back);
     return NLB_OK;
 }
 
@@ -403,7 +404,7 @@ template <bool BACK> int launch(const Rotate &a, int32_t dtype, hipStream_t s) {
 extern "C" int nlb_norm_rotate(const nlb_rotate_call *c, const nlb_att_rows *q_out, const nlb_att_rows *k_out,
                                void *stream) {
     Rotate a;
-    const int rc = fill(c, a);
+    const int rc = fill(c, a, false);
     if (rc != NLB_OK) return rc;
     const int64_t e = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
     if (!q_out || bad_rows(*q_out, c->q_rows, e)) return NLB_EINVAL;
@@ -423,7 +424,7 @@ extern "C" int nlb_norm_rotate(const nlb_rotate_call *c, const nlb_att_rows *q_o
 extern "C" int nlb_norm_rotate_work(const nlb_rotate_call *c, size_t *bytes) {
     Rotate a;
     if (!bytes) return NLB_EINVAL;
-    const int rc = fill(c, a);
+    const int rc = fill(c, a, true);
     if (rc != NLB_OK) return rc;
     *bytes = work_of(a);
     return NLB_OK;
@@ -433,7 +434,7 @@ extern "C" int nlb_norm_rotate_backward(const nlb_rotate_call *c, const nlb_att_
                                         const nlb_att_rows *dq, const nlb_att_rows *dk, float *dwq, float *dwk,
                                         void *work, size_t work_bytes, void *stream) {
     Rotate a;
-    int rc = fill(c, a);
+    int rc = fill(c, a, true);
     if (rc != NLB_OK) return rc;
     const int64_t e = c->dtype == NLB_DTYPE_BF16 ? 2 : 4;
     if (!dq_out || !dq || bad_rows(*dq_out, c->q_rows, e) || bad_rows(*dq, c->q_rows, e)) return NLB_EINVAL;
