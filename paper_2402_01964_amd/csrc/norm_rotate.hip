@@ -59,7 +59,7 @@ __device__ __forceinline__ void sincos_turns(double turns, float &s, float &c) {
 // values lo(p) and hi(p) of a head; the last pair behind the rotated ones may lack
 // the second.
 constexpr int kWhole = 0, kOverlap = 1, kStrided = 2;
-template <typename T, int L, int MODE> struct Pairs {
+template <typename T, int L, int MODE, bool BACK> struct Pairs {
     static constexpr int V = 16 / sizeof(T);
     uint32_t j, p0, skip;
     bool some;
@@ -111,6 +111,9 @@ template <typename T, int L, int MODE> struct Pairs {
             }
         }
     }
+    // Gradients go out past the caches (lists of width 50: 67 us with ordinary stores,
+    // 57 so), results, whose half lines the caches join, through them (rows of 64
+    // values of which 32 turn: 23 us so, 29 past them).
     // (pairs of two chunks are written twice, the same values: a head's lanes are
     // in one wavefront, and all have read before any writes)
     template <bool HI> __device__ __forceinline__ void store(const Rotate &a, uint8_t *y, const float (&f)[V]) const {
@@ -120,7 +123,9 @@ template <typename T, int L, int MODE> struct Pairs {
         if constexpr (MODE != kStrided) {
             u32x4 u;
             __builtin_memcpy(&u, v, 16);
-            if (some) *(u32x4_any *)(y + (HI ? hi(a, p0) : lo(a, p0)) * sizeof(T)) = u;
+            u32x4_any *to = (u32x4_any *)(y + (HI ? hi(a, p0) : lo(a, p0)) * sizeof(T));
+            if (some && BACK) __builtin_nontemporal_store(u, to);
+            else if (some) *to = u;
         } else {
 #pragma unroll
             for (int i = 0; i < V; i++) {
@@ -157,7 +162,7 @@ template <int L> __device__ __forceinline__ float head_sum(float x) {
 // one, the workgroup's groups of lanes tasks side by side.
 template <typename T, int L, int MODE, bool BACK>
 __global__ __launch_bounds__(kThreads) void rotate_heads(Rotate a) {
-    typedef Pairs<T, L, MODE> P;
+    typedef Pairs<T, L, MODE, BACK> P;
     constexpr int V = P::V, U = BACK ? 2 : 4;              // heads whose loads are in flight at once
     const uint32_t is_k = blockIdx.x >= a.side[0].blocks;
     const Side &s = a.side[is_k];
