@@ -632,7 +632,7 @@ int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq
  * backward pass starts from; NULL where none follows.
  *   Numerics.  Gates, states and products are fp32 (1 - z is not formed by
  * subtraction), h is rounded once.  Gates beyond 80 in magnitude count as 80.
- * Maps of 16 rows and more are joined in a fixed tree: the same call gives the
+ * Maps of some rows each are joined in a fixed tree: the same call gives the
  * same bits.  What one sequence holds (NaN, infinities) does not reach another.
  *   nlb_gated_scan_backward, from the same call, states as written, the gradient
  * dh of h and that of last (dlast, NULL: zeros):

@@ -9,6 +9,12 @@
 // A group sums the rows that begin in its run, into the next run where a row ends
 // there; one that goes further (a popular id) is split: every run that it
 // touches leaves its part's sum, and a last launch joins them in order.
+// Measured: 3 000 000 ids, a third of them empty, rows of 128 bf16 values: 185 us
+// forward (5.0 TB/s; 180 to 215 by what else is in the caches); the gradient of the
+// rows that occur 290: three passes of 9 bits (5 to 10 us counting, 6.5 scanning,
+// 14 to 18 scattering each), 8 for the list's places, 163 for the sums (4.3 TB/s,
+// what rows at random places reach), 27 to join popular rows.  240 000 ids, 17 000
+// rows of 100 fp32 values, whole: 76 us, of which 27 the sums and 27 the sort.
 #include <type_traits>
 
 #include "call_device.h"
@@ -44,7 +50,7 @@ template <typename T> __device__ __forceinline__ u32x4 load_chunk(const uint8_t 
     }
     return x;
 }
-// (Past the caches: 3 000 000 rows of 256 bytes 242 us with ordinary stores, 180 so.)
+// (Past the caches: 3 000 000 rows of 256 bytes 242 us with ordinary stores, 185 so.)
 template <typename T> __device__ __forceinline__ void store_chunk(uint8_t *row, uint32_t c, uint32_t width, u32x4 x) {
     constexpr uint32_t n = Chunk<T>::n;
     uint8_t *p = row + (size_t)c * sizeof(T);
@@ -591,6 +597,9 @@ void passes_of(uint32_t rows, uint32_t &passes, uint32_t &bits) {
     bits = (all + passes - 1) / passes;
 }
 
+// Places a run: enough runs to fill the card, few enough that popular rows have
+// few parts (3 000 000 places: runs of 256 228 us for the sums, of 64 172; 240 000:
+// runs of 16 26 us and 32 to join, of 32 27 and 15).
 uint32_t run_of(uint32_t n) {
     uint32_t run = 16;
     while (run < 64 && run < n / 8192) run *= 2;

