@@ -310,15 +310,28 @@ __global__ __launch_bounds__(1024) void sum_shares(const float *part, uint32_t q
 }
 
 // ---------------------------------------------------------------- host
+// A head's sum stays within 16 lanes.
+constexpr uint32_t kMaxLanes = 16;
+
+// Lanes that hold a head of which each part's pairs are in chunks of their own.
+template <typename T> uint32_t chunked_lanes(const Rotate &a) {
+    const uint32_t v = 16 / sizeof(T);
+    return (a.m + v - 1) / v + (a.rest + v - 1) / v;
+}
 template <typename T> int mode_of(const Rotate &a) {
     const uint32_t v = 16 / sizeof(T), rest = a.dim - 2 * a.m;
     if (a.m % v == 0 && rest % (2 * v) == 0) return kWhole;
-    // half a chunk's lanes idle at most, and pairs of both halves
-    return rest % 2 == 0 && (a.m == 0 || a.m >= v) && (rest == 0 || rest >= 2 * v) ? kOverlap : kStrided;
+    // half a chunk's lanes idle at most, pairs of both halves, and lanes enough
+    // (fp32 heads of 62 to 64 pairs in two parts can need 17 chunks; pair by pair
+    // they take 16 lanes: 32 768 rows of 16 + 4 heads of 128, 143 us with 32 pairs
+    // turned, in whole chunks, 163 with 31; backward 155 and 203)
+    return rest % 2 == 0 && (a.m == 0 || a.m >= v) && (rest == 0 || rest >= 2 * v) && chunked_lanes<T>(a) <= kMaxLanes
+               ? kOverlap
+               : kStrided;
 }
 template <typename T> uint32_t lanes_of(const Rotate &a) {
     const uint32_t v = 16 / sizeof(T);
-    const uint32_t need = mode_of<T>(a) == kStrided ? (a.m + a.rest + v - 1) / v : (a.m + v - 1) / v + (a.rest + v - 1) / v;
+    const uint32_t need = mode_of<T>(a) == kStrided ? (a.m + a.rest + v - 1) / v : chunked_lanes<T>(a);
     uint32_t l = 2;
     while (l < need) l *= 2;
     return l;
