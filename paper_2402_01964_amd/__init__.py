@@ -803,18 +803,21 @@ def lookup(table, ids, scale: float = 1.0, *, out=None, stream=None):
 
 
 def _lookup_gradient(dout, ids, rows, scale):
-    """dout as [n, width] and the call."""
     if dout.dim() < 1 or dout.shape[:-1] != ids.shape:
         raise ValueError("dout must be [*ids.shape, width]")
-    width = dout.shape[-1]
-    c = _lookup_call(dout, ids, rows, width, scale, "dout")
-    return (dout if dout.dim() == 2 else dout.reshape(c.n, width)), c
+    return _lookup_call(dout, ids, rows, dout.shape[-1], scale, "dout")
+
+
+def _flat_gradient(dout, c):
+    """dout as [n, width]: a copy, which belongs to the current stream, where its
+    strides allow no view."""
+    return dout if dout.dim() == 2 else dout.reshape(c.n, c.width)
 
 
 def lookup_work(dout, ids, rows: int, scale: float = 1.0, *, listed=False) -> int:
     """Bytes of working memory that lookup_backward (or, with ``listed``,
     lookup_backward_listed) of these takes (``work=``)."""
-    c = _lookup_gradient(dout, ids, rows, scale)[1]
+    c = _lookup_gradient(dout, ids, rows, scale)
     n = ctypes.c_size_t()
     _check(load_library().nlb_lookup_work(c, int(bool(listed)), n), "nlb_lookup_work")
     return n.value
@@ -826,10 +829,11 @@ def lookup_backward(dout, ids, rows: int, scale: float = 1.0, *, dtable=None, wo
     fills) dtable [rows, width].  ``work``: lookup_work bytes, allocated if
     None."""
     lib = load_library()
-    d, c = _lookup_gradient(dout, ids, rows, scale)
+    c = _lookup_gradient(dout, ids, rows, scale)
     if stream is not None:
         with _on(stream, dout.device):
             return lookup_backward(dout, ids, rows, scale, dtable=dtable, work=work)
+    d = _flat_gradient(dout, c)
     if dtable is None:
         dtable = dout.new_empty((c.rows, c.width))
     keep, p, size = _work(lib.nlb_lookup_work, c, (0,), work, dout, "nlb_lookup_backward")
@@ -848,10 +852,11 @@ def lookup_backward_listed(dout, ids, rows: int, scale: float = 1.0, *, grads=No
     count int32 [1], their number (on the device: nothing is waited for)."""
     import torch
     lib = load_library()
-    d, c = _lookup_gradient(dout, ids, rows, scale)
+    c = _lookup_gradient(dout, ids, rows, scale)
     if stream is not None:
         with _on(stream, dout.device):
             return lookup_backward_listed(dout, ids, rows, scale, grads=grads, row_ids=row_ids, count=count, work=work)
+    d = _flat_gradient(dout, c)
     ints = (torch.int32,)
     if grads is None:
         grads = dout.new_empty((c.n, c.width))
