@@ -429,12 +429,16 @@ __device__ __forceinline__ uint32_t heads_before(const Sums &a, uint32_t r) {
     return r < a.runs ? a.heads[r] + a.blocks[r / kBlock] : a.blocks[(a.runs + kBlock - 1) / kBlock];
 }
 
-// Whether the row at place i goes on behind the run after i's run `r`, so that
-// it is summed in parts: `first` is where that run ends.
+// Whether the entry at place `at` is one of row `id`.
 __device__ __forceinline__ bool goes_on(const Sums &a, uint32_t id, uint32_t at, uint32_t n) {
     return at < n && id_at(a, at) == id;
 }
 
+// A group of lanes sums the rows that begin in its run.  One that ends in the next
+// run is summed to its end there; one that goes on behind the next run is summed in
+// parts: `tail`, this run's part of a row that begins in it, and in the runs behind
+// it `head`, their parts of a row that began before (join_parts finds the same rows
+// by the same two places, the first ones of the next run and of the run behind it).
 template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums a) {
     constexpr int N = Chunk<T>::n, U = 8;
     const uint32_t n = *a.valid, lane = threadIdx.x % a.lanes;
@@ -454,6 +458,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void sum_runs(Sums 
     uint32_t id = id_at(a, begin), i = begin, stop = end;
     bool head = begin > 0 && id_at(a, begin - 1) == id, tail = false;
     if (head) {
+        // in parts if it goes on behind this run, or began before the last one
         const bool parts = goes_on(a, id, end, n) && end == begin + a.run;
         if (!parts && !(begin > a.run && id_at(a, begin - a.run - 1) == id)) {
             // the run before has summed it to its end
@@ -582,6 +587,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void join_parts
     __syncthreads();
     if (threadIdx.x < kLook && r < a.runs && (uint64_t)(r + 2) * a.run < n) {
         const uint32_t begin = r * a.run, end = begin + a.run, id = id_at(a, end - 1);
+        // the run's last row: begins in this run, and goes on behind the next
         const bool from_before = id_at(a, begin) == id && begin > 0 && id_at(a, begin - 1) == id;
         if (!from_before && id_at(a, end) == id && id_at(a, end + a.run) == id) found[atomicAdd(&number, 1u)] = r;
     }
