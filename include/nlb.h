@@ -535,8 +535,10 @@ int nlb_layer_norm_backward(const nlb_norm_call *call, const void *dy, int64_t d
  * ids, ascending, and -1 behind them, count (device uint32) their number, and
  * the first `count` rows of dtable ([n][width]) their gradients; the rows behind
  * them stay as they are.  The ids are sorted; a row's gradients are added up in
- * fp32 in an order that the ids alone set, no atomics on results: the same call
- * gives the same bits.  Rows of ids outside the table are not read.
+ * fp32 in an order that the ids, n, the width and the type set, no atomics on
+ * results: the same call gives the same bits, but a popular row's columns may
+ * differ in their last bits from those of a wider call.  Rows of ids outside the
+ * table are not read.
  *   Work: nlb_lookup_work bytes of device memory (16-byte aligned; listed = 0
  * for the whole gradient, 1 for the rows that occur), used by the call's kernels
  * only.  Only enqueues kernels: may be captured in a HIP graph.  Written rows
@@ -579,7 +581,10 @@ int nlb_lookup_backward(const nlb_lookup_call *call, const void *dout, int64_t d
  * NULL for ones.
  *   Numerics.  Angles are formed and reduced in 64 bits: their error is some
  * 2^-24 and |a| 2^-51.  Sums and products are fp32, each row's values are read
- * once and rounded once.
+ * once and rounded once.  The sum of a head's squares has to fit fp32, and its
+ * mean and eps have to be 2^-126 or more together (values of 2^60 at most, and
+ * of 2^-59 where eps is 0): others have no meaningful result.  With eps = 0 a
+ * head of zeros is NaN, as in the formula; an empty slot is zeros all the same.
  *   nlb_norm_rotate_backward, from the same call (q and k as they went in) and
  * the gradients dq_out, dk_out of the results: with du = the gradient rotated
  * by -a, g = du w, r = the norm's factor,
@@ -590,7 +595,8 @@ int nlb_lookup_backward(const nlb_lookup_call *call, const void *dout, int64_t d
  * call's kernels use.  Their sums are fp32 within a workgroup, then fp64, in a
  * fixed order: the same call gives the same bits.
  *   Only enqueues kernels: may be captured in a HIP graph.  Written rows must
- * not overlap each other.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
+ * not overlap each other or, but for the arrays named above, what the call
+ * reads.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
 typedef struct nlb_rotate_call {
     int32_t device;          /* HIP device ordinal, -1 = current */
     int32_t dtype;           /* NLB_DTYPE_F32 / _BF16: q, k, the results and their gradients */
@@ -623,7 +629,11 @@ int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq
  * int32 [batch + 1], non-decreasing; lengths may be zero, the host need not
  * know them).  start NULL: rows / batch rows each (no rest).  Starts outside
  * [0, rows] are taken as the nearest end.  Rows before the first and behind the
- * last sequence are neither read nor written.
+ * last sequence are neither read nor written.  The rows set how many workgroups
+ * there are, and each passes its share of the sequences without rows on one
+ * after the other: where there are many of them beside few rows, they are the
+ * call's time (2000 rows of 100 fp32 values in 20 000 sequences: 0.25 ms either
+ * pass, in 200 000: 3.3; a call of no rows at all: some 0.5 us a sequence).
  *   Rows.  x, g, h: [rows][width] of dtype, at any row stride (in values,
  * 0 .. 2^31 - 1); a row's values are contiguous.  h may be x.  h0, last: device
  * fp32 [batch][width], contiguous; last may be NULL, and may be h0 where start
@@ -632,8 +642,11 @@ int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq
  * backward pass starts from; NULL where none follows.
  *   Numerics.  Gates, states and products are fp32 (1 - z is not formed by
  * subtraction), h is rounded once.  Gates beyond 80 in magnitude count as 80.
+ * z and 1 - z are off by at most 12 x 2^-24 of themselves, in calls of bf16 rows
+ * by |g| 2^-23 more, which last, states and dh0 have too, fp32 as they are.
  * Maps of some rows each are joined in a fixed tree: the same call gives the
- * same bits.  What one sequence holds (NaN, infinities) does not reach another.
+ * same bits.  What one sequence holds (NaN, infinities) does not reach another;
+ * behind an infinity a channel's rows of that sequence are infinite or NaN.
  *   nlb_gated_scan_backward, from the same call, states as written, the gradient
  * dh of h and that of last (dlast, NULL: zeros):
  *   d_t = dh_t + z_{t+1} d_{t+1}  (behind the last row: dlast)
@@ -643,7 +656,8 @@ int nlb_norm_rotate_backward(const nlb_rotate_call *call, const nlb_att_rows *dq
  *   Work: nlb_gated_scan_work bytes of device memory (16-byte aligned, may be
  * NULL if that is 0) for either pass, used by the call's kernels only.  Only
  * enqueues kernels: may be captured in a HIP graph.  Written rows must not
- * overlap each other.  Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
+ * overlap each other or, but for the arrays named above, what the call reads.
+ * Errors: NLB_EINVAL, NLB_ESCRATCH, NLB_EDEVICE. */
 #define NLB_SCAN_MAX_WIDTH 65536
 #define NLB_SCAN_MAX_ROWS 2147480000u
 #define NLB_SCAN_STATE_ROWS 32

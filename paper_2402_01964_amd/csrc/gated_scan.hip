@@ -128,10 +128,11 @@ template <typename T, int R> __device__ __forceinline__ void limit(uint32_t (&ra
 
 // z = sigmoid(g) = 1 / (1 + e) and 1 - z = e z with e = exp(-g) = 2^t, t = -g / ln
 // 2, |g| up to 80.  EXACT: e (1 + lo) with what t's rounding left, lo = -g - t ln 2,
-// so that both have relative errors of some 2^-21.  Without it, for bf16 gates, e
-// and 1 - z are off by |g| 2^-24 more of themselves (z by less than 2^-24: where e
-// is off, z is near 1): below the rounding of what they go into, and two operations
-// of 14 less.
+// so that both have relative errors of some 2^-21.  Without it, for bf16 gates, t is
+// off by 2^-24 (its rounding) and 2^-26 (its constant) of itself, and z and 1 - z by
+// less than |g| 2^-23 more of themselves (z by less than 2^-24 absolutely): below the
+// rounding of what goes out as bf16, and two operations of 14 less.  The states,
+// which are fp32, have it too.
 template <bool EXACT> __device__ __forceinline__ void gate(float g, float &z, float &y) {
     const float t = g * -1.44269504f;
     float e = __builtin_amdgcn_exp2f(t);
