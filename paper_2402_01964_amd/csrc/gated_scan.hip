@@ -16,9 +16,9 @@
 // Measured: one sequence of a million rows of 128 bf16 values: 97 us for the maps
 // (5.3 TB/s), 8 to join them, 149 for h (5.2 TB/s); 48 sequences of 16 to 4096
 // rows of 1024: 33, 5 and 45 us, backward 29, 5 and 92; 20 000 of 1 to 60 rows of
-// 100 fp32 values: 17, 6 and 104, backward 10, 6 and 217.  Forward, HBM bounds it
-// (vector instructions: 0.75 of the cycles); backward of long sequences vector
-// instructions (57 a value, 0.64); short sequences each tile's chain of loads.
+// 100 fp32 values: 18, 6 and 105, backward 10, 6 and 215.  Forward, HBM bounds it
+// (vector instructions: 0.73 to 0.83 of the cycles); backward of long sequences
+// vector instructions (57 a value, 0.75); short sequences each tile's chain of loads.
 #include <algorithm>
 #include <type_traits>
 
